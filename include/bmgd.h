@@ -33,8 +33,8 @@
  *
  * General rules
  *   - Every function is extern "C", never throws and never aborts.  Except for
- *     bmgd_create(), bmgd_workspace_bytes() and bmgd_last_error() they return a
- *     status code; on failure bmgd_last_error() holds a message.
+ *     bmgd_create(), those that return sizes (bmgd_workspace_bytes(), ...) and messages
+ *     (bmgd_last_error(), ...) and those that return nothing they return a status code; on failure bmgd_last_error() holds a message.
  *   - A context belongs to one host thread at a time (no internal locking) and
  *     to the HIP device that was current when it was created.
  *   - "host" pointers are ordinary or pinned host memory, "device" pointers are
@@ -94,8 +94,8 @@ enum {
     BMGD_SOFTMAX = 2    /* x (softmax(x'W) - onehot(y))', W is p x C row-major */
 };
 
-/* storage type of X */
-enum { BMGD_F32 = 0, BMGD_BF16 = 1 };
+/* storage type of X (BMGD_F16: the gated block and the AdamW step only) */
+enum { BMGD_F32 = 0, BMGD_BF16 = 1, BMGD_F16 = 2 };
 
 /* how mini-batch partitions are drawn */
 enum {
@@ -422,6 +422,134 @@ const char* bmgd_last_error(const bmgd_ctx* ctx);
 
 /* Wait for enqueued work and release everything the library allocated.  NULL is ignored. */
 void bmgd_destroy(bmgd_ctx* ctx);
+
+/* ==== Predictors beyond x'theta: the gated block =================================================================
+ * Section 4 trains networks with buffered mini-batches.  The gated block is the predictor of a mini-batch X
+ * (rows x p) that has one hidden layer of `hidden` units, each gated by another:
+ *
+ *      G = X Wg,   U = X Wu,   H = act(G) * U,   Y = H Wd                  (* element by element)
+ *
+ * with Wg, Wu p x hidden and Wd hidden x out_n, row-major like softmax's W.  The caller owns the weights, forms the
+ * loss and its gradient dY (with its 1/n_b) from Y, and makes the update (bmgd_adamw_step, or any other).
+ *   act: BMGD_ACT_SILU  g / (1 + e^-g)
+ *        BMGD_ACT_GELU  g F(g), F the standard normal distribution function (not its tanh approximation)
+ *        BMGD_ACT_RELU  max(g, 0), derivative 0 at 0
+ * All matrices are BMGD_BF16 or BMGD_F16; every sum is in fp32 and rounded once.  What lies between two products (H; dG,
+ * dU) is rounded to that type, since it is an operand of the matrix instructions. */
+enum { BMGD_ACT_SILU = 0, BMGD_ACT_GELU = 1, BMGD_ACT_RELU = 2 };
+
+typedef struct bmgd_gated bmgd_gated;
+
+typedef struct bmgd_gated_config {
+    int64_t p;              /* features, hidden units and outputs: each in [1, 2^20] */
+    int64_t hidden;
+    int64_t out_n;
+    int64_t max_rows;       /* the largest number of rows a call may have: in [1, 2^30) */
+    int32_t dtype;          /* BMGD_BF16 or BMGD_F16 */
+    int32_t activation;     /* BMGD_ACT_* */
+    void*   workspace;      /* optional device memory, 256-byte aligned, valid until bmgd_gated_destroy(); NULL = the library
+                               allocates (and frees) it */
+    size_t  workspace_bytes;
+} bmgd_gated_config;
+
+/* A row-major matrix in device memory: element (i, j) at data + i * stride + j, stride in elements, not less than the number of
+ * columns (ignored where there is one row).  2-byte alignment is enough.  Operands of the products whose rows are not
+ * 16-byte aligned, of a multiple of 8 columns and of a stride that is a multiple of 8 (of one stride, for gate and up) are
+ * copied in the workspace first, in every call, since the caller may have changed them. */
+typedef struct bmgd_matrix {
+    void*   data;
+    int64_t stride;
+} bmgd_matrix;
+
+/* The matrices of a call; the ones that a call does not name are not looked at.  Results must not overlap operands or each
+ * other.  data = NULL leaves out what is marked optional. */
+typedef struct bmgd_gated_tensors {
+    bmgd_matrix x;          /* rows x p */
+    bmgd_matrix gate;       /* Wg, p x hidden */
+    bmgd_matrix up;         /* Wu, p x hidden */
+    bmgd_matrix down;       /* Wd, hidden x out_n */
+    bmgd_matrix y;          /* forward: rows x out_n, written */
+    bmgd_matrix g;          /* G and U, rows x hidden: forward writes them (optional, both or neither), backward reads them */
+    bmgd_matrix u;
+    bmgd_matrix dy;         /* backward: rows x out_n */
+    bmgd_matrix dx;         /* backward, written, each optional (dgate and dup both or neither): shaped like x, gate, up, down */
+    bmgd_matrix dgate;
+    bmgd_matrix dup;
+    bmgd_matrix ddown;
+} bmgd_gated_tensors;
+
+/* Device bytes that a block of this configuration needs; 0 if it is invalid.  Needs no GPU. */
+size_t bmgd_gated_workspace_bytes(const bmgd_gated_config* cfg);
+
+/* *out receives the block (its workspace; it holds no weights).  For the HIP device that is current.  Blocks.  Errors:
+ * BMGD_EINVAL, BMGD_EHIP, BMGD_ENOMEM; message from bmgd_last_error(NULL). */
+int bmgd_gated_create(const bmgd_gated_config* cfg, bmgd_gated** out);
+
+/* Y from X; with g and u, G and U too, as a later bmgd_gated_backward needs them.  rows in [0, max_rows]; 0 rows: nothing
+ * happens.  Asynchronous, allocates nothing, may be captured into a graph. */
+int bmgd_gated_forward(bmgd_gated* block, int64_t rows, const bmgd_gated_tensors* t, void* stream);
+
+/* From dY:   dH = dY Wd',  dU = dH * act(G),  dG = dH * U * act'(G),
+ *            dX = dG Wg' + dU Wu',  dWg = X' dG,  dWu = X' dU,  dWd = (act(G) * U)' dY.
+ * Results are written, not added to.  With 0 rows the weights' gradients are zeros.  Asynchronous like the forward call. */
+int bmgd_gated_backward(bmgd_gated* block, int64_t rows, const bmgd_gated_tensors* t, void* stream);
+
+/* Calls on one block share its workspace: they are made in the order of the calls, also on different streams (a call waits,
+ * on the device, for the one before if that was on another stream, which must still exist).  A call that is captured into a
+ * graph waits for nothing outside it; the caller orders the graph's launches and other calls on the same block. */
+
+const char* bmgd_gated_last_error(const bmgd_gated* block);
+/* Waits for the device if the block was used, and releases what the library allocated.  NULL is ignored. */
+void bmgd_gated_destroy(bmgd_gated* block);
+
+/* ==== AdamW over many tensors ====================================================================================
+ * Adam with decoupled weight decay for the k-th update, k = 1, 2, ...:
+ *
+ *      g <- grad_scale g;   m <- b1 m + (1 - b1) g;   s <- b2 s + (1 - b2) g^2
+ *      theta <- theta (1 - lr wd) - lr (m / (1 - b1^k)) / (sqrt(s / (1 - b2^k)) + eps)
+ *
+ * theta is fp32; the gradient fp32, bf16 or f16; a copy of the new theta rounded to bf16 or f16 (what a gated block multiplies
+ * by) is written on request.  Moments are fp32, or 8-bit codes with an fp32 scale per block of 256 neighbouring
+ * elements (the last block of a tensor may be shorter):
+ *      m = m_scale sgn(c) (c / 127)^2,  c int8 in [-127, 127];      s = s_scale (c / 255)^4,  c uint8
+ * The scale is the block's largest |m| (s); codes are the nearest, but an s > 0 has a code of at least 1.  A block whose largest value
+ * is below 2^-126 is held as zeros; a block in which a moment is not finite keeps that as its scale, with codes of zero: it stands for NaN from
+ * then on.  All zeros (codes and scales, or fp32) is the state before the first update. */
+typedef struct bmgd_adamw_tensor {      /* device memory; elements lie next to each other, n of each */
+    float*      theta;
+    const void* grad;                   /* of cfg->grad_dtype */
+    void*       copy;                   /* of cfg->copy_dtype, written; NULL: none */
+    void*       m;                      /* state_bits 32: fp32; 8: int8 codes, 4-byte aligned */
+    void*       s;                      /* state_bits 32: fp32; 8: uint8 codes, 4-byte aligned */
+    float*      m_scale;                /* state_bits 8: ceil(n / 256) scales each; otherwise not looked at */
+    float*      s_scale;
+    int64_t     n;                      /* 0: the tensor is passed over */
+} bmgd_adamw_tensor;
+
+typedef struct bmgd_adamw_config {
+    double  lr;             /* finite, >= 0 */
+    double  beta1;          /* in [0, 1) */
+    double  beta2;          /* in [0, 1) */
+    double  eps;            /* finite, >= 0; > 0 with moments in 8 bits */
+    double  weight_decay;   /* finite, >= 0 */
+    double  grad_scale;     /* finite: 1 / loss scale, times a clipping factor */
+    int32_t grad_dtype;     /* BMGD_F32, BMGD_BF16 or BMGD_F16 */
+    int32_t copy_dtype;     /* BMGD_BF16 or BMGD_F16 */
+    int32_t state_bits;     /* 32 or 8 */
+    int32_t reserved;
+} bmgd_adamw_config;
+
+/* lr 1e-3, beta1 0.9, beta2 0.999, eps 1e-8, weight_decay 0.01, grad_scale 1, fp32 gradients, bf16 copies, 32 bits. */
+void bmgd_adamw_default_config(bmgd_adamw_config* cfg);
+
+/* Update number `step` (>= 1) of all `count` tensors, in ceil(count / 48) launches on `stream`, which must belong to the current
+ * device.  `tensors` is host memory, read before the call returns.  Everything is checked before the first launch.
+ * Asynchronous, allocates nothing, keeps nothing.  Message of a failure: bmgd_last_error(NULL). */
+int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tensor* tensors, int64_t count, int64_t step, void* stream);
+
+/* The fp32 values that moments in 8 bits stand for: m_out[i], s_out[i] (host arrays of device addresses) receive n values each
+ * (theta, grad and copy are not looked at).  For checkpoints and for going on in 32 bits. */
+int bmgd_adamw_moments(const bmgd_adamw_tensor* tensors, int64_t count, float* const* m_out, float* const* s_out, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,7 +19,8 @@ LIB_PATH = os.path.join(_HERE, "libbmgd.so")
 
 BMGD_OK, BMGD_EINVAL, BMGD_ESTATE, BMGD_EHIP, BMGD_ENOMEM = 0, 1, 2, 3, 4
 BMGD_LINEAR, BMGD_LOGISTIC, BMGD_SOFTMAX = 0, 1, 2
-BMGD_F32, BMGD_BF16 = 0, 1
+BMGD_F32, BMGD_BF16, BMGD_F16 = 0, 1, 2
+BMGD_ACT_SILU, BMGD_ACT_GELU, BMGD_ACT_RELU = 0, 1, 2
 BMGD_RESHUFFLE_PER_PASS, BMGD_RESHUFFLE_FIXED = 0, 1
 BMGD_CHAIN_AUTO, BMGD_CHAIN_PERSISTENT, BMGD_CHAIN_LAUNCH, BMGD_CHAIN_GRAM, BMGD_CHAIN_GRAPH, BMGD_CHAIN_PRODUCT = 0, 1, 2, 3, 4, 5
 BMGD_OPT_SGD, BMGD_OPT_MOMENTUM, BMGD_OPT_NAG, BMGD_OPT_ADAM = 0, 1, 2, 3
@@ -32,6 +33,8 @@ EXPORTS = [
     "bmgd_load_buffer_async", "bmgd_run_buffer", "bmgd_run_buffer_adaptive", "bmgd_run_device_buffer", "bmgd_get_theta",
     "bmgd_set_theta", "bmgd_set_lr", "bmgd_set_passes", "bmgd_set_lr_schedule", "bmgd_reset_optimizer", "bmgd_eval_loss", "bmgd_eval_loss_static", "bmgd_set_position", "bmgd_get_perm", "bmgd_sync", "bmgd_get_stats",
     "bmgd_last_error", "bmgd_destroy",
+    "bmgd_gated_workspace_bytes", "bmgd_gated_create", "bmgd_gated_forward", "bmgd_gated_backward", "bmgd_gated_last_error", "bmgd_gated_destroy",
+    "bmgd_adamw_default_config", "bmgd_adamw_step", "bmgd_adamw_moments",
 ]
 
 
@@ -53,6 +56,36 @@ class bmgd_stats(C.Structure):
         ("wait_ms", C.c_double), ("n_workgroups", C.c_int32), ("threads_per_group", C.c_int32),
         ("chain", C.c_int32), ("reserved", C.c_int32), ("chain_ms", C.c_double), ("chain_launches", C.c_int64),
         ("prep_ms", C.c_double), ("prep_launches", C.c_int64),
+    ]
+
+
+class bmgd_gated_config(C.Structure):
+    _fields_ = [
+        ("p", C.c_int64), ("hidden", C.c_int64), ("out_n", C.c_int64), ("max_rows", C.c_int64), ("dtype", C.c_int32),
+        ("activation", C.c_int32), ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t),
+    ]
+
+
+class bmgd_matrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64)]
+
+
+class bmgd_gated_tensors(C.Structure):
+    _fields_ = [(name, bmgd_matrix) for name in ("x", "gate", "up", "down", "y", "g", "u", "dy", "dx", "dgate", "dup", "ddown")]
+
+
+class bmgd_adamw_tensor(C.Structure):
+    _fields_ = [
+        ("theta", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p), ("s", C.c_void_p),
+        ("m_scale", C.c_void_p), ("s_scale", C.c_void_p), ("n", C.c_int64),
+    ]
+
+
+class bmgd_adamw_config(C.Structure):
+    _fields_ = [
+        ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+        ("grad_scale", C.c_double), ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32), ("state_bits", C.c_int32),
+        ("reserved", C.c_int32),
     ]
 
 
@@ -106,6 +139,15 @@ def _load() -> C.CDLL:
     lib.bmgd_get_stats.argtypes, lib.bmgd_get_stats.restype = [vp, C.POINTER(bmgd_stats)], i32
     lib.bmgd_last_error.argtypes, lib.bmgd_last_error.restype = [vp], C.c_char_p
     lib.bmgd_destroy.argtypes, lib.bmgd_destroy.restype = [vp], None
+    lib.bmgd_gated_workspace_bytes.argtypes, lib.bmgd_gated_workspace_bytes.restype = [C.POINTER(bmgd_gated_config)], C.c_size_t
+    lib.bmgd_gated_create.argtypes, lib.bmgd_gated_create.restype = [C.POINTER(bmgd_gated_config), C.POINTER(vp)], i32
+    lib.bmgd_gated_forward.argtypes, lib.bmgd_gated_forward.restype = [vp, i64, vp, vp], i32
+    lib.bmgd_gated_backward.argtypes, lib.bmgd_gated_backward.restype = [vp, i64, vp, vp], i32
+    lib.bmgd_gated_last_error.argtypes, lib.bmgd_gated_last_error.restype = [vp], C.c_char_p
+    lib.bmgd_gated_destroy.argtypes, lib.bmgd_gated_destroy.restype = [vp], None
+    lib.bmgd_adamw_default_config.argtypes, lib.bmgd_adamw_default_config.restype = [C.POINTER(bmgd_adamw_config)], None
+    lib.bmgd_adamw_step.argtypes, lib.bmgd_adamw_step.restype = [C.POINTER(bmgd_adamw_config), vp, i64, i64, vp], i32
+    lib.bmgd_adamw_moments.argtypes, lib.bmgd_adamw_moments.restype = [vp, i64, vp, vp, vp], i32
     return lib
 
 
@@ -316,6 +358,50 @@ def bmgd_reader_last_error(reader=None) -> str:
 
 def bmgd_reader_close(reader) -> None:
     lib.bmgd_reader_close(reader)
+
+
+def bmgd_gated_workspace_bytes(cfg: bmgd_gated_config) -> int:
+    return lib.bmgd_gated_workspace_bytes(C.byref(cfg))
+
+
+def bmgd_gated_create(cfg: bmgd_gated_config):
+    out = C.c_void_p()
+    rc = lib.bmgd_gated_create(C.byref(cfg), C.byref(out))
+    return rc, out.value
+
+
+def bmgd_gated_forward(block, rows, tensors, stream=None) -> int:
+    """tensors: a bmgd_gated_tensors, or anything of its layout."""
+    return lib.bmgd_gated_forward(block, rows, C.addressof(tensors) if tensors is not None else None, _stream(stream))
+
+
+def bmgd_gated_backward(block, rows, tensors, stream=None) -> int:
+    return lib.bmgd_gated_backward(block, rows, C.addressof(tensors) if tensors is not None else None, _stream(stream))
+
+
+def bmgd_gated_last_error(block=None) -> str:
+    msg = lib.bmgd_gated_last_error(block)
+    return msg.decode() if msg else ""
+
+
+def bmgd_gated_destroy(block) -> None:
+    lib.bmgd_gated_destroy(block)
+
+
+def bmgd_adamw_default_config() -> bmgd_adamw_config:
+    cfg = bmgd_adamw_config()
+    lib.bmgd_adamw_default_config(C.byref(cfg))
+    return cfg
+
+
+def bmgd_adamw_step(cfg, tensors, count, step, stream=None) -> int:
+    """tensors: an array of bmgd_adamw_tensor."""
+    return lib.bmgd_adamw_step(C.byref(cfg), tensors, count, step, _stream(stream))
+
+
+def bmgd_adamw_moments(tensors, count, m_out, s_out, stream=None) -> int:
+    """m_out, s_out: arrays of device addresses (c_void_p)."""
+    return lib.bmgd_adamw_moments(tensors, count, m_out, s_out, _stream(stream))
 
 
 class Reader:

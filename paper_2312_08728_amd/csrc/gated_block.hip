@@ -1,0 +1,472 @@
+// Host side of the gated block Y = (act(X Wg) * (X Wu)) Wd: arguments, workspace, order of the launches; the kernel that copies matrices
+// whose rows cannot be read in pieces of 16 bytes.
+#include "../../include/bmgd.h"
+#include "bmgd_internal.h"
+#include "gated_internal.h"
+
+#include <stdio.h>
+
+#include <algorithm>
+#include <new>
+
+using namespace bmgd;
+
+namespace {
+
+constexpr int64_t kMaxWidth = int64_t(1) << 20;
+constexpr int64_t kMaxRows = (int64_t(1) << 30) - 1;
+
+int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
+
+struct Layout {
+    size_t h, d, x, gate, up, down, dy, partial, counter, zeros, total;
+};
+
+bool valid(const bmgd_gated_config& c, const char** why)
+{
+    if (c.p < 1 || c.hidden < 1 || c.out_n < 1 || c.p > kMaxWidth || c.hidden > kMaxWidth || c.out_n > kMaxWidth)
+        *why = "p, hidden and out_n must be in [1, 2^20]";
+    else if (c.max_rows < 1 || c.max_rows > kMaxRows) *why = "max_rows must be in [1, 2^30)";
+    else if (c.dtype != BMGD_BF16 && c.dtype != BMGD_F16) *why = "dtype must be BMGD_BF16 or BMGD_F16";
+    else if (c.activation != BMGD_ACT_SILU && c.activation != BMGD_ACT_GELU && c.activation != BMGD_ACT_RELU) *why = "unknown activation";
+    else if ((c.max_rows / 64 + 1) * (2 * std::max(c.p, std::max(c.hidden, c.out_n)) / 64 + 2) >= (int64_t(1) << 30) ||
+             (c.p / 64 + 1) * (2 * c.hidden / 64 + 2) >= (int64_t(1) << 30) || (c.hidden / 64 + 1) * (c.out_n / 64 + 1) >= (int64_t(1) << 30))
+        *why = "a product has 2^30 tiles of 64 x 64 or more";
+    else return true;
+    return false;
+}
+
+Layout make_layout(const bmgd_gated_config& c)
+{
+    Layout l{};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t r = at; at += (bytes + 255) / 256 * 256; return r; };
+    const size_t r = (size_t)c.max_rows, f64 = (size_t)up(c.hidden, 64), f8 = (size_t)up(c.hidden, 8), p8 = (size_t)up(c.p, 8), c8 = (size_t)up(c.out_n, 8);
+    l.h = take(2 * r * f64);
+    l.d = take(4 * r * f64);
+    l.x = take(2 * r * p8);
+    l.gate = take(2 * (size_t)c.p * f8);
+    l.up = take(2 * (size_t)c.p * f8);
+    l.down = take(2 * (size_t)c.hidden * c8);
+    l.dy = take(2 * r * c8);
+    l.partial = take(kGatedPartialBytes);
+    l.counter = take(kGatedCounters * sizeof(unsigned));
+    l.zeros = take(256);
+    l.total = at;
+    return l;
+}
+
+int fail_static(int code, const char* call, const char* msg)
+{
+    char buf[256];
+    snprintf(buf, sizeof buf, "%s: %s", call, msg);
+    set_create_error(buf);
+    return code;
+}
+
+struct PackArgs { GatedPack q; };
+
+// A thread moves eight elements.  Read one by one (their address is a multiple of 2 only), written as 16 bytes.
+__global__ void __launch_bounds__(256) gated_pack_kernel(PackArgs args)
+{
+    typedef unsigned short ushort8 __attribute__((ext_vector_type(8)));
+    const GatedPack::One m = args.q.m[blockIdx.y];
+    const int64_t per_row = m.to_ld >> 3, pieces = m.rows * per_row;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / per_row, c = 8 * (i - r * per_row);
+        const unsigned short* from = m.from + r * m.from_ld + c;
+        ushort8 v;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = c + k < m.cols ? from[k] : (unsigned short)0;
+        *(ushort8*)(m.to + r * m.to_ld + c) = v;
+    }
+}
+
+}  // namespace
+
+struct bmgd_gated {
+    bmgd_gated_config cfg;
+    Layout lay;
+    int device = 0, num_cus = 0;
+    char* base = nullptr;
+    bool owned = false, used = false;
+    hipStream_t last = nullptr;             // of the call before
+    hipEvent_t order = nullptr;
+    char err[256] = "";
+};
+
+namespace bmgd {
+
+hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
+{
+    int64_t most = 1;
+    for (int i = 0; i < q.count; ++i) most = std::max(most, q.m[i].rows * (q.m[i].to_ld >> 3));
+    const unsigned blocks = (unsigned)std::min<int64_t>((most + 255) / 256, 4096);
+    PackArgs a{q};
+    hipLaunchKernelGGL(gated_pack_kernel, dim3(blocks, (unsigned)q.count), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+void gated_plan(GatedProduct& q, GatedOp op, int num_cus)
+{
+    static const int bm[kTiles] = {256, 128, 64}, bn[kTiles] = {256, 128, 64}, per_cu[kTiles] = {1, 2, 4};
+    static const double step_us[kTiles] = {1.6, 0.9, 0.5}, once_us[kTiles] = {5.0, 3.0, 2.0};
+    const int64_t columns = op == kOpUp ? 2 * q.half : op == kOpDown ? q.half : op == kOpWeight && q.half ? 2 * q.half : q.N;
+    const int64_t steps = ((op == kOpInput ? 2 * q.half : q.K) + 63) / 64;
+    double best = 1e300;
+    for (int t = 0; t < kTiles; ++t) {
+        const int64_t tm = (q.M + bm[t] - 1) / bm[t], tn = (columns + bn[t] - 1) / bn[t], tiles = tm * tn;
+        if (tiles >= (int64_t(1) << 30)) continue;
+        for (int64_t want = 1; want <= 64; want += want < 4 ? 1 : want / 2) {
+            if (want > 1 && (tiles > kGatedCounters || (size_t)(tiles * want) * bm[t] * bn[t] * 4 > kGatedPartialBytes || steps < 2 * want)) break;
+            const int64_t per = std::max<int64_t>(1, (steps + want - 1) / want), splits = std::max<int64_t>(1, (steps + per - 1) / per);
+            const int64_t slots = (int64_t)num_cus * per_cu[t], rounds = (tiles * splits + slots - 1) / slots;
+            const double cost = rounds * (per * step_us[t] + once_us[t]) + (splits > 1 ? 4.0 + 0.5 * splits : 0.0);
+            if (cost < best) {
+                best = cost;
+                q.tile = t;
+                q.tiles_m = (int)tm;
+                q.tiles_n = (int)tn;
+                q.splits = (int)splits;
+                q.per_split = (int)per;
+            }
+        }
+    }
+}
+
+}  // namespace bmgd
+
+namespace {
+
+int fail(bmgd_gated* b, int code, const char* call, const char* what, const char* msg = "")
+{
+    snprintf(b->err, sizeof b->err, "%s: %s%s%s", call, what, *msg ? " " : "", msg);
+    return code;
+}
+
+int hip_fail(bmgd_gated* b, hipError_t e, const char* what)
+{
+    (void)hipGetLastError();
+    return fail(b, e == hipErrorOutOfMemory ? BMGD_ENOMEM : BMGD_EHIP, what, hipGetErrorString(e));
+}
+
+#define GATED_TRY(b, call)                                               \
+    do {                                                                 \
+        hipError_t e_ = (call);                                          \
+        if (e_ != hipSuccess) return hip_fail((b), e_, #call);           \
+    } while (0)
+
+// NULL if m describes rows x cols elements that a kernel can be given.
+const char* bad_matrix(const bmgd_matrix& m, int64_t rows, int64_t cols)
+{
+    if (rows == 0) return nullptr;
+    if (!m.data) return "must not be NULL";
+    if ((uintptr_t)m.data & 1) return "must be 2-byte aligned";
+    if (rows > 1 && m.stride < cols) return "has rows closer together than they are long";
+    if (m.stride > (int64_t(1) << 40)) return "has rows more than 2^40 elements apart";
+    return nullptr;
+}
+
+struct Named {
+    const char* name;
+    const bmgd_matrix* m;
+    int64_t rows, cols;
+    bool optional;
+};
+
+int check(bmgd_gated* b, const char* call, const Named* list, int n)
+{
+    for (int i = 0; i < n; ++i) {
+        if (list[i].optional && !list[i].m->data) continue;
+        if (const char* why = bad_matrix(*list[i].m, list[i].rows, list[i].cols))
+            return fail(b, BMGD_EINVAL, call, list[i].name, why);
+    }
+    return BMGD_OK;
+}
+
+// Operands as the kernels read them: rows of a multiple of eight elements, 16-byte aligned; others are copied to the workspace first.
+struct Operands {
+    bmgd_gated* b;
+    GatedPack pack{};
+
+    static bool direct(const bmgd_matrix& m, int64_t rows, int64_t cols)
+    {
+        return ((uintptr_t)m.data & 15) == 0 && cols % 8 == 0 && (rows <= 1 || m.stride % 8 == 0);
+    }
+    GatedMat copy(const bmgd_matrix& m, int64_t rows, int64_t cols, size_t area)
+    {
+        GatedPack::One& o = pack.m[pack.count++];
+        o.from = static_cast<const unsigned short*>(m.data);
+        o.to = reinterpret_cast<unsigned short*>(b->base + area);
+        o.from_ld = m.stride;
+        o.to_ld = up(cols, 8);
+        o.rows = rows;
+        o.cols = cols;
+        return GatedMat{o.to, o.to_ld};
+    }
+    GatedMat use(const bmgd_matrix& m, int64_t rows, int64_t cols, size_t area)
+    {
+        if (rows == 0) return GatedMat{b->base + area, up(cols, 8)};
+        if (direct(m, rows, cols)) return GatedMat{m.data, rows <= 1 ? cols : m.stride};
+        return copy(m, rows, cols, area);
+    }
+    // the two matrices that one product reads side by side: their rows are equally far apart
+    void use_pair(const bmgd_matrix& m, const bmgd_matrix& m2, int64_t rows, int64_t cols, size_t area, size_t area2, GatedMat* o, GatedMat* o2)
+    {
+        if (direct(m, rows, cols) && direct(m2, rows, cols) && (rows <= 1 || m.stride == m2.stride)) {
+            *o = GatedMat{m.data, rows <= 1 ? cols : m.stride};
+            *o2 = GatedMat{m2.data, o->ld};
+        } else {
+            *o = copy(m, rows, cols, area);
+            *o2 = copy(m2, rows, cols, area2);
+        }
+    }
+};
+
+GatedMat plain(const bmgd_matrix& m) { return GatedMat{m.data, m.stride}; }
+
+// Work of calls on different streams is made in the order of the calls: they share the workspace.
+int enter(bmgd_gated* b, hipStream_t s)
+{
+    GATED_TRY(b, hipSetDevice(b->device));
+    if (b->used && b->last != s) {
+        hipStreamCaptureStatus st = hipStreamCaptureStatusNone, st_last = hipStreamCaptureStatusNone;
+        GATED_TRY(b, hipStreamIsCapturing(s, &st));
+        if (st == hipStreamCaptureStatusNone) GATED_TRY(b, hipStreamIsCapturing(b->last, &st_last));
+        // (a graph's launches cannot wait for work outside it, nor that for them: the caller orders those)
+        if (st == hipStreamCaptureStatusNone && st_last == hipStreamCaptureStatusNone) {
+            GATED_TRY(b, hipEventRecord(b->order, b->last));
+            GATED_TRY(b, hipStreamWaitEvent(s, b->order, 0));
+        }
+    }
+    b->last = s;
+    b->used = true;
+    return BMGD_OK;
+}
+
+int launch(bmgd_gated* b, GatedProduct& q, GatedOp op, hipStream_t s)
+{
+    q.act = b->cfg.activation;
+    q.partial = reinterpret_cast<float*>(b->base + b->lay.partial);
+    q.counter = reinterpret_cast<unsigned*>(b->base + b->lay.counter);
+    q.zeros = b->base + b->lay.zeros;
+    gated_plan(q, op, b->num_cus);
+    const hipError_t e = b->cfg.dtype == BMGD_F16 ? gated_launch_f16(q, op, s) : gated_launch_bf16(q, op, s);
+    if (e != hipSuccess) return hip_fail(b, e, "launch of a product of the gated block");
+    return BMGD_OK;
+}
+
+#define GATED_DO(expr)                     \
+    do {                                   \
+        const int rc_ = (expr);            \
+        if (rc_ != BMGD_OK) return rc_;    \
+    } while (0)
+
+int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_t s)
+{
+    const bmgd_gated_config& c = b->cfg;
+    const Named list[] = {{"x", &t.x, rows, c.p, false},           {"gate", &t.gate, c.p, c.hidden, false}, {"up", &t.up, c.p, c.hidden, false},
+                          {"down", &t.down, c.hidden, c.out_n, false}, {"y", &t.y, rows, c.out_n, false},   {"g", &t.g, rows, c.hidden, true},
+                          {"u", &t.u, rows, c.hidden, true}};
+    GATED_DO(check(b, "bmgd_gated_forward", list, 7));
+    if (!t.g.data != !t.u.data) return fail(b, BMGD_EINVAL, "bmgd_gated_forward", "g and u are kept together or not at all");
+    if (rows == 0) return BMGD_OK;
+    GATED_DO(enter(b, s));
+    const int64_t half = up(c.hidden, 64);
+    Operands o{b};
+    const GatedMat x = o.use(t.x, rows, c.p, b->lay.x);
+    GatedMat gate, upw;
+    o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, &gate, &upw);
+    const GatedMat down = o.use(t.down, c.hidden, c.out_n, b->lay.down);
+    if (o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
+    const GatedMat h{b->base + b->lay.h, half};
+
+    GatedProduct q{};
+    q.a = x;
+    q.b = gate;
+    q.b2 = upw;
+    q.M = rows; q.N = c.hidden; q.K = c.p;
+    q.b_cols = up(c.hidden, 8);
+    q.half = half;
+    q.out = h;
+    q.g = plain(t.g);
+    q.u = plain(t.u);
+    GATED_DO(launch(b, q, kOpUp, s));
+
+    q = GatedProduct{};
+    q.a = h;
+    q.b = down;
+    q.M = rows; q.N = c.out_n; q.K = c.hidden;
+    q.b_cols = up(c.out_n, 8);
+    q.out = plain(t.y);
+    return launch(b, q, kOpMul, s);
+}
+
+int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_t s)
+{
+    const bmgd_gated_config& c = b->cfg;
+    const Named list[] = {{"dy", &t.dy, rows, c.out_n, false},  {"x", &t.x, rows, c.p, false},          {"gate", &t.gate, c.p, c.hidden, false},
+                          {"up", &t.up, c.p, c.hidden, false},  {"down", &t.down, c.hidden, c.out_n, false}, {"g", &t.g, rows, c.hidden, false},
+                          {"u", &t.u, rows, c.hidden, false},   {"dx", &t.dx, rows, c.p, true},         {"dgate", &t.dgate, c.p, c.hidden, true},
+                          {"dup", &t.dup, c.p, c.hidden, true}, {"ddown", &t.ddown, c.hidden, c.out_n, true}};
+    GATED_DO(check(b, "bmgd_gated_backward", list, 11));
+    if (!t.dgate.data != !t.dup.data) return fail(b, BMGD_EINVAL, "bmgd_gated_backward", "dgate and dup are wanted together or not at all");
+    GATED_DO(enter(b, s));
+    const int64_t half = up(c.hidden, 64);
+    Operands o{b};
+    const GatedMat x = o.use(t.x, rows, c.p, b->lay.x);
+    const GatedMat dy = o.use(t.dy, rows, c.out_n, b->lay.dy);
+    const GatedMat down = o.use(t.down, c.hidden, c.out_n, b->lay.down);
+    if (rows && o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
+    const GatedMat h{b->base + b->lay.h, half}, d{b->base + b->lay.d, 2 * half};
+
+    GatedProduct q{};
+    if (rows) {
+        q.a = dy;
+        q.b = down;
+        q.M = rows; q.N = c.hidden; q.K = up(c.out_n, 8);
+        q.half = half;
+        q.out = h;
+        q.out2 = d;
+        q.g = plain(t.g);
+        q.u = plain(t.u);
+        GATED_DO(launch(b, q, kOpDown, s));
+    }
+    if (rows && t.dx.data) {
+        o.pack = GatedPack{};
+        GatedMat gate, upw;
+        o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, &gate, &upw);
+        if (o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
+        q = GatedProduct{};
+        q.a = d;
+        q.b = gate;
+        q.b2 = upw;
+        q.M = rows; q.N = c.p; q.K = up(c.hidden, 8);
+        q.half = half;
+        q.out = plain(t.dx);
+        GATED_DO(launch(b, q, kOpInput, s));
+    }
+    if (t.ddown.data) {
+        q = GatedProduct{};
+        q.a = h;
+        q.b = dy;
+        q.M = c.hidden; q.N = c.out_n; q.K = rows;
+        q.a_cols = half;
+        q.b_cols = up(c.out_n, 8);
+        q.out = plain(t.ddown);
+        GATED_DO(launch(b, q, kOpWeight, s));
+    }
+    if (t.dgate.data) {
+        q = GatedProduct{};
+        q.a = x;
+        q.b = d;
+        q.M = c.p; q.N = c.hidden; q.K = rows;
+        q.a_cols = up(c.p, 8);
+        q.b_cols = 2 * half;
+        q.half = half;
+        q.out = plain(t.dgate);
+        q.out2 = plain(t.dup);
+        GATED_DO(launch(b, q, kOpWeight, s));
+    }
+    return BMGD_OK;
+}
+
+void destroy(bmgd_gated* b)
+{
+    if (!b) return;
+    int current = -1;
+    (void)hipGetDevice(&current);
+    if (hipSetDevice(b->device) == hipSuccess) {
+        if (b->used) (void)hipDeviceSynchronize();
+        if (b->order) (void)hipEventDestroy(b->order);
+        if (b->owned && b->base) (void)hipFree(b->base);
+    }
+    if (current >= 0) (void)hipSetDevice(current);
+    (void)hipGetLastError();
+    delete b;
+}
+
+}  // namespace
+
+#define BMGD_API __attribute__((visibility("default")))
+
+extern "C" {
+
+BMGD_API size_t bmgd_gated_workspace_bytes(const bmgd_gated_config* cfg)
+{
+    const char* why = "";
+    return cfg && valid(*cfg, &why) ? make_layout(*cfg).total : 0;
+}
+
+BMGD_API int bmgd_gated_create(const bmgd_gated_config* cfg, bmgd_gated** out)
+{
+    if (out) *out = nullptr;
+    if (!cfg || !out) return fail_static(BMGD_EINVAL, "bmgd_gated_create", "cfg and out must not be NULL");
+    const char* why = "";
+    if (!valid(*cfg, &why)) return fail_static(BMGD_EINVAL, "bmgd_gated_create", why);
+    const Layout lay = make_layout(*cfg);
+    if (cfg->workspace && ((uintptr_t)cfg->workspace & 255)) return fail_static(BMGD_EINVAL, "bmgd_gated_create", "workspace must be 256-byte aligned");
+    if (cfg->workspace && cfg->workspace_bytes < lay.total) return fail_static(BMGD_ENOMEM, "bmgd_gated_create", "workspace too small");
+    int ndev = 0;
+    if (hipGetDeviceCount(&ndev) != hipSuccess || ndev == 0) {
+        (void)hipGetLastError();
+        return fail_static(BMGD_EHIP, "bmgd_gated_create", "no HIP device available");
+    }
+    bmgd_gated* b = new (std::nothrow) bmgd_gated();
+    if (!b) return fail_static(BMGD_ENOMEM, "bmgd_gated_create", "out of host memory");
+    b->cfg = *cfg;
+    b->lay = lay;
+    auto bail = [&](hipError_t e, const char* what) {
+        const int code = hip_fail(b, e, what);
+        set_create_error(b->err);
+        destroy(b);
+        return code;
+    };
+    hipError_t e = hipGetDevice(&b->device);
+    if (e != hipSuccess) return bail(e, "hipGetDevice");
+    e = hipDeviceGetAttribute(&b->num_cus, hipDeviceAttributeMultiprocessorCount, b->device);
+    if (e != hipSuccess) return bail(e, "hipDeviceGetAttribute");
+    e = cfg->dtype == BMGD_F16 ? gated_prepare_f16() : gated_prepare_bf16();
+    if (e != hipSuccess) return bail(e, "hipFuncSetAttribute");
+    e = hipEventCreateWithFlags(&b->order, hipEventDisableTiming);
+    if (e != hipSuccess) return bail(e, "hipEventCreateWithFlags");
+    if (cfg->workspace) {
+        b->base = static_cast<char*>(cfg->workspace);
+    } else {
+        void* p = nullptr;
+        e = hipMalloc(&p, lay.total);
+        if (e != hipSuccess) return bail(e, "hipMalloc");
+        b->base = static_cast<char*>(p);
+        b->owned = true;
+    }
+    e = launch_fill_zero(b->base + lay.counter, lay.total - lay.counter, nullptr);
+    if (e == hipSuccess) e = hipStreamSynchronize(nullptr);
+    if (e != hipSuccess) return bail(e, "clearing the workspace");
+    *out = b;
+    return BMGD_OK;
+}
+
+BMGD_API int bmgd_gated_forward(bmgd_gated* block, int64_t rows, const bmgd_gated_tensors* t, void* stream)
+{
+    if (!block) return fail_static(BMGD_EINVAL, "bmgd_gated_forward", "block must not be NULL");
+    if (!t) return fail(block, BMGD_EINVAL, "bmgd_gated_forward", "tensors must not be NULL");
+    if (rows < 0 || rows > block->cfg.max_rows) return fail(block, BMGD_EINVAL, "bmgd_gated_forward", "rows must be in [0, max_rows]");
+    return forward(block, rows, *t, static_cast<hipStream_t>(stream));
+}
+
+BMGD_API int bmgd_gated_backward(bmgd_gated* block, int64_t rows, const bmgd_gated_tensors* t, void* stream)
+{
+    if (!block) return fail_static(BMGD_EINVAL, "bmgd_gated_backward", "block must not be NULL");
+    if (!t) return fail(block, BMGD_EINVAL, "bmgd_gated_backward", "tensors must not be NULL");
+    if (rows < 0 || rows > block->cfg.max_rows) return fail(block, BMGD_EINVAL, "bmgd_gated_backward", "rows must be in [0, max_rows]");
+    return backward(block, rows, *t, static_cast<hipStream_t>(stream));
+}
+
+BMGD_API const char* bmgd_gated_last_error(const bmgd_gated* block)
+{
+    return block ? block->err : bmgd_last_error(nullptr);
+}
+
+BMGD_API void bmgd_gated_destroy(bmgd_gated* block) { destroy(block); }
+
+}  // extern "C"

@@ -1,0 +1,68 @@
+// Internal interfaces between the host code of the gated block (gated_block.hip) and its kernels.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace bmgd {
+
+enum { kActSilu = 0, kActGelu = 1, kActRelu = 2 };
+
+// A product that the block is made of.  "Adjacent" operands have the elements of the summed index next to each other in memory,
+// "strided" ones a row of the matrix per value of the summed index.
+enum GatedOp {
+    kOpUp = 0,          // [G | U] = X [Wg | Wu]: left adjacent, right strided; H = act(G) * U leaves the kernel, G and U on request
+    kOpMul = 1,         // Y = H Wd: left adjacent, right strided
+    kOpDown = 2,        // dH = dY Wd': both adjacent; H, dG and dU leave the kernel
+    kOpInput = 3,       // dX = dG Wg' + dU Wu': both adjacent, the sum runs over both halves
+    kOpWeight = 4       // dWd = H' dY, [dWg | dWu] = X' [dG | dU]: both strided
+};
+
+struct GatedMat {
+    void* p;
+    int64_t ld;         // elements from one row to the next
+};
+
+struct GatedProduct {
+    GatedMat a;         // left operand
+    GatedMat b, b2;     // right operand; its second half for kOpUp and kOpInput
+    int64_t M, N, K;    // rows and columns of the result as stored, length of the sum.  kOpUp: N = hidden; kOpInput: K = hidden, the
+                        // length of one half; kOpWeight with two halves: N = hidden, the columns of one
+    int64_t a_cols, b_cols;             // strided operands: columns that may be read (a multiple of 8)
+    int64_t half;       // kOpUp, kOpDown: hidden rounded up to 64, the columns of H and of each half of D (zeros behind hidden);
+                        // kOpInput: the columns of each half of the left operand; kOpWeight: 0, or the columns of each half of the right operand
+    GatedMat out, out2; // result; kOpUp, kOpDown: H in `out`, kOpDown: D = [dG | dU] in `out2`
+    GatedMat g, u;      // kOpUp: written unless NULL; kOpDown: read
+    int act;
+    // how the result is cut into tiles: filled in by gated_plan
+    int tile;           // kTile*
+    int tiles_m, tiles_n, splits, per_split;    // tiles of the result; workgroups that share a tile's sum, and their share in steps of 64
+    float* partial;     // their sums
+    unsigned* counter;  // and how many of them have arrived, per tile; zero between launches
+    const void* zeros;  // 256 bytes of zeros
+};
+
+enum { kTileLarge = 0, kTileMedium = 1, kTileSmall = 2, kTiles = 3 };
+
+// Bytes of partial sums, and tiles, that a product may use where workgroups share tiles.
+constexpr size_t kGatedPartialBytes = size_t(64) << 20;
+constexpr int kGatedCounters = 4096;
+
+// Chooses tile and split.
+void gated_plan(GatedProduct& q, GatedOp op, int num_cus);
+
+// Once per process and device: lets the kernels use as much shared memory as they need.
+hipError_t gated_prepare_bf16();
+hipError_t gated_prepare_f16();
+hipError_t gated_launch_bf16(const GatedProduct& q, GatedOp op, hipStream_t stream);
+hipError_t gated_launch_f16(const GatedProduct& q, GatedOp op, hipStream_t stream);
+
+// Copies of up to four matrices of 16-bit elements whose rows cannot be read in pieces of 16 bytes: rows of `to_ld` elements (a multiple of
+// 8), zeros behind the last column.
+struct GatedPack {
+    struct One { const unsigned short* from; unsigned short* to; int64_t from_ld, to_ld, rows, cols; } m[4];
+    int count;
+};
+hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream);
+
+}  // namespace bmgd

@@ -1,0 +1,474 @@
+// The products of the gated block on the matrix cores, one kernel template for all five (see GatedOp).
+//
+// A workgroup makes a tile of BM x BN results.  Steps of 64 along the summed index go from memory straight to shared memory, one step ahead
+// of the matrix instructions, 16 bytes a lane.
+//   adjacent operand   tile [rows][64]: 128 bytes a row, eight pieces of 16; piece c of row r lies in place c ^ (r & 7), so that the 16 rows
+//                      that an instruction's lanes read at the same piece lie in different banks
+//   strided operand    tile [64][columns]; read with the transposing read of shared memory: of 16 lanes each gives the address of four
+//                      neighbouring columns (four lanes to a row, four rows), and gets four rows of one column.  Piece c of row k lies in
+//                      place c ^ (2 (k & 3) + 8 (k >> 3 & 1)): the rows that are read together lie in different banks
+// The instruction (v_mfma_f32_16x16x32: a = A[lane % 16][8 (lane / 16) + i], b = B[8 (lane / 16) + i][lane % 16], c[v] = C[4 (lane / 16) + v][lane % 16])
+// forms the transpose of the result, so that a lane ends with four neighbouring columns of a row.
+// Sums are in fp32.  Where few tiles leave compute units idle several workgroups share a tile's sum: each writes its part, the last one to
+// arrive adds the parts in the order of their index (the result does not depend on who was last) and goes on.
+#pragma once
+
+#include "gated_internal.h"
+#include "lds_load.h"
+
+#include <hip/hip_runtime.h>
+
+namespace bmgd {
+namespace {
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) short4v lds_short4;
+typedef __attribute__((address_space(3))) short8v lds_short8;
+
+template <typename T> struct Half;
+template <> struct Half<__bf16> {
+    static __device__ __forceinline__ float4v mma(short8v a, short8v b, float4v c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    }
+};
+template <> struct Half<_Float16> {
+    static __device__ __forceinline__ float4v mma(short8v a, short8v b, float4v c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+};
+
+// act(g) and its derivative.  silu g s, s = 1 / (1 + e^-g): derivative s (1 + g (1 - s)); gelu g F(g), F the normal distribution's: F + g f;
+// relu: 0 at 0.  s and F keep their relative accuracy far out on the left, where they are small (an exponential of -|g|, the complement of the error
+// function); the reciprocal is the hardware's (2^-23), of a number between 1 and 2.
+__device__ __forceinline__ float logistic(float g)
+{
+    const float e = expf(-fabsf(g));
+    return (g < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
+}
+__device__ __forceinline__ float normal_cdf(float g) { return 0.5f * erfcf(g * -0.70710678118654752f); }
+
+__device__ __forceinline__ float act_value(int act, float g)
+{
+    if (act == kActSilu) return g * logistic(g);
+    if (act == kActGelu) return g * normal_cdf(g);
+    return g <= 0.f ? 0.f : g;
+}
+
+__device__ __forceinline__ float act_both(int act, float g, float& slope)
+{
+    if (act == kActSilu) {
+        const float s = logistic(g);
+        slope = s * (1.f + g * (1.f - s));
+        return g * s;
+    }
+    if (act == kActGelu) {
+        const float cdf = normal_cdf(g);
+        slope = cdf + g * (0.39894228040143268f * __expf(-0.5f * g * g));
+        return g * cdf;
+    }
+    slope = g <= 0.f ? 0.f : 1.f;
+    return g <= 0.f ? 0.f : g;
+}
+
+template <typename T> __device__ __forceinline__ short bits_of(float x)
+{
+    const T t = (T)x;
+    return __builtin_bit_cast(short, t);
+}
+template <typename T> __device__ __forceinline__ float value_of(short b) { return (float)__builtin_bit_cast(T, b); }
+
+template <typename T> __device__ __forceinline__ short4v bits4(float4v x)
+{
+    short4v r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = bits_of<T>(x[i]);
+    return r;
+}
+
+__device__ __forceinline__ bool whole4(const GatedMat& m)    // four elements of a row at a multiple of four can be moved as 8 bytes
+{
+    return ((uintptr_t)m.p & 7) == 0 && (m.ld & 3) == 0;
+}
+
+// Four neighbouring elements of row r from column c on, as far as there are `cols` columns.
+__device__ __forceinline__ void store4(const GatedMat& m, int64_t r, int64_t c, int64_t cols, bool whole, short4v v)
+{
+    short* to = (short*)m.p + r * m.ld + c;
+    if (whole && c + 4 <= cols) {
+        *(short4v*)to = v;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (c + i < cols) to[i] = v[i];
+    }
+}
+
+__device__ __forceinline__ short4v load4(const GatedMat& m, int64_t r, int64_t c, int64_t cols, bool whole)
+{
+    const short* from = (const short*)m.p + r * m.ld + c;
+    if (whole && c + 4 <= cols) return *(const short4v*)from;
+    short4v v = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (c + i < cols) v[i] = from[i];
+    return v;
+}
+
+constexpr int kStep = 64;                                     // elements of the summed index per step
+
+// Wait until at most N of this wavefront's loads to shared memory are on their way and its reads of shared memory are done, then for the others.
+template <int N> __device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
+}
+
+// One operand's way to shared memory: R rows (adjacent) or columns (strided) of the tile, by `THREADS` threads.
+template <bool ADJ, int R, int THREADS> struct Mover {
+    static constexpr int kPieces = R * 8 / THREADS;           // 16-byte pieces a thread moves per step
+    static_assert(R * 8 % THREADS == 0, "");
+    static constexpr int kRow = ADJ ? 8 : R / 8;              // pieces in a row of the tile
+    const unsigned short* src[kPieces];
+    int at;                                                   // adjacent: the piece's place along the sum; strided: the first piece's row
+
+    static __device__ __forceinline__ int turn(int k)         // strided: how row k's pieces are turned
+    {
+        return 2 * (k & 3) + (R >= 128 ? 8 * ((k >> 3) & 1) : 0);
+    }
+    // Adjacent: element (row, k) at base + row * ld + k, rows of the tile from r0 on, `limit` rows in all.
+    // Strided: element (k, column) at base + k * ld + column, columns from r0 on, `limit` columns that may be read.
+    // pick(piece) turns a strided tile's piece into (base, column); the default is `base` and r0 + 8 piece.
+    template <typename Pick>
+    __device__ __forceinline__ void start(int64_t r0, int64_t limit, int64_t ld, int64_t k0, int tid, Pick pick)
+    {
+        if constexpr (ADJ) {
+            const int s = tid & 7;
+            at = 8 * (s ^ ((tid >> 3) & 7));                  // (rows of one thread's pieces are multiples of 8 apart)
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                int64_t r = r0 + i * (THREADS / 8) + (tid >> 3);
+                if (r >= limit) r = limit - 1;
+                src[i] = pick(0) + r * ld + k0 + at;
+            }
+        } else {
+            at = tid / kRow;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int k = i * (THREADS / kRow) + tid / kRow;
+                const int c = (tid % kRow) ^ turn(k);
+                src[i] = pick(c) + (k0 + k) * ld;
+            }
+        }
+    }
+    // Requests the next step; `left` elements of the sum are left (what is behind them is taken as zero).
+    __device__ __forceinline__ void request(unsigned lds, int64_t ld, int64_t left, const unsigned short* zeros)
+    {
+        if (left >= kStep) {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) load_to_lds(src[i], lds + i * THREADS * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int k = ADJ ? at : at + i * (THREADS / kRow);
+                load_to_lds(k < left ? src[i] : zeros, lds + i * THREADS * 16);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) src[i] += ADJ ? (int64_t)kStep : kStep * ld;
+    }
+};
+
+// Operands of an instruction from the tile: fragment f covers rows (columns) first + 16 f .. + 15, summed index 32 h + 8 (lane / 16) + i.
+template <bool ADJ, int R> struct Reader {
+    int lane_off;                                             // adjacent: bytes of this lane's place for h = 0 ...
+    int other;                                                // ... and for h = 1; strided: the lane's turn
+    int first;
+    __device__ __forceinline__ void start(int first_, int lane)
+    {
+        first = first_;
+        const int i = lane & 15, q = lane >> 4;
+        if constexpr (ADJ) {
+            lane_off = (first + i) * 128 + ((q ^ (i & 7)) << 4);
+            other = (first + i) * 128 + (((4 + q) ^ (i & 7)) << 4);
+        } else {
+            lane_off = (8 * q + (i >> 2)) * (2 * R) + ((i & 1) << 3) + (((i & 3) >> 1) << 4);
+            other = 2 * (i >> 2) + (R >= 128 ? 8 * (q & 1) : 0);
+        }
+    }
+    __device__ __forceinline__ short8v read(unsigned tile, int f, int h) const
+    {
+        if constexpr (ADJ) {
+            return *(lds_short8*)(size_t)(tile + (h ? other : lane_off) + f * 16 * 128);
+        } else {
+            const unsigned at = tile + lane_off + ((((first >> 3) + 2 * f) ^ other) << 4) + h * 32 * 2 * R;
+            const short4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(size_t)at);
+            const short4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4*)(size_t)(at + 4 * 2 * R));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+    }
+};
+
+template <int TILE> struct Shape;
+template <> struct Shape<kTileLarge> { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4; };       // tile; wavefronts along rows and columns
+template <> struct Shape<kTileMedium> { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2; };
+template <> struct Shape<kTileSmall> { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2; };
+
+template <int TILE> constexpr int tile_threads() { return 64 * Shape<TILE>::WM * Shape<TILE>::WN; }
+template <int TILE> constexpr unsigned tile_lds() { return 2u * (Shape<TILE>::BM + Shape<TILE>::BN) * 128u; }
+
+template <typename T, GatedOp OP, int TILE>
+__global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(GatedProduct q)
+{
+    using S = Shape<TILE>;
+    constexpr int threads = tile_threads<TILE>(), BM = S::BM, BN = S::BN;
+    constexpr int wm = BM / S::WM, wn = BN / S::WN, fm = wm / 16, fn = wn / 16;    // of a wavefront
+    constexpr bool a_adj = OP != kOpWeight, b_adj = OP == kOpDown || OP == kOpInput;
+    constexpr unsigned a_bytes = BM * 128, b_bytes = BN * 128;
+    extern __shared__ __align__(1024) unsigned short stage[];
+    __shared__ unsigned arrived;
+    const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned short*)stage;
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // Workgroups go to the eight dies in turn: a die gets neighbouring tiles, whose operands its L2 then holds.
+    const int total = q.tiles_m * q.tiles_n * q.splits;
+    int id = blockIdx.x;
+    {
+        const int die = id & 7, each = total >> 3, more = total & 7;
+        id = die * each + min(die, more) + (id >> 3);
+    }
+    const int split = id % q.splits;
+    const int tile = id / q.splits;
+    constexpr int kGroup = 8;                                  // tile rows that are walked through together
+    const int group = tile / (kGroup * q.tiles_n), in_group = tile % (kGroup * q.tiles_n);
+    const int rows_here = min(kGroup, q.tiles_m - group * kGroup);
+    const int tm = group * kGroup + in_group % rows_here, tn = in_group / rows_here;
+    const int64_t m0 = (int64_t)tm * BM;
+    const int64_t n0 = (int64_t)tn * (OP == kOpUp ? BN / 2 : BN);
+
+    // the share of the sum: steps [s0, s1); kOpInput: the steps of the first half, then those of the second
+    const int64_t len = OP == kOpInput ? 2 * q.half : q.K;
+    const int steps = (int)((len + kStep - 1) / kStep);
+    const int s0 = split * q.per_split, s1 = min(steps, s0 + q.per_split);
+    const unsigned short* zeros = (const unsigned short*)q.zeros;
+
+    Mover<a_adj, BM, threads> ma;
+    Mover<b_adj, BN, threads> mb;
+    const unsigned short* pa = (const unsigned short*)q.a.p;
+    const unsigned short* pb = (const unsigned short*)q.b.p;
+    const unsigned short* pb2 = (const unsigned short*)q.b2.p;
+    ma.start(m0, q.M, q.a.ld, (int64_t)s0 * kStep, tid, [&](int c) {
+        if constexpr (a_adj) return pa;
+        else { const int64_t col = m0 + 8 * c; return pa + (col < q.a_cols ? col : q.a_cols - 8); }
+    });
+    const int half_steps = OP == kOpInput ? (int)(q.half / kStep) : 0;
+    auto start_b = [&](int step) {
+        const bool second = OP == kOpInput && step >= half_steps;
+        mb.start(n0, q.N, q.b.ld, (int64_t)(second ? step - half_steps : step) * kStep, tid, [&](int c) {
+            if constexpr (b_adj) return second ? pb2 : pb;
+            else if constexpr (OP == kOpUp) {                  // a wavefront's columns: wn / 2 of Wg, then the same of Wu
+                const int w = c / (wn / 8), in = c % (wn / 8);
+                const int64_t col = n0 + w * (wn / 2) + (in % (wn / 16)) * 8;
+                return (in >= wn / 16 ? pb2 : pb) + (col < q.b_cols ? col : q.b_cols - 8);
+            } else { const int64_t col = n0 + 8 * c; return pb + (col < q.b_cols ? col : q.b_cols - 8); }
+        });
+    };
+    start_b(s0);
+    const unsigned lds_a = lds0 + (unsigned)__builtin_amdgcn_readfirstlane(wave * 1024), lds_b = lds_a + 2 * a_bytes;
+    auto request = [&](int step, int buf) {
+        const int64_t k0 = (int64_t)step * kStep;
+        // the left operand of kOpMul and kOpInput has zeros behind its columns
+        ma.request(lds_a + buf * a_bytes, q.a.ld, OP == kOpMul || OP == kOpInput ? (int64_t)kStep : q.K - k0, zeros);
+        if constexpr (OP == kOpInput) {
+            if (step == half_steps && step > s0) start_b(step);
+            mb.request(lds_b + buf * b_bytes, q.b.ld, q.K - (step >= half_steps ? k0 - q.half : k0), zeros);
+        } else {
+            mb.request(lds_b + buf * b_bytes, q.b.ld, q.K - k0, zeros);
+        }
+    };
+
+    Reader<a_adj, BM> ra;
+    Reader<b_adj, BN> rb;
+    const int wrow = (wave / S::WN) * wm, wcol = (wave % S::WN) * wn;
+    ra.start(wrow, lane);
+    rb.start(wcol, lane);
+
+    float4v acc[fm][fn];
+#pragma unroll
+    for (int i = 0; i < fm; ++i)
+#pragma unroll
+        for (int j = 0; j < fn; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
+
+    if (s0 < s1) request(s0, 0);
+    for (int s = s0; s < s1; ++s) {
+        const int buf = (s - s0) & 1;
+        wait_and_meet<0>();
+        if (s + 1 < s1) request(s + 1, buf ^ 1);
+        const unsigned ta = lds0 + buf * a_bytes, tb = lds0 + 2 * a_bytes + buf * b_bytes;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            short8v af[fm], bf[fn];
+#pragma unroll
+            for (int j = 0; j < fn; ++j) bf[j] = rb.read(tb, j, h);
+#pragma unroll
+            for (int i = 0; i < fm; ++i) af[i] = ra.read(ta, i, h);
+#pragma unroll
+            for (int i = 0; i < fm; ++i)
+#pragma unroll
+                for (int j = 0; j < fn; ++j) acc[i][j] = Half<T>::mma(bf[j], af[i], acc[i][j]);
+        }
+    }
+
+    if (q.splits > 1) {
+        // The parts of a tile, [split][fragment][thread] of four floats.  Written, made visible beyond the die, counted; the last one adds them up.
+        float4v* part = (float4v*)q.partial + (size_t)tile * q.splits * (fm * fn) * threads;
+        float4v* mine = part + (size_t)split * (fm * fn) * threads + tid;
+#pragma unroll
+        for (int i = 0; i < fm; ++i)
+#pragma unroll
+            for (int j = 0; j < fn; ++j) mine[(i * fn + j) * threads] = acc[i][j];
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) arrived = atomicAdd(q.counter + tile, 1u);
+        __syncthreads();
+        if (arrived != (unsigned)q.splits - 1) return;
+        __threadfence();
+        if (tid == 0) q.counter[tile] = 0;                     // for the next launch
+#pragma unroll
+        for (int i = 0; i < fm; ++i)
+#pragma unroll
+            for (int j = 0; j < fn; ++j) acc[i][j] = part[(i * fn + j) * threads + tid];
+        for (int p = 1; p < q.splits; ++p) {
+            const float4v* next = part + (size_t)p * (fm * fn) * threads + tid;
+#pragma unroll
+            for (int i = 0; i < fm; ++i)
+#pragma unroll
+                for (int j = 0; j < fn; ++j) acc[i][j] += next[(i * fn + j) * threads];
+        }
+    }
+
+    // A lane holds row m and columns n .. n + 3 of every fragment.
+    const int64_t m = m0 + wrow + (lane & 15);
+    const int cq = 4 * (lane >> 4);
+    if constexpr (OP == kOpUp) {
+        const bool keep = q.g.p != nullptr, wg = whole4(q.g), wu = whole4(q.u);
+#pragma unroll
+        for (int i = 0; i < fm; ++i) {
+            const int64_t r = m + 16 * i;
+            if (r >= q.M) continue;
+#pragma unroll
+            for (int j = 0; j < fn / 2; ++j) {
+                const int64_t c = n0 + (wave % S::WN) * (wn / 2) + 16 * j + cq;
+                if (c >= q.half) continue;
+                const float4v g = acc[i][j], u = acc[i][j + fn / 2];
+                float4v h;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) h[v] = c + v < q.N ? act_value(q.act, g[v]) * u[v] : 0.f;
+                store4(q.out, r, c, q.half, true, bits4<T>(h));
+                if (keep) {
+                    store4(q.g, r, c, q.N, wg, bits4<T>(g));
+                    store4(q.u, r, c, q.N, wu, bits4<T>(u));
+                }
+            }
+        }
+    } else if constexpr (OP == kOpDown) {
+        const bool wg = whole4(q.g), wu = whole4(q.u);
+#pragma unroll
+        for (int i = 0; i < fm; ++i) {
+            const int64_t r = m + 16 * i;
+            if (r >= q.M) continue;
+#pragma unroll
+            for (int j = 0; j < fn; ++j) {
+                const int64_t c = n0 + wcol + 16 * j + cq;
+                if (c >= q.half) continue;
+                const short4v gb = load4(q.g, r, c, q.N, wg), ub = load4(q.u, r, c, q.N, wu);
+                float4v h, dg, du;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    float slope;
+                    const float u = value_of<T>(ub[v]), a = act_both(q.act, value_of<T>(gb[v]), slope), dh = acc[i][j][v];
+                    const bool in = c + v < q.N;
+                    h[v] = in ? a * u : 0.f;
+                    du[v] = in ? dh * a : 0.f;
+                    dg[v] = in ? dh * u * slope : 0.f;
+                }
+                store4(q.out, r, c, q.half, true, bits4<T>(h));
+                store4(q.out2, r, c, q.half, true, bits4<T>(dg));
+                store4(q.out2, r, c + q.half, 2 * q.half, true, bits4<T>(du));
+            }
+        }
+    } else {
+        const bool w1 = whole4(q.out), w2 = whole4(q.out2);
+#pragma unroll
+        for (int i = 0; i < fm; ++i) {
+            const int64_t r = m + 16 * i;
+            if (r >= q.M) continue;
+#pragma unroll
+            for (int j = 0; j < fn; ++j) {
+                const int64_t c = n0 + wcol + 16 * j + cq;
+                if (OP == kOpWeight && q.half) {               // (q.half is a multiple of 64: four columns never straddle)
+                    const bool second = c >= q.half;
+                    store4(second ? q.out2 : q.out, r, second ? c - q.half : c, q.N, second ? w2 : w1, bits4<T>(acc[i][j]));
+                } else {
+                    store4(q.out, r, c, q.N, w1, bits4<T>(acc[i][j]));
+                }
+            }
+        }
+    }
+}
+
+template <typename T, GatedOp OP, int TILE> hipError_t prepare_tile()
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(&gated_tile_kernel<T, OP, TILE>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                               (int)tile_lds<TILE>());
+}
+
+template <typename T, GatedOp OP> hipError_t prepare_op()
+{
+    hipError_t e = prepare_tile<T, OP, kTileLarge>();
+    if (e == hipSuccess) e = prepare_tile<T, OP, kTileMedium>();
+    if (e == hipSuccess) e = prepare_tile<T, OP, kTileSmall>();
+    return e;
+}
+
+template <typename T> hipError_t prepare_all()
+{
+    hipError_t e = prepare_op<T, kOpUp>();
+    if (e == hipSuccess) e = prepare_op<T, kOpMul>();
+    if (e == hipSuccess) e = prepare_op<T, kOpDown>();
+    if (e == hipSuccess) e = prepare_op<T, kOpInput>();
+    if (e == hipSuccess) e = prepare_op<T, kOpWeight>();
+    return e;
+}
+
+template <typename T, GatedOp OP, int TILE> hipError_t launch_tile(const GatedProduct& q, hipStream_t stream)
+{
+    hipLaunchKernelGGL((gated_tile_kernel<T, OP, TILE>), dim3((unsigned)(q.tiles_m * q.tiles_n * q.splits)), dim3(tile_threads<TILE>()),
+                       tile_lds<TILE>(), stream, q);
+    return hipGetLastError();
+}
+
+template <typename T, GatedOp OP> hipError_t launch_op(const GatedProduct& q, hipStream_t stream)
+{
+    if (q.tile == kTileLarge) return launch_tile<T, OP, kTileLarge>(q, stream);
+    if (q.tile == kTileMedium) return launch_tile<T, OP, kTileMedium>(q, stream);
+    return launch_tile<T, OP, kTileSmall>(q, stream);
+}
+
+template <typename T> hipError_t launch_any(const GatedProduct& q, GatedOp op, hipStream_t stream)
+{
+    switch (op) {
+    case kOpUp: return launch_op<T, kOpUp>(q, stream);
+    case kOpMul: return launch_op<T, kOpMul>(q, stream);
+    case kOpDown: return launch_op<T, kOpDown>(q, stream);
+    case kOpInput: return launch_op<T, kOpInput>(q, stream);
+    default: return launch_op<T, kOpWeight>(q, stream);
+    }
+}
+
+}  // namespace
+}  // namespace bmgd

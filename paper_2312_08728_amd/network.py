@@ -1,0 +1,202 @@
+"""Gated block and AdamW step on torch tensors (bmgd_gated_*, bmgd_adamw_* of include/bmgd.h).
+
+Checks shapes, types and devices, fills in addresses and strides, and calls the library: no arithmetic happens here.
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import torch
+
+from . import binding as B
+
+_TYPES = {B.BMGD_BF16: torch.bfloat16, B.BMGD_F16: torch.float16, B.BMGD_F32: torch.float32}
+_CODES = {v: k for k, v in _TYPES.items()}
+_ROWS = object()                    # in place of a matrix's number of rows: that of the call
+
+
+class GatedBlock:
+    """Y = (act(X Wg) * (X Wu)) Wd with its backward pass, for up to `max_rows` rows a call; holds a workspace, no weights.
+
+    Matrices are torch tensors on the block's device, of type `dtype` (BMGD_BF16 or BMGD_F16), rows any distance apart.
+    """
+
+    def __init__(self, p, hidden, out_n, max_rows, dtype=B.BMGD_BF16, activation=B.BMGD_ACT_SILU, workspace=None):
+        cfg = B.bmgd_gated_config(p, hidden, out_n, max_rows, dtype, activation, None, 0)
+        if workspace is not None:
+            cfg.workspace, cfg.workspace_bytes = B._ptr(workspace), workspace.numel() * workspace.element_size()
+        self.h = None
+        self.cfg, self._keep = cfg, workspace
+        rc, h = B.bmgd_gated_create(cfg)
+        if rc != B.BMGD_OK:
+            raise B.BmgdError(rc, B.bmgd_last_error(None))
+        self.h = h
+        self._type = _TYPES[dtype]
+        self._device = torch.device("cuda", torch.cuda.current_device())
+        self._x, self._in, self._out, self._hid = (_ROWS, p), (p, hidden), (hidden, out_n), (_ROWS, hidden)
+        self._y = (_ROWS, out_n)
+
+    def _matrix(self, name, t, shape, rows):
+        n = rows if shape[0] is _ROWS else shape[0]
+        if t.dtype is not self._type or t.device != self._device:
+            raise ValueError(f"{name}: a {self._type} tensor on {self._device} is wanted, not {t.dtype} on {t.device}")
+        if t.dim() != 2 or t.shape[0] != n or t.shape[1] != shape[1]:
+            raise ValueError(f"{name}: shape {(n, shape[1])} is wanted, not {tuple(t.shape)}")
+        row, col = t.stride()
+        if col != 1 and shape[1] != 1:
+            raise ValueError(f"{name}: the elements of a row must lie next to each other (strides {t.stride()})")
+        return t.data_ptr(), row
+
+    def _call(self, fn, rows, list_, stream):
+        flat = []
+        for name, t, shape in list_:
+            flat += (0, 0) if t is None else self._matrix(name, t, shape, rows)
+        rc = fn(self.h, rows, (C.c_int64 * 24)(*flat), B._stream(stream))
+        if rc != B.BMGD_OK:
+            raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
+
+    def forward(self, x, gate, up, down, y, g=None, u=None, stream=None):
+        """y <- Y (and g <- G, u <- U, which `backward` needs).  Asynchronous."""
+        none = (None, None, None)
+        self._call(B.lib.bmgd_gated_forward, x.shape[0],
+                   [("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), ("y", y, self._y),
+                    ("g", g, self._hid), ("u", u, self._hid), none, none, none, none, none], stream)
+
+    def backward(self, dy, x, gate, up, down, g, u, dx=None, dgate=None, dup=None, ddown=None, stream=None):
+        """The gradients that are asked for (dgate and dup together) are written, from dy and the forward call's g and u.  Asynchronous."""
+        self._call(B.lib.bmgd_gated_backward, x.shape[0],
+                   [("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), (None, None, None),
+                    ("g", g, self._hid), ("u", u, self._hid), ("dy", dy, self._y), ("dx", dx, self._x), ("dgate", dgate, self._in),
+                    ("dup", dup, self._in), ("ddown", ddown, self._out)], stream)
+
+    def close(self):
+        if getattr(self, "h", None):
+            B.bmgd_gated_destroy(self.h)
+            self.h = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class AdamW:
+    """AdamW over the fp32 tensors `thetas` with the gradients that stand in the tensors `grads` at the time of a step.
+
+    grads: of one type (fp32, bf16, f16), sized like thetas; `set_grads` names others.
+    copies: None, or tensors of one 16-bit type that receive the rounded new values.
+    state_bits: 32, or 8 for 8-bit codes with a scale per 256 elements.
+    state: None (zeros), or a tuple of tensors per theta that are used in place: (m, s) in fp32, or (m codes int8, s codes uint8,
+    m scales, s scales fp32) with ceil(n / 256) scales each.  `self.state` holds them.
+    step: the number of updates already made.
+    All tensors are contiguous and on one device.
+    """
+
+    def __init__(self, thetas, grads, copies=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, state_bits=32,
+                 state=None, step=0):
+        self.thetas = list(thetas)
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 32 or 8")
+        self.device = self.thetas[0].device if self.thetas else None
+        self.count, self.steps, self.lr = len(self.thetas), int(step), lr
+        self._t = (B.bmgd_adamw_tensor * max(1, self.count))()
+        cfg = B.bmgd_adamw_default_config()
+        cfg.beta1, cfg.beta2, cfg.eps, cfg.weight_decay, cfg.state_bits = beta1, beta2, eps, weight_decay, state_bits
+        self.cfg = cfg
+        for t, e in zip(self.thetas, self._t):
+            self._check("theta", t, torch.float32, t.numel())
+            e.theta, e.n = t.data_ptr(), t.numel()
+        if state is None:
+            state = [self._zeros(t, state_bits) for t in self.thetas]
+        self.state = [tuple(s) for s in state]
+        kinds = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8, torch.float32, torch.float32)
+        fields = ("m", "s") if state_bits == 32 else ("m", "s", "m_scale", "s_scale")
+        if len(self.state) != self.count or any(len(s) != len(kinds) for s in self.state):
+            raise ValueError(f"state: {len(kinds)} tensors for each of {self.count} are wanted")
+        for t, s, e in zip(self.thetas, self.state, self._t):
+            for field, part, kind in zip(fields, s, kinds):
+                self._check(field, part, kind, -(-t.numel() // 256) if field.endswith("scale") else t.numel())
+                setattr(e, field, part.data_ptr())
+        self.copies = None
+        if copies is not None:
+            self.copies = list(copies)
+            kind = self._same_type("copies", self.copies, (torch.bfloat16, torch.float16))
+            for t, e in zip(self.copies, self._t):
+                self._check("copy", t, kind, e.n)
+                e.copy = t.data_ptr()
+            cfg.copy_dtype = _CODES[kind]
+        self.set_grads(grads)
+
+    @staticmethod
+    def _zeros(t, bits):
+        if bits == 32:
+            return torch.zeros_like(t), torch.zeros_like(t)
+        blocks = -(-t.numel() // 256)
+        new = lambda n, kind: torch.zeros(n, dtype=kind, device=t.device)  # noqa: E731
+        return new(t.numel(), torch.int8), new(t.numel(), torch.uint8), new(blocks, torch.float32), new(blocks, torch.float32)
+
+    def _check(self, name, t, kind, n):
+        if t.dtype is not kind or t.device != self.device or not t.is_cuda:
+            raise ValueError(f"{name}: a {kind} tensor on one GPU is wanted, not {t.dtype} on {t.device}")
+        if t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{name}: {n} contiguous elements are wanted, not {tuple(t.shape)} with strides {t.stride()}")
+
+    def _same_type(self, name, tensors, kinds):
+        if len(tensors) != self.count:
+            raise ValueError(f"{name}: {self.count} tensors are wanted, not {len(tensors)}")
+        kind = tensors[0].dtype if tensors else kinds[0]
+        if kind not in kinds:
+            raise ValueError(f"{name}: type {kind} is not one of {kinds}")
+        return kind
+
+    def set_grads(self, grads):
+        """The tensors that later steps read gradients from."""
+        grads = list(grads)
+        kind = self._same_type("grads", grads, (torch.float32, torch.bfloat16, torch.float16))
+        for t, e in zip(grads, self._t):
+            self._check("grad", t, kind, e.n)
+        for t, e in zip(grads, self._t):
+            e.grad = t.data_ptr()
+        self.grads, self.cfg.grad_dtype = grads, _CODES[kind]
+
+    def _launch(self, fn, *args):
+        if self.device is None or torch.cuda.current_device() == self.device.index:
+            rc = fn(*args)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(*args)
+        if rc != B.BMGD_OK:
+            raise B.BmgdError(rc, B.bmgd_last_error(None))
+
+    def step(self, lr=None, grad_scale=1.0, stream=None):
+        """One update with the gradients as they stand in stream order, times grad_scale.  Asynchronous."""
+        self.cfg.lr, self.cfg.grad_scale = self.lr if lr is None else lr, grad_scale
+        self._launch(B.lib.bmgd_adamw_step, C.byref(self.cfg), self._t, self.count, self.steps + 1, B._stream(stream))
+        self.steps += 1
+
+    def moments(self, out=None, stream=None):
+        """Pairs (m, s) of fp32 tensors with the values that the state stands for; `out`: pairs to write them to.  With moments in
+        32 bits the state itself, and `out` is refused."""
+        if self.cfg.state_bits == 32:
+            if out is not None:
+                raise ValueError("moments in 32 bits are the tensors in `state`")
+            return self.state
+        if out is None:
+            out = [(torch.empty(t.numel(), device=t.device), torch.empty(t.numel(), device=t.device)) for t in self.thetas]
+        out = list(out)
+        if len(out) != self.count:
+            raise ValueError(f"out: {self.count} pairs are wanted, not {len(out)}")
+        for t, (m, s) in zip(self.thetas, out):
+            self._check("m", m, torch.float32, t.numel())
+            self._check("s", s, torch.float32, t.numel())
+        address = C.c_void_p * max(1, self.count)
+        self._launch(B.lib.bmgd_adamw_moments, self._t, self.count, address(*[m.data_ptr() for m, _ in out]),
+                     address(*[s.data_ptr() for _, s in out]), B._stream(stream))
+        return out
