@@ -107,28 +107,61 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
     return hipGetLastError();
 }
 
-void gated_plan(GatedProduct& q, GatedOp op, int num_cus)
+void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus)
 {
-    static const int bm[kTiles] = {256, 128, 64}, bn[kTiles] = {256, 128, 64}, per_cu[kTiles] = {1, 2, 4};
-    static const double step_us[kTiles] = {1.6, 0.9, 0.5}, once_us[kTiles] = {5.0, 3.0, 2.0};
-    const int64_t columns = op == kOpUp ? 2 * q.half : op == kOpDown ? q.half : op == kOpWeight && q.half ? 2 * q.half : q.N;
-    const int64_t steps = ((op == kOpInput ? 2 * q.half : q.K) + 63) / 64;
+    static const int bm[kTiles] = {256, 128, 64, 32, 16}, bn[kTiles] = {256, 128, 64, 128, 128}, per_cu[kTiles] = {1, 2, 2, 2, 2};
+    static const double step_us[kTiles] = {1.2, 0.8, 0.4, 0.5, 0.5}, once_us[kTiles] = {5.0, 3.0, 2.0, 2.0, 2.0};
     double best = 1e300;
     for (int t = 0; t < kTiles; ++t) {
-        const int64_t tm = (q.M + bm[t] - 1) / bm[t], tn = (columns + bn[t] - 1) / bn[t], tiles = tm * tn;
-        if (tiles >= (int64_t(1) << 30)) continue;
+        bool fits = true;
+        for (int i = 0; i < count; ++i) fits = fits && !(t >= kTile32 && (count > 1 || qs[i]->M > bm[t]));
+        if (!fits) continue;
+        struct { int64_t tm, tn, splits, per; } plan[3];
+        const int64_t slots = (int64_t)num_cus * per_cu[t];
         for (int64_t want = 1; want <= 64; want += want < 4 ? 1 : want / 2) {
-            if (want > 1 && (tiles > kGatedCounters || (size_t)(tiles * want) * bm[t] * bn[t] * 4 > kGatedPartialBytes || steps < 2 * want)) break;
-            const int64_t per = std::max<int64_t>(1, (steps + want - 1) / want), splits = std::max<int64_t>(1, (steps + per - 1) / per);
-            const int64_t slots = (int64_t)num_cus * per_cu[t], rounds = (tiles * splits + slots - 1) / slots;
-            const double cost = rounds * (per * step_us[t] + once_us[t]) + (splits > 1 ? 4.0 + 0.5 * splits : 0.0);
+            double cost = 0.0;
+            int64_t groups = 0, counters = 0;
+            size_t bytes = 0;
+            double longest = 0.0;
+            bool ok = true;
+            for (int i = 0; i < count && ok; ++i) {
+                const GatedProduct& q = *qs[i];
+                const int64_t columns = ops[i] == kOpUp ? 2 * q.half : ops[i] == kOpDown ? q.half : ops[i] == kOpWeight && q.half ? 2 * q.half : q.N;
+                const int64_t steps = ((ops[i] == kOpInput ? 2 * q.half : q.K) + kGatedStep - 1) / kGatedStep;
+                const int64_t tm = (q.M + bm[t] - 1) / bm[t], tn = (columns + bn[t] - 1) / bn[t], tiles = tm * tn;
+                if (tiles >= (int64_t(1) << 28)) { ok = false; break; }
+                int64_t use = std::max<int64_t>(1, std::min(want, steps / 2));
+                const int64_t per = std::max<int64_t>(1, (steps + use - 1) / use), splits = std::max<int64_t>(1, (steps + per - 1) / per);
+                plan[i] = {tm, tn, splits, per};
+                groups += tiles * splits;
+                if (splits > 1) {
+                    counters += tiles;
+                    bytes += (size_t)(tiles * splits) * bm[t] * bn[t] * 4;
+                }
+                longest = std::max(longest, per * step_us[t] + once_us[t] + (splits > 1 ? 2.0 + 0.5 * splits : 0.0));
+                cost += (double)(tiles * splits) * (per * step_us[t] + once_us[t] + (splits > 1 ? 1.0 : 0.0));
+            }
+            if (!ok || counters > kGatedCounters || bytes > kGatedPartialBytes) break;
+            cost = std::max(longest, cost / slots);
+            if (groups > slots) cost += 0.5 * longest;
             if (cost < best) {
                 best = cost;
-                q.tile = t;
-                q.tiles_m = (int)tm;
-                q.tiles_n = (int)tn;
-                q.splits = (int)splits;
-                q.per_split = (int)per;
+                size_t at = 0;
+                int counter = 0;
+                for (int i = 0; i < count; ++i) {
+                    GatedProduct& q = *qs[i];
+                    q.tile = t;
+                    q.tiles_m = (int)plan[i].tm;
+                    q.tiles_n = (int)plan[i].tn;
+                    q.splits = (int)plan[i].splits;
+                    q.per_split = (int)plan[i].per;
+                    q.first_part = at;
+                    q.first_counter = counter;
+                    if (q.splits > 1) {
+                        at += (size_t)(plan[i].tm * plan[i].tn * plan[i].splits) * bm[t] * bn[t];
+                        counter += (int)(plan[i].tm * plan[i].tn);
+                    }
+                }
             }
         }
     }
@@ -244,13 +277,21 @@ int enter(bmgd_gated* b, hipStream_t s)
     return BMGD_OK;
 }
 
+void plan(bmgd_gated* b, GatedProduct* const* q, const GatedOp* op, int count)
+{
+    gated_plan(q, op, count, b->num_cus);
+    for (int i = 0; i < count; ++i) {
+        q[i]->act = b->cfg.activation;
+        q[i]->partial = reinterpret_cast<float*>(b->base + b->lay.partial) + q[i]->first_part;
+        q[i]->counter = reinterpret_cast<unsigned*>(b->base + b->lay.counter) + q[i]->first_counter;
+        q[i]->zeros = b->base + b->lay.zeros;
+    }
+}
+
 int launch(bmgd_gated* b, GatedProduct& q, GatedOp op, hipStream_t s)
 {
-    q.act = b->cfg.activation;
-    q.partial = reinterpret_cast<float*>(b->base + b->lay.partial);
-    q.counter = reinterpret_cast<unsigned*>(b->base + b->lay.counter);
-    q.zeros = b->base + b->lay.zeros;
-    gated_plan(q, op, b->num_cus);
+    GatedProduct* one = &q;
+    plan(b, &one, &op, 1);
     const hipError_t e = b->cfg.dtype == BMGD_F16 ? gated_launch_f16(q, op, s) : gated_launch_bf16(q, op, s);
     if (e != hipSuccess) return hip_fail(b, e, "launch of a product of the gated block");
     return BMGD_OK;
@@ -317,6 +358,8 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
     const GatedMat x = o.use(t.x, rows, c.p, b->lay.x);
     const GatedMat dy = o.use(t.dy, rows, c.out_n, b->lay.dy);
     const GatedMat down = o.use(t.down, c.hidden, c.out_n, b->lay.down);
+    GatedMat gate{}, upw{};
+    if (rows && t.dx.data) o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, &gate, &upw);
     if (rows && o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
     const GatedMat h{b->base + b->lay.h, half}, d{b->base + b->lay.d, 2 * half};
 
@@ -332,42 +375,47 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
         q.u = plain(t.u);
         GATED_DO(launch(b, q, kOpDown, s));
     }
+    GatedProduct input{}, ddown{}, dgate{};
+    GatedProduct* list3[3];
+    GatedOp ops[3];
+    int n = 0;
     if (rows && t.dx.data) {
-        o.pack = GatedPack{};
-        GatedMat gate, upw;
-        o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, &gate, &upw);
-        if (o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
-        q = GatedProduct{};
-        q.a = d;
-        q.b = gate;
-        q.b2 = upw;
-        q.M = rows; q.N = c.p; q.K = up(c.hidden, 8);
-        q.half = half;
-        q.out = plain(t.dx);
-        GATED_DO(launch(b, q, kOpInput, s));
+        input.a = d;
+        input.b = gate;
+        input.b2 = upw;
+        input.M = rows; input.N = c.p; input.K = up(c.hidden, 8);
+        input.half = half;
+        input.out = plain(t.dx);
+        list3[n] = &input;
+        ops[n++] = kOpInput;
     }
     if (t.ddown.data) {
-        q = GatedProduct{};
-        q.a = h;
-        q.b = dy;
-        q.M = c.hidden; q.N = c.out_n; q.K = rows;
-        q.a_cols = half;
-        q.b_cols = up(c.out_n, 8);
-        q.out = plain(t.ddown);
-        GATED_DO(launch(b, q, kOpWeight, s));
+        ddown.a = h;
+        ddown.b = dy;
+        ddown.M = c.hidden; ddown.N = c.out_n; ddown.K = rows;
+        ddown.a_cols = half;
+        ddown.b_cols = up(c.out_n, 8);
+        ddown.out = plain(t.ddown);
+        list3[n] = &ddown;
+        ops[n++] = kOpWeight;
     }
     if (t.dgate.data) {
-        q = GatedProduct{};
-        q.a = x;
-        q.b = d;
-        q.M = c.p; q.N = c.hidden; q.K = rows;
-        q.a_cols = up(c.p, 8);
-        q.b_cols = 2 * half;
-        q.half = half;
-        q.out = plain(t.dgate);
-        q.out2 = plain(t.dup);
-        GATED_DO(launch(b, q, kOpWeight, s));
+        dgate.a = x;
+        dgate.b = d;
+        dgate.M = c.p; dgate.N = c.hidden; dgate.K = rows;
+        dgate.a_cols = up(c.p, 8);
+        dgate.b_cols = 2 * half;
+        dgate.half = half;
+        dgate.out = plain(t.dgate);
+        dgate.out2 = plain(t.dup);
+        list3[n] = &dgate;
+        ops[n++] = kOpWeight;
     }
+    if (n == 0) return BMGD_OK;
+    plan(b, list3, ops, n);
+    const GatedProduct *pi = input.M ? &input : nullptr, *pd = ddown.M ? &ddown : nullptr, *pg = dgate.M ? &dgate : nullptr;
+    const hipError_t e = c.dtype == BMGD_F16 ? gated_launch_grads_f16(pi, pd, pg, s) : gated_launch_grads_bf16(pi, pd, pg, s);
+    if (e != hipSuccess) return hip_fail(b, e, "launch of the gradients of the gated block");
     return BMGD_OK;
 }
 

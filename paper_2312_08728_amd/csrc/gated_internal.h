@@ -39,28 +39,35 @@ struct GatedProduct {
     int tiles_m, tiles_n, splits, per_split;    // tiles of the result; workgroups that share a tile's sum, and their share in steps of 64
     float* partial;     // their sums
     unsigned* counter;  // and how many of them have arrived, per tile; zero between launches
+    size_t first_part;  // where its own begin among those of a launch
+    int first_counter;
     const void* zeros;  // 256 bytes of zeros
 };
 
-enum { kTileLarge = 0, kTileMedium = 1, kTileSmall = 2, kTiles = 3 };
+// rows x columns: 256 x 256, 128 x 128, 64 x 64; for few rows 32 x 128 and 16 x 128
+enum { kTileLarge = 0, kTileMedium = 1, kTileSmall = 2, kTile32 = 3, kTile16 = 4, kTiles = 5 };
 
 // Bytes of partial sums, and tiles, that a product may use where workgroups share tiles.
 constexpr size_t kGatedPartialBytes = size_t(64) << 20;
 constexpr int kGatedCounters = 4096;
+constexpr int kGatedStep = 64;         // elements of the summed index per step
 
-// Chooses tile and split.
-void gated_plan(GatedProduct& q, GatedOp op, int num_cus);
+// Chooses tile and split for the `count` products of one launch, which get one kind of tile.
+void gated_plan(GatedProduct* const* q, const GatedOp* op, int count, int num_cus);
 
 // Once per process and device: lets the kernels use as much shared memory as they need.
 hipError_t gated_prepare_bf16();
 hipError_t gated_prepare_f16();
 hipError_t gated_launch_bf16(const GatedProduct& q, GatedOp op, hipStream_t stream);
 hipError_t gated_launch_f16(const GatedProduct& q, GatedOp op, hipStream_t stream);
+// dX (kOpInput), dWd and [dWg | dWu] (kOpWeight) in one launch; NULL leaves one out
+hipError_t gated_launch_grads_bf16(const GatedProduct* input, const GatedProduct* down, const GatedProduct* gate, hipStream_t stream);
+hipError_t gated_launch_grads_f16(const GatedProduct* input, const GatedProduct* down, const GatedProduct* gate, hipStream_t stream);
 
-// Copies of up to four matrices of 16-bit elements whose rows cannot be read in pieces of 16 bytes: rows of `to_ld` elements (a multiple of
+// Copies of up to five matrices of 16-bit elements whose rows cannot be read in pieces of 16 bytes: rows of `to_ld` elements (a multiple of
 // 8), zeros behind the last column.
 struct GatedPack {
-    struct One { const unsigned short* from; unsigned short* to; int64_t from_ld, to_ld, rows, cols; } m[4];
+    struct One { const unsigned short* from; unsigned short* to; int64_t from_ld, to_ld, rows, cols; } m[5];
     int count;
 };
 hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream);

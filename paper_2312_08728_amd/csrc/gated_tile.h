@@ -18,6 +18,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 namespace bmgd {
 namespace {
 
@@ -120,7 +122,7 @@ __device__ __forceinline__ short4v load4(const GatedMat& m, int64_t r, int64_t c
     return v;
 }
 
-constexpr int kStep = 64;                                     // elements of the summed index per step
+constexpr int kStep = kGatedStep;
 
 // Wait until at most N of this wavefront's loads to shared memory are on their way and its reads of shared memory are done, then for the others.
 template <int N> __device__ __forceinline__ void wait_and_meet()
@@ -213,34 +215,68 @@ template <bool ADJ, int R> struct Reader {
     }
 };
 
+// Tile, wavefronts along its rows and columns, steps in shared memory (all but one of them on their way).
 template <int TILE> struct Shape;
-template <> struct Shape<kTileLarge> { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4; };       // tile; wavefronts along rows and columns
-template <> struct Shape<kTileMedium> { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2; };
-template <> struct Shape<kTileSmall> { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2; };
+template <> struct Shape<kTileLarge> { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, STAGES = 2; };
+template <> struct Shape<kTileMedium> { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, STAGES = 2; };
+template <> struct Shape<kTileSmall> { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, STAGES = 4; };
+template <> struct Shape<kTile32> { static constexpr int BM = 32, BN = 128, WM = 1, WN = 2, STAGES = 4; };
+template <> struct Shape<kTile16> { static constexpr int BM = 16, BN = 128, WM = 1, WN = 2, STAGES = 4; };
 
 template <int TILE> constexpr int tile_threads() { return 64 * Shape<TILE>::WM * Shape<TILE>::WN; }
-template <int TILE> constexpr unsigned tile_lds() { return 2u * (Shape<TILE>::BM + Shape<TILE>::BN) * 128u; }
+template <int TILE> constexpr unsigned tile_lds() { return (unsigned)Shape<TILE>::STAGES * (Shape<TILE>::BM + Shape<TILE>::BN) * 128u; }
 
+// Parts of a sum on their way between workgroups of different dies: written through to where all dies see them, and read from there.
+// (No inline assembly for the stores: only the compiler knows how long a matrix instruction's result must not be read.)
+__device__ __forceinline__ void store_shared(float4v* to, float4v v)
+{
+    typedef unsigned long long word2 __attribute__((ext_vector_type(2)));
+    const word2 w = __builtin_bit_cast(word2, v);
+    unsigned long long* at = reinterpret_cast<unsigned long long*>(to);
+    __hip_atomic_store(at, w[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(at + 1, w[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+// (the wait stands in the same block as the loads: the compiler does not know that they are on their way)
+__device__ __forceinline__ void load_shared(const float4v* p, int apart, float4v* v)
+{
+    asm volatile("global_load_dwordx4 %0, %4, off sc1\n\t"
+                 "global_load_dwordx4 %1, %5, off sc1\n\t"
+                 "global_load_dwordx4 %2, %6, off sc1\n\t"
+                 "global_load_dwordx4 %3, %7, off sc1\n\t"
+                 "s_waitcnt vmcnt(0)"
+                 : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+                 : "v"(p), "v"(p + apart), "v"(p + 2 * apart), "v"(p + 3 * apart) : "memory");
+}
+__device__ __forceinline__ void load_shared2(const float4v* p, const float4v* q, int apart, float4v* v)
+{
+    asm volatile("global_load_dwordx4 %0, %8, off sc1\n\t"
+                 "global_load_dwordx4 %1, %9, off sc1\n\t"
+                 "global_load_dwordx4 %2, %10, off sc1\n\t"
+                 "global_load_dwordx4 %3, %11, off sc1\n\t"
+                 "global_load_dwordx4 %4, %12, off sc1\n\t"
+                 "global_load_dwordx4 %5, %13, off sc1\n\t"
+                 "global_load_dwordx4 %6, %14, off sc1\n\t"
+                 "global_load_dwordx4 %7, %15, off sc1\n\t"
+                 "s_waitcnt vmcnt(0)"
+                 : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
+                 : "v"(p), "v"(p + apart), "v"(p + 2 * apart), "v"(p + 3 * apart), "v"(q), "v"(q + apart), "v"(q + 2 * apart), "v"(q + 3 * apart) : "memory");
+}
+
+// Workgroup `id` of a product's tiles_m * tiles_n * splits.
 template <typename T, GatedOp OP, int TILE>
-__global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(GatedProduct q)
+__device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
 {
     using S = Shape<TILE>;
     constexpr int threads = tile_threads<TILE>(), BM = S::BM, BN = S::BN;
     constexpr int wm = BM / S::WM, wn = BN / S::WN, fm = wm / 16, fn = wn / 16;    // of a wavefront
     constexpr bool a_adj = OP != kOpWeight, b_adj = OP == kOpDown || OP == kOpInput;
     constexpr unsigned a_bytes = BM * 128, b_bytes = BN * 128;
+    constexpr int stages = S::STAGES;
     extern __shared__ __align__(1024) unsigned short stage[];
     __shared__ unsigned arrived;
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned short*)stage;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    // Workgroups go to the eight dies in turn: a die gets neighbouring tiles, whose operands its L2 then holds.
-    const int total = q.tiles_m * q.tiles_n * q.splits;
-    int id = blockIdx.x;
-    {
-        const int die = id & 7, each = total >> 3, more = total & 7;
-        id = die * each + min(die, more) + (id >> 3);
-    }
     const int split = id % q.splits;
     const int tile = id / q.splits;
     constexpr int kGroup = 8;                                  // tile rows that are walked through together
@@ -278,7 +314,7 @@ __global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(Gat
         });
     };
     start_b(s0);
-    const unsigned lds_a = lds0 + (unsigned)__builtin_amdgcn_readfirstlane(wave * 1024), lds_b = lds_a + 2 * a_bytes;
+    const unsigned lds_a = lds0 + (unsigned)__builtin_amdgcn_readfirstlane(wave * 1024), lds_b = lds_a + stages * a_bytes;
     auto request = [&](int step, int buf) {
         const int64_t k0 = (int64_t)step * kStep;
         // the left operand of kOpMul and kOpInput has zeros behind its columns
@@ -303,12 +339,19 @@ __global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(Gat
 #pragma unroll
         for (int j = 0; j < fn; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    if (s0 < s1) request(s0, 0);
+    constexpr int loads = Mover<a_adj, BM, threads>::kPieces + Mover<b_adj, BN, threads>::kPieces;      // of a thread and step
+#pragma unroll
+    for (int i = 0; i < stages - 1; ++i)
+        if (s0 + i < s1) request(s0 + i, i);
+    int buf = 0;
     for (int s = s0; s < s1; ++s) {
-        const int buf = (s - s0) & 1;
-        wait_and_meet<0>();
-        if (s + 1 < s1) request(s + 1, buf ^ 1);
-        const unsigned ta = lds0 + buf * a_bytes, tb = lds0 + 2 * a_bytes + buf * b_bytes;
+        const int behind = s1 - 1 - s;                         // steps behind this one
+        if (stages > 2 && behind >= stages - 2) wait_and_meet<(stages - 2) * loads>();
+        else if (stages > 3 && behind == 1) wait_and_meet<loads>();
+        else wait_and_meet<0>();
+        // (all have read the step before this one, whose place is free now)
+        if (behind >= stages - 1) request(s + stages - 1, buf == 0 ? stages - 1 : buf - 1);
+        const unsigned ta = lds0 + buf * a_bytes, tb = lds0 + stages * a_bytes + buf * b_bytes;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             short8v af[fm], bf[fn];
@@ -321,33 +364,45 @@ __global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(Gat
 #pragma unroll
                 for (int j = 0; j < fn; ++j) acc[i][j] = Half<T>::mma(bf[j], af[i], acc[i][j]);
         }
+        buf = buf + 1 == stages ? 0 : buf + 1;
     }
 
     if (q.splits > 1) {
-        // The parts of a tile, [split][fragment][thread] of four floats.  Written, made visible beyond the die, counted; the last one adds them up.
-        float4v* part = (float4v*)q.partial + (size_t)tile * q.splits * (fm * fn) * threads;
-        float4v* mine = part + (size_t)split * (fm * fn) * threads + tid;
+        // The parts of a tile, [split][fragment][thread] of four floats (rows behind the last one are left out).  Written, waited for, counted; the last
+        // one adds them up.
+        static_assert(fm * fn % 4 == 0, "");
+        float4v* part = (float4v*)q.partial + (size_t)tile * q.splits * (fm * fn) * threads + tid;
+        float4v* mine = part + (size_t)split * (fm * fn) * threads;
 #pragma unroll
         for (int i = 0; i < fm; ++i)
+            if (m0 + wrow + (lane & 15) + 16 * i < q.M) {
 #pragma unroll
-            for (int j = 0; j < fn; ++j) mine[(i * fn + j) * threads] = acc[i][j];
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) arrived = atomicAdd(q.counter + tile, 1u);
+                for (int j = 0; j < fn; ++j) store_shared(mine + (i * fn + j) * threads, acc[i][j]);
+            }
+        wait_and_meet<0>();
+        if (tid == 0) arrived = __hip_atomic_fetch_add(q.counter + tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (arrived != (unsigned)q.splits - 1) return;
-        __threadfence();
-        if (tid == 0) q.counter[tile] = 0;                     // for the next launch
+        if (tid == 0) __hip_atomic_store(q.counter + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next launch
+        const size_t apart = (size_t)(fm * fn) * threads;      // from one part to the next
 #pragma unroll
-        for (int i = 0; i < fm; ++i)
+        for (int f = 0; f < fm * fn; f += 4) {
+            const float4v* from = part + f * threads;
+            float4v v[8], sum[4];
+            load_shared(from, threads, sum);
+            int p = 1;
+            for (; p + 1 < q.splits; p += 2) {
+                load_shared2(from + p * apart, from + (p + 1) * apart, threads, v);
 #pragma unroll
-            for (int j = 0; j < fn; ++j) acc[i][j] = part[(i * fn + j) * threads + tid];
-        for (int p = 1; p < q.splits; ++p) {
-            const float4v* next = part + (size_t)p * (fm * fn) * threads + tid;
+                for (int k = 0; k < 4; ++k) sum[k] = sum[k] + v[k] + v[4 + k];
+            }
+            if (p < q.splits) {
+                load_shared(from + p * apart, threads, v);
 #pragma unroll
-            for (int i = 0; i < fm; ++i)
+                for (int k = 0; k < 4; ++k) sum[k] += v[k];
+            }
 #pragma unroll
-                for (int j = 0; j < fn; ++j) acc[i][j] += next[(i * fn + j) * threads];
+            for (int k = 0; k < 4; ++k) acc[(f + k) / fn][(f + k) % fn] = sum[k];
         }
     }
 
@@ -421,53 +476,112 @@ __global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(Gat
     }
 }
 
-template <typename T, GatedOp OP, int TILE> hipError_t prepare_tile()
+// Workgroups go to the eight dies in turn: a die gets neighbouring tiles, whose operands its L2 then holds.
+__device__ __forceinline__ int neighbours(int id, int total)
 {
-    return hipFuncSetAttribute(reinterpret_cast<const void*>(&gated_tile_kernel<T, OP, TILE>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                               (int)tile_lds<TILE>());
+    const int die = id & 7, each = total >> 3, more = total & 7;
+    return die * each + min(die, more) + (id >> 3);
 }
 
-template <typename T, GatedOp OP> hipError_t prepare_op()
+template <typename T, GatedOp OP, int TILE>
+__global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(GatedProduct q)
 {
-    hipError_t e = prepare_tile<T, OP, kTileLarge>();
-    if (e == hipSuccess) e = prepare_tile<T, OP, kTileMedium>();
-    if (e == hipSuccess) e = prepare_tile<T, OP, kTileSmall>();
+    tile_body<T, OP, TILE>(q, neighbours(blockIdx.x, gridDim.x));
+}
+
+// The products that need nothing but what kOpDown left, in one launch: dX, dWd, [dWg | dWu], as far as they are wanted.  Each begins at a multiple of
+// eight workgroups.
+struct GradProducts {
+    GatedProduct input, down, gate;
+    int input_end, down_end, gate_end;
+};
+template <typename T, int TILE>
+__global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_grads_kernel(GradProducts g)
+{
+    int id = blockIdx.x;
+    if (id < g.input_end) {
+        const int n = g.input.tiles_m * g.input.tiles_n * g.input.splits;
+        if (id < n) tile_body<T, kOpInput, TILE>(g.input, neighbours(id, n));
+        return;
+    }
+    id -= g.input_end;
+    const bool down = id < g.down_end;
+    const GatedProduct& q = down ? g.down : g.gate;
+    if (!down) id -= g.down_end;
+    const int n = q.tiles_m * q.tiles_n * q.splits;
+    if (id < n) tile_body<T, kOpWeight, TILE>(q, neighbours(id, n));
+}
+
+template <typename K> hipError_t prepare_kernel(K kernel, unsigned lds)
+{
+    return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+}
+
+// f(tile) for every kind of tile until one fails
+template <typename F> hipError_t each_tile(F f)
+{
+    hipError_t e = f(std::integral_constant<int, kTileLarge>());
+    if (e == hipSuccess) e = f(std::integral_constant<int, kTileMedium>());
+    if (e == hipSuccess) e = f(std::integral_constant<int, kTileSmall>());
+    return e;
+}
+template <typename F> hipError_t each_row_tile(F f)
+{
+    hipError_t e = each_tile(f);
+    if (e == hipSuccess) e = f(std::integral_constant<int, kTile32>());
+    if (e == hipSuccess) e = f(std::integral_constant<int, kTile16>());
     return e;
 }
 
 template <typename T> hipError_t prepare_all()
 {
-    hipError_t e = prepare_op<T, kOpUp>();
-    if (e == hipSuccess) e = prepare_op<T, kOpMul>();
-    if (e == hipSuccess) e = prepare_op<T, kOpDown>();
-    if (e == hipSuccess) e = prepare_op<T, kOpInput>();
-    if (e == hipSuccess) e = prepare_op<T, kOpWeight>();
+    hipError_t e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpUp, t.value>, tile_lds<t.value>()); });
+    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpMul, t.value>, tile_lds<t.value>()); });
+    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpDown, t.value>, tile_lds<t.value>()); });
+    if (e == hipSuccess) e = each_tile([](auto t) { return prepare_kernel(&gated_grads_kernel<T, t.value>, tile_lds<t.value>()); });
     return e;
-}
-
-template <typename T, GatedOp OP, int TILE> hipError_t launch_tile(const GatedProduct& q, hipStream_t stream)
-{
-    hipLaunchKernelGGL((gated_tile_kernel<T, OP, TILE>), dim3((unsigned)(q.tiles_m * q.tiles_n * q.splits)), dim3(tile_threads<TILE>()),
-                       tile_lds<TILE>(), stream, q);
-    return hipGetLastError();
 }
 
 template <typename T, GatedOp OP> hipError_t launch_op(const GatedProduct& q, hipStream_t stream)
 {
-    if (q.tile == kTileLarge) return launch_tile<T, OP, kTileLarge>(q, stream);
-    if (q.tile == kTileMedium) return launch_tile<T, OP, kTileMedium>(q, stream);
-    return launch_tile<T, OP, kTileSmall>(q, stream);
+    const dim3 grid((unsigned)(q.tiles_m * q.tiles_n * q.splits));
+    return each_row_tile([&](auto t) {
+        if (q.tile != t.value) return hipSuccess;
+        hipLaunchKernelGGL((gated_tile_kernel<T, OP, t.value>), grid, dim3(tile_threads<t.value>()), tile_lds<t.value>(), stream, q);
+        return hipGetLastError();
+    });
 }
 
 template <typename T> hipError_t launch_any(const GatedProduct& q, GatedOp op, hipStream_t stream)
 {
-    switch (op) {
-    case kOpUp: return launch_op<T, kOpUp>(q, stream);
-    case kOpMul: return launch_op<T, kOpMul>(q, stream);
-    case kOpDown: return launch_op<T, kOpDown>(q, stream);
-    case kOpInput: return launch_op<T, kOpInput>(q, stream);
-    default: return launch_op<T, kOpWeight>(q, stream);
-    }
+    if (op == kOpUp) return launch_op<T, kOpUp>(q, stream);
+    if (op == kOpMul) return launch_op<T, kOpMul>(q, stream);
+    if (op == kOpDown) return launch_op<T, kOpDown>(q, stream);
+    return hipErrorInvalidValue;
+}
+
+// `input`, `down`, `gate` have one kind of tile; NULL: not wanted
+template <typename T> hipError_t launch_grads(const GatedProduct* input, const GatedProduct* down, const GatedProduct* gate, hipStream_t stream)
+{
+    GradProducts g{};
+    int tile = kTileLarge, end = 0;
+    auto add = [&](const GatedProduct* from, GatedProduct& to) {
+        if (!from) return 0;
+        to = *from;
+        tile = from->tile;
+        const int n = (from->tiles_m * from->tiles_n * from->splits + 7) / 8 * 8;
+        end += n;
+        return n;
+    };
+    g.input_end = add(input, g.input);
+    g.down_end = add(down, g.down);
+    g.gate_end = add(gate, g.gate);
+    if (end == 0) return hipSuccess;
+    return each_tile([&](auto t) {
+        if (tile != t.value) return hipSuccess;
+        hipLaunchKernelGGL((gated_grads_kernel<T, t.value>), dim3((unsigned)end), dim3(tile_threads<t.value>()), tile_lds<t.value>(), stream, g);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace
