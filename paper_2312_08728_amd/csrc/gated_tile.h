@@ -85,39 +85,27 @@ template <typename T> __device__ __forceinline__ short bits_of(float x)
 }
 template <typename T> __device__ __forceinline__ float value_of(short b) { return (float)__builtin_bit_cast(T, b); }
 
-template <typename T> __device__ __forceinline__ short4v bits4(float4v x)
-{
-    short4v r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = bits_of<T>(x[i]);
-    return r;
-}
-
-__device__ __forceinline__ bool whole4(const GatedMat& m)    // four elements of a row at a multiple of four can be moved as 8 bytes
-{
-    return ((uintptr_t)m.p & 7) == 0 && (m.ld & 3) == 0;
-}
-
-// Four neighbouring elements of row r from column c on, as far as there are `cols` columns.
-__device__ __forceinline__ void store4(const GatedMat& m, int64_t r, int64_t c, int64_t cols, bool whole, short4v v)
+// Eight neighbouring elements of row r from column c on, as far as there are `cols` columns.  (A vector at any even address is one instruction all the same.)
+typedef short short8u __attribute__((ext_vector_type(8), aligned(2)));
+__device__ __forceinline__ void store8(const GatedMat& m, int64_t r, int64_t c, int64_t cols, short8v v)
 {
     short* to = (short*)m.p + r * m.ld + c;
-    if (whole && c + 4 <= cols) {
-        *(short4v*)to = v;
+    if (c + 8 <= cols) {
+        *(short8u*)to = v;
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 8; ++i)
             if (c + i < cols) to[i] = v[i];
     }
 }
 
-__device__ __forceinline__ short4v load4(const GatedMat& m, int64_t r, int64_t c, int64_t cols, bool whole)
+__device__ __forceinline__ short8v load8(const GatedMat& m, int64_t r, int64_t c, int64_t cols)
 {
     const short* from = (const short*)m.p + r * m.ld + c;
-    if (whole && c + 4 <= cols) return *(const short4v*)from;
-    short4v v = {0, 0, 0, 0};
+    if (c + 8 <= cols) return *(const short8u*)from;
+    short8v v = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i)
         if (c + i < cols) v[i] = from[i];
     return v;
 }
@@ -224,7 +212,15 @@ template <> struct Shape<kTile32> { static constexpr int BM = 32, BN = 128, WM =
 template <> struct Shape<kTile16> { static constexpr int BM = 16, BN = 128, WM = 1, WN = 2, STAGES = 4; };
 
 template <int TILE> constexpr int tile_threads() { return 64 * Shape<TILE>::WM * Shape<TILE>::WN; }
-template <int TILE> constexpr unsigned tile_lds() { return (unsigned)Shape<TILE>::STAGES * (Shape<TILE>::BM + Shape<TILE>::BN) * 128u; }
+// The results leave through shared memory, in one or two turns.
+template <int TILE> constexpr int tile_turns() { return TILE == kTileLarge || TILE == kTileMedium ? 2 : 1; }
+template <int TILE> constexpr int tile_pitch() { return Shape<TILE>::BN + 4; }             // floats from one row to the next
+template <int TILE> constexpr unsigned tile_lds()
+{
+    using S = Shape<TILE>;
+    constexpr unsigned stages = (unsigned)S::STAGES * (S::BM + S::BN) * 128u, out = (unsigned)(S::BM / tile_turns<TILE>()) * tile_pitch<TILE>() * 4u;
+    return stages > out ? stages : out;
+}
 
 // Parts of a sum on their way between workgroups of different dies: written through to where all dies see them, and read from there.
 // (No inline assembly for the stores: only the compiler knows how long a matrix instruction's result must not be read.)
@@ -406,70 +402,74 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         }
     }
 
-    // A lane holds row m and columns n .. n + 3 of every fragment.
-    const int64_t m = m0 + wrow + (lane & 15);
-    const int cq = 4 * (lane >> 4);
-    if constexpr (OP == kOpUp) {
-        const bool keep = q.g.p != nullptr, wg = whole4(q.g), wu = whole4(q.u);
+    // Out: a lane holds row lane % 16 and four neighbouring columns of every fragment.  They go to shared memory and come back as eight neighbouring
+    // columns, so that memory is read and written in whole lines and the code for a result stands there once.
+    constexpr int turns = tile_turns<TILE>(), pitch = tile_pitch<TILE>(), wt = wm / turns;        // rows of a wavefront and turn
+    float* const res = reinterpret_cast<float*>(stage);
+    constexpr int cols8 = (OP == kOpUp ? BN / 2 : BN) / 8, pieces = (BM / turns) * cols8;
 #pragma unroll
-        for (int i = 0; i < fm; ++i) {
-            const int64_t r = m + 16 * i;
-            if (r >= q.M) continue;
+    for (int turn = 0; turn < turns; ++turn) {
+        __syncthreads();
 #pragma unroll
-            for (int j = 0; j < fn / 2; ++j) {
-                const int64_t c = n0 + (wave % S::WN) * (wn / 2) + 16 * j + cq;
-                if (c >= q.half) continue;
-                const float4v g = acc[i][j], u = acc[i][j + fn / 2];
-                float4v h;
-#pragma unroll
-                for (int v = 0; v < 4; ++v) h[v] = c + v < q.N ? act_value(q.act, g[v]) * u[v] : 0.f;
-                store4(q.out, r, c, q.half, true, bits4<T>(h));
-                if (keep) {
-                    store4(q.g, r, c, q.N, wg, bits4<T>(g));
-                    store4(q.u, r, c, q.N, wu, bits4<T>(u));
-                }
-            }
-        }
-    } else if constexpr (OP == kOpDown) {
-        const bool wg = whole4(q.g), wu = whole4(q.u);
-#pragma unroll
-        for (int i = 0; i < fm; ++i) {
-            const int64_t r = m + 16 * i;
-            if (r >= q.M) continue;
+        for (int i = 0; i < fm / turns; ++i)
 #pragma unroll
             for (int j = 0; j < fn; ++j) {
-                const int64_t c = n0 + wcol + 16 * j + cq;
+                int col = wcol + 16 * j;
+                if constexpr (OP == kOpUp) col = (j < fn / 2 ? 0 : BN / 2 - wn / 2) + (wave % S::WN) * (wn / 2) + 16 * j;      // G left, U right
+                *reinterpret_cast<float4v*>(res + ((wave / S::WN) * wt + 16 * i + (lane & 15)) * pitch + col + 4 * (lane >> 4)) = acc[turn * (fm / turns) + i][j];
+            }
+        __syncthreads();
+#pragma unroll 1
+        for (int id = tid; id < pieces; id += threads) {
+            const int lr = id / cols8, lc = 8 * (id % cols8);
+            const int64_t r = m0 + (lr / wt) * wm + turn * wt + lr % wt, c = n0 + lc;
+            if (r >= q.M) continue;
+            const float* const at = res + lr * pitch + lc;
+            float v[8];
+            *reinterpret_cast<float4v*>(v) = *reinterpret_cast<const float4v*>(at);
+            *reinterpret_cast<float4v*>(v + 4) = *reinterpret_cast<const float4v*>(at + 4);
+            if constexpr (OP == kOpUp) {
                 if (c >= q.half) continue;
-                const short4v gb = load4(q.g, r, c, q.N, wg), ub = load4(q.u, r, c, q.N, wu);
-                float4v h, dg, du;
+                float u[8];
+                *reinterpret_cast<float4v*>(u) = *reinterpret_cast<const float4v*>(at + BN / 2);
+                *reinterpret_cast<float4v*>(u + 4) = *reinterpret_cast<const float4v*>(at + BN / 2 + 4);
+                short8v hb, gb, ub;
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
+                for (int k = 0; k < 8; ++k) {
+                    hb[k] = c + k < q.N ? bits_of<T>(act_value(q.act, v[k]) * u[k]) : (short)0;
+                    gb[k] = bits_of<T>(v[k]);
+                    ub[k] = bits_of<T>(u[k]);
+                }
+                store8(q.out, r, c, q.half, hb);
+                if (q.g.p) {
+                    store8(q.g, r, c, q.N, gb);
+                    store8(q.u, r, c, q.N, ub);
+                }
+            } else if constexpr (OP == kOpDown) {
+                if (c >= q.half) continue;
+                const short8v gb = load8(q.g, r, c, q.N), ub = load8(q.u, r, c, q.N);
+                short8v hb, dgb, dub;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
                     float slope;
-                    const float u = value_of<T>(ub[v]), a = act_both(q.act, value_of<T>(gb[v]), slope), dh = acc[i][j][v];
-                    const bool in = c + v < q.N;
-                    h[v] = in ? a * u : 0.f;
-                    du[v] = in ? dh * a : 0.f;
-                    dg[v] = in ? dh * u * slope : 0.f;
+                    const float u = value_of<T>(ub[k]), a = act_both(q.act, value_of<T>(gb[k]), slope), dh = v[k];
+                    const bool in = c + k < q.N;
+                    hb[k] = in ? bits_of<T>(a * u) : (short)0;
+                    dub[k] = in ? bits_of<T>(dh * a) : (short)0;
+                    dgb[k] = in ? bits_of<T>(dh * u * slope) : (short)0;
                 }
-                store4(q.out, r, c, q.half, true, bits4<T>(h));
-                store4(q.out2, r, c, q.half, true, bits4<T>(dg));
-                store4(q.out2, r, c + q.half, 2 * q.half, true, bits4<T>(du));
-            }
-        }
-    } else {
-        const bool w1 = whole4(q.out), w2 = whole4(q.out2);
+                store8(q.out, r, c, q.half, hb);
+                store8(q.out2, r, c, q.half, dgb);
+                store8(q.out2, r, c + q.half, 2 * q.half, dub);
+            } else {
+                short8v b;
 #pragma unroll
-        for (int i = 0; i < fm; ++i) {
-            const int64_t r = m + 16 * i;
-            if (r >= q.M) continue;
-#pragma unroll
-            for (int j = 0; j < fn; ++j) {
-                const int64_t c = n0 + wcol + 16 * j + cq;
-                if (OP == kOpWeight && q.half) {               // (q.half is a multiple of 64: four columns never straddle)
+                for (int k = 0; k < 8; ++k) b[k] = bits_of<T>(v[k]);
+                if (OP == kOpWeight && q.half) {               // (q.half is a multiple of 64: eight columns never straddle)
                     const bool second = c >= q.half;
-                    store4(second ? q.out2 : q.out, r, second ? c - q.half : c, q.N, second ? w2 : w1, bits4<T>(acc[i][j]));
+                    store8(second ? q.out2 : q.out, r, second ? c - q.half : c, q.N, b);
                 } else {
-                    store4(q.out, r, c, q.N, w1, bits4<T>(acc[i][j]));
+                    store8(q.out, r, c, q.N, b);
                 }
             }
         }
