@@ -45,37 +45,47 @@ template <> struct Half<_Float16> {
     }
 };
 
-// act(g) and its derivative.  silu g s, s = 1 / (1 + e^-g): derivative s (1 + g (1 - s)); gelu g F(g), F the normal distribution's: F + g f;
-// relu: 0 at 0.  s and F keep their relative accuracy far out on the left, where they are small (an exponential of -|g|, the complement of the error
-// function); the reciprocal is the hardware's (2^-23), of a number between 1 and 2.
+// act(g) and its derivative.  silu g s, s = 1 / (1 + e^-g): derivative s + g s (1 - s); gelu g F(g), F the normal distribution's: F + g f;
+// relu: 0 at 0.  s and F keep their relative accuracy far out on the left, where they are small: an exponential of -|g|, taken 2^32 times too
+// large, since the hardware's knows no numbers below 2^-126, and the complement of the error function.  The hardware's exponential and reciprocal are
+// good to 2^-22 here (for |g| < 20; the exponent's own rounding adds 2^-24 |g|).
 __device__ __forceinline__ float logistic(float g)
 {
-    const float e = expf(-fabsf(g));
+    const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(fabsf(g), -1.4426950408889634f, 32.f)) * 0x1p-32f;
     return (g < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
 }
 __device__ __forceinline__ float normal_cdf(float g) { return 0.5f * erfcf(g * -0.70710678118654752f); }
 
-__device__ __forceinline__ float act_value(int act, float g)
+template <int ACT> __device__ __forceinline__ float act_value(float g)
 {
-    if (act == kActSilu) return g * logistic(g);
-    if (act == kActGelu) return g * normal_cdf(g);
-    return g <= 0.f ? 0.f : g;
+    if constexpr (ACT == kActSilu) return g * logistic(g);
+    else if constexpr (ACT == kActGelu) return g * normal_cdf(g);
+    else return g <= 0.f ? 0.f : g;
 }
 
-__device__ __forceinline__ float act_both(int act, float g, float& slope)
+template <int ACT> __device__ __forceinline__ float act_both(float g, float& slope)
 {
-    if (act == kActSilu) {
+    if constexpr (ACT == kActSilu) {
         const float s = logistic(g);
-        slope = s * (1.f + g * (1.f - s));
-        return g * s;
-    }
-    if (act == kActGelu) {
+        const float a = g * s;
+        slope = __builtin_fmaf(a, 1.f - s, s);
+        return a;
+    } else if constexpr (ACT == kActGelu) {
         const float cdf = normal_cdf(g);
         slope = cdf + g * (0.39894228040143268f * __expf(-0.5f * g * g));
         return g * cdf;
+    } else {
+        slope = g <= 0.f ? 0.f : 1.f;
+        return g <= 0.f ? 0.f : g;
     }
-    slope = g <= 0.f ? 0.f : 1.f;
-    return g <= 0.f ? 0.f : g;
+}
+
+// f(constant) with the activation that `act` names
+template <typename F> __device__ __forceinline__ void with_act(int act, F f)
+{
+    if (act == kActSilu) f(std::integral_constant<int, kActSilu>());
+    else if (act == kActGelu) f(std::integral_constant<int, kActGelu>());
+    else f(std::integral_constant<int, kActRelu>());
 }
 
 template <typename T> __device__ __forceinline__ short bits_of(float x)
@@ -85,30 +95,11 @@ template <typename T> __device__ __forceinline__ short bits_of(float x)
 }
 template <typename T> __device__ __forceinline__ float value_of(short b) { return (float)__builtin_bit_cast(T, b); }
 
-// Eight neighbouring elements of row r from column c on, as far as there are `cols` columns.  (A vector at any even address is one instruction all the same.)
+// Eight neighbouring elements at any even address: one instruction all the same.
 typedef short short8u __attribute__((ext_vector_type(8), aligned(2)));
-__device__ __forceinline__ void store8(const GatedMat& m, int64_t r, int64_t c, int64_t cols, short8v v)
-{
-    short* to = (short*)m.p + r * m.ld + c;
-    if (c + 8 <= cols) {
-        *(short8u*)to = v;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < cols) to[i] = v[i];
-    }
-}
-
-__device__ __forceinline__ short8v load8(const GatedMat& m, int64_t r, int64_t c, int64_t cols)
-{
-    const short* from = (const short*)m.p + r * m.ld + c;
-    if (c + 8 <= cols) return *(const short8u*)from;
-    short8v v = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (c + i < cols) v[i] = from[i];
-    return v;
-}
+__device__ __forceinline__ short* element(const GatedMat& m, int64_t r, int64_t c) { return (short*)m.p + r * m.ld + c; }
+__device__ __forceinline__ void store8(const GatedMat& m, int64_t r, int64_t c, short8v v) { *(short8u*)element(m, r, c) = v; }
+__device__ __forceinline__ short8v load8(const GatedMat& m, int64_t r, int64_t c) { return *(const short8u*)element(m, r, c); }
 
 constexpr int kStep = kGatedStep;
 
@@ -207,18 +198,19 @@ template <bool ADJ, int R> struct Reader {
 template <int TILE> struct Shape;
 template <> struct Shape<kTileLarge> { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, STAGES = 2; };
 template <> struct Shape<kTileMedium> { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, STAGES = 2; };
-template <> struct Shape<kTileSmall> { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, STAGES = 4; };
+template <> struct Shape<kTileSmall> { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, STAGES = 3; };
 template <> struct Shape<kTile32> { static constexpr int BM = 32, BN = 128, WM = 1, WN = 2, STAGES = 4; };
 template <> struct Shape<kTile16> { static constexpr int BM = 16, BN = 128, WM = 1, WN = 2, STAGES = 4; };
 
 template <int TILE> constexpr int tile_threads() { return 64 * Shape<TILE>::WM * Shape<TILE>::WN; }
-// The results leave through shared memory, in one or two turns.
-template <int TILE> constexpr int tile_turns() { return TILE == kTileLarge || TILE == kTileMedium ? 2 : 1; }
+// The results leave through shared memory, in turns; kOpDown's have G and U beside them.
+template <GatedOp OP, int TILE> constexpr int tile_turns() { return TILE == kTileLarge ? (OP == kOpDown ? 4 : 2) : TILE == kTileMedium ? 2 : 1; }
 template <int TILE> constexpr int tile_pitch() { return Shape<TILE>::BN + 4; }             // floats from one row to the next
-template <int TILE> constexpr unsigned tile_lds()
+template <GatedOp OP, int TILE> constexpr unsigned tile_lds()
 {
     using S = Shape<TILE>;
-    constexpr unsigned stages = (unsigned)S::STAGES * (S::BM + S::BN) * 128u, out = (unsigned)(S::BM / tile_turns<TILE>()) * tile_pitch<TILE>() * 4u;
+    constexpr unsigned stages = (unsigned)S::STAGES * (S::BM + S::BN) * 128u, rows = S::BM / tile_turns<OP, TILE>();
+    constexpr unsigned out = rows * (tile_pitch<TILE>() * 4u + (OP == kOpDown ? S::BN * 4u : 0u));
     return stages > out ? stages : out;
 }
 
@@ -403,76 +395,154 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
     }
 
     // Out: a lane holds row lane % 16 and four neighbouring columns of every fragment.  They go to shared memory and come back as eight neighbouring
-    // columns, so that memory is read and written in whole lines and the code for a result stands there once.
-    constexpr int turns = tile_turns<TILE>(), pitch = tile_pitch<TILE>(), wt = wm / turns;        // rows of a wavefront and turn
+    // columns, so that memory is read and written in whole lines and the code for a result stands there once: code that runs once is paid for with the
+    // time that its fetching takes (unrolled, these lines took 20 to 40 us at kOpDown's tiles of 128 and 256).
+    constexpr int turns = tile_turns<OP, TILE>(), pitch = tile_pitch<TILE>(), wt = wm / turns;    // rows of a wavefront and turn
     float* const res = reinterpret_cast<float*>(stage);
-    constexpr int cols8 = (OP == kOpUp ? BN / 2 : BN) / 8, pieces = (BM / turns) * cols8;
+    constexpr int cols8 = (OP == kOpUp ? BN / 2 : BN) / 8, pieces = (BM / turns) * cols8, mine = pieces / threads;
+    static_assert(pieces % threads == 0, "");
+    // piece i of this thread in this turn: its row and first column, and where it stands in shared memory
+    auto place = [&](int turn, int i, int64_t& r, int64_t& c) {
+        const int id = tid + i * threads, lr = id / cols8, lc = 8 * (id % cols8);
+        r = m0 + (lr / wt) * wm + turn * wt + lr % wt;
+        c = n0 + lc;
+        return res + lr * pitch + lc;
+    };
+    auto floats8 = [](const float* from, float* v) {
+        *reinterpret_cast<float4v*>(v) = *reinterpret_cast<const float4v*>(from);
+        *reinterpret_cast<float4v*>(v + 4) = *reinterpret_cast<const float4v*>(from + 4);
+    };
+    constexpr int keep = OP == kOpDown ? mine : 1;
+    short8v gk[keep], uk[keep];                                // G and U of the next turn, on their way
+    short8v* const gus = reinterpret_cast<short8v*>(res + (BM / turns) * pitch) + tid;            // of this turn, a thread's own
+    auto request_gu = [&](int turn) {
+        if constexpr (OP == kOpDown) {
 #pragma unroll
-    for (int turn = 0; turn < turns; ++turn) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < fm / turns; ++i)
-#pragma unroll
-            for (int j = 0; j < fn; ++j) {
-                int col = wcol + 16 * j;
-                if constexpr (OP == kOpUp) col = (j < fn / 2 ? 0 : BN / 2 - wn / 2) + (wave % S::WN) * (wn / 2) + 16 * j;      // G left, U right
-                *reinterpret_cast<float4v*>(res + ((wave / S::WN) * wt + 16 * i + (lane & 15)) * pitch + col + 4 * (lane >> 4)) = acc[turn * (fm / turns) + i][j];
-            }
-        __syncthreads();
-#pragma unroll 1
-        for (int id = tid; id < pieces; id += threads) {
-            const int lr = id / cols8, lc = 8 * (id % cols8);
-            const int64_t r = m0 + (lr / wt) * wm + turn * wt + lr % wt, c = n0 + lc;
-            if (r >= q.M) continue;
-            const float* const at = res + lr * pitch + lc;
-            float v[8];
-            *reinterpret_cast<float4v*>(v) = *reinterpret_cast<const float4v*>(at);
-            *reinterpret_cast<float4v*>(v + 4) = *reinterpret_cast<const float4v*>(at + 4);
-            if constexpr (OP == kOpUp) {
-                if (c >= q.half) continue;
-                float u[8];
-                *reinterpret_cast<float4v*>(u) = *reinterpret_cast<const float4v*>(at + BN / 2);
-                *reinterpret_cast<float4v*>(u + 4) = *reinterpret_cast<const float4v*>(at + BN / 2 + 4);
-                short8v hb, gb, ub;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    hb[k] = c + k < q.N ? bits_of<T>(act_value(q.act, v[k]) * u[k]) : (short)0;
-                    gb[k] = bits_of<T>(v[k]);
-                    ub[k] = bits_of<T>(u[k]);
-                }
-                store8(q.out, r, c, q.half, hb);
-                if (q.g.p) {
-                    store8(q.g, r, c, q.N, gb);
-                    store8(q.u, r, c, q.N, ub);
-                }
-            } else if constexpr (OP == kOpDown) {
-                if (c >= q.half) continue;
-                const short8v gb = load8(q.g, r, c, q.N), ub = load8(q.u, r, c, q.N);
-                short8v hb, dgb, dub;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    float slope;
-                    const float u = value_of<T>(ub[k]), a = act_both(q.act, value_of<T>(gb[k]), slope), dh = v[k];
-                    const bool in = c + k < q.N;
-                    hb[k] = in ? bits_of<T>(a * u) : (short)0;
-                    dub[k] = in ? bits_of<T>(dh * a) : (short)0;
-                    dgb[k] = in ? bits_of<T>(dh * u * slope) : (short)0;
-                }
-                store8(q.out, r, c, q.half, hb);
-                store8(q.out2, r, c, q.half, dgb);
-                store8(q.out2, r, c + q.half, 2 * q.half, dub);
-            } else {
-                short8v b;
-#pragma unroll
-                for (int k = 0; k < 8; ++k) b[k] = bits_of<T>(v[k]);
-                if (OP == kOpWeight && q.half) {               // (q.half is a multiple of 64: eight columns never straddle)
-                    const bool second = c >= q.half;
-                    store8(second ? q.out2 : q.out, r, second ? c - q.half : c, q.N, b);
-                } else {
-                    store8(q.out, r, c, q.N, b);
+            for (int i = 0; i < mine; ++i) {
+                int64_t r, c;
+                place(turn, i, r, c);
+                if (r < q.M && c + 8 <= q.N) {
+                    gk[i] = load8(q.g, r, c);
+                    uk[i] = load8(q.u, r, c);
                 }
             }
         }
+    };
+    request_gu(0);
+#pragma unroll 1
+    for (int turn = 0; turn < turns; ++turn) {
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < turns; ++t)
+            if (t == turn) {
+#pragma unroll
+                for (int i = 0; i < fm / turns; ++i)
+#pragma unroll
+                    for (int j = 0; j < fn; ++j) {
+                        int col = wcol + 16 * j;
+                        if constexpr (OP == kOpUp) col = (j < fn / 2 ? 0 : BN / 2 - wn / 2) + (wave % S::WN) * (wn / 2) + 16 * j;      // G left, U right
+                        *reinterpret_cast<float4v*>(res + ((wave / S::WN) * wt + 16 * i + (lane & 15)) * pitch + col + 4 * (lane >> 4)) =
+                            acc[t * (fm / turns) + i][j];
+                    }
+            }
+        if constexpr (OP == kOpDown) {
+#pragma unroll
+            for (int i = 0; i < mine; ++i) {
+                gus[2 * i * threads] = gk[i];
+                gus[(2 * i + 1) * threads] = uk[i];
+            }
+            if (turn + 1 < turns) request_gu(turn + 1);
+        }
+        __syncthreads();
+        auto work = [&](auto act) {
+#pragma unroll 1
+            for (int i = 0; i < mine; ++i) {
+                int64_t r, c;
+                const float* const at = place(turn, i, r, c);
+                if (r >= q.M) continue;
+                if constexpr (OP == kOpUp) {
+                    if (c + 8 <= q.N) {
+                        float g[8], u[8];
+                        floats8(at, g);
+                        floats8(at + BN / 2, u);
+                        short8v hb, gb, ub;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            hb[k] = bits_of<T>(act_value<act.value>(g[k]) * u[k]);
+                            gb[k] = bits_of<T>(g[k]);
+                            ub[k] = bits_of<T>(u[k]);
+                        }
+                        store8(q.out, r, c, hb);
+                        if (q.g.p) {
+                            store8(q.g, r, c, gb);
+                            store8(q.u, r, c, ub);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int k = 0; k < 8 && c + k < q.half; ++k) {
+                            const bool in = c + k < q.N;
+                            const float g = at[k], u = at[BN / 2 + k];
+                            *element(q.out, r, c + k) = in ? bits_of<T>(act_value<act.value>(g) * u) : (short)0;
+                            if (in && q.g.p) {
+                                *element(q.g, r, c + k) = bits_of<T>(g);
+                                *element(q.u, r, c + k) = bits_of<T>(u);
+                            }
+                        }
+                    }
+                } else if constexpr (OP == kOpDown) {
+                    if (c + 8 <= q.N) {
+                        float dh[8];
+                        floats8(at, dh);
+                        const short8v gb = gus[2 * i * threads], ub = gus[(2 * i + 1) * threads];
+                        short8v hb, dgb, dub;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            float slope;
+                            const float u = value_of<T>(ub[k]), a = act_both<act.value>(value_of<T>(gb[k]), slope);
+                            hb[k] = bits_of<T>(a * u);
+                            dub[k] = bits_of<T>(dh[k] * a);
+                            dgb[k] = bits_of<T>(dh[k] * u * slope);
+                        }
+                        store8(q.out, r, c, hb);
+                        store8(q.out2, r, c, dgb);
+                        store8(q.out2, r, c + q.half, dub);
+                    } else {
+#pragma unroll 1
+                        for (int k = 0; k < 8 && c + k < q.half; ++k) {
+                            float h = 0.f, dg = 0.f, du = 0.f;
+                            if (c + k < q.N) {
+                                float slope;
+                                const float u = value_of<T>(*element(q.u, r, c + k)), a = act_both<act.value>(value_of<T>(*element(q.g, r, c + k)), slope), dh = at[k];
+                                h = a * u;
+                                du = dh * a;
+                                dg = dh * u * slope;
+                            }
+                            *element(q.out, r, c + k) = bits_of<T>(h);
+                            *element(q.out2, r, c + k) = bits_of<T>(dg);
+                            *element(q.out2, r, c + k + q.half) = bits_of<T>(du);
+                        }
+                    }
+                } else {
+                    // (two halves: q.half is a multiple of 64, eight columns never straddle)
+                    const bool second = OP == kOpWeight && q.half && c >= q.half;
+                    const GatedMat& to = second ? q.out2 : q.out;
+                    const int64_t cc = second ? c - q.half : c;
+                    if (cc + 8 <= q.N) {
+                        float v[8];
+                        floats8(at, v);
+                        short8v b;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) b[k] = bits_of<T>(v[k]);
+                        store8(to, r, cc, b);
+                    } else {
+#pragma unroll 1
+                        for (int k = 0; k < 8 && cc + k < q.N; ++k) *element(to, r, cc + k) = bits_of<T>(at[k]);
+                    }
+                }
+            }
+        };
+        if constexpr (OP == kOpUp || OP == kOpDown) with_act(q.act, work);
+        else work(std::integral_constant<int, 0>());
     }
 }
 
@@ -535,10 +605,10 @@ template <typename F> hipError_t each_row_tile(F f)
 
 template <typename T> hipError_t prepare_all()
 {
-    hipError_t e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpUp, t.value>, tile_lds<t.value>()); });
-    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpMul, t.value>, tile_lds<t.value>()); });
-    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpDown, t.value>, tile_lds<t.value>()); });
-    if (e == hipSuccess) e = each_tile([](auto t) { return prepare_kernel(&gated_grads_kernel<T, t.value>, tile_lds<t.value>()); });
+    hipError_t e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpUp, t.value>, tile_lds<kOpUp, t.value>()); });
+    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpMul, t.value>, tile_lds<kOpMul, t.value>()); });
+    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpDown, t.value>, tile_lds<kOpDown, t.value>()); });
+    if (e == hipSuccess) e = each_tile([](auto t) { return prepare_kernel(&gated_grads_kernel<T, t.value>, tile_lds<kOpWeight, t.value>()); });
     return e;
 }
 
@@ -547,7 +617,7 @@ template <typename T, GatedOp OP> hipError_t launch_op(const GatedProduct& q, hi
     const dim3 grid((unsigned)(q.tiles_m * q.tiles_n * q.splits));
     return each_row_tile([&](auto t) {
         if (q.tile != t.value) return hipSuccess;
-        hipLaunchKernelGGL((gated_tile_kernel<T, OP, t.value>), grid, dim3(tile_threads<t.value>()), tile_lds<t.value>(), stream, q);
+        hipLaunchKernelGGL((gated_tile_kernel<T, OP, t.value>), grid, dim3(tile_threads<t.value>()), (tile_lds<OP, t.value>()), stream, q);
         return hipGetLastError();
     });
 }
@@ -579,7 +649,7 @@ template <typename T> hipError_t launch_grads(const GatedProduct* input, const G
     if (end == 0) return hipSuccess;
     return each_tile([&](auto t) {
         if (tile != t.value) return hipSuccess;
-        hipLaunchKernelGGL((gated_grads_kernel<T, t.value>), dim3((unsigned)end), dim3(tile_threads<t.value>()), tile_lds<t.value>(), stream, g);
+        hipLaunchKernelGGL((gated_grads_kernel<T, t.value>), dim3((unsigned)end), dim3(tile_threads<t.value>()), (tile_lds<kOpWeight, t.value>()), stream, g);
         return hipGetLastError();
     });
 }
