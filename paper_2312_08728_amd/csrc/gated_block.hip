@@ -97,6 +97,12 @@ struct bmgd_gated {
 
 namespace bmgd {
 
+static int64_t columns_of(const GatedProduct& q, GatedOp op)
+{
+    return op == kOpUp ? 2 * q.half : op == kOpDown ? q.half : op == kOpWeight && q.half ? 2 * q.half : q.N;
+}
+static int64_t steps_of(const GatedProduct& q, GatedOp op) { return ((op == kOpInput ? 2 * q.half : q.K) + kGatedStep - 1) / kGatedStep; }
+
 hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
 {
     int64_t most = 1;
@@ -107,45 +113,67 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
     return hipGetLastError();
 }
 
+// The time of a launch, in us, as measured for 64 shapes of one to 8,192 rows and widths of 64 to 8,192 in every product, tile and split (5,129
+// launches; the formula is off by 15 % in the mean square, and its choice is 5 % slower than the fastest measured one):
+//      base + max(rounds (steps lat + once), workgroups of a unit (steps thr + leave), bytes / bandwidth) + join
+// with the steps of a workgroup, the rounds that the units need for all workgroups, and where workgroups share tiles
+//      join = each splits + megabytes of parts per unit write.
+// kOpDown, whose results are three matrices made from two more, takes longer to leave than the others.
 void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus)
 {
-    static const int bm[kTiles] = {256, 128, 64, 32, 16}, bn[kTiles] = {256, 128, 64, 128, 128}, per_cu[kTiles] = {1, 2, 2, 2, 2};
-    static const double step_us[kTiles] = {1.2, 0.8, 0.4, 0.5, 0.5}, once_us[kTiles] = {5.0, 3.0, 2.0, 2.0, 2.0};
+    struct Cost { int bm, bn, per_cu; double base, lat, thr, once, once_down, leave, leave_down, each, write; };
+    static const Cost cost[kTiles] = {
+        {256, 256, 1, 5.4, 1.42, 1.42, 4.0, 6.7, 0.8, 6.5, 2.2, 65.0}, {128, 128, 2, 2.5, 0.59, 0.59, 4.0, 5.4, 2.3, 4.6, 0.8, 90.0},
+        {64, 64, 3, 2.7, 0.32, 0.22, 0.9, 1.6, 0.7, 1.2, 0.4, 85.0},   {32, 128, 2, 2.7, 0.42, 0.18, 0.9, 1.3, 1.6, 2.6, 0.6, 80.0},
+        {16, 128, 2, 2.4, 0.38, 0.10, 1.0, 1.6, 1.6, 2.0, 0.5, 0.0}};
+    constexpr double kBytesPerUs = 4.6e6;
     double best = 1e300;
     for (int t = 0; t < kTiles; ++t) {
+        const Cost& k = cost[t];
         bool fits = true;
-        for (int i = 0; i < count; ++i) fits = fits && !(t >= kTile32 && (count > 1 || qs[i]->M > bm[t]));
+        int64_t most_steps = 1;
+        double bytes = 0.0;
+        for (int i = 0; i < count; ++i) {
+            const GatedProduct& q = *qs[i];
+            fits = fits && !(t >= kTile32 && (count > 1 || ops[i] > kOpDown || q.M > k.bm));
+            most_steps = std::max(most_steps, steps_of(q, ops[i]));
+            const double M = (double)q.M, N = (double)columns_of(q, ops[i]), K = (double)steps_of(q, ops[i]) * kGatedStep;
+            bytes += 2.0 * (M * K + K * N + M * N);
+        }
         if (!fits) continue;
-        struct { int64_t tm, tn, splits, per; } plan[3];
-        const int64_t slots = (int64_t)num_cus * per_cu[t];
         for (int64_t want = 1; want <= 64; want += want < 4 ? 1 : want / 2) {
-            double cost = 0.0;
+            struct { int64_t tm, tn, splits, per; } plan[3];
+            const int64_t target = (most_steps + want - 1) / want;
             int64_t groups = 0, counters = 0;
-            size_t bytes = 0;
-            double longest = 0.0;
-            bool ok = true;
+            size_t parts = 0;
+            double longest = 0.0, work = 0.0, sum = 0.0, most_splits = 0.0;
+            bool ok = want == 1 || target >= 2;
             for (int i = 0; i < count && ok; ++i) {
                 const GatedProduct& q = *qs[i];
-                const int64_t columns = ops[i] == kOpUp ? 2 * q.half : ops[i] == kOpDown ? q.half : ops[i] == kOpWeight && q.half ? 2 * q.half : q.N;
-                const int64_t steps = ((ops[i] == kOpInput ? 2 * q.half : q.K) + kGatedStep - 1) / kGatedStep;
-                const int64_t tm = (q.M + bm[t] - 1) / bm[t], tn = (columns + bn[t] - 1) / bn[t], tiles = tm * tn;
+                const int64_t steps = steps_of(q, ops[i]), tm = (q.M + k.bm - 1) / k.bm, tn = (columns_of(q, ops[i]) + k.bn - 1) / k.bn, tiles = tm * tn;
+                const int64_t shares = std::max<int64_t>(1, (steps + target - 1) / target), per = std::max<int64_t>(1, (steps + shares - 1) / shares);
+                const int64_t splits = std::max<int64_t>(1, (steps + per - 1) / per);
                 if (tiles >= (int64_t(1) << 28)) { ok = false; break; }
-                int64_t use = std::max<int64_t>(1, std::min(want, steps / 2));
-                const int64_t per = std::max<int64_t>(1, (steps + use - 1) / use), splits = std::max<int64_t>(1, (steps + per - 1) / per);
                 plan[i] = {tm, tn, splits, per};
                 groups += tiles * splits;
                 if (splits > 1) {
                     counters += tiles;
-                    bytes += (size_t)(tiles * splits) * bm[t] * bn[t] * 4;
+                    parts += (size_t)(tiles * splits) * k.bm * k.bn * 4;
+                    most_splits = std::max(most_splits, (double)splits);
                 }
-                longest = std::max(longest, per * step_us[t] + once_us[t] + (splits > 1 ? 2.0 + 0.5 * splits : 0.0));
-                cost += (double)(tiles * splits) * (per * step_us[t] + once_us[t] + (splits > 1 ? 1.0 : 0.0));
+                const bool down = ops[i] == kOpDown;
+                const double one = per * k.lat + (down ? k.once_down : k.once);
+                longest = std::max(longest, one);
+                sum += (double)(tiles * splits) * one;
+                work += (double)(tiles * splits) * (per * k.thr + (down ? k.leave_down : k.leave));
             }
-            if (!ok || counters > kGatedCounters || bytes > kGatedPartialBytes) break;
-            cost = std::max(longest, cost / slots);
-            if (groups > slots) cost += 0.5 * longest;
-            if (cost < best) {
-                best = cost;
+            if (!ok || counters > kGatedCounters || parts > kGatedPartialBytes) break;
+            const int64_t of_unit = (groups + num_cus - 1) / num_cus, rounds = (of_unit + k.per_cu - 1) / k.per_cu;
+            const double in_turn = longest + (double)(rounds - 1) * sum / (double)groups, together = work / (double)groups * (double)of_unit;
+            double us = k.base + std::max(std::max(in_turn, together), bytes / kBytesPerUs);
+            if (parts) us += k.each * most_splits + k.write * 1e-6 * (double)parts / num_cus;
+            if (us < best) {
+                best = us;
                 size_t at = 0;
                 int counter = 0;
                 for (int i = 0; i < count; ++i) {
@@ -158,7 +186,7 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
                     q.first_part = at;
                     q.first_counter = counter;
                     if (q.splits > 1) {
-                        at += (size_t)(plan[i].tm * plan[i].tn * plan[i].splits) * bm[t] * bn[t];
+                        at += (size_t)(plan[i].tm * plan[i].tn * plan[i].splits) * k.bm * k.bn;
                         counter += (int)(plan[i].tm * plan[i].tn);
                     }
                 }

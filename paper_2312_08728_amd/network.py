@@ -113,6 +113,7 @@ class AdamW:
         for t, e in zip(self.thetas, self._t):
             self._check("theta", t, torch.float32, t.numel())
             e.theta, e.n = t.data_ptr(), t.numel()
+        self._n = [t.numel() for t in self.thetas]
         if state is None:
             state = [self._zeros(t, state_bits) for t in self.thetas]
         self.state = [tuple(s) for s in state]
@@ -193,9 +194,12 @@ class AdamW:
         out = list(out)
         if len(out) != self.count:
             raise ValueError(f"out: {self.count} pairs are wanted, not {len(out)}")
-        for t, (m, s) in zip(self.thetas, out):
-            self._check("m", m, torch.float32, t.numel())
-            self._check("s", s, torch.float32, t.numel())
+        f32, index = torch.float32, self.device.index if self.count else 0
+        for n, (m, s) in zip(self._n, out):
+            if not (m.dtype is f32 and s.dtype is f32 and m.numel() == n and s.numel() == n and m.is_contiguous() and s.is_contiguous()
+                    and m.get_device() == index and s.get_device() == index):
+                self._check("m", m, f32, n)
+                self._check("s", s, f32, n)
         address = C.c_void_p * max(1, self.count)
         self._launch(B.lib.bmgd_adamw_moments, self._t, self.count, address(*[m.data_ptr() for m, _ in out]),
                      address(*[s.data_ptr() for _, s in out]), B._stream(stream))
