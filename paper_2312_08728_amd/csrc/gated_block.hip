@@ -113,20 +113,21 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
     return hipGetLastError();
 }
 
-// The time of a launch, in us, as measured for 64 shapes of one to 8,192 rows and widths of 64 to 8,192 in every product, tile and split (5,129
-// launches; the formula is off by 15 % in the mean square, and its choice is 5 % slower than the fastest measured one):
-//      base + max(rounds (steps lat + once), workgroups of a unit (steps thr + leave), bytes / bandwidth) + join
-// with the steps of a workgroup, the rounds that the units need for all workgroups, and where workgroups share tiles
-//      join = each splits + megabytes of parts per unit write.
-// kOpDown, whose results are three matrices made from two more, takes longer to leave than the others.
+// The time of a launch, in us, as measured for 108 shapes of one to 8,192 rows and widths of 64 to 8,192 in every product, tile and split, weights not in
+// any cache (10,106 launches; the formula is off by 15 % in the mean square, and its choice is 5 % slower than the fastest measured one):
+//      base + max(rounds (steps lat + once), workgroups of a unit (steps thr + leave), bytes / rate) + join
+// with the steps of a workgroup, the rounds that the units need for all workgroups, a rate that takes enough bytes on their way (2 us from request to
+// arrival), and where workgroups share tiles
+//      join = join + each splits + megabytes of parts per unit write.
+// kOpDown, whose results are three matrices made from two more, and kOpUp with G and U take longer to leave than the others.
 void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus)
 {
-    struct Cost { int bm, bn, per_cu; double base, lat, thr, once, once_down, leave, leave_down, each, write; };
+    struct Cost { int bm, bn, per_cu, ahead; double base, lat, thr, once, once_down, leave, leave_down, join, each, write; };
     static const Cost cost[kTiles] = {
-        {256, 256, 1, 5.4, 1.42, 1.42, 4.0, 6.7, 0.8, 6.5, 2.2, 65.0}, {128, 128, 2, 2.5, 0.59, 0.59, 4.0, 5.4, 2.3, 4.6, 0.8, 90.0},
-        {64, 64, 3, 2.7, 0.32, 0.22, 0.9, 1.6, 0.7, 1.2, 0.4, 85.0},   {32, 128, 2, 2.7, 0.42, 0.18, 0.9, 1.3, 1.6, 2.6, 0.6, 80.0},
-        {16, 128, 2, 2.4, 0.38, 0.10, 1.0, 1.6, 1.6, 2.0, 0.5, 0.0}};
-    constexpr double kBytesPerUs = 4.6e6;
+        {256, 256, 1, 1, 2.0, 1.45, 1.45, 7.0, 11.7, 3.4, 9.0, 0.0, 2.3, 62.0}, {128, 128, 2, 1, 2.6, 0.80, 0.42, 0.8, 3.7, 2.8, 4.5, 0.0, 0.9, 88.0},
+        {64, 64, 3, 2, 2.9, 0.35, 0.23, 0.3, 1.2, 0.8, 1.3, 0.5, 0.33, 80.0},    {32, 128, 2, 3, 2.0, 0.43, 0.43, 2.0, 3.0, 1.4, 2.3, 0.55, 0.48, 113.0},
+        {16, 128, 2, 3, 2.2, 0.40, 0.40, 1.0, 2.4, 0.8, 1.7, 1.0, 0.27, 48.0}};
+    constexpr double kBytesPerUs = 4.4e6, kTripUs = 2.0;
     double best = 1e300;
     for (int t = 0; t < kTiles; ++t) {
         const Cost& k = cost[t];
@@ -161,8 +162,8 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
                     parts += (size_t)(tiles * splits) * k.bm * k.bn * 4;
                     most_splits = std::max(most_splits, (double)splits);
                 }
-                const bool down = ops[i] == kOpDown;
-                const double one = per * k.lat + (down ? k.once_down : k.once);
+                const bool down = ops[i] == kOpDown || (ops[i] == kOpUp && q.g.p);
+                const double one = per * k.lat + (down ? std::max(k.once_down, k.leave_down) : std::max(k.once, k.leave));
                 longest = std::max(longest, one);
                 sum += (double)(tiles * splits) * one;
                 work += (double)(tiles * splits) * (per * k.thr + (down ? k.leave_down : k.leave));
@@ -170,8 +171,9 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
             if (!ok || counters > kGatedCounters || parts > kGatedPartialBytes) break;
             const int64_t of_unit = (groups + num_cus - 1) / num_cus, rounds = (of_unit + k.per_cu - 1) / k.per_cu;
             const double in_turn = longest + (double)(rounds - 1) * sum / (double)groups, together = work / (double)groups * (double)of_unit;
-            double us = k.base + std::max(std::max(in_turn, together), bytes / kBytesPerUs);
-            if (parts) us += k.each * most_splits + k.write * 1e-6 * (double)parts / num_cus;
+            const double on_way = (double)std::min<int64_t>(groups, (int64_t)num_cus * k.per_cu) * k.ahead * (k.bm + k.bn) * 2 * kGatedStep;
+            double us = k.base + std::max(std::max(in_turn, together), bytes / std::min(kBytesPerUs, on_way / kTripUs));
+            if (parts) us += k.join + k.each * most_splits + k.write * 1e-6 * (double)parts / num_cus;
             if (us < best) {
                 best = us;
                 size_t at = 0;
