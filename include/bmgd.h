@@ -530,7 +530,7 @@ typedef struct bmgd_adamw_config {
     double  lr;             /* finite, >= 0 */
     double  beta1;          /* in [0, 1) */
     double  beta2;          /* in [0, 1) */
-    double  eps;            /* finite, >= 0; > 0 with moments in 8 bits */
+    double  eps;            /* finite, >= 0; >= 2^-126 with moments in 8 bits */
     double  weight_decay;   /* finite, >= 0 */
     double  grad_scale;     /* finite: 1 / loss scale, times a clipping factor */
     int32_t grad_dtype;     /* BMGD_F32, BMGD_BF16 or BMGD_F16 */
@@ -542,8 +542,8 @@ typedef struct bmgd_adamw_config {
 /* lr 1e-3, beta1 0.9, beta2 0.999, eps 1e-8, weight_decay 0.01, grad_scale 1, fp32 gradients, bf16 copies, 32 bits. */
 void bmgd_adamw_default_config(bmgd_adamw_config* cfg);
 
-/* Update number `step` (>= 1) of all `count` tensors, in ceil(count / 48) launches on `stream`, which must belong to the current
- * device.  `tensors` is host memory, read before the call returns.  Everything is checked before the first launch.
+/* Update number `step` (>= 1) of all `count` tensors, in one launch for 108 tensors or fewer (more where their
+ * addresses are 2^32 elements apart), on `stream`, which must belong to the current device.  `tensors` is host memory, read before the call returns.  Everything is checked before the first launch.
  * Asynchronous, allocates nothing, keeps nothing.  Message of a failure: bmgd_last_error(NULL). */
 int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tensor* tensors, int64_t count, int64_t step, void* stream);
 

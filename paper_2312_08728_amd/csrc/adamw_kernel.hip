@@ -28,7 +28,7 @@ namespace {
 
 constexpr int kThreads = 256, kBlock = 256;                  // threads of a workgroup; elements that share a scale
 constexpr int kPiece = 4 * kThreads;                          // elements that a workgroup takes at a time
-constexpr int kMaxTensors = 48;                               // of a launch: they travel as kernel arguments
+constexpr int kMaxTensors = 108;                              // of a launch: they travel as kernel arguments
 
 static_assert(sizeof(bmgd_adamw_tensor) == 64, "");
 
@@ -38,18 +38,27 @@ struct Rates {
     float keep, lr, eps, grad_scale;
 };
 
-struct Args {
-    bmgd_adamw_tensor t[kMaxTensors];
-    unsigned first[kMaxTensors + 1];                          // first workgroup of each tensor; behind the last one the number of workgroups
+// The tensors of a launch.  Addresses are told as distances from the lowest of their kind, in elements (codes: in words of four), so that a tensor takes 36 bytes of
+// the kernel arguments' 4 KB; tensors too far apart for that go to different launches.
+enum { kTheta, kGrad, kCopy, kM, kS, kMScale, kSScale, kKinds };
+struct Table {
+    char* base[kKinds];
+    unsigned far[kMaxTensors][kKinds];
+    unsigned n[kMaxTensors];
+    unsigned first[kMaxTensors];                              // first workgroup of each tensor
     int count;
-    int copy_dtype;
+};
+
+constexpr unsigned kNone = ~0u;                               // no copy of this tensor
+
+struct Args {
+    Table t;
+    int has_copy, copy_dtype;
     Rates r;
 };
 
-struct MomentArgs {
-    struct One { const signed char* m; const unsigned char* s; const float* m_scale; const float* s_scale; float* m_out; float* s_out; int64_t n; } t[kMaxTensors];
-    unsigned first[kMaxTensors + 1];
-    int count;
+struct MomentArgs {                                           // kTheta: m's values, kGrad: s's
+    Table t;
 };
 static_assert(sizeof(Args) <= 4096 && sizeof(MomentArgs) <= 4096, "kernel arguments");
 
@@ -58,11 +67,14 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 typedef short short4u __attribute__((ext_vector_type(4), aligned(2)));
 
 // Which tensor workgroup `id` works on.
-__device__ __forceinline__ int tensor_of(const unsigned* first, int count, unsigned id)
+__device__ __forceinline__ int tensor_of(const Table& t, unsigned id)
 {
     const int lane = threadIdx.x & 63;
-    return __popcll(__ballot(lane < count && first[min(lane, count)] <= id)) - 1;
+    int n = __popcll(__ballot(lane < t.count && t.first[min(lane, kMaxTensors - 1)] <= id));
+    if (t.count > 64) n += __popcll(__ballot(64 + lane < t.count && t.first[min(64 + lane, kMaxTensors - 1)] <= id));
+    return __builtin_amdgcn_readfirstlane(n - 1);
 }
+static_assert(kMaxTensors <= 128, "");
 
 template <typename T> __device__ __forceinline__ float4v load_grad(const void* p, int64_t at, int64_t left);
 
@@ -161,118 +173,131 @@ __device__ __forceinline__ float s_value(unsigned code, float scale)
     return scale * (t * t);
 }
 
-// One element.  Products and sums are rounded one by one, so that the codes do not depend on what the compiler joins.
-__device__ __forceinline__ float update(const Rates& r, float theta, float g, float& m, float& s)
+// The square root to 2^-23 of its value, also of what the hardware's takes for zero.
+__device__ __forceinline__ float quick_sqrt(float x)
+{
+    const bool small = x < 0x1p-96f;
+    return __builtin_amdgcn_sqrtf(small ? x * 0x1p64f : x) * (small ? 0x1p-32f : 1.f);
+}
+
+// One element.  Products and sums are rounded one by one, so that the codes do not depend on what the compiler joins.  QUICK: the hardware's square root and
+// reciprocal (with moments in 8 bits the instructions count, and what they add, 2^-22 of the step, is far below what the codes do; eps is a normal number there).
+template <bool QUICK> __device__ __forceinline__ float update(const Rates& r, float theta, float g, float& m, float& s)
 {
 #pragma clang fp contract(off)
     g = g * r.grad_scale;
     m = r.b1 * m + r.c1 * g;
     s = r.b2 * s + r.c2 * (g * g);
-    const float bottom = sqrtf(s * r.s_fix) + r.eps;
-    return theta * r.keep - r.lr * (m * r.m_fix / bottom);
+    if constexpr (QUICK) return theta * r.keep - r.lr * (m * r.m_fix * __builtin_amdgcn_rcpf(quick_sqrt(s * r.s_fix) + r.eps));
+    return theta * r.keep - r.lr * (m * r.m_fix / (sqrtf(s * r.s_fix) + r.eps));
 }
 
-template <typename G, bool EIGHT, int U>
+template <typename G, bool EIGHT>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(Args a)
 {
-    const int which = __builtin_amdgcn_readfirstlane(tensor_of(a.first, a.count, blockIdx.x));
-    const bmgd_adamw_tensor t = a.t[which];
-    const int64_t start = (int64_t)(blockIdx.x - a.first[which]) * (kPiece * U) + 4 * threadIdx.x;
-    float4v theta[U], g[U], m[U], s[U];
-    unsigned mc[U], sc[U];
-    float ma[U], sa[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t at = start + u * kPiece, left = t.n - at;
-        g[u] = load_grad<G>(t.grad, at, left);
-        theta[u] = load_grad<float>(t.theta, at, left);
-        if constexpr (EIGHT) {
-            mc[u] = sc[u] = 0u;
-            ma[u] = sa[u] = 0.f;
-            if (left >= 4) {
-                mc[u] = *reinterpret_cast<const unsigned*>(static_cast<const char*>(t.m) + at);
-                sc[u] = *reinterpret_cast<const unsigned*>(static_cast<const char*>(t.s) + at);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < left) {
-                        mc[u] |= (unsigned)static_cast<const unsigned char*>(t.m)[at + i] << (8 * i);
-                        sc[u] |= (unsigned)static_cast<const unsigned char*>(t.s)[at + i] << (8 * i);
-                    }
-            }
-            if (left > 0) {
-                ma[u] = t.m_scale[at / kBlock];
-                sa[u] = t.s_scale[at / kBlock];
-            }
-        } else {
-            m[u] = load_grad<float>(t.m, at, left);
-            s[u] = load_grad<float>(t.s, at, left);
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int64_t at = start + u * kPiece, left = t.n - at;
-        if constexpr (EIGHT) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                m[u][i] = m_value((int)(signed char)(mc[u] >> (8 * i)), ma[u]);
-                s[u][i] = s_value(sc[u] >> (8 * i) & 255u, sa[u]);
-            }
-        }
+    const int which = tensor_of(a.t, blockIdx.x);
+    const unsigned* const far = a.t.far[which];
+    float* const theta_at = reinterpret_cast<float*>(a.t.base[kTheta]) + far[kTheta];
+    const char* const grad_at = a.t.base[kGrad] + sizeof(G) * (size_t)far[kGrad];
+    char* const copy_at = a.t.base[kCopy] + 2 * (size_t)far[kCopy];
+    char* const m_at = a.t.base[kM] + 4 * (size_t)far[kM];
+    char* const s_at = a.t.base[kS] + 4 * (size_t)far[kS];
+    const bool copies = a.has_copy && far[kCopy] != kNone;
+    const int64_t at = (int64_t)(blockIdx.x - a.t.first[which]) * kPiece + 4 * threadIdx.x, left = (int64_t)a.t.n[which] - at;
+    const float4v g = load_grad<G>(grad_at, at, left);
+    float4v theta = load_grad<float>(theta_at, at, left);
+    if constexpr (!EIGHT) {
+        if (left <= 0) return;
+        float4v m = load_grad<float>(m_at, at, left), s = load_grad<float>(s_at, at, left);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float mi = m[u][i], si = s[u][i];
-            theta[u][i] = update(a.r, theta[u][i], g[u][i], mi, si);
-            m[u][i] = mi;
-            s[u][i] = si;
+            float mi = m[i], si = s[i];
+            theta[i] = update<false>(a.r, theta[i], g[i], mi, si);
+            m[i] = mi;
+            s[i] = si;
+        }
+        store_floats(theta_at + at, left, theta);
+        store_floats(reinterpret_cast<float*>(m_at) + at, left, m);
+        store_floats(reinterpret_cast<float*>(s_at) + at, left, s);
+        if (copies) store_copy(copy_at, a.copy_dtype, at, left, theta);
+    } else {
+#pragma clang fp contract(off)
+        // (a wavefront whose block lies behind the tensor's end leaves as a whole)
+        if (left + 4 * (int64_t)(threadIdx.x & 63) <= 0) return;
+        float* const ma_at = reinterpret_cast<float*>(a.t.base[kMScale]) + far[kMScale] + at / kBlock;
+        float* const sa_at = reinterpret_cast<float*>(a.t.base[kSScale]) + far[kSScale] + at / kBlock;
+        unsigned mc = 0u, sc = 0u;
+        if (left >= 4) {
+            mc = *reinterpret_cast<const unsigned*>(m_at + at);
+            sc = *reinterpret_cast<const unsigned*>(s_at + at);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (i < left) {
+                    mc |= (unsigned)(unsigned char)m_at[at + i] << (8 * i);
+                    sc |= (unsigned)(unsigned char)s_at[at + i] << (8 * i);
+                }
+        }
+        const float ma = *ma_at, sa = *sa_at;
+        float m[4], s[4];
+        unsigned m_top = 0u, s_top = 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            m[i] = m_value((int)(signed char)(mc >> (8 * i)), ma);
+            s[i] = s_value(sc >> (8 * i) & 255u, sa);
+            theta[i] = update<true>(a.r, theta[i], g[i], m[i], s[i]);
+            if (i < left) {
+                m_top = max(m_top, __float_as_uint(m[i]) & 0x7FFFFFFFu);
+                s_top = max(s_top, __float_as_uint(s[i]) & 0x7FFFFFFFu);
+            }
         }
         if (left > 0) {
-            store_floats(t.theta + at, left, theta[u]);
-            if (t.copy) store_copy(t.copy, a.copy_dtype, at, left, theta[u]);
-            if constexpr (!EIGHT) {
-                store_floats(static_cast<float*>(t.m) + at, left, m[u]);
-                store_floats(static_cast<float*>(t.s) + at, left, s[u]);
+            store_floats(theta_at + at, left, theta);
+            if (copies) store_copy(copy_at, a.copy_dtype, at, left, theta);
+        }
+        float m_inv, s_inv;
+        const float m_scale = scale_of(wave_max(m_top), m_inv), s_scale = scale_of(wave_max(s_top), s_inv);
+        // Where the codes lie, with the hardware's square root (2^-23); the next to a middle between two codes is taken again with the exact one, so that
+        // codes are those of exact roots.  255 2^-22 is the most that the two can be apart.
+        float mr[4], sr[4], middle = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = fabsf(m[i]) * m_inv, y = s[i] * s_inv;
+            const float mf = 127.f * __builtin_amdgcn_sqrtf(x), sf = 255.f * __builtin_amdgcn_sqrtf(__builtin_amdgcn_sqrtf(y));
+            mr[i] = rintf(mf);
+            sr[i] = rintf(sf);
+            middle = fmaxf(middle, fmaxf(fabsf(mf - mr[i]), fabsf(sf - sr[i])));
+        }
+        if (middle > 0.4999f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                mr[i] = rintf(127.f * sqrtf(fabsf(m[i]) * m_inv));
+                sr[i] = rintf(255.f * sqrtf(sqrtf(s[i] * s_inv)));
             }
         }
-        if constexpr (EIGHT) {
-#pragma clang fp contract(off)
-            unsigned m_top = 0u, s_top = 0u;
+        unsigned mb = 0u, sb = 0u;
+        if (m_inv > 0.f) {                                     // (otherwise a scale that is zero or not finite: all codes are zero)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < 4; ++i) mb |= ((unsigned)(int)copysignf(mr[i], m[i]) & 255u) << (8 * i);
+        }
+        if (s_inv > 0.f) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sb |= (unsigned)(s[i] > 0.f ? fmaxf(sr[i], 1.f) : 0.f) << (8 * i);
+        }
+        if (left >= 4) {
+            *reinterpret_cast<unsigned*>(m_at + at) = mb;
+            *reinterpret_cast<unsigned*>(s_at + at) = sb;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
                 if (i < left) {
-                    m_top = max(m_top, __float_as_uint(m[u][i]) & 0x7FFFFFFFu);
-                    s_top = max(s_top, __float_as_uint(s[u][i]) & 0x7FFFFFFFu);
+                    m_at[at + i] = (char)(mb >> (8 * i));
+                    s_at[at + i] = (char)(sb >> (8 * i));
                 }
-            }
-            float m_inv, s_inv;
-            const float m_scale = scale_of(wave_max(m_top), m_inv), s_scale = scale_of(wave_max(s_top), s_inv);
-            unsigned mb = 0u, sb = 0u;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                // (an inverse of zero: a scale that is zero or not finite; all codes are zero then)
-                const float size = rintf(127.f * sqrtf(fabsf(m[u][i]) * m_inv));
-                const int mq = m_inv > 0.f ? (int)copysignf(size, m[u][i]) : 0;
-                float root = rintf(255.f * sqrtf(sqrtf(s[u][i] * s_inv)));
-                if (s[u][i] > 0.f) root = fmaxf(root, 1.f);
-                const unsigned sq = s_inv > 0.f ? (unsigned)root : 0u;
-                mb |= ((unsigned)mq & 255u) << (8 * i);
-                sb |= sq << (8 * i);
-            }
-            if (left >= 4) {
-                *reinterpret_cast<unsigned*>(static_cast<char*>(t.m) + at) = mb;
-                *reinterpret_cast<unsigned*>(static_cast<char*>(t.s) + at) = sb;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < left) {
-                        static_cast<unsigned char*>(t.m)[at + i] = (unsigned char)(mb >> (8 * i));
-                        static_cast<unsigned char*>(t.s)[at + i] = (unsigned char)(sb >> (8 * i));
-                    }
-            }
-            if (left > 0 && (threadIdx.x & 63) == 0) {
-                t.m_scale[at / kBlock] = m_scale;
-                t.s_scale[at / kBlock] = s_scale;
-            }
+        }
+        if ((threadIdx.x & 63) == 0) {
+            *ma_at = m_scale;
+            *sa_at = s_scale;
         }
     }
 }
@@ -292,9 +317,17 @@ __device__ __forceinline__ float s_exported(unsigned code, float scale)
 
 __global__ void __launch_bounds__(kThreads) adamw_moments_kernel(MomentArgs a)
 {
-    const int which = __builtin_amdgcn_readfirstlane(tensor_of(a.first, a.count, blockIdx.x));
-    const MomentArgs::One t = a.t[which];
-    const int64_t at = (int64_t)(blockIdx.x - a.first[which]) * kPiece + 4 * threadIdx.x, left = t.n - at;
+    const int which = tensor_of(a.t, blockIdx.x);
+    const unsigned* const far = a.t.far[which];
+    struct { const signed char* m; const unsigned char* s; const float* m_scale; const float* s_scale; float* m_out; float* s_out; int64_t n; } t;
+    t.m = reinterpret_cast<const signed char*>(a.t.base[kM] + 4 * (size_t)far[kM]);
+    t.s = reinterpret_cast<const unsigned char*>(a.t.base[kS] + 4 * (size_t)far[kS]);
+    t.m_scale = reinterpret_cast<const float*>(a.t.base[kMScale]) + far[kMScale];
+    t.s_scale = reinterpret_cast<const float*>(a.t.base[kSScale]) + far[kSScale];
+    t.m_out = reinterpret_cast<float*>(a.t.base[kTheta]) + far[kTheta];
+    t.s_out = reinterpret_cast<float*>(a.t.base[kGrad]) + far[kGrad];
+    t.n = a.t.n[which];
+    const int64_t at = (int64_t)(blockIdx.x - a.t.first[which]) * kPiece + 4 * threadIdx.x, left = t.n - at;
     if (left <= 0) return;
     const float ma = t.m_scale[at / kBlock], sa = t.s_scale[at / kBlock];
     float4v m = {0.f, 0.f, 0.f, 0.f}, s = {0.f, 0.f, 0.f, 0.f};
@@ -343,17 +376,74 @@ bool aligned(const void* p, size_t to) { return (reinterpret_cast<uintptr_t>(p) 
 constexpr int64_t kMaxElements = int64_t(1) << 38;
 constexpr int64_t kMaxWorkgroups = int64_t(1) << 30;
 
-template <typename G, bool EIGHT, int U> hipError_t launch_step(const Args& a, hipStream_t s)
+template <typename G> hipError_t launch_step(const Args& a, unsigned groups, bool eight, hipStream_t s)
 {
-    hipLaunchKernelGGL((adamw_kernel<G, EIGHT, U>), dim3(a.first[a.count]), dim3(kThreads), 0, s, a);
+    if (eight) hipLaunchKernelGGL((adamw_kernel<G, true>), dim3(groups), dim3(kThreads), 0, s, a);
+    else hipLaunchKernelGGL((adamw_kernel<G, false>), dim3(groups), dim3(kThreads), 0, s, a);
     return hipGetLastError();
 }
 
-template <typename G> hipError_t launch_step(const Args& a, bool eight, int per, hipStream_t s)
+// Collects tensors into tables of one launch each.
+struct Collector {
+    Table t;
+    uintptr_t lo[kKinds], hi[kKinds];       // of the addresses of each kind that the table has
+    uintptr_t at[kMaxTensors][kKinds];
+    int64_t groups;
+
+    void clear()
+    {
+        t.count = 0;
+        groups = 0;
+        for (int k = 0; k < kKinds; ++k) lo[k] = hi[k] = 0;
+    }
+    // False if the table has no place for it: close the table first.  p[k] = 0: none of this kind.
+    bool add(const uintptr_t* p, const int* size, int64_t n, int64_t need)
+    {
+        if (t.count == kMaxTensors || (t.count > 0 && groups + need > kMaxWorkgroups)) return false;
+        uintptr_t l[kKinds], h[kKinds];
+        for (int k = 0; k < kKinds; ++k) {
+            l[k] = lo[k];
+            h[k] = hi[k];
+            if (!p[k]) continue;
+            if (!l[k] || p[k] < l[k]) l[k] = p[k];
+            if (p[k] > h[k]) h[k] = p[k];
+            // (distances are whole elements: an address is a multiple of its element's size)
+            if ((h[k] - l[k]) / size[k] >= kNone) return false;
+        }
+        for (int k = 0; k < kKinds; ++k) {
+            lo[k] = l[k];
+            hi[k] = h[k];
+            at[t.count][k] = p[k];
+        }
+        t.n[t.count] = (unsigned)n;
+        t.first[t.count++] = (unsigned)groups;
+        groups += need;
+        return true;
+    }
+    const Table& close(const int* size)
+    {
+        for (int k = 0; k < kKinds; ++k) t.base[k] = reinterpret_cast<char*>(lo[k]);
+        for (int i = 0; i < t.count; ++i)
+            for (int k = 0; k < kKinds; ++k) t.far[i][k] = at[i][k] ? (unsigned)((at[i][k] - lo[k]) / size[k]) : kNone;
+        return t;
+    }
+};
+
+constexpr int64_t kEntry = int64_t(1) << 31;                  // elements of one entry of a table: longer tensors take several
+
+// f(entry's addresses, elements) for the pieces of a tensor; advance[k]: bytes that 256 elements take
+template <typename F> int entries_of(const uintptr_t* p, const int* advance, int64_t n, F f)
 {
-    if (eight) return per == 1 ? launch_step<G, true, 1>(a, s) : launch_step<G, true, 4>(a, s);
-    return per == 1 ? launch_step<G, false, 1>(a, s) : launch_step<G, false, 4>(a, s);
+    for (int64_t from = 0; from < n; from += kEntry) {
+        uintptr_t q[kKinds];
+        for (int k = 0; k < kKinds; ++k) q[k] = p[k] ? p[k] + (uintptr_t)(from / kBlock) * advance[k] : 0;
+        const int rc = f(q, n - from < kEntry ? n - from : kEntry);
+        if (rc != BMGD_OK) return rc;
+    }
+    return BMGD_OK;
 }
+
+uintptr_t address(const void* p) { return reinterpret_cast<uintptr_t>(p); }
 
 }  // namespace
 
@@ -392,9 +482,8 @@ BMGD_API int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tens
     if (cfg->copy_dtype != BMGD_BF16 && cfg->copy_dtype != BMGD_F16) return fail(BMGD_EINVAL, "bmgd_adamw_step: copy_dtype must be BMGD_BF16 or BMGD_F16");
     if (cfg->state_bits != 32 && cfg->state_bits != 8) return fail(BMGD_EINVAL, "bmgd_adamw_step: state_bits must be 32 or 8");
     const bool eight = cfg->state_bits == 8;
-    if (eight && (float)cfg->eps == 0.f) return fail(BMGD_EINVAL, "bmgd_adamw_step: moments in 8 bits need eps > 0");
+    if (eight && !((float)cfg->eps >= 0x1p-126f)) return fail(BMGD_EINVAL, "bmgd_adamw_step: moments in 8 bits need eps >= 2^-126");
     if (step < 1 || step > (int64_t(1) << 53)) return fail(BMGD_EINVAL, "bmgd_adamw_step: step must be in [1, 2^53]");
-    int64_t total = 0;
     for (int64_t i = 0; i < count; ++i) {
         const bmgd_adamw_tensor& t = tensors[i];
         if (t.n < 0 || t.n > kMaxElements) return tensor_fail(call, i, "n must be in [0, 2^38]");
@@ -404,10 +493,7 @@ BMGD_API int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tens
             return tensor_fail(call, i, "an address is not a multiple of its element's size (codes: of 4)");
         if (eight && (!t.m_scale || !t.s_scale || !aligned(t.m_scale, 4) || !aligned(t.s_scale, 4)))
             return tensor_fail(call, i, "m_scale and s_scale must not be NULL and 4-byte aligned");
-        total += t.n;
     }
-    // A workgroup takes 4096 elements; 1024 where that would leave compute units without one.
-    const int per = total >= (int64_t(1) << 20) ? 4 : 1;
     Args a;
     a.copy_dtype = cfg->copy_dtype;
     const double k = (double)step;
@@ -421,26 +507,34 @@ BMGD_API int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tens
     a.r.lr = (float)cfg->lr;
     a.r.eps = (float)cfg->eps;
     a.r.grad_scale = (float)cfg->grad_scale;
-    a.count = 0;
-    int64_t groups = 0;
-    for (int64_t i = 0; i <= count; ++i) {
-        const int64_t n = i < count ? tensors[i].n : 0, need = (n + kPiece * per - 1) / (kPiece * per);
-        if (a.count > 0 && (i == count || a.count == kMaxTensors || groups + need > kMaxWorkgroups)) {
-            a.first[a.count] = (unsigned)groups;
-            const hipStream_t s = static_cast<hipStream_t>(stream);
-            const hipError_t e = cfg->grad_dtype == BMGD_F32 ? launch_step<float>(a, eight, per, s)
-                                 : cfg->grad_dtype == BMGD_BF16 ? launch_step<__bf16>(a, eight, per, s) : launch_step<_Float16>(a, eight, per, s);
-            if (e != hipSuccess) return hip_fail(e, "launch of the AdamW step");
-            a.count = 0;
-            groups = 0;
-        }
-        if (need > 0) {
-            a.t[a.count] = tensors[i];
-            a.first[a.count++] = (unsigned)groups;
-            groups += need;
-        }
+    const int grad = cfg->grad_dtype == BMGD_F32 ? 4 : 2;
+    const int size[kKinds] = {4, grad, 2, 4, 4, 4, 4}, advance[kKinds] = {4 * kBlock, grad * kBlock, 2 * kBlock, eight ? kBlock : 4 * kBlock, eight ? kBlock : 4 * kBlock, 4, 4};
+    Collector c;
+    c.clear();
+    auto send = [&]() {
+        if (c.t.count == 0) return (int)BMGD_OK;
+        a.has_copy = c.lo[kCopy] != 0;
+        a.t = c.close(size);
+        const hipStream_t s = static_cast<hipStream_t>(stream);
+        const unsigned groups = (unsigned)c.groups;
+        const hipError_t e = cfg->grad_dtype == BMGD_F32 ? launch_step<float>(a, groups, eight, s)
+                             : cfg->grad_dtype == BMGD_BF16 ? launch_step<__bf16>(a, groups, eight, s) : launch_step<_Float16>(a, groups, eight, s);
+        c.clear();
+        return e == hipSuccess ? (int)BMGD_OK : hip_fail(e, "launch of the AdamW step");
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        const bmgd_adamw_tensor& t = tensors[i];
+        const uintptr_t p[kKinds] = {address(t.theta), address(t.grad), address(t.copy), address(t.m), address(t.s), eight ? address(t.m_scale) : 0, eight ? address(t.s_scale) : 0};
+        const int rc = entries_of(p, advance, t.n, [&](const uintptr_t* q, int64_t n) {
+            const int64_t need = (n + kPiece - 1) / kPiece;
+            if (c.add(q, size, n, need)) return (int)BMGD_OK;
+            const int r = send();
+            c.add(q, size, n, need);
+            return r;
+        });
+        if (rc != BMGD_OK) return rc;
     }
-    return BMGD_OK;
+    return send();
 }
 
 BMGD_API int bmgd_adamw_moments(const bmgd_adamw_tensor* tensors, int64_t count, float* const* m_out, float* const* s_out, void* stream)
@@ -455,27 +549,31 @@ BMGD_API int bmgd_adamw_moments(const bmgd_adamw_tensor* tensors, int64_t count,
         if (!aligned(t.m, 4) || !aligned(t.s, 4) || !aligned(t.m_scale, 4) || !aligned(t.s_scale, 4) || !aligned(m_out[i], 4) || !aligned(s_out[i], 4))
             return tensor_fail(call, i, "addresses must be multiples of 4");
     }
-    MomentArgs a;
-    a.count = 0;
-    int64_t groups = 0;
-    for (int64_t i = 0; i <= count; ++i) {
-        const int64_t n = i < count ? tensors[i].n : 0, need = (n + kPiece - 1) / kPiece;
-        if (a.count > 0 && (i == count || a.count == kMaxTensors || groups + need > kMaxWorkgroups)) {
-            a.first[a.count] = (unsigned)groups;
-            hipLaunchKernelGGL(adamw_moments_kernel, dim3(a.first[a.count]), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return hip_fail(e, "launch of the moments' values");
-            a.count = 0;
-            groups = 0;
-        }
-        if (need > 0) {
-            const bmgd_adamw_tensor& t = tensors[i];
-            a.t[a.count] = {static_cast<const signed char*>(t.m), static_cast<const unsigned char*>(t.s), t.m_scale, t.s_scale, m_out[i], s_out[i], t.n};
-            a.first[a.count++] = (unsigned)groups;
-            groups += need;
-        }
+    const int size[kKinds] = {4, 4, 2, 4, 4, 4, 4}, advance[kKinds] = {4 * kBlock, 4 * kBlock, 0, kBlock, kBlock, 4, 4};
+    Collector c;
+    c.clear();
+    auto send = [&]() {
+        if (c.t.count == 0) return (int)BMGD_OK;
+        MomentArgs a;
+        a.t = c.close(size);
+        hipLaunchKernelGGL(adamw_moments_kernel, dim3((unsigned)c.groups), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
+        c.clear();
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? (int)BMGD_OK : hip_fail(e, "launch of the moments' values");
+    };
+    for (int64_t i = 0; i < count; ++i) {
+        const bmgd_adamw_tensor& t = tensors[i];
+        const uintptr_t p[kKinds] = {address(m_out[i]), address(s_out[i]), 0, address(t.m), address(t.s), address(t.m_scale), address(t.s_scale)};
+        const int rc = entries_of(p, advance, t.n, [&](const uintptr_t* q, int64_t n) {
+            const int64_t need = (n + kPiece - 1) / kPiece;
+            if (c.add(q, size, n, need)) return (int)BMGD_OK;
+            const int r = send();
+            c.add(q, size, n, need);
+            return r;
+        });
+        if (rc != BMGD_OK) return rc;
     }
-    return BMGD_OK;
+    return send();
 }
 
 }  // extern "C"
