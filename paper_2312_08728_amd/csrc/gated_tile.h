@@ -121,21 +121,16 @@ template <bool ADJ, int R, int THREADS> struct Mover {
     {
         return 2 * (k & 3) + (R >= 128 ? 8 * ((k >> 3) & 1) : 0);
     }
-    // Adjacent: element (row, k) at base + row * ld + k, rows of the tile from r0 on, `limit` rows in all.
-    // Strided: element (k, column) at base + k * ld + column, columns from r0 on, `limit` columns that may be read.
-    // pick(piece) turns a strided tile's piece into (base, column); the default is `base` and r0 + 8 piece.
+    // Adjacent: element (row, k) at base + row * ld + k; pick(row of the tile) is where its row begins.
+    // Strided: element (k, column) at base + k * ld + column; pick(piece of a row of the tile) is where its eight columns begin.
     template <typename Pick>
-    __device__ __forceinline__ void start(int64_t r0, int64_t limit, int64_t ld, int64_t k0, int tid, Pick pick)
+    __device__ __forceinline__ void start(int64_t ld, int64_t k0, int tid, Pick pick)
     {
         if constexpr (ADJ) {
             const int s = tid & 7;
             at = 8 * (s ^ ((tid >> 3) & 7));                  // (rows of one thread's pieces are multiples of 8 apart)
 #pragma unroll
-            for (int i = 0; i < kPieces; ++i) {
-                int64_t r = r0 + i * (THREADS / 8) + (tid >> 3);
-                if (r >= limit) r = limit - 1;
-                src[i] = pick(0) + r * ld + k0 + at;
-            }
+            for (int i = 0; i < kPieces; ++i) src[i] = pick(i * (THREADS / 8) + (tid >> 3)) + k0 + at;
         } else {
             at = tid / kRow;
 #pragma unroll
@@ -280,20 +275,20 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
     const int s0 = split * q.per_split, s1 = min(steps, s0 + q.per_split);
     const unsigned short* zeros = (const unsigned short*)q.zeros;
 
-    Mover<a_adj, BM, threads> ma;
-    Mover<b_adj, BN, threads> mb;
     const unsigned short* pa = (const unsigned short*)q.a.p;
     const unsigned short* pb = (const unsigned short*)q.b.p;
     const unsigned short* pb2 = (const unsigned short*)q.b2.p;
-    ma.start(m0, q.M, q.a.ld, (int64_t)s0 * kStep, tid, [&](int c) {
-        if constexpr (a_adj) return pa;
-        else { const int64_t col = m0 + 8 * c; return pa + (col < q.a_cols ? col : q.a_cols - 8); }
-    });
+    // where row (adjacent) or the eight columns from `at` on (strided) of the left tile begin; what is behind the last ones is read from these
+    auto left_at = [&](int at) {
+        if constexpr (a_adj) { const int64_t r = m0 + at; return pa + (r < q.M ? r : q.M - 1) * q.a.ld; }
+        else { const int64_t c = m0 + at; return pa + (c < q.a_cols ? c : q.a_cols - 8); }
+    };
     const int half_steps = OP == kOpInput ? (int)(q.half / kStep) : 0;
+    Mover<b_adj, BN, threads> mb;
     auto start_b = [&](int step) {
         const bool second = OP == kOpInput && step >= half_steps;
-        mb.start(n0, q.N, q.b.ld, (int64_t)(second ? step - half_steps : step) * kStep, tid, [&](int c) {
-            if constexpr (b_adj) return second ? pb2 : pb;
+        mb.start(q.b.ld, (int64_t)(second ? step - half_steps : step) * kStep, tid, [&](int c) {
+            if constexpr (b_adj) { const int64_t r = n0 + c; return (second ? pb2 : pb) + (r < q.N ? r : q.N - 1) * q.b.ld; }
             else if constexpr (OP == kOpUp) {                  // a wavefront's columns: wn / 2 of Wg, then the same of Wu
                 const int w = c / (wn / 8), in = c % (wn / 8);
                 const int64_t col = n0 + w * (wn / 2) + (in % (wn / 16)) * 8;
@@ -303,22 +298,15 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
     };
     start_b(s0);
     const unsigned lds_a = lds0 + (unsigned)__builtin_amdgcn_readfirstlane(wave * 1024), lds_b = lds_a + stages * a_bytes;
-    auto request = [&](int step, int buf) {
-        const int64_t k0 = (int64_t)step * kStep;
-        // the left operand of kOpMul and kOpInput has zeros behind its columns
-        ma.request(lds_a + buf * a_bytes, q.a.ld, OP == kOpMul || OP == kOpInput ? (int64_t)kStep : q.K - k0, zeros);
-        if constexpr (OP == kOpInput) {
-            if (step == half_steps && step > s0) start_b(step);
-            mb.request(lds_b + buf * b_bytes, q.b.ld, q.K - (step >= half_steps ? k0 - q.half : k0), zeros);
-        } else {
-            mb.request(lds_b + buf * b_bytes, q.b.ld, q.K - k0, zeros);
-        }
+    // elements of the sum that are left from `step` on; the left operand of kOpMul and kOpInput has zeros behind its columns
+    auto left_a = [&](int step) { return OP == kOpMul || OP == kOpInput ? (int64_t)kStep : q.K - (int64_t)step * kStep; };
+    auto request_b = [&](int step, int buf) {
+        if (OP == kOpInput && step == half_steps && step > s0) start_b(step);
+        mb.request(lds_b + buf * b_bytes, q.b.ld, q.K - (int64_t)(OP == kOpInput && step >= half_steps ? step - half_steps : step) * kStep, zeros);
     };
 
-    Reader<a_adj, BM> ra;
     Reader<b_adj, BN> rb;
     const int wrow = (wave / S::WN) * wm, wcol = (wave % S::WN) * wn;
-    ra.start(wrow, lane);
     rb.start(wcol, lane);
 
     float4v acc[fm][fn];
@@ -327,32 +315,121 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
 #pragma unroll
         for (int j = 0; j < fn; ++j) acc[i][j] = float4v{0.f, 0.f, 0.f, 0.f};
 
-    constexpr int loads = Mover<a_adj, BM, threads>::kPieces + Mover<b_adj, BN, threads>::kPieces;      // of a thread and step
+    if constexpr (TILE == kTileLarge) {
+        // One workgroup to a unit, so the matrix units wait for whatever its wavefronts wait for.  What took the time was the way from L2 to shared memory:
+        // 64 KB a step, 2,760 cycles if nothing else is done and requests never pause, against 2,048 of the matrix units; asked for in one go at the head
+        // of a step and waited for at its end it took 3,600.  So the requests are spread over the step, and each has a whole step to come back.
+        // The left tile is two sub-tiles, of the first and of the second 64 rows of both rows of wavefronts, and a step's matrix instructions go through
+        // the first, then through the second.  The right operands of a step are all in registers before its first half is done: with the first half, the place of
+        // the right tile and of the first sub-tile are free for the step after the next.
+        //   first half    requests the second sub-tile of the next step;    ends when this step's second sub-tile has come
+        //   second half   requests the right tile and the first sub-tile of the step after the next;    ends when those of the next step have come
+        // Operands are read two fragments ahead, across the meetings too.
+        static_assert(S::WM == 2 && wm == 128 && fn == 4 && stages == 2, "");
+        using Sub = Mover<a_adj, 128, threads>;
+        constexpr unsigned sub_bytes = 128 * 128;
+        constexpr int sub_loads = Sub::kPieces, late = sub_loads, early = sub_loads + Mover<b_adj, BN, threads>::kPieces;
+        Sub sub[2];
 #pragma unroll
-    for (int i = 0; i < stages - 1; ++i)
-        if (s0 + i < s1) request(s0 + i, i);
-    int buf = 0;
-    for (int s = s0; s < s1; ++s) {
-        const int behind = s1 - 1 - s;                         // steps behind this one
-        if (stages > 2 && behind >= stages - 2) wait_and_meet<(stages - 2) * loads>();
-        else if (stages > 3 && behind == 1) wait_and_meet<loads>();
-        else wait_and_meet<0>();
-        // (all have read the step before this one, whose place is free now)
-        if (behind >= stages - 1) request(s + stages - 1, buf == 0 ? stages - 1 : buf - 1);
-        const unsigned ta = lds0 + buf * a_bytes, tb = lds0 + stages * a_bytes + buf * b_bytes;
+        for (int x = 0; x < 2; ++x)
+            sub[x].start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { const int at = a_adj ? r : 8 * r; return left_at(at + (at & 64) + 64 * x); });
+        Reader<a_adj, 128> ra;
+        ra.start((wave / S::WN) * 64, lane);
+        auto request_sub = [&](int step, int x) { sub[x].request(lds_a + ((step - s0) & 1) * a_bytes + x * sub_bytes, q.a.ld, left_a(step), zeros); };
+        // fragment e of a step: rows 16 (e / 2) .. + 15 of the wavefront's, half e % 2 of the sum
+        auto read_a = [&](unsigned t, int e) { return ra.read(t + (e >= 8 ? sub_bytes : 0u), (e >> 1) & 3, e & 1); };
+        short8v af[4], bf[2][fn];
+        if (s0 < s1) {
+            request_b(s0, 0);
+            request_sub(s0, 0);
+            request_sub(s0, 1);
+            if (s0 + 1 < s1) {
+                request_b(s0 + 1, 1);
+                request_sub(s0 + 1, 0);
+                wait_and_meet<late + early>();
+            } else {
+                wait_and_meet<0>();
+            }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            short8v af[fm], bf[fn];
-#pragma unroll
-            for (int j = 0; j < fn; ++j) bf[j] = rb.read(tb, j, h);
-#pragma unroll
-            for (int i = 0; i < fm; ++i) af[i] = ra.read(ta, i, h);
-#pragma unroll
-            for (int i = 0; i < fm; ++i)
-#pragma unroll
-                for (int j = 0; j < fn; ++j) acc[i][j] = Half<T>::mma(bf[j], af[i], acc[i][j]);
+            for (int j = 0; j < fn; ++j) {
+                bf[0][j] = rb.read(lds0 + stages * a_bytes, j, 0);
+                bf[1][j] = rb.read(lds0 + stages * a_bytes, j, 1);
+            }
+            af[0] = read_a(lds0, 0);
+            af[1] = read_a(lds0, 1);
         }
-        buf = buf + 1 == stages ? 0 : buf + 1;
+        for (int s = s0; s < s1; ++s) {
+            const int buf = (s - s0) & 1;
+            const unsigned ta = lds0 + buf * a_bytes, na = lds0 + (buf ^ 1) * a_bytes, nb = lds0 + stages * a_bytes + (buf ^ 1) * b_bytes;
+            const bool next = s + 1 < s1, after = s + 2 < s1;
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                if (e == 2 && next) request_sub(s + 1, 1);
+                if (e == 6) {
+                    if (next) wait_and_meet<late + early>();
+                    else wait_and_meet<0>();
+                }
+                if (e == 8 && after) request_sub(s + 2, 0);
+                if (e == 10 && after) request_b(s + 2, buf);
+                if (e == 14) {
+                    if (after) wait_and_meet<late + early>();
+                    else wait_and_meet<0>();
+                }
+                if (e < 14) {
+                    af[(e + 2) & 3] = read_a(ta, e + 2);
+                    af[(e + 3) & 3] = read_a(ta, e + 3);
+                } else if (next) {
+                    af[0] = read_a(na, 0);
+                    af[1] = read_a(na, 1);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int j = 0; j < fn; ++j) acc[e >> 1][j] = Half<T>::mma(bf[h][j], af[(e + h) & 3], acc[e >> 1][j]);
+                    if (e == 14 && next) {
+#pragma unroll
+                        for (int j = 0; j < fn; ++j) bf[h][j] = rb.read(nb, j, h);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+    } else {
+        Mover<a_adj, BM, threads> ma;
+        ma.start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { return left_at(a_adj ? r : 8 * r); });
+        Reader<a_adj, BM> ra;
+        ra.start(wrow, lane);
+        auto request = [&](int step, int buf) {
+            ma.request(lds_a + buf * a_bytes, q.a.ld, left_a(step), zeros);
+            request_b(step, buf);
+        };
+        constexpr int loads = Mover<a_adj, BM, threads>::kPieces + Mover<b_adj, BN, threads>::kPieces;      // of a thread and step
+#pragma unroll
+        for (int i = 0; i < stages - 1; ++i)
+            if (s0 + i < s1) request(s0 + i, i);
+        int buf = 0;
+        for (int s = s0; s < s1; ++s) {
+            const int behind = s1 - 1 - s;                         // steps behind this one
+            if (stages > 2 && behind >= stages - 2) wait_and_meet<(stages - 2) * loads>();
+            else if (stages > 3 && behind == 1) wait_and_meet<loads>();
+            else wait_and_meet<0>();
+            // (all have read the step before this one, whose place is free now)
+            if (behind >= stages - 1) request(s + stages - 1, buf == 0 ? stages - 1 : buf - 1);
+            const unsigned ta = lds0 + buf * a_bytes, tb = lds0 + stages * a_bytes + buf * b_bytes;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                short8v af[fm], bf[fn];
+#pragma unroll
+                for (int j = 0; j < fn; ++j) bf[j] = rb.read(tb, j, h);
+#pragma unroll
+                for (int i = 0; i < fm; ++i) af[i] = ra.read(ta, i, h);
+#pragma unroll
+                for (int i = 0; i < fm; ++i)
+#pragma unroll
+                    for (int j = 0; j < fn; ++j) acc[i][j] = Half<T>::mma(bf[j], af[i], acc[i][j]);
+            }
+            buf = buf + 1 == stages ? 0 : buf + 1;
+        }
     }
 
     if (q.splits > 1) {
