@@ -119,13 +119,14 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
 // with the steps of a workgroup, the rounds that the units need for all workgroups, a rate that takes enough bytes on their way (2.2 us from request to
 // arrival), and where workgroups share tiles
 //      join = join + each splits + megabytes of parts per unit write.
-// kOpDown, whose results are three matrices made from two more, and kOpUp with G and U take longer to leave than the others.
+// kOpDown, whose results are three matrices made from two more, and kOpUp, which may leave G and U, take longer to leave than the others.  (Whether G and U
+// are wanted does not count: Y has the same bits either way.)
 void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus)
 {
     struct Cost { int bm, bn, per_cu, ahead; double base, lat, thr, once, once_down, leave, leave_down, join, each, write; };
     static const Cost cost[kTiles] = {
-        {256, 256, 1, 1, 2.0, 1.45, 1.45, 7.0, 11.7, 3.4, 9.0, 0.0, 2.3, 62.0}, {128, 128, 2, 1, 2.6, 0.80, 0.42, 0.8, 3.7, 2.8, 4.5, 0.0, 0.9, 88.0},
-        {64, 64, 3, 2, 2.9, 0.35, 0.23, 0.3, 1.2, 0.8, 1.3, 0.5, 0.33, 80.0},    {32, 128, 2, 3, 2.0, 0.43, 0.43, 2.0, 3.0, 1.4, 2.3, 0.55, 0.48, 60.0},
+        {256, 256, 1, 1, 2.0, 1.27, 1.27, 4.5, 9.0, 4.5, 9.9, 0.0, 2.35, 61.0}, {128, 128, 2, 1, 2.0, 0.65, 0.65, 2.2, 4.3, 2.2, 4.3, 0.0, 0.65, 77.0},
+        {64, 64, 3, 2, 3.0, 0.29, 0.29, 0.8, 1.4, 0.6, 1.2, 0.55, 0.32, 70.0},   {32, 128, 2, 3, 2.0, 0.43, 0.43, 2.0, 3.0, 1.4, 2.3, 0.55, 0.48, 60.0},
         {16, 128, 2, 3, 2.2, 0.40, 0.40, 1.0, 2.4, 0.8, 1.7, 1.0, 0.27, 48.0}};
     constexpr double kBytesPerUs = 4.4e6, kTripUs = 2.2;
     double best = 1e300;
@@ -162,7 +163,7 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
                     parts += (size_t)(tiles * splits) * k.bm * k.bn * 4;
                     most_splits = std::max(most_splits, (double)splits);
                 }
-                const bool down = ops[i] == kOpDown || (ops[i] == kOpUp && q.g.p);
+                const bool down = ops[i] == kOpDown || ops[i] == kOpUp;
                 const double one = per * k.lat + (down ? std::max(k.once_down, k.leave_down) : std::max(k.once, k.leave));
                 longest = std::max(longest, one);
                 sum += (double)(tiles * splits) * one;

@@ -212,7 +212,7 @@ template <bool ADJ, int R> struct Reader {
 // Tile, wavefronts along its rows and columns, steps in shared memory (all but one of them on their way).
 template <int TILE> struct Shape;
 template <> struct Shape<kTileLarge> { static constexpr int BM = 256, BN = 256, WM = 2, WN = 4, STAGES = 2; };
-template <> struct Shape<kTileMedium> { static constexpr int BM = 128, BN = 128, WM = 2, WN = 2, STAGES = 2; };
+template <> struct Shape<kTileMedium> { static constexpr int BM = 128, BN = 128, WM = 2, WN = 4, STAGES = 2; };
 template <> struct Shape<kTileSmall> { static constexpr int BM = 64, BN = 64, WM = 2, WN = 2, STAGES = 3; };
 template <> struct Shape<kTile32> { static constexpr int BM = 32, BN = 128, WM = 1, WN = 2, STAGES = 4; };
 template <> struct Shape<kTile16> { static constexpr int BM = 16, BN = 128, WM = 1, WN = 2, STAGES = 4; };
