@@ -7,6 +7,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <atomic>
 #include <new>
 
 using namespace bmgd;
@@ -114,20 +115,20 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
 }
 
 // The time of a launch, in us, as measured for 108 shapes of one to 8,192 rows and widths of 64 to 8,192 in every product, tile and split, weights not in
-// any cache (10,106 launches; the formula is off by 15 % in the mean square, and its choice is 5 % slower than the fastest measured one):
+// any cache (10,106 launches; near the fastest ones of a shape the formula is off by 13 % in the mean square, and its choice is 4 % slower than the fastest):
 //      base + max(rounds (steps lat + once), workgroups of a unit (steps thr + leave), bytes / rate) + join
 // with the steps of a workgroup, the rounds that the units need for all workgroups, a rate that takes enough bytes on their way (2.2 us from request to
 // arrival), and where workgroups share tiles
 //      join = join + each splits + megabytes of parts per unit write.
-// kOpDown, whose results are three matrices made from two more, and kOpUp, which may leave G and U, take longer to leave than the others.  (Whether G and U
-// are wanted does not count: Y has the same bits either way.)
+// Nothing but sizes counts, not what is at hand or wanted besides: Y has the same bits whether G and U are kept or not.
 void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus)
 {
-    struct Cost { int bm, bn, per_cu, ahead; double base, lat, thr, once, once_down, leave, leave_down, join, each, write; };
+    struct Cost { int bm, bn, per_cu, ahead; double lat, thr, once[3], leave[3], join, each, write; };       // [kOpUp, kOpDown, the others]
     static const Cost cost[kTiles] = {
-        {256, 256, 1, 1, 2.0, 1.27, 1.27, 4.5, 9.0, 4.5, 9.9, 0.0, 2.35, 61.0}, {128, 128, 2, 1, 2.0, 0.65, 0.65, 2.2, 4.3, 2.2, 4.3, 0.0, 0.65, 77.0},
-        {64, 64, 3, 2, 3.0, 0.29, 0.29, 0.8, 1.4, 0.6, 1.2, 0.55, 0.32, 70.0},   {32, 128, 2, 3, 2.0, 0.43, 0.43, 2.0, 3.0, 1.4, 2.3, 0.55, 0.48, 60.0},
-        {16, 128, 2, 3, 2.2, 0.40, 0.40, 1.0, 2.4, 0.8, 1.7, 1.0, 0.27, 48.0}};
+        {256, 256, 1, 1, 0.17, 1.30, {8.6, 13.7, 10.3}, {7.8, 12.4, 5.2}, 0.0, 2.1, 70.0}, {128, 128, 2, 1, 0.27, 0.62, {1.9, 4.0, 2.8}, {2.0, 3.9, 1.9}, 0.0, 0.6, 73.0},
+        {64, 64, 3, 2, 0.01, 0.27, {1.0, 0.3, 1.2}, {0.7, 1.3, 0.65}, 0.8, 0.29, 66.0},    {32, 128, 2, 3, 0.06, 0.43, {1.3, 2.2, 0.3}, {0.7, 1.5, 0.0}, 0.8, 0.42, 60.0},
+        {16, 128, 2, 3, 0.38, 0.33, {0.9, 1.5, 0.0}, {1.1, 1.7, 0.1}, 0.8, 0.26, 27.0}};
+    constexpr double kBase = 2.8;                              // a launch that does nothing
     constexpr double kBytesPerUs = 4.4e6, kTripUs = 2.2;
     double best = 1e300;
     for (int t = 0; t < kTiles; ++t) {
@@ -163,17 +164,17 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
                     parts += (size_t)(tiles * splits) * k.bm * k.bn * 4;
                     most_splits = std::max(most_splits, (double)splits);
                 }
-                const bool down = ops[i] == kOpDown || ops[i] == kOpUp;
-                const double one = per * k.lat + (down ? std::max(k.once_down, k.leave_down) : std::max(k.once, k.leave));
-                longest = std::max(longest, one);
-                sum += (double)(tiles * splits) * one;
-                work += (double)(tiles * splits) * (per * k.thr + (down ? k.leave_down : k.leave));
+                const int kind = ops[i] == kOpUp ? 0 : ops[i] == kOpDown ? 1 : 2;
+                const double turn = per * k.lat + k.once[kind], share = per * k.thr + k.leave[kind];
+                longest = std::max(longest, std::max(turn, share));
+                sum += (double)(tiles * splits) * turn;
+                work += (double)(tiles * splits) * share;
             }
             if (!ok || counters > kGatedCounters || parts > kGatedPartialBytes) break;
             const int64_t of_unit = (groups + num_cus - 1) / num_cus, rounds = (of_unit + k.per_cu - 1) / k.per_cu;
             const double in_turn = longest + (double)(rounds - 1) * sum / (double)groups, together = work / (double)groups * (double)of_unit;
             const double on_way = (double)std::min<int64_t>(groups, (int64_t)num_cus * k.per_cu) * k.ahead * (k.bm + k.bn) * 2 * kGatedStep;
-            double us = k.base + std::max(std::max(in_turn, together), bytes / std::min(kBytesPerUs, on_way / kTripUs));
+            double us = kBase + std::max(std::max(in_turn, together), bytes / std::min(kBytesPerUs, on_way / kTripUs));
             if (parts) us += k.join + k.each * most_splits + k.write * 1e-6 * (double)parts / num_cus;
             if (us < best) {
                 best = us;
@@ -450,6 +451,18 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
     return BMGD_OK;
 }
 
+// The kernels' shared memory, once per device and type.
+hipError_t prepare_once(int device, bool f16)
+{
+    constexpr int kDevices = 64;
+    static std::atomic<bool> done[kDevices][2];
+    const bool known = device >= 0 && device < kDevices;
+    if (known && done[device][f16].load(std::memory_order_acquire)) return hipSuccess;
+    const hipError_t e = f16 ? gated_prepare_f16() : gated_prepare_bf16();
+    if (e == hipSuccess && known) done[device][f16].store(true, std::memory_order_release);
+    return e;
+}
+
 void destroy(bmgd_gated* b)
 {
     if (!b) return;
@@ -505,7 +518,7 @@ BMGD_API int bmgd_gated_create(const bmgd_gated_config* cfg, bmgd_gated** out)
     if (e != hipSuccess) return bail(e, "hipGetDevice");
     e = hipDeviceGetAttribute(&b->num_cus, hipDeviceAttributeMultiprocessorCount, b->device);
     if (e != hipSuccess) return bail(e, "hipDeviceGetAttribute");
-    e = cfg->dtype == BMGD_F16 ? gated_prepare_f16() : gated_prepare_bf16();
+    e = prepare_once(b->device, cfg->dtype == BMGD_F16);
     if (e != hipSuccess) return bail(e, "hipFuncSetAttribute");
     e = hipEventCreateWithFlags(&b->order, hipEventDisableTiming);
     if (e != hipSuccess) return bail(e, "hipEventCreateWithFlags");

@@ -219,7 +219,7 @@ template <> struct Shape<kTile16> { static constexpr int BM = 16, BN = 128, WM =
 
 template <int TILE> constexpr int tile_threads() { return 64 * Shape<TILE>::WM * Shape<TILE>::WN; }
 // The results leave through shared memory, in turns; kOpDown's have G and U beside them.
-template <GatedOp OP, int TILE> constexpr int tile_turns() { return TILE == kTileLarge ? (OP == kOpDown ? 4 : 2) : TILE == kTileMedium ? 2 : 1; }
+template <GatedOp OP, int TILE> constexpr int tile_turns() { return TILE == kTileLarge ? (OP == kOpDown ? 4 : 2) : TILE == kTileMedium && OP == kOpDown ? 2 : 1; }
 template <int TILE> constexpr int tile_pitch() { return Shape<TILE>::BN + 4; }             // floats from one row to the next
 template <GatedOp OP, int TILE> constexpr unsigned tile_lds()
 {

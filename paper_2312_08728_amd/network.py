@@ -23,9 +23,17 @@ class GatedBlock:
 
     def __init__(self, p, hidden, out_n, max_rows, dtype=B.BMGD_BF16, activation=B.BMGD_ACT_SILU, workspace=None):
         cfg = B.bmgd_gated_config(p, hidden, out_n, max_rows, dtype, activation, None, 0)
+        self.h = None
+        if workspace is None and torch.cuda.is_available():
+            # from torch's pool, where a block of the same size that was closed has left one (an invalid configuration needs 0 bytes and is refused below)
+            need = B.bmgd_gated_workspace_bytes(cfg)
+            if need:
+                workspace = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
+                torch.cuda.current_stream().synchronize()      # work of tensors that had this memory before
+                at = -workspace.data_ptr() % 256
+                workspace = workspace[at:at + need]
         if workspace is not None:
             cfg.workspace, cfg.workspace_bytes = B._ptr(workspace), workspace.numel() * workspace.element_size()
-        self.h = None
         self.cfg, self._keep = cfg, workspace
         rc, h = B.bmgd_gated_create(cfg)
         if rc != B.BMGD_OK:
