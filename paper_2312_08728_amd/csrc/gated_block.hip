@@ -94,6 +94,7 @@ struct bmgd_gated {
     hipStream_t last = nullptr;             // of the call before
     hipEvent_t order = nullptr;
     char err[256] = "";
+    int tile = -1, shares = 0;              // asked for by tests
 };
 
 namespace bmgd {
@@ -121,7 +122,7 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
 // arrival), and where workgroups share tiles
 //      join = join + each splits + megabytes of parts per unit write.
 // Nothing but sizes counts, not what is at hand or wanted besides: Y has the same bits whether G and U are kept or not.
-void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus)
+void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus, int asked_tile, int64_t asked)
 {
     struct Cost { int bm, bn, per_cu, ahead; double lat, thr, once[3], leave[3], join, each, write; };       // [kOpUp, kOpDown, the others]
     static const Cost cost[kTiles] = {
@@ -132,6 +133,7 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
     constexpr double kBytesPerUs = 4.4e6, kTripUs = 2.2;
     double best = 1e300;
     for (int t = 0; t < kTiles; ++t) {
+        if (asked_tile >= 0 && t != asked_tile) continue;
         const Cost& k = cost[t];
         bool fits = true;
         int64_t most_steps = 1;
@@ -144,7 +146,7 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
             bytes += 2.0 * (M * K + K * N + M * N);
         }
         if (!fits) continue;
-        for (int64_t want = 1; want <= 64; want += want < 4 ? 1 : want / 2) {
+        for (int64_t want = asked_tile >= 0 ? asked : 1; want <= 64; want += asked_tile >= 0 ? 64 : want < 4 ? 1 : want / 2) {
             struct { int64_t tm, tn, splits, per; } plan[3];
             const int64_t target = (most_steps + want - 1) / want;
             int64_t groups = 0, counters = 0;
@@ -197,6 +199,7 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
             }
         }
     }
+    if (best == 1e300 && asked_tile >= 0) gated_plan(qs, ops, count, num_cus);
 }
 
 }  // namespace bmgd
@@ -311,7 +314,7 @@ int enter(bmgd_gated* b, hipStream_t s)
 
 void plan(bmgd_gated* b, GatedProduct* const* q, const GatedOp* op, int count)
 {
-    gated_plan(q, op, count, b->num_cus);
+    gated_plan(q, op, count, b->num_cus, b->tile, b->shares);
     for (int i = 0; i < count; ++i) {
         q[i]->act = b->cfg.activation;
         q[i]->partial = reinterpret_cast<float*>(b->base + b->lay.partial) + q[i]->first_part;
@@ -560,5 +563,14 @@ BMGD_API const char* bmgd_gated_last_error(const bmgd_gated* block)
 }
 
 BMGD_API void bmgd_gated_destroy(bmgd_gated* block) { destroy(block); }
+
+// For tests: the kind of tile and the shares of a tile's sum that later calls use where they fit; tile < 0: their own choice again.
+BMGD_API int bmgd_internal_gated_tile(bmgd_gated* block, int32_t tile, int32_t shares)
+{
+    if (!block || tile >= kTiles || shares < 1 || shares > 64) return BMGD_EINVAL;
+    block->tile = tile;
+    block->shares = shares;
+    return BMGD_OK;
+}
 
 }  // extern "C"

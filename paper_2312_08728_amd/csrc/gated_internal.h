@@ -53,7 +53,8 @@ constexpr int kGatedCounters = 4096;
 constexpr int kGatedStep = 64;         // elements of the summed index per step
 
 // Chooses tile and split for the `count` products of one launch, which get one kind of tile.
-void gated_plan(GatedProduct* const* q, const GatedOp* op, int count, int num_cus);
+// tile >= 0: this one and `want` shares of a tile's sum where they fit (tests).
+void gated_plan(GatedProduct* const* q, const GatedOp* op, int count, int num_cus, int tile = -1, int64_t want = 0);
 
 // Once per process and device: lets the kernels use as much shared memory as they need.
 hipError_t gated_prepare_bf16();

@@ -253,3 +253,72 @@ def test_refusals():
     with pytest.raises(B.BmgdError):
         codes = torch.zeros(304, dtype=torch.int8, device="cuda")[1:301]
         B.AdamW([t], [g], state_bits=8, state=[(codes, codes.view(torch.uint8), t[:2], g[:2])]).step()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_more_tensors_than_a_launch_takes(bits):
+    """300 tensors, three launches: each gets its own values."""
+    import torch
+    import paper_2312_08728_amd as B
+    sizes = [1 + (37 * i) % 700 for i in range(300)]
+    thetas, grads, copies = _tensors(sizes, "bf16", "f16", 11)
+    before = [_np(t) for t in thetas]
+    opt = B.AdamW(thetas, grads, copies, lr=LR, beta1=B1, beta2=B2, eps=EPS, weight_decay=WD, state_bits=bits)
+    opt.step()
+    for th0, g, t, c in zip(before, grads, thetas, copies):
+        th1, _, _ = N.adamw(th0, _np(g), 0.0, 0.0, 1, LR, B1, B2, EPS, WD)
+        _check_theta(t, th0, th1, LR)
+        _check_copy(c, t)
+    if bits == 8:
+        for (m, s), g in zip(opt.moments(), grads):
+            assert torch.allclose(m, 0.1 * g.float(), rtol=0.02, atol=1e-4 * float(g.abs().max()))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_tensors_far_apart_in_memory(bits):
+    """Two pieces of one allocation 2^32 elements and more apart, and a copy for one of them only."""
+    import ctypes
+    import torch
+    import paper_2312_08728_amd as B
+    arena = torch.empty((1 << 32) + 5_000, device="cuda")          # 17 GB
+    thetas = [arena[:700], arena[(1 << 32) + 64:(1 << 32) + 64 + 900], arena[1_000:1_300]]
+    for t in thetas:
+        t.copy_(torch.randn(t.numel(), device="cuda"))
+    before = [_np(t) for t in thetas]
+    grads = [torch.randn(t.numel(), device="cuda") for t in thetas]
+    copies = [torch.zeros(t.numel(), dtype=torch.bfloat16, device="cuda") for t in thetas]
+    opt = B.AdamW(thetas, grads, copies, lr=LR, eps=EPS, weight_decay=WD, state_bits=bits)
+    opt._t[0].copy = None
+    opt.step()
+    for th0, g, t in zip(before, grads, thetas):
+        th1, _, _ = N.adamw(th0, _np(g), 0.0, 0.0, 1, LR, 0.9, 0.999, EPS, WD)
+        _check_theta(t, th0, th1, LR)
+    assert (copies[0] == 0).all()
+    _check_copy(copies[1], thetas[1])
+    _check_copy(copies[2], thetas[2])
+    del arena, thetas, opt
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_tensor_of_more_than_two_to_the_31_elements(bits):
+    """Its two entries of a launch meet at element 2^31; values are looked at around there and at both ends."""
+    import torch
+    import paper_2312_08728_amd as B
+    n = (1 << 31) + 3_001
+    theta, g = torch.ones(n, device="cuda"), torch.full((n,), 0.5, dtype=torch.bfloat16, device="cuda")
+    copy = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    opt = B.AdamW([theta], [g], [copy], lr=LR, eps=EPS, weight_decay=0.0, state_bits=bits)
+    opt.step()
+    # the first step of every element is lr (its moments are equal)
+    for at in (0, (1 << 31) - 2_000, n - 4_000):
+        part = theta[at:at + 4_000].double()
+        assert torch.all((part - (1 - LR)).abs() <= 16 * E)
+        assert torch.equal(copy[at:at + 4_000], theta[at:at + 4_000].bfloat16())
+    assert float(theta.min()) == float(theta.max())
+    if bits == 8:
+        m, s = opt.moments()[0]
+        assert torch.all((m[-4_000:] - 0.05).abs() <= 1e-7) and torch.all((s[(1 << 31) - 2_000:(1 << 31) + 2_000] - 2.5e-4).abs() <= 1e-9)
+        del m, s
+    del theta, g, copy, opt
+    torch.cuda.empty_cache()

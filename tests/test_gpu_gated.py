@@ -369,3 +369,75 @@ def test_refusals():
         block.forward(x, gate, up, down, y)
         _check_forward("bf16", "silu", x, gate, up, down, y)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("shares", [1, 3])
+@pytest.mark.parametrize("tile,rows", [(0, (1, 300, 520)), (1, (5, 130, 257)), (2, (1, 63, 200)), (3, (1, 17, 32)), (4, (1, 7, 16))])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_every_kind_of_tile_with_and_without_shared_sums(kind, tile, rows, shares):
+    """Sizes that end inside a tile, inside a step of 64 and at their edges, for each tile whatever the block's own choice would be."""
+    import ctypes
+    import paper_2312_08728_amd as B
+    dtype, code = _types()[kind]
+    for i, (r, (p, f, c)) in enumerate(zip(rows, ((200, 264, 136), (512, 320, 700), (333, 517, 65)))):
+        act = ("silu", "gelu", "relu")[i]
+        x, gate, up, down = _data(r, p, f, c, dtype, 100 + i)
+        dy = _dev(np.random.default_rng(i).standard_normal((r, c)), dtype)
+        with B.GatedBlock(p, f, c, r, dtype=code, activation=_act(act)) as block:
+            assert B.lib.bmgd_internal_gated_tile(ctypes.c_void_p(block.h), tile, shares) == B.BMGD_OK
+            for _ in range(2):                                 # (counters are zero again after a launch)
+                y, g, u = _empty(r, c, dtype), _empty(r, f, dtype), _empty(r, f, dtype)
+                block.forward(x, gate, up, down, y, g, u)
+                _check_forward(kind, act, x, gate, up, down, y, g, u)
+                out = _empty(r, p, dtype), _empty(p, f, dtype), _empty(p, f, dtype), _empty(f, c, dtype)
+                block.backward(dy, x, gate, up, down, g, u, *out)
+                _check_backward(kind, act, dy, x, gate, up, down, g, u, *out)
+
+
+def test_many_rows_at_the_block_s_own_choice():
+    """Enough tiles for the large kind in every product; columns and sums that end inside a tile and a step."""
+    import paper_2312_08728_amd as B
+    dtype, code = _types()["bf16"]
+    r, p, f, c = 2_900, 712, 2_056, 1_416
+    x, gate, up, down = _data(r, p, f, c, dtype, 3)
+    dy = _dev(np.random.default_rng(4).standard_normal((r, c)), dtype)
+    with B.GatedBlock(p, f, c, r, dtype=code) as block:
+        y, g, u = _empty(r, c, dtype), _empty(r, f, dtype), _empty(r, f, dtype)
+        block.forward(x, gate, up, down, y, g, u)
+        _check_forward("bf16", "silu", x, gate, up, down, y, g, u)
+        out = _empty(r, p, dtype), _empty(p, f, dtype), _empty(p, f, dtype), _empty(f, c, dtype)
+        block.backward(dy, x, gate, up, down, g, u, *out)
+        _check_backward("bf16", "silu", dy, x, gate, up, down, g, u, *out)
+
+
+@pytest.mark.parametrize("stride", [1 << 26, (1 << 26) + 3])
+def test_rows_so_far_apart_that_offsets_pass_32_bits(stride):
+    """40 rows of 5.4 GB: element offsets beyond 2^31, in place and through the copy."""
+    import torch
+    import paper_2312_08728_amd as B
+    dtype, code = _types()["bf16"]
+    r, p, f, c = 40, 64, 72, 24
+    x, gate, up, down = _data(r, p, f, c, dtype, 3)
+    far = torch.empty(39 * stride + p, dtype=dtype, device="cuda").as_strided((r, p), (stride, 1))
+    far.copy_(x)
+    out_far = torch.empty(39 * stride + c, dtype=dtype, device="cuda").as_strided((r, c), (stride, 1))
+    with B.GatedBlock(p, f, c, r, dtype=code) as block:
+        block.forward(far, gate, up, down, out_far)
+        _check_forward("bf16", "silu", x, gate, up, down, out_far)
+    del far, out_far
+    torch.cuda.empty_cache()
+
+
+def test_unequal_strides_of_the_two_projections():
+    import paper_2312_08728_amd as B
+    dtype, code = _types()["f16"]
+    r, p, f, c = 30, 64, 128, 64
+    x, gate, up, down = _data(r, p, f, c, dtype, 5, lds=(None, f + 8, f + 64, None))
+    dy = _dev(np.random.default_rng(3).standard_normal((r, c)), dtype)
+    with B.GatedBlock(p, f, c, r, dtype=code) as block:
+        y, g, u = _empty(r, c, dtype), _empty(r, f, dtype), _empty(r, f, dtype)
+        block.forward(x, gate, up, down, y, g, u)
+        _check_forward("f16", "silu", x, gate, up, down, y, g, u)
+        dx = _empty(r, p, dtype)
+        block.backward(dy, x, gate, up, down, g, u, dx=dx)
+        _check_backward("f16", "silu", dy, x, gate, up, down, g, u, dx, None, None, None)

@@ -79,3 +79,7 @@ def test_step_arguments():
     one = (ctypes.c_void_p * 1)(64)
     for m, s in ((None, one), (one, None), ((ctypes.c_void_p * 1)(0), one), (one, (ctypes.c_void_p * 1)(66))):
         assert B.bmgd_adamw_moments(t, 1, m, s) == B.BMGD_EINVAL
+
+
+def test_an_internal_tile_is_checked():
+    assert B.lib.bmgd_internal_gated_tile(None, 0, 1) == B.BMGD_EINVAL
