@@ -67,18 +67,23 @@ int fail_static(int code, const char* call, const char* msg)
 
 struct PackArgs { GatedPack q; };
 
-// A thread moves eight elements.  Read one by one (their address is a multiple of 2 only), written as 16 bytes.
+// A thread moves eight elements, from any even address (one instruction all the same) to 16-byte aligned ones.
 __global__ void __launch_bounds__(256) gated_pack_kernel(PackArgs args)
 {
     typedef unsigned short ushort8 __attribute__((ext_vector_type(8)));
+    typedef unsigned short ushort8u __attribute__((ext_vector_type(8), aligned(2)));
     const GatedPack::One m = args.q.m[blockIdx.y];
     const int64_t per_row = m.to_ld >> 3, pieces = m.rows * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per_row, c = 8 * (i - r * per_row);
+        const int64_t r = pieces >> 31 ? i / per_row : (int64_t)((unsigned)i / (unsigned)per_row), c = 8 * (i - r * per_row);
         const unsigned short* from = m.from + r * m.from_ld + c;
         ushort8 v;
+        if (c + 8 <= m.cols) {
+            v = *(const ushort8u*)from;
+        } else {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = c + k < m.cols ? from[k] : (unsigned short)0;
+            for (int k = 0; k < 8; ++k) v[k] = c + k < m.cols ? from[k] : (unsigned short)0;
+        }
         *(ushort8*)(m.to + r * m.to_ld + c) = v;
     }
 }

@@ -13,6 +13,7 @@ from . import binding as B
 _TYPES = {B.BMGD_BF16: torch.bfloat16, B.BMGD_F16: torch.float16, B.BMGD_F32: torch.float32}
 _CODES = {v: k for k, v in _TYPES.items()}
 _ROWS = object()                    # in place of a matrix's number of rows: that of the call
+_Matrices = C.c_int64 * 24          # bmgd_gated_tensors: twelve addresses and strides
 
 
 class GatedBlock:
@@ -41,41 +42,46 @@ class GatedBlock:
         self.h = h
         self._type = _TYPES[dtype]
         self._device = torch.device("cuda", torch.cuda.current_device())
-        self._x, self._in, self._out, self._hid = (_ROWS, p), (p, hidden), (hidden, out_n), (_ROWS, hidden)
-        self._y = (_ROWS, out_n)
+        self._index = self._device.index
+        self._x, self._in, self._out, self._hid, self._y = (_ROWS, p), (p, hidden), (hidden, out_n), (_ROWS, hidden), (_ROWS, out_n)
 
-    def _matrix(self, name, t, shape, rows):
-        n = rows if shape[0] is _ROWS else shape[0]
+    def _refuse(self, name, t, shape):
         if t.dtype is not self._type or t.device != self._device:
             raise ValueError(f"{name}: a {self._type} tensor on {self._device} is wanted, not {t.dtype} on {t.device}")
-        if t.dim() != 2 or t.shape[0] != n or t.shape[1] != shape[1]:
-            raise ValueError(f"{name}: shape {(n, shape[1])} is wanted, not {tuple(t.shape)}")
-        row, col = t.stride()
-        if col != 1 and shape[1] != 1:
-            raise ValueError(f"{name}: the elements of a row must lie next to each other (strides {t.stride()})")
-        return t.data_ptr(), row
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{name}: shape {shape} is wanted, not {tuple(t.shape)}")
+        raise ValueError(f"{name}: the elements of a row must lie next to each other (strides {t.stride()})")
 
-    def _call(self, fn, rows, list_, stream):
+    def _call(self, fn, rows, matrices, stream):
         flat = []
-        for name, t, shape in list_:
-            flat += (0, 0) if t is None else self._matrix(name, t, shape, rows)
-        rc = fn(self.h, rows, (C.c_int64 * 24)(*flat), B._stream(stream))
+        for name, t, shape in matrices:
+            if t is None:
+                flat += (0, 0)
+                continue
+            if shape[0] is _ROWS:
+                shape = (rows, shape[1])
+            if t.dtype is not self._type or t.get_device() != self._index or t.shape != shape:
+                self._refuse(name, t, shape)
+            stride = t.stride()
+            if stride[1] != 1 and shape[1] != 1:
+                self._refuse(name, t, shape)
+            flat += (t.data_ptr(), stride[0])
+        rc = fn(self.h, rows, _Matrices(*flat), B._stream(stream))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
 
     def forward(self, x, gate, up, down, y, g=None, u=None, stream=None):
         """y <- Y (and g <- G, u <- U, which `backward` needs).  Asynchronous."""
-        none = (None, None, None)
         self._call(B.lib.bmgd_gated_forward, x.shape[0],
-                   [("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), ("y", y, self._y),
-                    ("g", g, self._hid), ("u", u, self._hid), none, none, none, none, none], stream)
+                   (("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), ("y", y, self._y),
+                    ("g", g, self._hid), ("u", u, self._hid)), stream)
 
     def backward(self, dy, x, gate, up, down, g, u, dx=None, dgate=None, dup=None, ddown=None, stream=None):
         """The gradients that are asked for (dgate and dup together) are written, from dy and the forward call's g and u.  Asynchronous."""
         self._call(B.lib.bmgd_gated_backward, x.shape[0],
-                   [("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), (None, None, None),
+                   (("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), ("y", None, self._y),
                     ("g", g, self._hid), ("u", u, self._hid), ("dy", dy, self._y), ("dx", dx, self._x), ("dgate", dgate, self._in),
-                    ("dup", dup, self._in), ("ddown", ddown, self._out)], stream)
+                    ("dup", dup, self._in), ("ddown", ddown, self._out)), stream)
 
     def close(self):
         if getattr(self, "h", None):

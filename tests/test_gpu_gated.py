@@ -441,3 +441,28 @@ def test_unequal_strides_of_the_two_projections():
         dx = _empty(r, p, dtype)
         block.backward(dy, x, gate, up, down, g, u, dx=dx)
         _check_backward("f16", "silu", dy, x, gate, up, down, g, u, dx, None, None, None)
+
+
+def test_small_half_precision_numbers_are_not_taken_for_zero():
+    """Rows far below f16's normal range (6.1e-5), in both directions."""
+    import torch
+    import paper_2312_08728_amd as B
+    dtype, code = _types()["f16"]
+    for r in (1, 40, 300):
+        p, f, c = 64, 128, 72
+        x, gate, up, down = _data(r, p, f, c, dtype, 6)
+        x *= 1e-6
+        up *= 1e3
+        with B.GatedBlock(p, f, c, r, dtype=code) as block:
+            y, g, u = _empty(r, c, dtype), _empty(r, f, dtype), _empty(r, f, dtype)
+            block.forward(x, gate, up, down, y, g, u)
+            _check_forward("f16", "silu", x, gate, up, down, y, g, u)
+            assert (g != 0).float().mean() > 0.9 and float(g.abs().max()) < 2e-5
+            x *= 1e6
+            block.forward(x, gate, up, down, y, g, u)
+            dy = _dev(1e-6 * np.random.default_rng(r).standard_normal((r, c)), dtype)
+            out = _empty(r, p, dtype), _empty(p, f, dtype), _empty(p, f, dtype), _empty(f, c, dtype)
+            block.backward(dy, x, gate, up, down, g, u, *out)
+            _check_backward("f16", "silu", dy, x, gate, up, down, g, u, *out)
+            assert (out[3] != 0).any()
+    torch.cuda.synchronize()
