@@ -239,30 +239,37 @@ __device__ __forceinline__ void store_shared(float4v* to, float4v v)
     __hip_atomic_store(at, w[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __hip_atomic_store(at + 1, w[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// (the wait stands in the same block as the loads: the compiler does not know that they are on their way)
-__device__ __forceinline__ void load_shared(const float4v* p, int apart, float4v* v)
+template <typename P> __device__ __forceinline__ P* uniform(P* p)           // a wavefront's common address, for scalar registers
 {
-    asm volatile("global_load_dwordx4 %0, %4, off sc1\n\t"
-                 "global_load_dwordx4 %1, %5, off sc1\n\t"
-                 "global_load_dwordx4 %2, %6, off sc1\n\t"
-                 "global_load_dwordx4 %3, %7, off sc1\n\t"
-                 "s_waitcnt vmcnt(0)"
-                 : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-                 : "v"(p), "v"(p + apart), "v"(p + 2 * apart), "v"(p + 3 * apart) : "memory");
+    const uint64_t a = (uint64_t)p;
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)a), hi = __builtin_amdgcn_readfirstlane((unsigned)(a >> 32));
+    return (P*)((uint64_t)hi << 32 | lo);
 }
-__device__ __forceinline__ void load_shared2(const float4v* p, const float4v* q, int apart, float4v* v)
+
+// Four pieces of each of four parts, which begin at the addresses p: 16 bytes a lane at far[k] behind them.  (The wait stands in the same block as the loads: the
+// compiler does not know that they are on their way.)
+__device__ __forceinline__ void load_shared(const float4v* const* p, const unsigned* far, float4v* v)
 {
-    asm volatile("global_load_dwordx4 %0, %8, off sc1\n\t"
-                 "global_load_dwordx4 %1, %9, off sc1\n\t"
-                 "global_load_dwordx4 %2, %10, off sc1\n\t"
-                 "global_load_dwordx4 %3, %11, off sc1\n\t"
-                 "global_load_dwordx4 %4, %12, off sc1\n\t"
-                 "global_load_dwordx4 %5, %13, off sc1\n\t"
-                 "global_load_dwordx4 %6, %14, off sc1\n\t"
-                 "global_load_dwordx4 %7, %15, off sc1\n\t"
+    asm volatile("global_load_dwordx4 %0, %16, %20 sc1\n\t"
+                 "global_load_dwordx4 %1, %17, %20 sc1\n\t"
+                 "global_load_dwordx4 %2, %18, %20 sc1\n\t"
+                 "global_load_dwordx4 %3, %19, %20 sc1\n\t"
+                 "global_load_dwordx4 %4, %16, %21 sc1\n\t"
+                 "global_load_dwordx4 %5, %17, %21 sc1\n\t"
+                 "global_load_dwordx4 %6, %18, %21 sc1\n\t"
+                 "global_load_dwordx4 %7, %19, %21 sc1\n\t"
+                 "global_load_dwordx4 %8, %16, %22 sc1\n\t"
+                 "global_load_dwordx4 %9, %17, %22 sc1\n\t"
+                 "global_load_dwordx4 %10, %18, %22 sc1\n\t"
+                 "global_load_dwordx4 %11, %19, %22 sc1\n\t"
+                 "global_load_dwordx4 %12, %16, %23 sc1\n\t"
+                 "global_load_dwordx4 %13, %17, %23 sc1\n\t"
+                 "global_load_dwordx4 %14, %18, %23 sc1\n\t"
+                 "global_load_dwordx4 %15, %19, %23 sc1\n\t"
                  "s_waitcnt vmcnt(0)"
-                 : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7])
-                 : "v"(p), "v"(p + apart), "v"(p + 2 * apart), "v"(p + 3 * apart), "v"(q), "v"(q + apart), "v"(q + 2 * apart), "v"(q + 3 * apart) : "memory");
+                 : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3]), "=&v"(v[4]), "=&v"(v[5]), "=&v"(v[6]), "=&v"(v[7]), "=&v"(v[8]), "=&v"(v[9]),
+                   "=&v"(v[10]), "=&v"(v[11]), "=&v"(v[12]), "=&v"(v[13]), "=&v"(v[14]), "=&v"(v[15])
+                 : "v"(far[0]), "v"(far[1]), "v"(far[2]), "v"(far[3]), "s"(p[0]), "s"(p[1]), "s"(p[2]), "s"(p[3]) : "memory");
 }
 
 // Workgroup `id` of a product's tiles_m * tiles_n * splits.
@@ -456,8 +463,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         // The parts of a tile, [split][fragment][thread] of four floats (rows behind the last one are left out).  Written, waited for, counted; the last
         // one adds them up.
         static_assert(fm * fn % 4 == 0, "");
-        float4v* part = (float4v*)q.partial + (size_t)tile * q.splits * (fm * fn) * threads + tid;
-        float4v* mine = part + (size_t)split * (fm * fn) * threads;
+        float4v* mine = (float4v*)q.partial + ((size_t)tile * q.splits + split) * (fm * fn) * threads + tid;
 #pragma unroll
         for (int i = 0; i < fm; ++i)
             if (m0 + wrow + (lane & 15) + 16 * i < q.M) {
@@ -469,22 +475,38 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         __syncthreads();
         if (arrived != (unsigned)q.splits - 1) return;
         if (tid == 0) __hip_atomic_store(q.counter + tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next launch
-        const size_t apart = (size_t)(fm * fn) * threads;      // from one part to the next
+        // Four parts at a time: a trip to what other dies wrote takes 0.8 us.
+        const float4v* const first = (const float4v*)q.partial + (size_t)tile * q.splits * (fm * fn) * threads;
 #pragma unroll
         for (int f = 0; f < fm * fn; f += 4) {
-            const float4v* from = part + f * threads;
-            float4v v[8], sum[4];
-            load_shared(from, threads, sum);
-            int p = 1;
-            for (; p + 1 < q.splits; p += 2) {
-                load_shared2(from + p * apart, from + (p + 1) * apart, threads, v);
+            float4v sum[4];
+            unsigned far[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) sum[k] = sum[k] + v[k] + v[4 + k];
+            for (int k = 0; k < 4; ++k) {
+                sum[k] = float4v{0.f, 0.f, 0.f, 0.f};
+                far[k] = (unsigned)((f + k) * threads + tid) * 16u;
             }
-            if (p < q.splits) {
-                load_shared(from + p * apart, threads, v);
+#pragma unroll 1
+            for (int p = 0; p < q.splits; p += 4) {
+                const float4v* from[4];
+                float4v v[16];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) from[k] = uniform(first + (size_t)min(p + k, q.splits - 1) * (fm * fn) * threads);
+                load_shared(from, far, v);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) sum[k] += v[k];
+                if (p + 1 < q.splits) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[k] += v[4 + k];
+                }
+                if (p + 2 < q.splits) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[k] += v[8 + k];
+                }
+                if (p + 3 < q.splits) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[k] += v[12 + k];
+                }
             }
 #pragma unroll
             for (int k = 0; k < 4; ++k) acc[(f + k) / fn][(f + k) % fn] = sum[k];
