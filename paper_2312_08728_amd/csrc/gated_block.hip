@@ -120,8 +120,8 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
     return hipGetLastError();
 }
 
-// The time of a launch, in us, as measured for 108 shapes of one to 8,192 rows and widths of 64 to 8,192 in every product, tile and split, weights not in
-// any cache (10,106 launches; near the fastest ones of a shape the formula is off by 15 % in the mean square, and its choice is 3 % slower than the fastest):
+// The time of a launch, in us, as measured for 123 shapes of one to 8,192 rows and widths of 64 to 8,192 in every product, tile and split, weights not in
+// any cache (13,971 launches; near the fastest ones of a shape the formula is off by 18 % in the mean square, and its choice is 3 % slower than the fastest):
 //      base + max(rounds (steps lat + once), workgroups of a unit (steps thr + leave), bytes / rate) + join
 // with the steps of a workgroup, the rounds that the units need for all workgroups, a rate that takes enough bytes on their way (2.2 us from request to
 // arrival), and where workgroups share tiles
@@ -131,7 +131,8 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
 {
     struct Cost { int bm, bn, per_cu, ahead; double lat, thr, once[3], leave[3], join, each, write; };       // [kOpUp, kOpDown, the others]
     static const Cost cost[kTiles] = {
-        {256, 256, 1, 1, 0.17, 1.30, {8.6, 13.7, 10.3}, {7.8, 12.4, 5.2}, 0.0, 2.1, 70.0}, {128, 128, 2, 1, 0.30, 0.62, {1.5, 5.6, 3.9}, {1.3, 3.9, 1.6}, 0.0, 1.0, 87.0},
+        {256, 256, 1, 1, 1.38, 1.45, {7.0, 25.6, 13.4}, {8.7, 8.1, 2.6}, 0.55, 0.4, 117.0}, {128, 128, 2, 1, 0.29, 0.58, {1.3, 3.2, 2.95}, {1.15, 3.0, 1.45}, 0.05, 0.53, 122.0},
+        {128, 128, 1, 2, 0.56, 0.36, {1.5, 4.5, 2.75}, {1.45, 1.15, 0.55}, 0.0, 0.32, 111.0},
         {64, 64, 3, 2, 0.01, 0.27, {0.85, 0.35, 2.35}, {0.6, 0.65, 0.45}, 0.95, 0.37, 40.0}, {32, 128, 2, 3, 0.05, 0.55, {1.3, 2.2, 0.3}, {0.7, 1.5, 0.0}, 0.8, 0.5, 60.0},
         {16, 128, 2, 3, 0.41, 0.46, {0.8, 1.05, 0.0}, {0.8, 1.7, 0.1}, 1.2, 0.28, 60.0}};
     constexpr double kBase = 2.8;                              // a launch that does nothing

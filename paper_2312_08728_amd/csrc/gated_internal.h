@@ -44,8 +44,8 @@ struct GatedProduct {
     const void* zeros;  // 256 bytes of zeros
 };
 
-// rows x columns: 256 x 256, 128 x 128, 64 x 64; for few rows 32 x 128 and 16 x 128
-enum { kTileLarge = 0, kTileMedium = 1, kTileSmall = 2, kTile32 = 3, kTile16 = 4, kTiles = 5 };
+// rows x columns: 256 x 256, 128 x 128 (two workgroups to a unit; one, steps further ahead), 64 x 64; for few rows 32 x 128 and 16 x 128
+enum { kTileLarge = 0, kTileMedium = 1, kTileDeep = 2, kTileSmall = 3, kTile32 = 4, kTile16 = 5, kTiles = 6 };
 
 // Bytes of partial sums, and tiles, that a product may use where workgroups share tiles.
 constexpr size_t kGatedPartialBytes = size_t(64) << 20;

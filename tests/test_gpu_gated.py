@@ -372,7 +372,7 @@ def test_refusals():
 
 
 @pytest.mark.parametrize("shares", [1, 3])
-@pytest.mark.parametrize("tile,rows", [(0, (1, 300, 520)), (1, (5, 130, 257)), (2, (1, 63, 200)), (3, (1, 17, 32)), (4, (1, 7, 16))])
+@pytest.mark.parametrize("tile,rows", [(0, (1, 300, 520)), (1, (5, 130, 257)), (2, (5, 130, 257)), (3, (1, 63, 200)), (4, (1, 17, 32)), (5, (1, 7, 16))])
 @pytest.mark.parametrize("kind", ["bf16", "f16"])
 def test_every_kind_of_tile_with_and_without_shared_sums(kind, tile, rows, shares):
     """Sizes that end inside a tile, inside a step of 64 and at their edges, for each tile whatever the block's own choice would be."""
