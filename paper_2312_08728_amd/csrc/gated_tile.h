@@ -33,6 +33,7 @@ namespace {
 
 typedef short short4v __attribute__((ext_vector_type(4)));
 typedef short short8v __attribute__((ext_vector_type(8)));
+typedef unsigned uint4v __attribute__((ext_vector_type(4)));
 typedef float float4v __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -128,6 +129,35 @@ typedef short short8u __attribute__((ext_vector_type(8), aligned(2)));
 __device__ __forceinline__ short* element(const GatedMat& m, int64_t r, int64_t c) { return (short*)m.p + r * m.ld + c; }
 __device__ __forceinline__ void store8(const GatedMat& m, int64_t r, int64_t c, short8v v) { *(short8u*)element(m, r, c) = v; }
 __device__ __forceinline__ short8v load8(const GatedMat& m, int64_t r, int64_t c) { return *(const short8u*)element(m, r, c); }
+
+// The first `n` of eight elements, zeros behind them (bits, whatever they mean: NaN goes too); a vector without its first `n` (1 to 7).
+__device__ __forceinline__ short8v first_of(short8v v, int n)
+{
+    uint4v w = __builtin_bit_cast(uint4v, v);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = n >= 2 * j + 2 ? w[j] : n == 2 * j + 1 ? w[j] & 0xffffu : 0u;
+    return __builtin_bit_cast(short8v, w);
+}
+__device__ __forceinline__ short8v without_first(short8v v, int n)
+{
+    uint4v w = __builtin_bit_cast(uint4v, v);
+    if (n & 4) w = uint4v{w[2], w[3], 0u, 0u};
+    if (n & 2) w = uint4v{w[1], w[2], w[3], 0u};
+    if (n & 1) w = uint4v{__builtin_amdgcn_alignbit(w[1], w[0], 16), __builtin_amdgcn_alignbit(w[2], w[1], 16), __builtin_amdgcn_alignbit(w[3], w[2], 16), w[3] >> 16};
+    return __builtin_bit_cast(short8v, w);
+}
+// Columns c to c + 7 of row r as far as there are `cols`: the last piece of a row goes out element by element, all at once.
+__device__ __forceinline__ void store_some(const GatedMat& m, int64_t r, int64_t c, int64_t cols, short8v v)
+{
+    if (c + 8 <= cols) store8(m, r, c, v);
+    else {
+        short* const to = element(m, r, c);
+        const int n = (int)(cols - c);
+#pragma unroll
+        for (int k = 0; k < 7; ++k)
+            if (k < n) to[k] = v[k];
+    }
+}
 
 constexpr int kStep = kGatedStep;
 
@@ -230,6 +260,8 @@ template <> struct Shape<kTile32> { static constexpr int BM = 32, BN = 128, WM =
 template <> struct Shape<kTile16> { static constexpr int BM = 16, BN = 128, WM = 1, WN = 2, STAGES = 4; };
 
 template <int TILE> constexpr int tile_threads() { return 64 * Shape<TILE>::WM * Shape<TILE>::WN; }
+// Wavefronts that share a SIMD's registers: two workgroups to a unit need 128 a lane (one register more, and 1,910 rows of hidden 2,688 in kOpDown take 88 us for 57).
+template <int TILE> constexpr int tile_waves() { return TILE == kTileMedium ? 4 : 1; }
 // The results leave through shared memory, in turns; kOpDown's have G and U beside them.
 template <GatedOp OP, int TILE> constexpr int tile_turns() { return TILE == kTileLarge ? (OP == kOpDown ? 4 : 2) : (TILE == kTileMedium || TILE == kTileDeep) && OP == kOpDown ? 2 : 1; }
 template <int TILE> constexpr int tile_pitch() { return Shape<TILE>::BN + 4; }             // floats from one row to the next
@@ -606,9 +638,10 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
             for (int i = 0; i < mine; ++i) {
                 int64_t r, c;
                 place(turn, i, r, c);
-                if (r < q.M && c + 8 <= q.N) {
-                    gk[i] = load8(q.g, r, c);
-                    uk[i] = load8(q.u, r, c);
+                if (r < q.M && q.N >= 8) {
+                    const int64_t from = min(c, q.N - 8);      // a row's last piece, and those behind it: its last eight columns, shifted later
+                    gk[i] = load8(q.g, r, from);
+                    uk[i] = load8(q.u, r, from);
                 }
             }
         }
@@ -633,6 +666,13 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         if constexpr (OP == kOpDown) {
 #pragma unroll
             for (int i = 0; i < mine; ++i) {
+                int64_t r, c;
+                place(turn, i, r, c);
+                if (c + 8 > q.N) {                             // zeros behind the last column
+                    const int left = (int)max(q.N - c, (int64_t)0);
+                    gk[i] = first_of(without_first(gk[i], 8 - left), left);
+                    uk[i] = first_of(without_first(uk[i], 8 - left), left);
+                }
                 gus[2 * i * threads] = gk[i];
                 gus[(2 * i + 1) * threads] = uk[i];
             }
@@ -645,84 +685,65 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                 int64_t r, c;
                 const float* const at = place(turn, i, r, c);
                 if (r >= q.M) continue;
+                // (H, dG and dU have q.half columns, a multiple of 64: whole pieces, zeros behind the last column)
+                const int left = (int)min(q.N - c, (int64_t)8);
                 if constexpr (OP == kOpUp) {
-                    if (c + 8 <= q.N) {
-                        float g[8], u[8];
-                        floats8(at, g);
-                        floats8(at + BN / 2, u);
-                        short8v hb, gb, ub;
+                    if (c >= q.half) continue;
+                    float g[8], u[8];
+                    floats8(at, g);
+                    floats8(at + BN / 2, u);
+                    short8v hb, gb, ub;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            hb[k] = bits_of<T>(act_value<act.value>(g[k]) * u[k]);
-                            gb[k] = bits_of<T>(g[k]);
-                            ub[k] = bits_of<T>(u[k]);
-                        }
-                        store8(q.out, r, c, hb);
-                        if (q.g.p) {
-                            store8(q.g, r, c, gb);
-                            store8(q.u, r, c, ub);
-                        }
-                    } else {
-#pragma unroll 1
-                        for (int k = 0; k < 8 && c + k < q.half; ++k) {
-                            const bool in = c + k < q.N;
-                            const float g = at[k], u = at[BN / 2 + k];
-                            *element(q.out, r, c + k) = in ? bits_of<T>(act_value<act.value>(g) * u) : (short)0;
-                            if (in && q.g.p) {
-                                *element(q.g, r, c + k) = bits_of<T>(g);
-                                *element(q.u, r, c + k) = bits_of<T>(u);
-                            }
-                        }
+                    for (int k = 0; k < 8; ++k) {
+                        hb[k] = bits_of<T>(act_value<act.value>(g[k]) * u[k]);
+                        gb[k] = bits_of<T>(g[k]);
+                        ub[k] = bits_of<T>(u[k]);
+                    }
+                    store8(q.out, r, c, left == 8 ? hb : first_of(hb, left));
+                    if (q.g.p) {
+                        store_some(q.g, r, c, q.N, gb);
+                        store_some(q.u, r, c, q.N, ub);
                     }
                 } else if constexpr (OP == kOpDown) {
-                    if (c + 8 <= q.N) {
-                        float dh[8];
-                        floats8(at, dh);
-                        const short8v gb = gus[2 * i * threads], ub = gus[(2 * i + 1) * threads];
-                        short8v hb, dgb, dub;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) {
-                            float slope;
-                            const float u = value_of<T>(ub[k]), a = act_both<act.value>(value_of<T>(gb[k]), slope);
-                            hb[k] = bits_of<T>(a * u);
-                            dub[k] = bits_of<T>(dh[k] * a);
-                            dgb[k] = bits_of<T>(dh[k] * u * slope);
-                        }
-                        store8(q.out, r, c, hb);
-                        store8(q.out2, r, c, dgb);
-                        store8(q.out2, r, c + q.half, dub);
-                    } else {
+                    if (c >= q.half) continue;
+                    short8v& gs = gus[2 * i * threads];
+                    short8v& us = gus[(2 * i + 1) * threads];
+                    if (q.N < 8)
 #pragma unroll 1
-                        for (int k = 0; k < 8 && c + k < q.half; ++k) {
-                            float h = 0.f, dg = 0.f, du = 0.f;
-                            if (c + k < q.N) {
-                                float slope;
-                                const float u = value_of<T>(*element(q.u, r, c + k)), a = act_both<act.value>(value_of<T>(*element(q.g, r, c + k)), slope), dh = at[k];
-                                h = a * u;
-                                du = dh * a;
-                                dg = dh * u * slope;
-                            }
-                            *element(q.out, r, c + k) = bits_of<T>(h);
-                            *element(q.out2, r, c + k) = bits_of<T>(dg);
-                            *element(q.out2, r, c + k + q.half) = bits_of<T>(du);
+                        for (int k = 0; k < left; ++k) {
+                            reinterpret_cast<short*>(&gs)[k] = *element(q.g, r, c + k);
+                            reinterpret_cast<short*>(&us)[k] = *element(q.u, r, c + k);
                         }
+                    float dh[8];
+                    floats8(at, dh);
+                    if (left < 8) {                            // (an infinity in dY times the zeros behind the last row of Wd is no number)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) dh[k] = k < left ? dh[k] : 0.f;
                     }
+                    const short8v gb = gs, ub = us;
+                    short8v hb, dgb, dub;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        float slope;
+                        const float u = value_of<T>(ub[k]), a = act_both<act.value>(value_of<T>(gb[k]), slope);
+                        hb[k] = bits_of<T>(a * u);
+                        dub[k] = bits_of<T>(dh[k] * a);
+                        dgb[k] = bits_of<T>(dh[k] * u * slope);
+                    }
+                    store8(q.out, r, c, hb);
+                    store8(q.out2, r, c, dgb);
+                    store8(q.out2, r, c + q.half, dub);
                 } else {
                     // (two halves: q.half is a multiple of 64, eight columns never straddle)
                     const bool second = OP == kOpWeight && q.half && c >= q.half;
                     const GatedMat& to = second ? q.out2 : q.out;
                     const int64_t cc = second ? c - q.half : c;
-                    if (cc + 8 <= q.N) {
-                        float v[8];
-                        floats8(at, v);
-                        short8v b;
+                    float v[8];
+                    floats8(at, v);
+                    short8v b;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) b[k] = bits_of<T>(v[k]);
-                        store8(to, r, cc, b);
-                    } else {
-#pragma unroll 1
-                        for (int k = 0; k < 8 && cc + k < q.N; ++k) *element(to, r, cc + k) = bits_of<T>(at[k]);
-                    }
+                    for (int k = 0; k < 8; ++k) b[k] = bits_of<T>(v[k]);
+                    store_some(to, r, cc, q.N, b);
                 }
             }
         };
@@ -739,7 +760,7 @@ __device__ __forceinline__ int neighbours(int id, int total)
 }
 
 template <typename T, GatedOp OP, int TILE>
-__global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_tile_kernel(GatedProduct q)
+__global__ void __launch_bounds__(tile_threads<TILE>(), tile_waves<TILE>()) gated_tile_kernel(GatedProduct q)
 {
     tile_body<T, OP, TILE>(q, neighbours(blockIdx.x, gridDim.x));
 }
@@ -751,7 +772,7 @@ struct GradProducts {
     int input_end, down_end, gate_end;
 };
 template <typename T, int TILE>
-__global__ void __launch_bounds__(tile_threads<TILE>(), 1) gated_grads_kernel(GradProducts g)
+__global__ void __launch_bounds__(tile_threads<TILE>(), tile_waves<TILE>()) gated_grads_kernel(GradProducts g)
 {
     int id = blockIdx.x;
     if (id < g.input_end) {

@@ -466,3 +466,29 @@ def test_small_half_precision_numbers_are_not_taken_for_zero():
             _check_backward("f16", "silu", dy, x, gate, up, down, g, u, *out)
             assert (out[3] != 0).any()
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("f", [1, 3, 7, 8, 9, 63, 70, 129])
+@pytest.mark.parametrize("r", [3, 200])
+def test_an_infinite_gradient_meets_no_zeros_of_columns_that_are_not_there(r, f):
+    """All terms positive, one element of dY infinite: the formula has no difference and no product with zero, so its row of dX, all of dWg and dWu and its column of dWd are infinite."""
+    import torch
+    import paper_2312_08728_amd as B
+    p, c = 24, 11
+    rng = np.random.default_rng(f)
+    x, gate, up, down = (_dev(0.5 + rng.random(s), torch.bfloat16) for s in ((r, p), (p, f), (p, f), (f, c)))
+    g, u = (_dev(0.5 + rng.random((r, f)), torch.bfloat16, ld=f + 5) for _ in range(2))
+    grad = 0.5 + rng.random((r, c))
+    grad[1, 4] = np.inf
+    dy = _dev(grad, torch.bfloat16)
+    dx, dgate, dup, ddown = _empty(r, p, torch.bfloat16), _empty(p, f, torch.bfloat16, ld=f + 3), _empty(p, f, torch.bfloat16, ld=f + 3), _empty(f, c, torch.bfloat16)
+    with B.GatedBlock(p, f, c, r, dtype=B.BMGD_BF16, activation=B.BMGD_ACT_RELU) as block:
+        block.backward(dy, x, gate, up, down, g, u, dx, dgate, dup, ddown)
+    inf = lambda t: torch.isinf(t) & (t > 0)  # noqa: E731
+    rows, cols = torch.arange(r, device="cuda") == 1, torch.arange(c, device="cuda") == 4
+    assert inf(dx)[rows].all() and torch.isfinite(dx)[~rows].all()
+    assert inf(dgate).all() and inf(dup).all()
+    assert inf(ddown)[:, cols].all() and torch.isfinite(ddown)[:, ~cols].all()
+    for t in (dgate, dup):                                     # nothing between the rows is written
+        between = torch.as_strided(t, (p - 1, 3), (f + 3, 1), f)
+        assert (between == 7).all()
