@@ -100,6 +100,7 @@ struct bmgd_gated {
     hipEvent_t order = nullptr;
     char err[256] = "";
     int tile = -1, shares = 0;              // asked for by tests
+    struct Kept { int64_t rows = -1; int what = 0; bmgd::GatedCut cut[3]; } kept[32];      // by rows modulo 8 and launch, see plan()
 };
 
 namespace bmgd {
@@ -318,21 +319,29 @@ int enter(bmgd_gated* b, hipStream_t s)
     return BMGD_OK;
 }
 
-void plan(bmgd_gated* b, GatedProduct* const* q, const GatedOp* op, int count)
+// The choice takes 1 us for a product and 2 for three, a fifth of what a call of few rows takes in all, and depends on the block's sizes and the rows alone:
+// it is kept for the next call of as many rows.  `what`: the product, or 8 and a bit for each of those made in one launch.
+void plan(bmgd_gated* b, GatedProduct* const* q, const GatedOp* op, int count, int64_t rows, int what)
 {
-    gated_plan(q, op, count, b->num_cus, b->tile, b->shares);
+    bmgd_gated::Kept& k = b->kept[(rows & 7) * 4 + (what < 8 ? what : 3)];
+    const bool known = k.rows == rows && k.what == what && b->tile < 0;
+    if (!known) gated_plan(q, op, count, b->num_cus, b->tile, b->shares);
     for (int i = 0; i < count; ++i) {
+        if (known) static_cast<GatedCut&>(*q[i]) = k.cut[i];
+        else k.cut[i] = *q[i];
         q[i]->act = b->cfg.activation;
         q[i]->partial = reinterpret_cast<float*>(b->base + b->lay.partial) + q[i]->first_part;
         q[i]->counter = reinterpret_cast<unsigned*>(b->base + b->lay.counter) + q[i]->first_counter;
         q[i]->zeros = b->base + b->lay.zeros;
     }
+    k.rows = b->tile < 0 ? rows : -1;
+    k.what = what;
 }
 
-int launch(bmgd_gated* b, GatedProduct& q, GatedOp op, hipStream_t s)
+int launch(bmgd_gated* b, GatedProduct& q, GatedOp op, int64_t rows, hipStream_t s)
 {
     GatedProduct* one = &q;
-    plan(b, &one, &op, 1);
+    plan(b, &one, &op, 1, rows, op);
     const hipError_t e = b->cfg.dtype == BMGD_F16 ? gated_launch_f16(q, op, s) : gated_launch_bf16(q, op, s);
     if (e != hipSuccess) return hip_fail(b, e, "launch of a product of the gated block");
     return BMGD_OK;
@@ -373,7 +382,7 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     q.out = h;
     q.g = plain(t.g);
     q.u = plain(t.u);
-    GATED_DO(launch(b, q, kOpUp, s));
+    GATED_DO(launch(b, q, kOpUp, rows, s));
 
     q = GatedProduct{};
     q.a = h;
@@ -381,7 +390,7 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     q.M = rows; q.N = c.out_n; q.K = c.hidden;
     q.b_cols = up(c.out_n, 8);
     q.out = plain(t.y);
-    return launch(b, q, kOpMul, s);
+    return launch(b, q, kOpMul, rows, s);
 }
 
 int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_t s)
@@ -414,7 +423,7 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
         q.out2 = d;
         q.g = plain(t.g);
         q.u = plain(t.u);
-        GATED_DO(launch(b, q, kOpDown, s));
+        GATED_DO(launch(b, q, kOpDown, rows, s));
     }
     GatedProduct input{}, ddown{}, dgate{};
     GatedProduct* list3[3];
@@ -453,7 +462,7 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
         ops[n++] = kOpWeight;
     }
     if (n == 0) return BMGD_OK;
-    plan(b, list3, ops, n);
+    plan(b, list3, ops, n, rows, 8 | (input.M ? 1 : 0) | (ddown.M ? 2 : 0) | (dgate.M ? 4 : 0));
     const GatedProduct *pi = input.M ? &input : nullptr, *pd = ddown.M ? &ddown : nullptr, *pg = dgate.M ? &dgate : nullptr;
     const hipError_t e = c.dtype == BMGD_F16 ? gated_launch_grads_f16(pi, pd, pg, s) : gated_launch_grads_bf16(pi, pd, pg, s);
     if (e != hipSuccess) return hip_fail(b, e, "launch of the gradients of the gated block");

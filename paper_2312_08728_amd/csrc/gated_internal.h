@@ -23,7 +23,15 @@ struct GatedMat {
     int64_t ld;         // elements from one row to the next
 };
 
-struct GatedProduct {
+// How a result is cut into tiles.
+struct GatedCut {
+    int tile;           // kTile*
+    int tiles_m, tiles_n, splits, per_split;    // tiles of the result; workgroups that share a tile's sum, and their share in steps of 64
+    int first_counter;
+    size_t first_part;  // where its own counters and sums begin among those of a launch
+};
+
+struct GatedProduct : GatedCut {
     GatedMat a;         // left operand
     GatedMat b, b2;     // right operand; its second half for kOpUp and kOpInput
     int64_t M, N, K;    // rows and columns of the result as stored, length of the sum.  kOpUp: N = hidden; kOpInput: K = hidden, the
@@ -34,13 +42,8 @@ struct GatedProduct {
     GatedMat out, out2; // result; kOpUp, kOpDown: H in `out`, kOpDown: D = [dG | dU] in `out2`
     GatedMat g, u;      // kOpUp: written unless NULL; kOpDown: read
     int act;
-    // how the result is cut into tiles: filled in by gated_plan
-    int tile;           // kTile*
-    int tiles_m, tiles_n, splits, per_split;    // tiles of the result; workgroups that share a tile's sum, and their share in steps of 64
-    float* partial;     // their sums
+    float* partial;     // sums of workgroups that share a tile
     unsigned* counter;  // and how many of them have arrived, per tile; zero between launches
-    size_t first_part;  // where its own begin among those of a launch
-    int first_counter;
     const void* zeros;  // 256 bytes of zeros
 };
 

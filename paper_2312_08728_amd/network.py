@@ -5,6 +5,7 @@ Checks shapes, types and devices, fills in addresses and strides, and calls the 
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -12,8 +13,8 @@ from . import binding as B
 
 _TYPES = {B.BMGD_BF16: torch.bfloat16, B.BMGD_F16: torch.float16, B.BMGD_F32: torch.float32}
 _CODES = {v: k for k, v in _TYPES.items()}
-_ROWS = object()                    # in place of a matrix's number of rows: that of the call
-_Matrices = C.c_int64 * 24          # bmgd_gated_tensors: twelve addresses and strides
+_NAMES = ("x", "gate", "up", "down", "y", "g", "u", "dy", "dx", "dgate", "dup", "ddown")      # bmgd_gated_tensors: an address and a stride each
+_seven, _twelve = struct.Struct("14q80x").pack, struct.Struct("24q").pack
 
 
 class GatedBlock:
@@ -43,7 +44,7 @@ class GatedBlock:
         self._type = _TYPES[dtype]
         self._device = torch.device("cuda", torch.cuda.current_device())
         self._index = self._device.index
-        self._x, self._in, self._out, self._hid, self._y = (_ROWS, p), (p, hidden), (hidden, out_n), (_ROWS, hidden), (_ROWS, out_n)
+        self._p, self._hidden, self._out_n, self._in, self._out = p, hidden, out_n, (p, hidden), (hidden, out_n)
 
     def _refuse(self, name, t, shape):
         if t.dtype is not self._type or t.device != self._device:
@@ -52,36 +53,39 @@ class GatedBlock:
             raise ValueError(f"{name}: shape {shape} is wanted, not {tuple(t.shape)}")
         raise ValueError(f"{name}: the elements of a row must lie next to each other (strides {t.stride()})")
 
-    def _call(self, fn, rows, matrices, stream):
-        flat = []
-        for name, t, shape in matrices:
+    def _addresses(self, tensors, shapes):
+        # (a call of few rows waits for these lines: each property of a tensor is asked for once)
+        kind, index, flat = self._type, self._index, []
+        for t, shape in zip(tensors, shapes):
             if t is None:
                 flat += (0, 0)
                 continue
-            if shape[0] is _ROWS:
-                shape = (rows, shape[1])
-            if t.dtype is not self._type or t.get_device() != self._index or t.shape != shape:
-                self._refuse(name, t, shape)
-            stride = t.stride()
-            if stride[1] != 1 and shape[1] != 1:
-                self._refuse(name, t, shape)
-            flat += (t.data_ptr(), stride[0])
-        rc = fn(self.h, rows, _Matrices(*flat), B._stream(stream))
-        if rc != B.BMGD_OK:
-            raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
+            if t.dtype is not kind or t.get_device() != index or t.shape != shape:
+                self._refuse(_NAMES[len(flat) // 2], t, shape)
+            stride, apart = t.stride()
+            if apart != 1 and shape[1] != 1:
+                self._refuse(_NAMES[len(flat) // 2], t, shape)
+            flat += (t.data_ptr(), stride)
+        return flat
 
     def forward(self, x, gate, up, down, y, g=None, u=None, stream=None):
         """y <- Y (and g <- G, u <- U, which `backward` needs).  Asynchronous."""
-        self._call(B.lib.bmgd_gated_forward, x.shape[0],
-                   (("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), ("y", y, self._y),
-                    ("g", g, self._hid), ("u", u, self._hid)), stream)
+        rows = x.shape[0]
+        hid = (rows, self._hidden)
+        flat = self._addresses((x, gate, up, down, y, g, u), ((rows, self._p), self._in, self._in, self._out, (rows, self._out_n), hid, hid))
+        rc = B.lib.bmgd_gated_forward(self.h, rows, _seven(*flat), B._stream(stream))
+        if rc != B.BMGD_OK:
+            raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
 
     def backward(self, dy, x, gate, up, down, g, u, dx=None, dgate=None, dup=None, ddown=None, stream=None):
         """The gradients that are asked for (dgate and dup together) are written, from dy and the forward call's g and u.  Asynchronous."""
-        self._call(B.lib.bmgd_gated_backward, x.shape[0],
-                   (("x", x, self._x), ("gate", gate, self._in), ("up", up, self._in), ("down", down, self._out), ("y", None, self._y),
-                    ("g", g, self._hid), ("u", u, self._hid), ("dy", dy, self._y), ("dx", dx, self._x), ("dgate", dgate, self._in),
-                    ("dup", dup, self._in), ("ddown", ddown, self._out)), stream)
+        rows = x.shape[0]
+        at, hid, wide = (rows, self._p), (rows, self._hidden), self._in
+        out = (rows, self._out_n)
+        flat = self._addresses((x, gate, up, down, None, g, u, dy, dx, dgate, dup, ddown), (at, wide, wide, self._out, out, hid, hid, out, at, wide, wide, self._out))
+        rc = B.lib.bmgd_gated_backward(self.h, rows, _twelve(*flat), B._stream(stream))
+        if rc != B.BMGD_OK:
+            raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
 
     def close(self):
         if getattr(self, "h", None):
