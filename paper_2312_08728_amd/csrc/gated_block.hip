@@ -100,6 +100,7 @@ struct bmgd_gated {
     hipEvent_t order = nullptr;
     char err[256] = "";
     int tile = -1, shares = 0;              // asked for by tests
+    bool wide = false;                      // every row has eight elements or more, as loose tiles want them
     struct Kept { int64_t rows = -1; int what = 0; bmgd::GatedCut cut[3]; } kept[32];      // by rows modulo 8 and launch, see plan()
 };
 
@@ -259,7 +260,8 @@ int check(bmgd_gated* b, const char* call, const Named* list, int n)
     return BMGD_OK;
 }
 
-// Operands as the kernels read them: rows of a multiple of eight elements, 16-byte aligned; others are copied to the workspace first.
+// Operands as the kernels read them: rows of a multiple of eight elements, 16-byte aligned; a launch of loose tiles reads others too, for the rest they are
+// copied to the workspace first.
 struct Operands {
     bmgd_gated* b;
     GatedPack pack{};
@@ -279,16 +281,20 @@ struct Operands {
         o.cols = cols;
         return GatedMat{o.to, o.to_ld};
     }
-    GatedMat use(const bmgd_matrix& m, int64_t rows, int64_t cols, size_t area)
+    // `loose`: whether the launch may read the operand where it is, and on return whether it has to be a loose one for that
+    GatedMat use(const bmgd_matrix& m, int64_t rows, int64_t cols, size_t area, bool may, bool* loose)
     {
         if (rows == 0) return GatedMat{b->base + area, up(cols, 8)};
-        if (direct(m, rows, cols)) return GatedMat{m.data, rows <= 1 ? cols : m.stride};
-        return copy(m, rows, cols, area);
+        if (may) *loose = *loose || !direct(m, rows, cols);
+        else if (!direct(m, rows, cols)) return copy(m, rows, cols, area);
+        return GatedMat{m.data, rows <= 1 ? cols : m.stride};
     }
     // the two matrices that one product reads side by side: their rows are equally far apart
-    void use_pair(const bmgd_matrix& m, const bmgd_matrix& m2, int64_t rows, int64_t cols, size_t area, size_t area2, GatedMat* o, GatedMat* o2)
+    void use_pair(const bmgd_matrix& m, const bmgd_matrix& m2, int64_t rows, int64_t cols, size_t area, size_t area2, bool may, bool* loose, GatedMat* o, GatedMat* o2)
     {
-        if (direct(m, rows, cols) && direct(m2, rows, cols) && (rows <= 1 || m.stride == m2.stride)) {
+        const bool whole = direct(m, rows, cols) && direct(m2, rows, cols);
+        if ((whole || may) && (rows <= 1 || m.stride == m2.stride)) {
+            *loose = *loose || !whole;
             *o = GatedMat{m.data, rows <= 1 ? cols : m.stride};
             *o2 = GatedMat{m2.data, o->ld};
         } else {
@@ -338,10 +344,14 @@ void plan(bmgd_gated* b, GatedProduct* const* q, const GatedOp* op, int count, i
     k.what = what;
 }
 
-int launch(bmgd_gated* b, GatedProduct& q, GatedOp op, int64_t rows, hipStream_t s)
+void plan(bmgd_gated* b, GatedProduct& q, GatedOp op, int64_t rows)
 {
     GatedProduct* one = &q;
     plan(b, &one, &op, 1, rows, op);
+}
+
+int launch(bmgd_gated* b, const GatedProduct& q, GatedOp op, hipStream_t s)
+{
     const hipError_t e = b->cfg.dtype == BMGD_F16 ? gated_launch_f16(q, op, s) : gated_launch_bf16(q, op, s);
     if (e != hipSuccess) return hip_fail(b, e, "launch of a product of the gated block");
     return BMGD_OK;
@@ -364,33 +374,29 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     if (rows == 0) return BMGD_OK;
     GATED_DO(enter(b, s));
     const int64_t half = up(c.hidden, 64);
-    Operands o{b};
-    const GatedMat x = o.use(t.x, rows, c.p, b->lay.x);
-    GatedMat gate, upw;
-    o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, &gate, &upw);
-    const GatedMat down = o.use(t.down, c.hidden, c.out_n, b->lay.down);
-    if (o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
-    const GatedMat h{b->base + b->lay.h, half};
-
-    GatedProduct q{};
-    q.a = x;
-    q.b = gate;
-    q.b2 = upw;
+    GatedProduct q{}, y{};
     q.M = rows; q.N = c.hidden; q.K = c.p;
-    q.b_cols = up(c.hidden, 8);
     q.half = half;
-    q.out = h;
+    plan(b, q, kOpUp, rows);
+    y.M = rows; y.N = c.out_n; y.K = c.hidden;
+    plan(b, y, kOpMul, rows);
+
+    Operands o{b};
+    const bool any = b->wide && gated_can_be_loose(q.tile), any_y = b->wide && gated_can_be_loose(y.tile);
+    q.a = o.use(t.x, rows, c.p, b->lay.x, any, &q.loose);
+    o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, any, &q.loose, &q.b, &q.b2);
+    y.b = o.use(t.down, c.hidden, c.out_n, b->lay.down, any_y, &y.loose);
+    if (o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
+    q.b_cols = q.loose ? c.hidden : up(c.hidden, 8);
+    q.out = GatedMat{b->base + b->lay.h, half};
     q.g = plain(t.g);
     q.u = plain(t.u);
-    GATED_DO(launch(b, q, kOpUp, rows, s));
+    GATED_DO(launch(b, q, kOpUp, s));
 
-    q = GatedProduct{};
-    q.a = h;
-    q.b = down;
-    q.M = rows; q.N = c.out_n; q.K = c.hidden;
-    q.b_cols = up(c.out_n, 8);
-    q.out = plain(t.y);
-    return launch(b, q, kOpMul, rows, s);
+    y.a = q.out;
+    y.b_cols = y.loose ? c.out_n : up(c.out_n, 8);
+    y.out = plain(t.y);
+    return launch(b, y, kOpMul, s);
 }
 
 int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_t s)
@@ -404,65 +410,72 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
     if (!t.dgate.data != !t.dup.data) return fail(b, BMGD_EINVAL, "bmgd_gated_backward", "dgate and dup are wanted together or not at all");
     GATED_DO(enter(b, s));
     const int64_t half = up(c.hidden, 64);
-    Operands o{b};
-    const GatedMat x = o.use(t.x, rows, c.p, b->lay.x);
-    const GatedMat dy = o.use(t.dy, rows, c.out_n, b->lay.dy);
-    const GatedMat down = o.use(t.down, c.hidden, c.out_n, b->lay.down);
-    GatedMat gate{}, upw{};
-    if (rows && t.dx.data) o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, &gate, &upw);
-    if (rows && o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
     const GatedMat h{b->base + b->lay.h, half}, d{b->base + b->lay.d, 2 * half};
-
-    GatedProduct q{};
-    if (rows) {
-        q.a = dy;
-        q.b = down;
-        q.M = rows; q.N = c.hidden; q.K = up(c.out_n, 8);
-        q.half = half;
-        q.out = h;
-        q.out2 = d;
-        q.g = plain(t.g);
-        q.u = plain(t.u);
-        GATED_DO(launch(b, q, kOpDown, rows, s));
-    }
-    GatedProduct input{}, ddown{}, dgate{};
+    GatedProduct q{}, input{}, ddown{}, dgate{};
     GatedProduct* list3[3];
     GatedOp ops[3];
     int n = 0;
+    if (rows) {
+        q.M = rows; q.N = c.hidden; q.K = c.out_n;
+        q.half = half;
+        plan(b, q, kOpDown, rows);
+    }
     if (rows && t.dx.data) {
-        input.a = d;
-        input.b = gate;
-        input.b2 = upw;
-        input.M = rows; input.N = c.p; input.K = up(c.hidden, 8);
+        input.M = rows; input.N = c.p; input.K = c.hidden;
         input.half = half;
-        input.out = plain(t.dx);
         list3[n] = &input;
         ops[n++] = kOpInput;
     }
     if (t.ddown.data) {
-        ddown.a = h;
-        ddown.b = dy;
         ddown.M = c.hidden; ddown.N = c.out_n; ddown.K = rows;
-        ddown.a_cols = half;
-        ddown.b_cols = up(c.out_n, 8);
-        ddown.out = plain(t.ddown);
         list3[n] = &ddown;
         ops[n++] = kOpWeight;
     }
     if (t.dgate.data) {
-        dgate.a = x;
-        dgate.b = d;
         dgate.M = c.p; dgate.N = c.hidden; dgate.K = rows;
-        dgate.a_cols = up(c.p, 8);
-        dgate.b_cols = 2 * half;
         dgate.half = half;
-        dgate.out = plain(t.dgate);
-        dgate.out2 = plain(t.dup);
         list3[n] = &dgate;
         ops[n++] = kOpWeight;
     }
+    if (n) plan(b, list3, ops, n, rows, 8 | (input.M ? 1 : 0) | (ddown.M ? 2 : 0) | (dgate.M ? 4 : 0));
+
+    // (dY is read by both launches: where one needs a copy, both read that)
+    Operands o{b};
+    const bool any = b->wide && gated_can_be_loose(q.tile), any_grads = b->wide && n && gated_can_be_loose(list3[0]->tile);
+    bool loose = false;
+    const GatedMat dy = o.use(t.dy, rows, c.out_n, b->lay.dy, any && (any_grads || !ddown.M), &q.loose);
+    if (ddown.M) loose = q.loose;
+    q.b = o.use(t.down, c.hidden, c.out_n, b->lay.down, any, &q.loose);
+    GatedMat x{};
+    if (dgate.M) x = o.use(t.x, rows, c.p, b->lay.x, any_grads, &loose);
+    if (input.M) o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, any_grads, &loose, &input.b, &input.b2);
+    if (rows && o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
+    if (rows) {
+        if (!q.loose) q.K = up(c.out_n, 8);
+        q.a = dy;
+        q.out = h;
+        q.out2 = d;
+        q.g = plain(t.g);
+        q.u = plain(t.u);
+        GATED_DO(launch(b, q, kOpDown, s));
+    }
     if (n == 0) return BMGD_OK;
-    plan(b, list3, ops, n, rows, 8 | (input.M ? 1 : 0) | (ddown.M ? 2 : 0) | (dgate.M ? 4 : 0));
+    auto cols = [&](int64_t n) { return loose ? n : up(n, 8); };
+    input.loose = ddown.loose = dgate.loose = loose;
+    input.a = d;
+    input.K = cols(c.hidden);
+    input.out = plain(t.dx);
+    ddown.a = h;
+    ddown.b = dy;
+    ddown.a_cols = half;
+    ddown.b_cols = cols(c.out_n);
+    ddown.out = plain(t.ddown);
+    dgate.a = x;
+    dgate.b = d;
+    dgate.a_cols = cols(c.p);
+    dgate.b_cols = 2 * half;
+    dgate.out = plain(t.dgate);
+    dgate.out2 = plain(t.dup);
     const GatedProduct *pi = input.M ? &input : nullptr, *pd = ddown.M ? &ddown : nullptr, *pg = dgate.M ? &dgate : nullptr;
     const hipError_t e = c.dtype == BMGD_F16 ? gated_launch_grads_f16(pi, pd, pg, s) : gated_launch_grads_bf16(pi, pd, pg, s);
     if (e != hipSuccess) return hip_fail(b, e, "launch of the gradients of the gated block");
@@ -526,6 +539,7 @@ BMGD_API int bmgd_gated_create(const bmgd_gated_config* cfg, bmgd_gated** out)
     if (!b) return fail_static(BMGD_ENOMEM, "bmgd_gated_create", "out of host memory");
     b->cfg = *cfg;
     b->lay = lay;
+    b->wide = std::min(std::min(cfg->p, cfg->hidden), cfg->out_n) >= 8;
     auto bail = [&](hipError_t e, const char* what) {
         const int code = hip_fail(b, e, what);
         set_create_error(b->err);

@@ -36,7 +36,8 @@ struct GatedProduct : GatedCut {
     GatedMat b, b2;     // right operand; its second half for kOpUp and kOpInput
     int64_t M, N, K;    // rows and columns of the result as stored, length of the sum.  kOpUp: N = hidden; kOpInput: K = hidden, the
                         // length of one half; kOpWeight with two halves: N = hidden, the columns of one
-    int64_t a_cols, b_cols;             // strided operands: columns that may be read (a multiple of 8)
+    int64_t a_cols, b_cols;             // strided operands: columns that may be read
+    bool loose;         // rows of the operands begin anywhere; else at multiples of 16 bytes, and columns and adjacent lengths are multiples of 8
     int64_t half;       // kOpUp, kOpDown: hidden rounded up to 64, the columns of H and of each half of D (zeros behind hidden);
                         // kOpInput: the columns of each half of the left operand; kOpWeight: 0, or the columns of each half of the right operand
     GatedMat out, out2; // result; kOpUp, kOpDown: H in `out`, kOpDown: D = [dG | dU] in `out2`
@@ -59,6 +60,9 @@ constexpr int kGatedStep = 64;         // elements of the summed index per step
 // tile >= 0: this one and `want` shares of a tile's sum where they fit (tests).
 void gated_plan(GatedProduct* const* q, const GatedOp* op, int count, int num_cus, int tile = -1, int64_t want = 0);
 
+// Whether a kind of tile has a form for operands at any address (whose rows have eight elements or more).
+inline bool gated_can_be_loose(int tile) { return tile >= kTileSmall; }
+
 // Once per process and device: lets the kernels use as much shared memory as they need.
 hipError_t gated_prepare_bf16();
 hipError_t gated_prepare_f16();
@@ -68,7 +72,7 @@ hipError_t gated_launch_f16(const GatedProduct& q, GatedOp op, hipStream_t strea
 hipError_t gated_launch_grads_bf16(const GatedProduct* input, const GatedProduct* down, const GatedProduct* gate, hipStream_t stream);
 hipError_t gated_launch_grads_f16(const GatedProduct* input, const GatedProduct* down, const GatedProduct* gate, hipStream_t stream);
 
-// Copies of up to five matrices of 16-bit elements whose rows cannot be read in pieces of 16 bytes: rows of `to_ld` elements (a multiple of
+// Copies of up to five matrices of 16-bit elements whose rows do not begin at multiples of 16 bytes: rows of `to_ld` elements (a multiple of
 // 8), zeros behind the last column.
 struct GatedPack {
     struct One { const unsigned short* from; unsigned short* to; int64_t from_ld, to_ld, rows, cols; } m[5];

@@ -217,6 +217,59 @@ template <bool ADJ, int R, int THREADS> struct Mover {
     }
 };
 
+// The same way by registers, for rows at any address and of any length of 8 or more: pieces that end behind the last element of a row are its last eight,
+// shifted when they go to shared memory.
+template <bool ADJ, int R, int THREADS> struct Loose {
+    using Whole = Mover<ADJ, R, THREADS>;
+    static constexpr int kPieces = Whole::kPieces, kRow = Whole::kRow, kShifts = ADJ ? 1 : kPieces;
+    const unsigned short* src[kPieces];
+    int at, shift[kShifts];
+
+    // Adjacent: pick(row of the tile) is where its row begins.  Strided: pick(piece of a row of the tile, its first column) is where column 0 of its matrix begins; the
+    // matrix has `cols` columns.
+    template <typename Pick>
+    __device__ __forceinline__ void start(int64_t ld, int64_t k0, int64_t cols, int tid, Pick pick)
+    {
+        if constexpr (ADJ) {
+            const int s = tid & 7;
+            at = 8 * (s ^ ((tid >> 3) & 7));
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) src[i] = pick(i * (THREADS / 8) + (tid >> 3)) + k0 + at;
+        } else {
+            at = tid / kRow;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                const int k = i * (THREADS / kRow) + tid / kRow;
+                int64_t col;
+                const unsigned short* const base = pick((tid % kRow) ^ Whole::turn(k), col);
+                src[i] = base + min(col, cols - 8) + (k0 + k) * ld;
+                shift[i] = col < cols ? (int)max(col + 8 - cols, (int64_t)0) : 0;         // (results of columns that are not there go nowhere)
+            }
+        }
+    }
+    __device__ __forceinline__ void request(short8v* v, int64_t ld, int64_t left, const unsigned short* zeros)
+    {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const unsigned short* from = src[i];
+            if constexpr (ADJ) {
+                const int64_t n = left - at;
+                if (n < 8) from = n > 0 ? from - (8 - n) : zeros;
+            } else if (at + i * (THREADS / kRow) >= left) from = zeros;
+            v[i] = *(const short8u*)from;
+            src[i] += ADJ ? (int64_t)kStep : kStep * ld;
+        }
+    }
+    __device__ __forceinline__ void put(unsigned lds, const short8v* v, int64_t left, int tid) const
+    {
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int n = ADJ ? (int)max(min(at + 8 - left, (int64_t)8), (int64_t)0) & 7 : shift[i < kShifts ? i : 0];     // (8: nothing but zeros)
+            *(lds_short8*)(size_t)(lds + (i * THREADS + tid) * 16) = n ? without_first(v[i], n) : v[i];
+        }
+    }
+};
+
 // Operands of an instruction from the tile: fragment f covers rows (columns) first + 16 f .. + 15, summed index 32 h + 8 (lane / 16) + i.
 template <bool ADJ, int R> struct Reader {
     int lane_off;                                             // adjacent: bytes of this lane's place for h = 0 ...
@@ -316,8 +369,8 @@ __device__ __forceinline__ void load_shared(const float4v* const* p, const unsig
                  : "v"(far[0]), "v"(far[1]), "v"(far[2]), "v"(far[3]), "s"(p[0]), "s"(p[1]), "s"(p[2]), "s"(p[3]) : "memory");
 }
 
-// Workgroup `id` of a product's tiles_m * tiles_n * splits.
-template <typename T, GatedOp OP, int TILE>
+// Workgroup `id` of a product's tiles_m * tiles_n * splits.  LOOSE: operands at any address, widths as they are.
+template <typename T, GatedOp OP, int TILE, bool LOOSE>
 __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
 {
     using S = Shape<TILE>;
@@ -367,7 +420,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
             } else { const int64_t col = n0 + 8 * c; return pb + (col < q.b_cols ? col : q.b_cols - 8); }
         });
     };
-    start_b(s0);
+    if constexpr (!LOOSE) start_b(s0);
     const unsigned lds_a = lds0 + (unsigned)__builtin_amdgcn_readfirstlane(wave * 1024), lds_b = lds_a + stages * a_bytes;
     // elements of the sum that are left from `step` on; the left operand of kOpMul and kOpInput has zeros behind its columns
     auto left_a = [&](int step) { return OP == kOpMul || OP == kOpInput ? (int64_t)kStep : q.K - (int64_t)step * kStep; };
@@ -518,6 +571,70 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
             }
             ta = na;
             tb = nb;
+        }
+    } else if constexpr (LOOSE) {
+        // Through registers, as many steps ahead as otherwise, and two places in shared memory.
+        constexpr int ahead = stages - 1;
+        using A = Loose<a_adj, BM, threads>;
+        using B = Loose<b_adj, BN, threads>;
+        A la;
+        B lb;
+        Reader<a_adj, BM> ra;
+        ra.start(wrow, lane);
+        if constexpr (a_adj) la.start(q.a.ld, (int64_t)s0 * kStep, 0, tid, left_at);
+        else la.start(q.a.ld, (int64_t)s0 * kStep, q.a_cols, tid, [&](int c, int64_t& col) { col = m0 + 8 * c; return pa; });
+        auto second_half = [&](int step) { return OP == kOpInput && step >= half_steps; };
+        auto begin_b = [&](int step) {
+            const bool second = second_half(step);
+            const int64_t k0 = (int64_t)(second ? step - half_steps : step) * kStep;
+            if constexpr (b_adj) lb.start(q.b.ld, k0, 0, tid, [&](int c) { const int64_t r = n0 + c; return (second ? pb2 : pb) + (r < q.N ? r : q.N - 1) * q.b.ld; });
+            else lb.start(q.b.ld, k0, q.b_cols, tid, [&](int c, int64_t& col) {
+                if constexpr (OP == kOpUp) {
+                    const int w = c / (wn / 8), in = c % (wn / 8);
+                    col = n0 + w * (wn / 2) + (in % (wn / 16)) * 8;
+                    return in >= wn / 16 ? pb2 : pb;
+                } else {
+                    col = n0 + 8 * c;
+                    return pb;
+                }
+            });
+        };
+        begin_b(s0);
+        auto left_b = [&](int step) { return q.K - (int64_t)(second_half(step) ? step - half_steps : step) * kStep; };
+        short8v va[ahead][A::kPieces], vb[ahead][B::kPieces];
+        auto request = [&](int step, int u) {
+            if (OP == kOpInput && step == half_steps && step > s0) begin_b(step);
+            la.request(va[u], q.a.ld, left_a(step), zeros);
+            lb.request(vb[u], q.b.ld, left_b(step), zeros);
+        };
+#pragma unroll
+        for (int u = 0; u < ahead; ++u)
+            if (s0 + u < s1) request(s0 + u, u);
+        int buf = 0;
+        for (int s = s0; s < s1; s += ahead) {
+#pragma unroll
+            for (int u = 0; u < ahead; ++u) {
+                if (s + u >= s1) break;
+                const unsigned ta = lds0 + buf * a_bytes, tb = lds0 + stages * a_bytes + buf * b_bytes;
+                la.put(ta, va[u], left_a(s + u), tid);
+                lb.put(tb, vb[u], left_b(s + u), tid);
+                if (s + u + ahead < s1) request(s + u + ahead, u);
+                // (behind it all have read the step before this one, whose place the next one takes)
+                asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    short8v af[fm], bf[fn];
+#pragma unroll
+                    for (int j = 0; j < fn; ++j) bf[j] = rb.read(tb, j, h);
+#pragma unroll
+                    for (int i = 0; i < fm; ++i) af[i] = ra.read(ta, i, h);
+#pragma unroll
+                    for (int i = 0; i < fm; ++i)
+#pragma unroll
+                        for (int j = 0; j < fn; ++j) acc[i][j] = Half<T>::mma(bf[j], af[i], acc[i][j]);
+                }
+                buf ^= 1;
+            }
         }
     } else {
         Mover<a_adj, BM, threads> ma;
@@ -759,10 +876,10 @@ __device__ __forceinline__ int neighbours(int id, int total)
     return die * each + min(die, more) + (id >> 3);
 }
 
-template <typename T, GatedOp OP, int TILE>
+template <typename T, GatedOp OP, int TILE, bool LOOSE>
 __global__ void __launch_bounds__(tile_threads<TILE>(), tile_waves<TILE>()) gated_tile_kernel(GatedProduct q)
 {
-    tile_body<T, OP, TILE>(q, neighbours(blockIdx.x, gridDim.x));
+    tile_body<T, OP, TILE, LOOSE>(q, neighbours(blockIdx.x, gridDim.x));
 }
 
 // The products that need nothing but what kOpDown left, in one launch: dX, dWd, [dWg | dWu], as far as they are wanted.  Each begins at a multiple of
@@ -771,13 +888,13 @@ struct GradProducts {
     GatedProduct input, down, gate;
     int input_end, down_end, gate_end;
 };
-template <typename T, int TILE>
+template <typename T, int TILE, bool LOOSE>
 __global__ void __launch_bounds__(tile_threads<TILE>(), tile_waves<TILE>()) gated_grads_kernel(GradProducts g)
 {
     int id = blockIdx.x;
     if (id < g.input_end) {
         const int n = g.input.tiles_m * g.input.tiles_n * g.input.splits;
-        if (id < n) tile_body<T, kOpInput, TILE>(g.input, neighbours(id, n));
+        if (id < n) tile_body<T, kOpInput, TILE, LOOSE>(g.input, neighbours(id, n));
         return;
     }
     id -= g.input_end;
@@ -785,7 +902,7 @@ __global__ void __launch_bounds__(tile_threads<TILE>(), tile_waves<TILE>()) gate
     const GatedProduct& q = down ? g.down : g.gate;
     if (!down) id -= g.down_end;
     const int n = q.tiles_m * q.tiles_n * q.splits;
-    if (id < n) tile_body<T, kOpWeight, TILE>(q, neighbours(id, n));
+    if (id < n) tile_body<T, kOpWeight, TILE, LOOSE>(q, neighbours(id, n));
 }
 
 template <typename K> hipError_t prepare_kernel(K kernel, unsigned lds)
@@ -793,38 +910,48 @@ template <typename K> hipError_t prepare_kernel(K kernel, unsigned lds)
     return hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
 }
 
-// f(tile) for every kind of tile until one fails
+// f(tile, loose) for every kind of tile, and every one that takes operands at any address, until one fails
 template <typename F> hipError_t each_tile(F f)
 {
-    hipError_t e = f(std::integral_constant<int, kTileLarge>());
-    if (e == hipSuccess) e = f(std::integral_constant<int, kTileMedium>());
-    if (e == hipSuccess) e = f(std::integral_constant<int, kTileDeep>());
-    if (e == hipSuccess) e = f(std::integral_constant<int, kTileSmall>());
+    constexpr std::integral_constant<int, kTileSmall> small{};
+    hipError_t e = f(std::integral_constant<int, kTileLarge>(), std::false_type());
+    if (e == hipSuccess) e = f(std::integral_constant<int, kTileMedium>(), std::false_type());
+    if (e == hipSuccess) e = f(std::integral_constant<int, kTileDeep>(), std::false_type());
+    if (e == hipSuccess) e = f(small, std::false_type());
+    if (e == hipSuccess) e = f(small, std::true_type());
     return e;
 }
 template <typename F> hipError_t each_row_tile(F f)
 {
+    constexpr std::integral_constant<int, kTile32> of_32{};
+    constexpr std::integral_constant<int, kTile16> of_16{};
     hipError_t e = each_tile(f);
-    if (e == hipSuccess) e = f(std::integral_constant<int, kTile32>());
-    if (e == hipSuccess) e = f(std::integral_constant<int, kTile16>());
+    if (e == hipSuccess) e = f(of_32, std::false_type());
+    if (e == hipSuccess) e = f(of_32, std::true_type());
+    if (e == hipSuccess) e = f(of_16, std::false_type());
+    if (e == hipSuccess) e = f(of_16, std::true_type());
     return e;
 }
 
+template <typename T, GatedOp OP> hipError_t prepare_op()
+{
+    return each_row_tile([](auto t, auto loose) { return prepare_kernel(&gated_tile_kernel<T, OP, t.value, loose.value>, tile_lds<OP, t.value>()); });
+}
 template <typename T> hipError_t prepare_all()
 {
-    hipError_t e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpUp, t.value>, tile_lds<kOpUp, t.value>()); });
-    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpMul, t.value>, tile_lds<kOpMul, t.value>()); });
-    if (e == hipSuccess) e = each_row_tile([](auto t) { return prepare_kernel(&gated_tile_kernel<T, kOpDown, t.value>, tile_lds<kOpDown, t.value>()); });
-    if (e == hipSuccess) e = each_tile([](auto t) { return prepare_kernel(&gated_grads_kernel<T, t.value>, tile_lds<kOpWeight, t.value>()); });
+    hipError_t e = prepare_op<T, kOpUp>();
+    if (e == hipSuccess) e = prepare_op<T, kOpMul>();
+    if (e == hipSuccess) e = prepare_op<T, kOpDown>();
+    if (e == hipSuccess) e = each_tile([](auto t, auto loose) { return prepare_kernel(&gated_grads_kernel<T, t.value, loose.value>, tile_lds<kOpWeight, t.value>()); });
     return e;
 }
 
 template <typename T, GatedOp OP> hipError_t launch_op(const GatedProduct& q, hipStream_t stream)
 {
     const dim3 grid((unsigned)(q.tiles_m * q.tiles_n * q.splits));
-    return each_row_tile([&](auto t) {
-        if (q.tile != t.value) return hipSuccess;
-        hipLaunchKernelGGL((gated_tile_kernel<T, OP, t.value>), grid, dim3(tile_threads<t.value>()), (tile_lds<OP, t.value>()), stream, q);
+    return each_row_tile([&](auto t, auto loose) {
+        if (q.tile != t.value || q.loose != loose.value) return hipSuccess;
+        hipLaunchKernelGGL((gated_tile_kernel<T, OP, t.value, loose.value>), grid, dim3(tile_threads<t.value>()), (tile_lds<OP, t.value>()), stream, q);
         return hipGetLastError();
     });
 }
@@ -837,15 +964,17 @@ template <typename T> hipError_t launch_any(const GatedProduct& q, GatedOp op, h
     return hipErrorInvalidValue;
 }
 
-// `input`, `down`, `gate` have one kind of tile; NULL: not wanted
+// `input`, `down`, `gate` have one kind of tile, and are all loose or none; NULL: not wanted
 template <typename T> hipError_t launch_grads(const GatedProduct* input, const GatedProduct* down, const GatedProduct* gate, hipStream_t stream)
 {
     GradProducts g{};
     int tile = kTileLarge, end = 0;
+    bool loose = false;
     auto add = [&](const GatedProduct* from, GatedProduct& to) {
         if (!from) return 0;
         to = *from;
         tile = from->tile;
+        loose = from->loose;
         const int n = (from->tiles_m * from->tiles_n * from->splits + 7) / 8 * 8;
         end += n;
         return n;
@@ -854,9 +983,9 @@ template <typename T> hipError_t launch_grads(const GatedProduct* input, const G
     g.down_end = add(down, g.down);
     g.gate_end = add(gate, g.gate);
     if (end == 0) return hipSuccess;
-    return each_tile([&](auto t) {
-        if (tile != t.value) return hipSuccess;
-        hipLaunchKernelGGL((gated_grads_kernel<T, t.value>), dim3((unsigned)end), dim3(tile_threads<t.value>()), (tile_lds<kOpWeight, t.value>()), stream, g);
+    return each_tile([&](auto t, auto any) {
+        if (tile != t.value || loose != any.value) return hipSuccess;
+        hipLaunchKernelGGL((gated_grads_kernel<T, t.value, any.value>), dim3((unsigned)end), dim3(tile_threads<t.value>()), (tile_lds<kOpWeight, t.value>()), stream, g);
         return hipGetLastError();
     });
 }
