@@ -260,16 +260,22 @@ int check(bmgd_gated* b, const char* call, const Named* list, int n)
     return BMGD_OK;
 }
 
+bool direct(const bmgd_matrix& m, int64_t rows, int64_t cols) { return ((uintptr_t)m.data & 15) == 0 && cols % 8 == 0 && (rows <= 1 || m.stride % 8 == 0); }
+bool pair_direct(const bmgd_matrix& m, const bmgd_matrix& m2, int64_t rows, int64_t cols)
+{
+    return direct(m, rows, cols) && direct(m2, rows, cols) && (rows <= 1 || m.stride == m2.stride);
+}
+
+// Up to so many rows every weight is read by one workgroup only.  With more of them loose tiles take up to 10 % longer, which pays if it saves the copying launch:
+// where one of a call's launches cannot be loose and needs copies, the others take copies too (777 rows, p = 123, hidden 1,365, out 130: 17.2 us for 17.9).
+constexpr int64_t kFewRows = 64;
+
 // Operands as the kernels read them: rows of a multiple of eight elements, 16-byte aligned; a launch of loose tiles reads others too, for the rest they are
 // copied to the workspace first.
 struct Operands {
     bmgd_gated* b;
     GatedPack pack{};
 
-    static bool direct(const bmgd_matrix& m, int64_t rows, int64_t cols)
-    {
-        return ((uintptr_t)m.data & 15) == 0 && cols % 8 == 0 && (rows <= 1 || m.stride % 8 == 0);
-    }
     GatedMat copy(const bmgd_matrix& m, int64_t rows, int64_t cols, size_t area)
     {
         GatedPack::One& o = pack.m[pack.count++];
@@ -292,8 +298,8 @@ struct Operands {
     // the two matrices that one product reads side by side: their rows are equally far apart
     void use_pair(const bmgd_matrix& m, const bmgd_matrix& m2, int64_t rows, int64_t cols, size_t area, size_t area2, bool may, bool* loose, GatedMat* o, GatedMat* o2)
     {
-        const bool whole = direct(m, rows, cols) && direct(m2, rows, cols);
-        if ((whole || may) && (rows <= 1 || m.stride == m2.stride)) {
+        const bool whole = pair_direct(m, m2, rows, cols);
+        if (whole || (may && (rows <= 1 || m.stride == m2.stride))) {
             *loose = *loose || !whole;
             *o = GatedMat{m.data, rows <= 1 ? cols : m.stride};
             *o2 = GatedMat{m2.data, o->ld};
@@ -382,7 +388,9 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     plan(b, y, kOpMul, rows);
 
     Operands o{b};
-    const bool any = b->wide && gated_can_be_loose(q.tile), any_y = b->wide && gated_can_be_loose(y.tile);
+    const bool all_x = direct(t.x, rows, c.p) && pair_direct(t.gate, t.up, c.p, c.hidden), all_y = direct(t.down, c.hidden, c.out_n);
+    bool any = b->wide && gated_can_be_loose(q.tile), any_y = b->wide && gated_can_be_loose(y.tile);
+    if (rows > kFewRows && ((!any && !all_x) || (!any_y && !all_y))) any = any_y = false;
     q.a = o.use(t.x, rows, c.p, b->lay.x, any, &q.loose);
     o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, any, &q.loose, &q.b, &q.b2);
     y.b = o.use(t.down, c.hidden, c.out_n, b->lay.down, any_y, &y.loose);
@@ -441,7 +449,10 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
 
     // (dY is read by both launches: where one needs a copy, both read that)
     Operands o{b};
-    const bool any = b->wide && gated_can_be_loose(q.tile), any_grads = b->wide && n && gated_can_be_loose(list3[0]->tile);
+    const bool all_dy = direct(t.dy, rows, c.out_n), all_down = all_dy && direct(t.down, c.hidden, c.out_n);
+    const bool all_grads = (!ddown.M || all_dy) && (!dgate.M || direct(t.x, rows, c.p)) && (!input.M || pair_direct(t.gate, t.up, c.p, c.hidden));
+    bool any = b->wide && gated_can_be_loose(q.tile), any_grads = b->wide && n && gated_can_be_loose(list3[0]->tile);
+    if (rows > kFewRows && ((!any && !all_down) || (!any_grads && !all_grads))) any = any_grads = false;
     bool loose = false;
     const GatedMat dy = o.use(t.dy, rows, c.out_n, b->lay.dy, any && (any_grads || !ddown.M), &q.loose);
     if (ddown.M) loose = q.loose;
