@@ -193,6 +193,7 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
                 for (int i = 0; i < count; ++i) {
                     GatedProduct& q = *qs[i];
                     q.tile = t;
+                    q.us = us;
                     q.tiles_m = (int)plan[i].tm;
                     q.tiles_n = (int)plan[i].tn;
                     q.splits = (int)plan[i].splits;
@@ -266,9 +267,26 @@ bool pair_direct(const bmgd_matrix& m, const bmgd_matrix& m2, int64_t rows, int6
     return direct(m, rows, cols) && direct(m2, rows, cols) && (rows <= 1 || m.stride == m2.stride);
 }
 
-// Up to so many rows every weight is read by one workgroup only.  With more of them loose tiles take up to 10 % longer, which pays if it saves the copying launch:
-// where one of a call's launches cannot be loose and needs copies, the others take copies too (777 rows, p = 123, hidden 1,365, out 130: 17.2 us for 17.9).
-constexpr int64_t kFewRows = 64;
+inline int64_t unless(bool nothing, int64_t elements) { return nothing ? 0 : elements; }
+
+// Which of a call's two launches are loose.  A loose launch takes 10 to 30 % longer (14 rows, p = 860, hidden 2,992, out 141, backward: 24.9 us for 21.7 in both), a copying
+// launch 3.3 us and the time for its bytes (2.6 MB a us: 4.1 there): 100 rows, p = 200, hidden 600, out 130, backward, take 14.8 us loose and 17.0 with copies,
+// 7 rows, p = 157, hidden 7,614, out 2,409, forward, 21.6 and 32.6.
+struct Way { bool can; int64_t elements; double us; };         // of a launch: may it be loose, what is to copy where it is not, what it takes then
+void choose(const Way& x, const Way& y, bool* loose_x, bool* loose_y)
+{
+    double best = 1e300;
+    for (int m = 3; m >= 0; --m) {
+        if (((m & 1) && !x.can) || ((m & 2) && !y.can)) continue;
+        const int64_t copied = (m & 1 ? 0 : x.elements) + (m & 2 ? 0 : y.elements);
+        const double us = (copied ? 3.3 + (double)copied * (2 / 2.6e6) : 0.0) + 0.2 * ((m & 1) && x.elements ? x.us : 0.0) + 0.2 * ((m & 2) && y.elements ? y.us : 0.0);
+        if (us < best) {
+            best = us;
+            *loose_x = m & 1;
+            *loose_y = m & 2;
+        }
+    }
+}
 
 // Operands as the kernels read them: rows of a multiple of eight elements, 16-byte aligned; a launch of loose tiles reads others too, for the rest they are
 // copied to the workspace first.
@@ -388,9 +406,9 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     plan(b, y, kOpMul, rows);
 
     Operands o{b};
-    const bool all_x = direct(t.x, rows, c.p) && pair_direct(t.gate, t.up, c.p, c.hidden), all_y = direct(t.down, c.hidden, c.out_n);
-    bool any = b->wide && gated_can_be_loose(q.tile), any_y = b->wide && gated_can_be_loose(y.tile);
-    if (rows > kFewRows && ((!any && !all_x) || (!any_y && !all_y))) any = any_y = false;
+    bool any, any_y;
+    choose({b->wide && gated_can_be_loose(q.tile), unless(direct(t.x, rows, c.p), rows * c.p) + unless(pair_direct(t.gate, t.up, c.p, c.hidden), 2 * c.p * c.hidden), q.us},
+           {b->wide && gated_can_be_loose(y.tile), unless(direct(t.down, c.hidden, c.out_n), c.hidden * c.out_n), y.us}, &any, &any_y);
     q.a = o.use(t.x, rows, c.p, b->lay.x, any, &q.loose);
     o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, any, &q.loose, &q.b, &q.b2);
     y.b = o.use(t.down, c.hidden, c.out_n, b->lay.down, any_y, &y.loose);
@@ -449,10 +467,11 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
 
     // (dY is read by both launches: where one needs a copy, both read that)
     Operands o{b};
-    const bool all_dy = direct(t.dy, rows, c.out_n), all_down = all_dy && direct(t.down, c.hidden, c.out_n);
-    const bool all_grads = (!ddown.M || all_dy) && (!dgate.M || direct(t.x, rows, c.p)) && (!input.M || pair_direct(t.gate, t.up, c.p, c.hidden));
-    bool any = b->wide && gated_can_be_loose(q.tile), any_grads = b->wide && n && gated_can_be_loose(list3[0]->tile);
-    if (rows > kFewRows && ((!any && !all_down) || (!any_grads && !all_grads))) any = any_grads = false;
+    bool any, any_grads;
+    const int64_t of_dy = unless(!rows || direct(t.dy, rows, c.out_n), rows * c.out_n);
+    choose({b->wide && gated_can_be_loose(q.tile), of_dy + unless(direct(t.down, c.hidden, c.out_n), c.hidden * c.out_n), q.us},
+           {b->wide && n && gated_can_be_loose(list3[0]->tile), unless(!ddown.M, of_dy) + unless(!rows || !dgate.M || direct(t.x, rows, c.p), rows * c.p) +
+                unless(!input.M || pair_direct(t.gate, t.up, c.p, c.hidden), 2 * c.p * c.hidden), n ? list3[0]->us : 0.0}, &any, &any_grads);
     bool loose = false;
     const GatedMat dy = o.use(t.dy, rows, c.out_n, b->lay.dy, any && (any_grads || !ddown.M), &q.loose);
     if (ddown.M) loose = q.loose;

@@ -29,6 +29,7 @@ struct GatedCut {
     int tiles_m, tiles_n, splits, per_split;    // tiles of the result; workgroups that share a tile's sum, and their share in steps of 64
     int first_counter;
     size_t first_part;  // where its own counters and sums begin among those of a launch
+    double us;          // what the launch is expected to take
 };
 
 struct GatedProduct : GatedCut {

@@ -315,7 +315,7 @@ template <> struct Shape<kTile16> { static constexpr int BM = 16, BN = 128, WM =
 template <int TILE> constexpr int tile_threads() { return 64 * Shape<TILE>::WM * Shape<TILE>::WN; }
 // Wavefronts that share a SIMD's registers: two workgroups of the medium kind to a unit need 128 a lane (one register more, and 1,910 rows of hidden 2,688 in kOpDown
 // take 88 us for 57), three of the small kind 168.
-template <int TILE> constexpr int tile_waves() { return TILE == kTileMedium ? 4 : TILE == kTileSmall ? 3 : 1; }
+template <int TILE> constexpr int tile_waves() { return TILE == kTileMedium ? 4 : TILE == kTileSmall ? 3 : 2; }
 // The results leave through shared memory, in turns; kOpDown's have G and U beside them.
 template <GatedOp OP, int TILE> constexpr int tile_turns() { return TILE == kTileLarge ? (OP == kOpDown ? 4 : 2) : (TILE == kTileMedium || TILE == kTileDeep) && OP == kOpDown ? 2 : 1; }
 template <int TILE> constexpr int tile_pitch() { return Shape<TILE>::BN + 4; }             // floats from one row to the next

@@ -492,3 +492,43 @@ def test_an_infinite_gradient_meets_no_zeros_of_columns_that_are_not_there(r, f)
     for t in (dgate, dup):                                     # nothing between the rows is written
         between = torch.as_strided(t, (p - 1, 3), (f + 3, 1), f)
         assert (between == 7).all()
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("r,p,f,c", [(1, 512, 1000, 136), (17, 328, 240, 640), (40, 104, 200, 96), (134, 696, 136, 160), (300, 72, 64, 200), (700, 1024, 512, 264)])
+def test_operands_at_odd_addresses_give_the_same_bits(r, p, f, c, kind):
+    """Rows that begin anywhere come another way to the same sums in the same order."""
+    import torch
+    import paper_2312_08728_amd as B
+    dtype, code = _types()[kind]
+    results = []
+    for extra, offset in ((0, 0), (3, 1), (8, 3)):
+        x, gate, up, down = _data(r, p, f, c, dtype, seed=r, lds=(p + extra, f + extra, f + extra, c + extra), offset=offset)
+        dy = _dev(np.random.default_rng(r).standard_normal((r, c)), dtype, ld=c + extra, offset=offset)
+        y, g, u = _empty(r, c, dtype), _empty(r, f, dtype), _empty(r, f, dtype)
+        out = _empty(r, p, dtype), _empty(p, f, dtype), _empty(p, f, dtype), _empty(f, c, dtype)
+        with B.GatedBlock(p, f, c, r, dtype=code) as block:
+            block.forward(x, gate, up, down, y, g, u)
+            block.backward(dy, x, gate, up, down, g, u, *out)
+        results.append((y, g, u, *out))
+    for other in results[1:]:
+        for name, a, b in zip(("y", "g", "u", "dx", "dgate", "dup", "ddown"), results[0], other):
+            assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("r", [1, 3, 20, 70, 200])
+@pytest.mark.parametrize("p,f,c", [(8, 9, 10), (11, 12, 13), (14, 15, 17), (9, 65, 127), (71, 63, 9), (8, 8, 9), (7, 100, 100), (100, 100, 7), (100, 7, 100), (129, 130, 131)])
+def test_widths_about_a_piece_and_a_step(r, p, f, c):
+    import torch
+    import paper_2312_08728_amd as B
+    x, gate, up, down = _data(r, p, f, c, torch.bfloat16, seed=p + f)
+    with B.GatedBlock(p, f, c, r, dtype=B.BMGD_BF16, activation=B.BMGD_ACT_SILU) as block:
+        y, g, u = _empty(r, c, torch.bfloat16), _empty(r, f, torch.bfloat16), _empty(r, f, torch.bfloat16)
+        block.forward(x, gate, up, down, y, g, u)
+        _check_forward("bf16", "silu", x, gate, up, down, y, g, u)
+        dy = _dev(np.random.default_rng(r).standard_normal((r, c)), torch.bfloat16)
+        out = _empty(r, p, torch.bfloat16), _empty(p, f, torch.bfloat16), _empty(p, f, torch.bfloat16), _empty(f, c, torch.bfloat16)
+        block.backward(dy, x, gate, up, down, g, u, *out)
+        _check_backward("bf16", "silu", dy, x, gate, up, down, g, u, *out)
+        for t in (y, g, u, *out):                              # nothing behind the last row is written
+            assert (t.as_strided((8,), (1,), t.storage_offset() + t.numel()) == 7).all()
