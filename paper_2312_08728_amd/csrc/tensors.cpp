@@ -1,0 +1,135 @@
+// What the library's calls need to know of torch tensors, asked for in one go: type, device, sizes, strides and address of a tensor cost 0.4 us from Python,
+// as much as some of these calls take for all their work (64 tensors with moments in 8 bits: 128 tensors, 36 us; here 1.6).
+//
+//   matrices(tensors, shapes, dtype, device)    bytes: address and row stride (int64) of each, zeros for None
+//   pairs(pairs, numels, dtype, device)         (bytes, bytes): the addresses of the first and of the second tensors; numels: bytes of int64
+//
+// Both return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <torch/csrc/Dtype.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <cstdint>
+#include <cstring>
+
+namespace {
+
+struct Kind {
+    c10::ScalarType type;
+    int64_t device;
+};
+
+bool kind_of(PyObject* dtype, PyObject* device, Kind* k)
+{
+    if (!THPDtype_Check(dtype)) {
+        PyErr_SetString(PyExc_TypeError, "a torch.dtype is wanted");
+        return false;
+    }
+    k->type = reinterpret_cast<THPDtype*>(dtype)->scalar_type;
+    k->device = PyLong_AsLongLong(device);
+    return !PyErr_Occurred();
+}
+
+const at::Tensor* tensor_of(PyObject* o, const Kind& k)
+{
+    if (!THPVariable_Check(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.scalar_type() != k.type || t.layout() != c10::kStrided || !t.has_storage()) return nullptr;
+    if (t.is_cuda() ? t.get_device() != k.device : k.device != -1 || !t.is_cpu()) return nullptr;
+    return &t;
+}
+
+PyObject* matrices_(PyObject* const* args, Py_ssize_t n)
+{
+    Kind k;
+    if (n != 4 || !PyTuple_Check(args[0]) || !PyTuple_Check(args[1]) || PyTuple_GET_SIZE(args[0]) != PyTuple_GET_SIZE(args[1])) {
+        PyErr_SetString(PyExc_TypeError, "matrices(tensors, shapes, dtype, device): two tuples of one length");
+        return nullptr;
+    }
+    if (!kind_of(args[2], args[3], &k)) return nullptr;
+    const Py_ssize_t count = PyTuple_GET_SIZE(args[0]);
+    PyObject* out = PyBytes_FromStringAndSize(nullptr, count * 16);
+    if (!out) return nullptr;
+    char* to = PyBytes_AS_STRING(out);
+    for (Py_ssize_t i = 0; i < count; ++i, to += 16) {
+        PyObject* o = PyTuple_GET_ITEM(args[0], i);
+        int64_t v[2] = {0, 0};
+        if (o != Py_None) {
+            PyObject* shape = PyTuple_GET_ITEM(args[1], i);
+            if (!PyTuple_Check(shape) || PyTuple_GET_SIZE(shape) != 2) {
+                Py_DECREF(out);
+                PyErr_SetString(PyExc_TypeError, "matrices(): a shape is a pair");
+                return nullptr;
+            }
+            const int64_t rows = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 0)), cols = PyLong_AsLongLong(PyTuple_GET_ITEM(shape, 1));
+            const at::Tensor* t = PyErr_Occurred() ? nullptr : tensor_of(o, k);
+            if (PyErr_Occurred()) {
+                Py_DECREF(out);
+                return nullptr;
+            }
+            if (!t || t->dim() != 2 || t->size(0) != rows || t->size(1) != cols || (t->stride(1) != 1 && cols != 1)) {
+                Py_DECREF(out);
+                return PyLong_FromSsize_t(i);
+            }
+            v[0] = (int64_t)(uintptr_t)t->data_ptr();
+            v[1] = t->stride(0);
+        }
+        std::memcpy(to, v, 16);
+    }
+    return out;
+}
+
+PyObject* pairs_(PyObject* const* args, Py_ssize_t n)
+{
+    Kind k;
+    if (n != 4 || !PyList_Check(args[0]) || !PyBytes_Check(args[1]) || PyBytes_GET_SIZE(args[1]) != 8 * PyList_GET_SIZE(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "pairs(pairs, numels, dtype, device): a list and eight bytes for each of its pairs");
+        return nullptr;
+    }
+    if (!kind_of(args[2], args[3], &k)) return nullptr;
+    const Py_ssize_t count = PyList_GET_SIZE(args[0]);
+    PyObject* out[2] = {PyBytes_FromStringAndSize(nullptr, count * 8), PyBytes_FromStringAndSize(nullptr, count * 8)};
+    PyObject* answer = nullptr;
+    for (Py_ssize_t i = 0; i < count && out[0] && out[1] && !answer; ++i) {
+        PyObject* pair = PyList_GET_ITEM(args[0], i);
+        const bool tuple = PyTuple_Check(pair) && PyTuple_GET_SIZE(pair) == 2, list = PyList_Check(pair) && PyList_GET_SIZE(pair) == 2;
+        int64_t numel;
+        std::memcpy(&numel, PyBytes_AS_STRING(args[1]) + 8 * i, 8);
+        for (int j = 0; j < 2 && !answer; ++j) {
+            const at::Tensor* t = tuple ? tensor_of(PyTuple_GET_ITEM(pair, j), k) : list ? tensor_of(PyList_GET_ITEM(pair, j), k) : nullptr;
+            if (!t || t->numel() != numel || !t->is_contiguous()) {
+                answer = PyLong_FromSsize_t(i);
+                break;
+            }
+            const int64_t at = (int64_t)(uintptr_t)t->data_ptr();
+            std::memcpy(PyBytes_AS_STRING(out[j]) + 8 * i, &at, 8);
+        }
+    }
+    if (!answer && out[0] && out[1]) answer = PyTuple_Pack(2, out[0], out[1]);
+    Py_XDECREF(out[0]);
+    Py_XDECREF(out[1]);
+    return answer;
+}
+
+// (no C++ exception leaves these)
+template <PyObject* F(PyObject* const*, Py_ssize_t)> PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n)
+{
+    try {
+        return F(args, n);
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+PyMethodDef methods[] = {
+    {"matrices", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<matrices_>)), METH_FASTCALL, "addresses and row strides of matrices"},
+    {"pairs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<pairs_>)), METH_FASTCALL, "addresses of pairs of contiguous tensors"},
+    {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module); }

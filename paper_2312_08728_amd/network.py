@@ -9,12 +9,13 @@ import struct
 
 import torch
 
+from . import _tensors
 from . import binding as B
 
 _TYPES = {B.BMGD_BF16: torch.bfloat16, B.BMGD_F16: torch.float16, B.BMGD_F32: torch.float32}
 _CODES = {v: k for k, v in _TYPES.items()}
 _NAMES = ("x", "gate", "up", "down", "y", "g", "u", "dy", "dx", "dgate", "dup", "ddown")      # bmgd_gated_tensors: an address and a stride each
-_seven, _twelve = struct.Struct("14q80x").pack, struct.Struct("24q").pack
+_REST = bytes(16 * 5)                 # those behind the first seven, which a forward call does not have
 
 
 class GatedBlock:
@@ -54,26 +55,17 @@ class GatedBlock:
         raise ValueError(f"{name}: the elements of a row must lie next to each other (strides {t.stride()})")
 
     def _addresses(self, tensors, shapes):
-        # (a call of few rows waits for these lines: each property of a tensor is asked for once)
-        kind, index, flat = self._type, self._index, []
-        for t, shape in zip(tensors, shapes):
-            if t is None:
-                flat += (0, 0)
-                continue
-            if t.dtype is not kind or t.get_device() != index or t.shape != shape:
-                self._refuse(_NAMES[len(flat) // 2], t, shape)
-            stride, apart = t.stride()
-            if apart != 1 and shape[1] != 1:
-                self._refuse(_NAMES[len(flat) // 2], t, shape)
-            flat += (t.data_ptr(), stride)
-        return flat
+        found = _tensors.matrices(tensors, shapes, self._type, self._index)
+        if type(found) is int:
+            self._refuse(_NAMES[found], tensors[found], shapes[found])
+        return found
 
     def forward(self, x, gate, up, down, y, g=None, u=None, stream=None):
         """y <- Y (and g <- G, u <- U, which `backward` needs).  Asynchronous."""
         rows = x.shape[0]
         hid = (rows, self._hidden)
-        flat = self._addresses((x, gate, up, down, y, g, u), ((rows, self._p), self._in, self._in, self._out, (rows, self._out_n), hid, hid))
-        rc = B.lib.bmgd_gated_forward(self.h, rows, _seven(*flat), B._stream(stream))
+        found = self._addresses((x, gate, up, down, y, g, u), ((rows, self._p), self._in, self._in, self._out, (rows, self._out_n), hid, hid))
+        rc = B.lib.bmgd_gated_forward(self.h, rows, found + _REST, B._stream(stream))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
 
@@ -82,8 +74,8 @@ class GatedBlock:
         rows = x.shape[0]
         at, hid, wide = (rows, self._p), (rows, self._hidden), self._in
         out = (rows, self._out_n)
-        flat = self._addresses((x, gate, up, down, None, g, u, dy, dx, dgate, dup, ddown), (at, wide, wide, self._out, out, hid, hid, out, at, wide, wide, self._out))
-        rc = B.lib.bmgd_gated_backward(self.h, rows, _twelve(*flat), B._stream(stream))
+        found = self._addresses((x, gate, up, down, None, g, u, dy, dx, dgate, dup, ddown), (at, wide, wide, self._out, out, hid, hid, out, at, wide, wide, self._out))
+        rc = B.lib.bmgd_gated_backward(self.h, rows, found, B._stream(stream))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
 
@@ -131,7 +123,7 @@ class AdamW:
         for t, e in zip(self.thetas, self._t):
             self._check("theta", t, torch.float32, t.numel())
             e.theta, e.n = t.data_ptr(), t.numel()
-        self._n = [t.numel() for t in self.thetas]
+        self._n = struct.pack(f"{self.count}q", *[t.numel() for t in self.thetas])
         if state is None:
             state = [self._zeros(t, state_bits) for t in self.thetas]
         self.state = [tuple(s) for s in state]
@@ -212,13 +204,10 @@ class AdamW:
         out = list(out)
         if len(out) != self.count:
             raise ValueError(f"out: {self.count} pairs are wanted, not {len(out)}")
-        f32, index = torch.float32, self.device.index if self.count else 0
-        for n, (m, s) in zip(self._n, out):
-            if not (m.dtype is f32 and s.dtype is f32 and m.numel() == n and s.numel() == n and m.is_contiguous() and s.is_contiguous()
-                    and m.get_device() == index and s.get_device() == index):
-                self._check("m", m, f32, n)
-                self._check("s", s, f32, n)
-        address = C.c_void_p * max(1, self.count)
-        self._launch(B.lib.bmgd_adamw_moments, self._t, self.count, address(*[m.data_ptr() for m, _ in out]),
-                     address(*[s.data_ptr() for _, s in out]), B._stream(stream))
+        found = _tensors.pairs(out, self._n, torch.float32, self.device.index if self.count else -1)
+        if type(found) is int:
+            for name, t in zip(("m", "s"), out[found]):
+                self._check(name, t, torch.float32, self.thetas[found].numel())
+            raise ValueError(f"out: pairs (m, s) are wanted, not {len(out[found])} tensors")
+        self._launch(B.lib.bmgd_adamw_moments, self._t, self.count, found[0], found[1], B._stream(stream))
         return out

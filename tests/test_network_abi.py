@@ -83,3 +83,30 @@ def test_step_arguments():
 
 def test_an_internal_tile_is_checked():
     assert B.lib.bmgd_internal_gated_tile(None, 0, 1) == B.BMGD_EINVAL
+
+
+def test_what_is_read_of_tensors():
+    """Addresses and strides of matrices and of pairs, and the index of the first tensor that is not what was asked for."""
+    import struct
+    import torch
+    from paper_2312_08728_amd import _tensors as T
+    bf16 = torch.bfloat16
+    a, b = torch.zeros(5, 8, dtype=bf16)[:, 1:4], torch.zeros(7, 1, dtype=bf16).expand(7, 1)
+    one = torch.zeros(1, 6, dtype=bf16)
+    got = T.matrices((a, None, b, one), ((5, 3), (1, 1), (7, 1), (1, 6)), bf16, -1)
+    assert struct.unpack("8q", got) == (a.data_ptr(), 8, 0, 0, b.data_ptr(), b.stride(0), one.data_ptr(), one.stride(0))
+    assert T.matrices((a, torch.zeros(4, 8, dtype=bf16).t()), ((5, 3), (8, 4)), bf16, -1) == 1             # elements of a row apart
+    column = torch.zeros(4, 8, dtype=bf16)[:, :1]
+    assert struct.unpack("2q", T.matrices((column,), ((4, 1),), bf16, -1)) == (column.data_ptr(), 8)
+    for wrong in (a.float(), a[:4], a[0], a.reshape(3, 5), "no tensor", a.to("meta"), torch.zeros(5, 3, dtype=bf16).to_sparse()):
+        assert T.matrices((one, wrong), ((1, 6), (5, 3)), bf16, -1) == 1
+    assert T.matrices((a,), ((5, 3),), bf16, 0) == 0                                                          # of another device
+    m, s = torch.zeros(10), torch.zeros(2, 5)
+    assert T.pairs([(m, s), [s, m]], struct.pack("2q", 10, 10), torch.float32, -1) == (struct.pack("2q", m.data_ptr(), s.data_ptr()), struct.pack("2q", s.data_ptr(), m.data_ptr()))
+    assert T.pairs([], b"", torch.float32, -1) == (b"", b"")
+    for wrong in ((m, s[:1]), (m, s.t()), (m.double(), s), (m,), (m, s, s), m, None, (m, None)):
+        assert T.pairs([(m, s), wrong], struct.pack("2q", 10, 10), torch.float32, -1) == 1
+    for call in (lambda: T.matrices((a,), (), bf16, -1), lambda: T.matrices([a], [(5, 3)], bf16, -1), lambda: T.matrices((a,), ((5, 3),), "bf16", -1), lambda: T.matrices((a,), (5,), bf16, -1),
+                 lambda: T.matrices((a,), (("5", 3),), bf16, -1), lambda: T.matrices((a,)), lambda: T.pairs([(m, s)], b"", torch.float32, -1), lambda: T.pairs([(m, s)], bytes(8), torch.float32, None)):
+        with pytest.raises(TypeError):
+            call()
