@@ -453,9 +453,9 @@ typedef struct bmgd_gated_config {
 } bmgd_gated_config;
 
 /* A row-major matrix in device memory: element (i, j) at data + i * stride + j, stride in elements, not less than the number of
- * columns (ignored where there is one row).  2-byte alignment is enough.  Operands of the products whose rows are not
- * 16-byte aligned, of a multiple of 8 columns and of a stride that is a multiple of 8 (of one stride, for gate and up) are
- * copied in the workspace first, in every call, since the caller may have changed them. */
+ * columns (ignored where there is one row).  2-byte alignment is enough.  Large products want operands whose rows are 16-byte
+ * aligned, of a multiple of 8 columns and of a stride that is a multiple of 8 (of one stride, for gate and up); they copy others
+ * in the workspace first, in every call, since the caller may have changed them.  Small ones read any where they are. */
 typedef struct bmgd_matrix {
     void*   data;
     int64_t stride;

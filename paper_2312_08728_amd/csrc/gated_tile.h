@@ -1,7 +1,7 @@
 // The products of the gated block on the matrix cores, one kernel template for all five (see GatedOp).
 //
 // A workgroup makes a tile of BM x BN results.  Steps of 64 along the summed index go from memory straight to shared memory, one to three steps ahead
-// of the matrix instructions, 16 bytes a lane.
+// of the matrix instructions, 16 bytes a lane; where rows begin anywhere small tiles take them through registers (Loose).
 //   adjacent operand   tile [rows][64]: 128 bytes a row, eight pieces of 16; piece c of row r lies in place c ^ (r & 7), so that the 16 rows
 //                      that an instruction's lanes read at the same piece lie in different banks
 //   strided operand    tile [64][columns]; read with the transposing read of shared memory: of 16 lanes each gives the address of four
@@ -17,8 +17,8 @@
 //   products of these sizes reach 1.05 to 1.35.  Matrix units busy two thirds of the time at 1.85 GHz (2.1 without load): they and the
 //   way from L2 through shared memory to registers, 256 KB of reads and writes a step, share what shared memory delivers.
 //   One row of the same block: kOpUp 33.4 (134 MB at 4.0 TB/s), kOpMul 16.0: memory, and 2.8 us of an empty launch.
-//   100 rows, p = 200, hidden 600, out 130: kOpDown 7.4, the gradients 8: an empty launch, one trip to memory that nothing precedes (2 us) and the
-//   trips of shared sums (0.8 us each).
+//   100 rows, p = 200, hidden 600, out 130: kOpDown 6.0, the gradients 9.5: an empty launch, one trip to memory that nothing precedes (2 us) and the
+//   trips of shared sums (0.8 us each); both loose, which adds 0.5 and 1.0 and saves copies of 3.3.
 #pragma once
 
 #include "gated_internal.h"
