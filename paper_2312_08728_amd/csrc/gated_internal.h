@@ -62,7 +62,7 @@ constexpr int kGatedStep = 64;         // elements of the summed index per step
 void gated_plan(GatedProduct* const* q, const GatedOp* op, int count, int num_cus, int tile = -1, int64_t want = 0);
 
 // Whether a kind of tile has a form for operands at any address (whose rows have eight elements or more).
-inline bool gated_can_be_loose(int tile) { return tile >= kTileSmall; }
+inline bool gated_can_be_loose(int tile) { return tile != kTileLarge; }
 
 // Once per process and device: lets the kernels use as much shared memory as they need.
 hipError_t gated_prepare_bf16();

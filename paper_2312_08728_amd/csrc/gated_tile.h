@@ -1,7 +1,7 @@
 // The products of the gated block on the matrix cores, one kernel template for all five (see GatedOp).
 //
 // A workgroup makes a tile of BM x BN results.  Steps of 64 along the summed index go from memory straight to shared memory, one to three steps ahead
-// of the matrix instructions, 16 bytes a lane; where rows begin anywhere small tiles take them through registers (Loose).
+// of the matrix instructions, 16 bytes a lane; where rows begin anywhere all but the largest tiles take them through registers (Loose).
 //   adjacent operand   tile [rows][64]: 128 bytes a row, eight pieces of 16; piece c of row r lies in place c ^ (r & 7), so that the 16 rows
 //                      that an instruction's lanes read at the same piece lie in different banks
 //   strided operand    tile [64][columns]; read with the transposing read of shared memory: of 16 lanes each gives the address of four
@@ -519,7 +519,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                 }
             }
         }
-    } else if constexpr (TILE == kTileDeep) {
+    } else if constexpr (TILE == kTileDeep && !LOOSE) {
         // As many tiles as units or fewer: one workgroup to a unit, three steps in shared memory, operands read two fragments ahead, across steps too (a
         // step's last two rows of fragments are multiplied when all its operands have been read and the next step has come).
         // Against the medium kind at up to 256 tiles up to 30 % less time, 8 % in the middle (500 rows, p = 2,048, hidden 4,096, kOpUp: 27.7 us for 35.3),
@@ -914,10 +914,14 @@ template <typename K> hipError_t prepare_kernel(K kernel, unsigned lds)
 // f(tile, loose) for every kind of tile, and every one that takes operands at any address, until one fails
 template <typename F> hipError_t each_tile(F f)
 {
+    constexpr std::integral_constant<int, kTileMedium> medium{};
+    constexpr std::integral_constant<int, kTileDeep> deep{};
     constexpr std::integral_constant<int, kTileSmall> small{};
     hipError_t e = f(std::integral_constant<int, kTileLarge>(), std::false_type());
-    if (e == hipSuccess) e = f(std::integral_constant<int, kTileMedium>(), std::false_type());
-    if (e == hipSuccess) e = f(std::integral_constant<int, kTileDeep>(), std::false_type());
+    if (e == hipSuccess) e = f(medium, std::false_type());
+    if (e == hipSuccess) e = f(medium, std::true_type());
+    if (e == hipSuccess) e = f(deep, std::false_type());
+    if (e == hipSuccess) e = f(deep, std::true_type());
     if (e == hipSuccess) e = f(small, std::false_type());
     if (e == hipSuccess) e = f(small, std::true_type());
     return e;
