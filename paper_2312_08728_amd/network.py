@@ -7,6 +7,7 @@ from __future__ import annotations
 import ctypes as C
 import struct
 
+import numpy as np
 import torch
 
 from . import _tensors
@@ -15,6 +16,7 @@ from . import binding as B
 _TYPES = {B.BMGD_BF16: torch.bfloat16, B.BMGD_F16: torch.float16, B.BMGD_F32: torch.float32}
 _CODES = {v: k for k, v in _TYPES.items()}
 _NAMES = ("x", "gate", "up", "down", "y", "g", "u", "dy", "dx", "dgate", "dup", "ddown")      # bmgd_gated_tensors: an address and a stride each
+_FIELDS = [name for name, _ in B.bmgd_adamw_tensor._fields_]                                   # eight bytes each
 _REST = bytes(16 * 5)                 # those behind the first seven, which a forward call does not have
 
 
@@ -117,31 +119,28 @@ class AdamW:
         self.device = self.thetas[0].device if self.thetas else None
         self.count, self.steps, self.lr = len(self.thetas), int(step), lr
         self._t = (B.bmgd_adamw_tensor * max(1, self.count))()
+        self._rows = np.frombuffer(self._t, dtype=np.int64).reshape(-1, len(_FIELDS))
         cfg = B.bmgd_adamw_default_config()
         cfg.beta1, cfg.beta2, cfg.eps, cfg.weight_decay, cfg.state_bits = beta1, beta2, eps, weight_decay, state_bits
         self.cfg = cfg
-        for t, e in zip(self.thetas, self._t):
-            self._check("theta", t, torch.float32, t.numel())
-            e.theta, e.n = t.data_ptr(), t.numel()
-        self._n = struct.pack(f"{self.count}q", *[t.numel() for t in self.thetas])
+        sizes = [t.numel() for t in self.thetas]
+        self._n = struct.pack(f"{self.count}q", *sizes)
+        blocks = struct.pack(f"{self.count}q", *[-(-n // 256) for n in sizes])
+        self._rows[:self.count, _FIELDS.index("n")] = sizes
+        self._fill("theta", self.thetas, torch.float32, self._n)
         if state is None:
             state = [self._zeros(t, state_bits) for t in self.thetas]
         self.state = [tuple(s) for s in state]
         kinds = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8, torch.float32, torch.float32)
-        fields = ("m", "s") if state_bits == 32 else ("m", "s", "m_scale", "s_scale")
         if len(self.state) != self.count or any(len(s) != len(kinds) for s in self.state):
             raise ValueError(f"state: {len(kinds)} tensors for each of {self.count} are wanted")
-        for t, s, e in zip(self.thetas, self.state, self._t):
-            for field, part, kind in zip(fields, s, kinds):
-                self._check(field, part, kind, -(-t.numel() // 256) if field.endswith("scale") else t.numel())
-                setattr(e, field, part.data_ptr())
+        for i, (field, kind) in enumerate(zip(("m", "s", "m_scale", "s_scale"), kinds)):
+            self._fill(field, [s[i] for s in self.state], kind, blocks if field.endswith("scale") else self._n)
         self.copies = None
         if copies is not None:
             self.copies = list(copies)
             kind = self._same_type("copies", self.copies, (torch.bfloat16, torch.float16))
-            for t, e in zip(self.copies, self._t):
-                self._check("copy", t, kind, e.n)
-                e.copy = t.data_ptr()
+            self._fill("copy", self.copies, kind, self._n)
             cfg.copy_dtype = _CODES[kind]
         self.set_grads(grads)
 
@@ -159,6 +158,18 @@ class AdamW:
         if t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{name}: {n} contiguous elements are wanted, not {tuple(t.shape)} with strides {t.stride()}")
 
+    def _addresses(self, read, name, tensors, kind, sizes):
+        found = read(tensors, sizes, kind, self.device.index if self.count and self.device.type == "cuda" else -2)
+        if type(found) is int:
+            n = struct.unpack_from("q", sizes, 8 * found)[0]
+            for t in tensors[found] if read is _tensors.pairs else (tensors[found],):
+                self._check(name, t, kind, n)
+            raise ValueError(f"{name}: tensor {found} is not one that was asked for")
+        return found
+
+    def _fill(self, field, tensors, kind, sizes):
+        self._rows[:self.count, _FIELDS.index(field)] = np.frombuffer(self._addresses(_tensors.vectors, field, tensors, kind, sizes), dtype=np.int64)
+
     def _same_type(self, name, tensors, kinds):
         if len(tensors) != self.count:
             raise ValueError(f"{name}: {self.count} tensors are wanted, not {len(tensors)}")
@@ -171,10 +182,7 @@ class AdamW:
         """The tensors that later steps read gradients from."""
         grads = list(grads)
         kind = self._same_type("grads", grads, (torch.float32, torch.bfloat16, torch.float16))
-        for t, e in zip(grads, self._t):
-            self._check("grad", t, kind, e.n)
-        for t, e in zip(grads, self._t):
-            e.grad = t.data_ptr()
+        self._fill("grad", grads, kind, self._n)
         self.grads, self.cfg.grad_dtype = grads, _CODES[kind]
 
     def _launch(self, fn, *args):
@@ -204,10 +212,6 @@ class AdamW:
         out = list(out)
         if len(out) != self.count:
             raise ValueError(f"out: {self.count} pairs are wanted, not {len(out)}")
-        found = _tensors.pairs(out, self._n, torch.float32, self.device.index if self.count else -1)
-        if type(found) is int:
-            for name, t in zip(("m", "s"), out[found]):
-                self._check(name, t, torch.float32, self.thetas[found].numel())
-            raise ValueError(f"out: pairs (m, s) are wanted, not {len(out[found])} tensors")
+        found = self._addresses(_tensors.pairs, "out", out, torch.float32, self._n)
         self._launch(B.lib.bmgd_adamw_moments, self._t, self.count, found[0], found[1], B._stream(stream))
         return out

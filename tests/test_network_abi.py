@@ -106,6 +106,12 @@ def test_what_is_read_of_tensors():
     assert T.pairs([], b"", torch.float32, -1) == (b"", b"")
     for wrong in ((m, s[:1]), (m, s.t()), (m.double(), s), (m,), (m, s, s), m, None, (m, None)):
         assert T.pairs([(m, s), wrong], struct.pack("2q", 10, 10), torch.float32, -1) == 1
+    assert T.vectors([m, s], struct.pack("2q", 10, 10), torch.float32, -1) == struct.pack("2q", m.data_ptr(), s.data_ptr()) and T.vectors([], b"", torch.float32, -1) == b""
+    for wrong in (m[:9], s.t(), m.double(), m.to("meta"), None, (m,)):
+        assert T.vectors([m, wrong, s], struct.pack("3q", 10, 10, 10), torch.float32, -1) == 1
+    for call in (lambda: T.vectors((m,), bytes(8), torch.float32, -1), lambda: T.vectors([m], b"", torch.float32, -1), lambda: T.vectors([m], bytes(8), 3, -1)):
+        with pytest.raises(TypeError):
+            call()
     for call in (lambda: T.matrices((a,), (), bf16, -1), lambda: T.matrices([a], [(5, 3)], bf16, -1), lambda: T.matrices((a,), ((5, 3),), "bf16", -1), lambda: T.matrices((a,), (5,), bf16, -1),
                  lambda: T.matrices((a,), (("5", 3),), bf16, -1), lambda: T.matrices((a,)), lambda: T.pairs([(m, s)], b"", torch.float32, -1), lambda: T.pairs([(m, s)], bytes(8), torch.float32, None)):
         with pytest.raises(TypeError):
