@@ -495,8 +495,9 @@ int bmgd_gated_forward(bmgd_gated* block, int64_t rows, const bmgd_gated_tensors
 int bmgd_gated_backward(bmgd_gated* block, int64_t rows, const bmgd_gated_tensors* t, void* stream);
 
 /* Calls on one block share its workspace: they are made in the order of the calls, also on different streams (a call waits,
- * on the device, for the one before if that was on another stream, which must still exist).  A call that is captured into a
- * graph waits for nothing outside it; the caller orders the graph's launches and other calls on the same block. */
+ * on the device, for the one before if that was on another stream, which must still exist; while that stream is being captured
+ * into a graph there is no such wait, and the call returns BMGD_ESTATE).  A call that is itself captured waits for nothing outside
+ * its graph and is not what later calls wait for; the caller orders the graph's launches and other calls on the same block. */
 
 const char* bmgd_gated_last_error(const bmgd_gated* block);
 /* Waits for the device if the block was used, and releases what the library allocated.  NULL is ignored. */

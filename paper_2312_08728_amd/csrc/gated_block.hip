@@ -95,8 +95,8 @@ struct bmgd_gated {
     Layout lay;
     int device = 0, num_cus = 0;
     char* base = nullptr;
-    bool owned = false, used = false;
-    hipStream_t last = nullptr;             // of the call before
+    bool owned = false, used = false, captured = false;        // `used`: by calls that were not captured into a graph
+    hipStream_t last = nullptr;             // of the last such call
     hipEvent_t order = nullptr;
     char err[256] = "";
     int tile = -1, shares = 0;              // asked for by tests
@@ -330,19 +330,24 @@ struct Operands {
 
 GatedMat plain(const bmgd_matrix& m) { return GatedMat{m.data, m.stride}; }
 
-// Work of calls on different streams is made in the order of the calls: they share the workspace.
+// Work of calls on different streams is made in the order of the calls: they share the workspace.  A call that is captured into a graph runs when the graph is
+// launched: it waits for nothing outside, and is not what a later call waits for, which is still the one before it.
 int enter(bmgd_gated* b, hipStream_t s)
 {
     GATED_TRY(b, hipSetDevice(b->device));
-    if (b->used && b->last != s) {
-        hipStreamCaptureStatus st = hipStreamCaptureStatusNone, st_last = hipStreamCaptureStatusNone;
-        GATED_TRY(b, hipStreamIsCapturing(s, &st));
-        if (st == hipStreamCaptureStatusNone) GATED_TRY(b, hipStreamIsCapturing(b->last, &st_last));
-        // (a graph's launches cannot wait for work outside it, nor that for them: the caller orders those)
-        if (st == hipStreamCaptureStatusNone && st_last == hipStreamCaptureStatusNone) {
-            GATED_TRY(b, hipEventRecord(b->order, b->last));
-            GATED_TRY(b, hipStreamWaitEvent(s, b->order, 0));
-        }
+    if (b->used && b->last == s) return BMGD_OK;
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    GATED_TRY(b, hipStreamIsCapturing(s, &st));
+    if (st != hipStreamCaptureStatusNone) {
+        b->captured = true;
+        return BMGD_OK;
+    }
+    if (b->used) {
+        GATED_TRY(b, hipStreamIsCapturing(b->last, &st));
+        if (st != hipStreamCaptureStatusNone)
+            return fail(b, BMGD_ESTATE, "the gated block", "cannot wait for its last call: that one's stream is being captured into a graph");
+        GATED_TRY(b, hipEventRecord(b->order, b->last));
+        GATED_TRY(b, hipStreamWaitEvent(s, b->order, 0));
     }
     b->last = s;
     b->used = true;
@@ -530,7 +535,7 @@ void destroy(bmgd_gated* b)
     int current = -1;
     (void)hipGetDevice(&current);
     if (hipSetDevice(b->device) == hipSuccess) {
-        if (b->used) (void)hipDeviceSynchronize();
+        if (b->used || b->captured) (void)hipDeviceSynchronize();
         if (b->order) (void)hipEventDestroy(b->order);
         if (b->owned && b->base) (void)hipFree(b->base);
     }

@@ -1,0 +1,56 @@
+"""Work of the gated block and of the AdamW step on streams: what follows what."""
+import numpy as np
+import pytest
+
+from test_gpu_gated import _check_forward, _data, _empty, _types
+
+pytestmark = pytest.mark.gpu
+
+
+def _busy(stream, times=100):
+    """Keeps a stream at work for some hundred milliseconds."""
+    import torch
+    with torch.cuda.stream(stream):
+        m = torch.randn(4096, 4096, device="cuda")
+        for _ in range(times):
+            m = m @ m * 1e-3
+
+
+def _marker(stream):
+    import torch
+    e = torch.cuda.Event()
+    e.record(stream)
+    return e
+
+
+def test_a_captured_call_does_not_come_between_the_calls_around_it():
+    """A call behind a busy stream, one captured on a second stream, one on a third: the third ends after the first, and the graph gives the right results too."""
+    import torch
+    import paper_2312_08728_amd as B
+    dtype, code = _types()["bf16"]
+    r, p, f, c = 200, 1500, 64, 100                            # (several workgroups share a tile's sum)
+    s1, s2, s3 = (torch.cuda.Stream() for _ in range(3))
+    with B.GatedBlock(p, f, c, r, dtype=code) as block:
+        sets = [_data(r, p, f, c, dtype, seed) for seed in (1, 2, 3)]
+        ys = [_empty(r, c, dtype) for _ in sets]
+        block.forward(*sets[2], ys[2], stream=s2)
+        torch.cuda.synchronize()
+        ys[2].fill_(7.0)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        _busy(s1)
+        block.forward(*sets[0], ys[0], stream=s1)
+        first = _marker(s1)
+        with torch.cuda.stream(s2):
+            graph.capture_begin(capture_error_mode="relaxed")
+            block.forward(*sets[2], ys[2], stream=s2)
+            graph.capture_end()
+        block.forward(*sets[1], ys[1], stream=s3)
+        _marker(s3).synchronize()
+        assert first.query()
+        torch.cuda.synchronize()
+        assert (ys[2] == 7.0).all()
+        graph.replay()
+        torch.cuda.synchronize()
+        for data, y in zip(sets, ys):
+            _check_forward("bf16", "silu", *data, y)
