@@ -1,5 +1,4 @@
 """Work of the gated block and of the AdamW step on streams: what follows what."""
-import numpy as np
 import pytest
 
 from test_gpu_gated import _check_forward, _data, _empty, _types
@@ -54,3 +53,25 @@ def test_a_captured_call_does_not_come_between_the_calls_around_it():
         torch.cuda.synchronize()
         for data, y in zip(sets, ys):
             _check_forward("bf16", "silu", *data, y)
+
+
+def test_a_call_on_another_stream_ends_after_the_one_before():
+    """The first call stands behind a busy stream, the second reads what it writes, on a stream that has nothing else to wait for."""
+    import torch
+    import paper_2312_08728_amd as B
+    dtype, code = _types()["bf16"]
+    r, n, f = 300, 64, 512
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    with B.GatedBlock(n, f, n, r, dtype=code) as block:
+        x, gate, up, down = _data(r, n, f, n, dtype, 1)
+        y, z = _empty(r, n, dtype), _empty(r, n, dtype)
+        torch.cuda.synchronize()
+        _busy(s1)
+        block.forward(x, gate, up, down, y, stream=s1)
+        first = _marker(s1)
+        block.forward(y, gate, up, down, z, stream=s2)
+        _marker(s2).synchronize()
+        assert first.query()
+        torch.cuda.synchronize()
+        _check_forward("bf16", "silu", x, gate, up, down, y)
+        _check_forward("bf16", "silu", y, gate, up, down, z)
