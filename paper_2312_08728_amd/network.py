@@ -20,10 +20,16 @@ _FIELDS = [name for name, _ in B.bmgd_adamw_tensor._fields_]                    
 _REST = bytes(16 * 5)                 # those behind the first seven, which a forward call does not have
 
 
+def _stream(stream, index):
+    """The handle of `stream`, or of the stream that is torch's current one on device `index`: the one that work on the operands is on."""
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else B._stream(stream)
+
+
 class GatedBlock:
     """Y = (act(X Wg) * (X Wu)) Wd with its backward pass, for up to `max_rows` rows a call; holds a workspace, no weights.
 
-    Matrices are torch tensors on the block's device, of type `dtype` (BMGD_BF16 or BMGD_F16), rows any distance apart.
+    Matrices are torch tensors on the block's device, of type `dtype` (BMGD_BF16 or BMGD_F16), rows any distance apart.  Results must not overlap operands or each other.
+    Calls run on `stream` (a torch stream or a handle), by default on torch's current one; the caller orders other streams that operands are made or results read on.
     """
 
     def __init__(self, p, hidden, out_n, max_rows, dtype=B.BMGD_BF16, activation=B.BMGD_ACT_SILU, workspace=None):
@@ -67,7 +73,7 @@ class GatedBlock:
         rows = x.shape[0]
         hid = (rows, self._hidden)
         found = self._addresses((x, gate, up, down, y, g, u), ((rows, self._p), self._in, self._in, self._out, (rows, self._out_n), hid, hid))
-        rc = B.lib.bmgd_gated_forward(self.h, rows, found + _REST, B._stream(stream))
+        rc = B.lib.bmgd_gated_forward(self.h, rows, found + _REST, _stream(stream, self._index))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
 
@@ -77,7 +83,7 @@ class GatedBlock:
         at, hid, wide = (rows, self._p), (rows, self._hidden), self._in
         out = (rows, self._out_n)
         found = self._addresses((x, gate, up, down, None, g, u, dy, dx, dgate, dup, ddown), (at, wide, wide, self._out, out, hid, hid, out, at, wide, wide, self._out))
-        rc = B.lib.bmgd_gated_backward(self.h, rows, found, B._stream(stream))
+        rc = B.lib.bmgd_gated_backward(self.h, rows, found, _stream(stream, self._index))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
 
@@ -108,7 +114,8 @@ class AdamW:
     state: None (zeros), or a tuple of tensors per theta that are used in place: (m, s) in fp32, or (m codes int8, s codes uint8,
     m scales, s scales fp32) with ceil(n / 256) scales each.  `self.state` holds them.
     step: the number of updates already made.
-    All tensors are contiguous and on one device.
+    All tensors are contiguous and on one device.  Calls run on `stream` (a torch stream or a handle), by default on torch's current one; the caller orders other
+    streams that the tensors are written or read on.
     """
 
     def __init__(self, thetas, grads, copies=None, lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, state_bits=32,
@@ -185,19 +192,21 @@ class AdamW:
         self._fill("grad", grads, kind, self._n)
         self.grads, self.cfg.grad_dtype = grads, _CODES[kind]
 
-    def _launch(self, fn, *args):
-        if self.device is None or torch.cuda.current_device() == self.device.index:
-            rc = fn(*args)
+    def _launch(self, stream, fn, *args):
+        if self.device is None:
+            rc = fn(*args, None)                               # (no tensors: checks only)
+        elif torch.cuda.current_device() == self.device.index:
+            rc = fn(*args, _stream(stream, self.device.index))
         else:
             with torch.cuda.device(self.device):
-                rc = fn(*args)
+                rc = fn(*args, _stream(stream, self.device.index))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_last_error(None))
 
     def step(self, lr=None, grad_scale=1.0, stream=None):
         """One update with the gradients as they stand in stream order, times grad_scale.  Asynchronous."""
         self.cfg.lr, self.cfg.grad_scale = self.lr if lr is None else lr, grad_scale
-        self._launch(B.lib.bmgd_adamw_step, C.byref(self.cfg), self._t, self.count, self.steps + 1, B._stream(stream))
+        self._launch(stream, B.lib.bmgd_adamw_step, C.byref(self.cfg), self._t, self.count, self.steps + 1)
         self.steps += 1
 
     def moments(self, out=None, stream=None):
@@ -213,5 +222,5 @@ class AdamW:
         if len(out) != self.count:
             raise ValueError(f"out: {self.count} pairs are wanted, not {len(out)}")
         found = self._addresses(_tensors.pairs, "out", out, torch.float32, self._n)
-        self._launch(B.lib.bmgd_adamw_moments, self._t, self.count, found[0], found[1], B._stream(stream))
+        self._launch(stream, B.lib.bmgd_adamw_moments, self._t, self.count, found[0], found[1])
         return out
