@@ -137,6 +137,10 @@ class AdamW:
         self._fill("theta", self.thetas, torch.float32, self._n)
         if state is None:
             state = [self._zeros(t, state_bits) for t in self.thetas]
+            if self.thetas and self.thetas[0].is_cuda:
+                # the caller does not see these fills, so steps on any stream must find them done
+                if not torch.cuda.is_current_stream_capturing():
+                    torch.cuda.current_stream(self.device).synchronize()
         self.state = [tuple(s) for s in state]
         kinds = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8, torch.float32, torch.float32)
         if len(self.state) != self.count or any(len(s) != len(kinds) for s in self.state):
@@ -195,11 +199,13 @@ class AdamW:
     def _launch(self, stream, fn, *args):
         if self.device is None:
             rc = fn(*args, None)                               # (no tensors: checks only)
-        elif torch.cuda.current_device() == self.device.index:
-            rc = fn(*args, _stream(stream, self.device.index))
         else:
-            with torch.cuda.device(self.device):
-                rc = fn(*args, _stream(stream, self.device.index))
+            stream = _stream(stream, self.device.index)
+            if torch.cuda.current_device() == self.device.index:
+                rc = fn(*args, stream)
+            else:
+                with torch.cuda.device(self.device):
+                    rc = fn(*args, stream)
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_last_error(None))
 

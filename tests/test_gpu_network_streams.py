@@ -112,3 +112,22 @@ def test_calls_run_on_the_current_stream():
         torch.cuda.synchronize()
     for a, b in zip(found, (*want, *refs, *sum(moments, ()))):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_that_the_optimizer_makes_are_there_for_steps_on_any_stream(bits):
+    """The constructor's fills stand behind a busy stream: it returns when they are done, and a step on another stream finds zeros."""
+    import torch
+    import paper_2312_08728_amd as B
+    home, other = torch.cuda.Stream(), torch.cuda.Stream()
+    theta, grad = torch.randn(100_000, device="cuda"), torch.randn(100_000, device="cuda")
+    want = theta.clone()
+    B.AdamW([want], [grad], state_bits=bits).step()
+    torch.cuda.synchronize()
+    _busy(home)
+    with torch.cuda.stream(home):
+        opt = B.AdamW([theta], [grad], state_bits=bits)
+    assert home.query()
+    opt.step(stream=other)
+    torch.cuda.synchronize()
+    assert torch.equal(theta, want)
