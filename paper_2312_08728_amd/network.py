@@ -5,6 +5,7 @@ Checks shapes, types and devices, fills in addresses and strides, and calls the 
 from __future__ import annotations
 
 import ctypes as C
+import itertools
 import struct
 
 import numpy as np
@@ -135,12 +136,15 @@ class AdamW:
         blocks = struct.pack(f"{self.count}q", *[-(-n // 256) for n in sizes])
         self._rows[:self.count, _FIELDS.index("n")] = sizes
         self._fill("theta", self.thetas, torch.float32, self._n)
+        self._seen = None                                      # streams that the moments made here are known to be used on
         if state is None:
             state = [self._zeros(t, state_bits) for t in self.thetas]
             if self.thetas and self.thetas[0].is_cuda:
                 # the caller does not see these fills, so steps on any stream must find them done
+                home = torch.cuda.current_stream(self.device)
+                self._seen = {home.cuda_stream}
                 if not torch.cuda.is_current_stream_capturing():
-                    torch.cuda.current_stream(self.device).synchronize()
+                    home.synchronize()
         self.state = [tuple(s) for s in state]
         kinds = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8, torch.float32, torch.float32)
         if len(self.state) != self.count or any(len(s) != len(kinds) for s in self.state):
@@ -201,6 +205,11 @@ class AdamW:
             rc = fn(*args, None)                               # (no tensors: checks only)
         else:
             stream = _stream(stream, self.device.index)
+            if self._seen is not None and stream not in self._seen:
+                # torch must not give their memory away, once they are dropped, before the work on this stream has ended
+                self._seen.add(stream)
+                for t in itertools.chain.from_iterable(self.state):
+                    t.record_stream(torch.cuda.ExternalStream(stream, self.device))
             if torch.cuda.current_device() == self.device.index:
                 rc = fn(*args, stream)
             else:

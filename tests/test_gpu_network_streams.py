@@ -131,3 +131,21 @@ def test_moments_that_the_optimizer_makes_are_there_for_steps_on_any_stream(bits
     opt.step(stream=other)
     torch.cuda.synchronize()
     assert torch.equal(theta, want)
+
+
+def test_moments_that_the_optimizer_made_are_not_given_away_under_a_step():
+    """The optimizer is dropped while its step stands behind a busy stream: the moments' memory is not free yet for the stream that they were made on."""
+    import torch
+    import paper_2312_08728_amd as B
+    other, n = torch.cuda.Stream(), 3_000_000
+    theta, grad = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    opt = B.AdamW([theta], [grad])
+    torch.cuda.synchronize()
+    _busy(other)
+    opt.step(stream=other)
+    end = _marker(other)
+    places = {t.data_ptr() for t in opt.state[0]}
+    del opt
+    new = [torch.empty(n, device="cuda") for _ in range(4)]
+    assert not end.query() and not places & {t.data_ptr() for t in new}
+    torch.cuda.synchronize()
