@@ -225,14 +225,21 @@ class AdamW:
         self.steps += 1
 
     def moments(self, out=None, stream=None):
-        """Pairs (m, s) of fp32 tensors with the values that the state stands for; `out`: pairs to write them to.  With moments in
-        32 bits the state itself, and `out` is refused."""
+        """Pairs (m, s) of fp32 tensors with the values that the state stands for; `out`: pairs to write them to (otherwise new ones, which belong to
+        torch's current stream).  With moments in 32 bits the state itself, and `out` is refused."""
         if self.cfg.state_bits == 32:
             if out is not None:
                 raise ValueError("moments in 32 bits are the tensors in `state`")
             return self.state
         if out is None:
             out = [(torch.empty(t.numel(), device=t.device), torch.empty(t.numel(), device=t.device)) for t in self.thetas]
+            if out and stream is not None:
+                # memory that work on the current stream may still use, and that torch must not give away before the work on this one has ended
+                here, there = torch.cuda.current_stream(self.device), torch.cuda.ExternalStream(B._stream(stream), self.device)
+                if here != there:
+                    there.wait_stream(here)
+                    for t in itertools.chain.from_iterable(out):
+                        t.record_stream(there)
         out = list(out)
         if len(out) != self.count:
             raise ValueError(f"out: {self.count} pairs are wanted, not {len(out)}")

@@ -149,3 +149,36 @@ def test_moments_that_the_optimizer_made_are_not_given_away_under_a_step():
     new = [torch.empty(n, device="cuda") for _ in range(4)]
     assert not end.query() and not places & {t.data_ptr() for t in new}
     torch.cuda.synchronize()
+
+
+def test_values_of_moments_go_to_memory_that_nothing_else_uses():
+    """New results of a call on another stream lie where work of the current one may still write: they wait for it, and their memory stays theirs until they are made."""
+    import torch
+    import paper_2312_08728_amd as B
+    home, other, n = torch.cuda.Stream(), torch.cuda.Stream(), 3_000_000
+    theta, grad = torch.randn(n, device="cuda"), torch.randn(n, device="cuda")
+    opt = B.AdamW([theta], [grad], state_bits=8)
+    opt.step()
+    want = opt.moments()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(home):
+        late = [torch.empty(n, device="cuda") for _ in range(2)]
+        _busy(home)
+        for t in late:
+            t.fill_(3.0)
+        filled = _marker(home)
+        del late, t                                            # (their memory is free for what is made on this stream next)
+        found = opt.moments(stream=other)
+        _marker(other).synchronize()
+        assert filled.query()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(found[0], want[0]))
+    _busy(other)
+    with torch.cuda.stream(home):
+        dropped = opt.moments(stream=other)
+        end = _marker(other)
+        places = {t.data_ptr() for t in dropped[0]}
+        del dropped
+        new = [torch.empty(n, device="cuda") for _ in range(4)]
+    assert not end.query() and not places & {t.data_ptr() for t in new}
+    torch.cuda.synchronize()
