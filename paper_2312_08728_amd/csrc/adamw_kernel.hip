@@ -20,6 +20,7 @@
 #include "../../include/bmgd.h"
 #include "bmgd_internal.h"
 
+#include <float.h>
 #include <math.h>
 #include <stdio.h>
 #include <string.h>
@@ -39,7 +40,7 @@ static_assert(sizeof(bmgd_adamw_tensor) == 64, "");
 struct Rates {
     float b1, c1, b2, c2;           // beta1, 1 - beta1, beta2, 1 - beta2
     float m_fix, s_fix;             // 1 / (1 - beta1^k), 1 / (1 - beta2^k)
-    float keep, lr, eps, grad_scale;
+    float decay, lr, eps, grad_scale;                         // lr * weight_decay, ...
 };
 
 // The tensors of a launch.  Addresses are told as distances from the lowest of their kind, in elements (codes: in words of four), so that a tensor takes 36 bytes of
@@ -186,14 +187,18 @@ __device__ __forceinline__ float quick_sqrt(float x)
 
 // One element.  Products and sums are rounded one by one, so that the codes do not depend on what the compiler joins.  QUICK: the hardware's square root and
 // reciprocal (with moments in 8 bits the instructions count, and what they add, 2^-22 of the step, is far below what the codes do; eps is a normal number there).
+// Decay and step are added first and taken off theta with one rounding: a factor 1 - lr wd, rounded to 32 bits, is off by up to 2^-25 the same way in every step and
+// element, a third of a decay of 1e-7.  (An infinite theta stays what it is: no infinity is taken off it.)
 template <bool QUICK> __device__ __forceinline__ float update(const Rates& r, float theta, float g, float& m, float& s)
 {
 #pragma clang fp contract(off)
     g = g * r.grad_scale;
     m = r.b1 * m + r.c1 * g;
     s = r.b2 * s + r.c2 * (g * g);
-    if constexpr (QUICK) return theta * r.keep - r.lr * (m * r.m_fix * __builtin_amdgcn_rcpf(quick_sqrt(s * r.s_fix) + r.eps));
-    return theta * r.keep - r.lr * (m * r.m_fix / (sqrtf(s * r.s_fix) + r.eps));
+    float way;
+    if constexpr (QUICK) way = m * r.m_fix * __builtin_amdgcn_rcpf(quick_sqrt(s * r.s_fix) + r.eps);
+    else way = m * r.m_fix / (sqrtf(s * r.s_fix) + r.eps);
+    return theta - (r.decay * __builtin_amdgcn_fmed3f(theta, -FLT_MAX, FLT_MAX) + r.lr * way);
 }
 
 template <typename G, bool EIGHT>
@@ -507,7 +512,7 @@ BMGD_API int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tens
     a.r.c2 = (float)(1.0 - cfg->beta2);
     a.r.m_fix = (float)(1.0 / (1.0 - pow(cfg->beta1, k)));
     a.r.s_fix = (float)(1.0 / (1.0 - pow(cfg->beta2, k)));
-    a.r.keep = (float)(1.0 - cfg->lr * cfg->weight_decay);
+    a.r.decay = (float)(cfg->lr * cfg->weight_decay);
     a.r.lr = (float)cfg->lr;
     a.r.eps = (float)cfg->eps;
     a.r.grad_scale = (float)cfg->grad_scale;
