@@ -528,7 +528,7 @@ typedef struct bmgd_adamw_tensor {      /* device memory; elements lie next to e
 } bmgd_adamw_tensor;
 
 typedef struct bmgd_adamw_config {
-    double  lr;             /* finite, >= 0 */
+    double  lr;             /* finite, >= 0; this, eps, grad_scale and lr * weight_decay finite in fp32 too */
     double  beta1;          /* in [0, 1) */
     double  beta2;          /* in [0, 1) */
     double  eps;            /* finite, >= 0; >= 2^-126 with moments in 8 bits */

@@ -486,6 +486,8 @@ BMGD_API int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tens
     if (!(cfg->eps >= 0.0) || !isfinite(cfg->eps)) return fail(BMGD_EINVAL, "bmgd_adamw_step: eps must be finite and >= 0");
     if (!(cfg->weight_decay >= 0.0) || !isfinite(cfg->weight_decay)) return fail(BMGD_EINVAL, "bmgd_adamw_step: weight_decay must be finite and >= 0");
     if (!isfinite(cfg->grad_scale)) return fail(BMGD_EINVAL, "bmgd_adamw_step: grad_scale must be finite");
+    if (!isfinite((float)cfg->lr) || !isfinite((float)cfg->eps) || !isfinite((float)cfg->grad_scale) || !isfinite((float)(cfg->lr * cfg->weight_decay)))
+        return fail(BMGD_EINVAL, "bmgd_adamw_step: lr, eps, grad_scale and lr * weight_decay must be finite in fp32");
     if (cfg->grad_dtype != BMGD_F32 && cfg->grad_dtype != BMGD_BF16 && cfg->grad_dtype != BMGD_F16)
         return fail(BMGD_EINVAL, "bmgd_adamw_step: unknown grad_dtype");
     if (cfg->copy_dtype != BMGD_BF16 && cfg->copy_dtype != BMGD_F16) return fail(BMGD_EINVAL, "bmgd_adamw_step: copy_dtype must be BMGD_BF16 or BMGD_F16");

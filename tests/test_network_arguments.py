@@ -1,0 +1,22 @@
+"""Arguments of the gated block and of the AdamW step that are refused, or taken as they are, without a GPU."""
+import pytest
+
+import paper_2312_08728_amd as B
+
+
+@pytest.mark.parametrize("kw", [dict(lr=1e39), dict(lr=1e300), dict(eps=1e39), dict(grad_scale=-1e39), dict(grad_scale=1e300), dict(lr=1e30, weight_decay=1e10),
+                                dict(weight_decay=1e300)])
+def test_rates_that_are_infinite_in_32_bits_are_refused(kw):
+    """The kernels compute in fp32: such a rate would make every theta infinite or NaN."""
+    cfg = B.bmgd_adamw_default_config()
+    for k, v in kw.items():
+        setattr(cfg, k, v)
+    assert B.bmgd_adamw_step(cfg, None, 0, 1) == B.BMGD_EINVAL and "fp32" in B.bmgd_last_error(None)
+
+
+def test_the_largest_rates_are_taken():
+    cfg = B.bmgd_adamw_default_config()
+    cfg.lr, cfg.weight_decay, cfg.eps, cfg.grad_scale = 3e38, 1.0, 3e38, -3e38
+    assert B.bmgd_adamw_step(cfg, None, 0, 1) == B.BMGD_OK
+    cfg.lr, cfg.weight_decay = 0.0, 1e300
+    assert B.bmgd_adamw_step(cfg, None, 0, 1) == B.BMGD_OK
