@@ -37,7 +37,7 @@ const at::Tensor* tensor_of(PyObject* o, const Kind& k)
 {
     if (!THPVariable_Check(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (t.scalar_type() != k.type || t.layout() != c10::kStrided || !t.has_storage()) return nullptr;
+    if (t.scalar_type() != k.type || t.layout() != c10::kStrided || !t.has_storage() || t.is_neg()) return nullptr;
     if (t.is_cuda() ? t.get_device() != k.device : k.device != -1 || !t.is_cpu()) return nullptr;
     return &t;
 }

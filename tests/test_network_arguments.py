@@ -20,3 +20,16 @@ def test_the_largest_rates_are_taken():
     assert B.bmgd_adamw_step(cfg, None, 0, 1) == B.BMGD_OK
     cfg.lr, cfg.weight_decay = 0.0, 1e300
     assert B.bmgd_adamw_step(cfg, None, 0, 1) == B.BMGD_OK
+
+
+def test_tensors_that_stand_for_their_negatives_are_refused():
+    """The imaginary part of a conjugate is a view whose elements count with the other sign: its memory is not its value."""
+    import struct
+    import torch
+    from paper_2312_08728_amd import _tensors as T
+    t = torch.imag(torch.tensor([1 + 2j], dtype=torch.complex64).conj())
+    assert t.is_neg() and t.is_contiguous()
+    assert T.vectors([t], struct.pack("q", 1), torch.float32, -1) == 0
+    assert T.pairs([(t, t)], struct.pack("q", 1), torch.float32, -1) == 0
+    assert T.matrices((t.reshape(1, 1),), ((1, 1),), torch.float32, -1) == 0
+    assert isinstance(T.vectors([t.resolve_neg()], struct.pack("q", 1), torch.float32, -1), bytes)
