@@ -330,11 +330,29 @@ struct Operands {
 
 GatedMat plain(const bmgd_matrix& m) { return GatedMat{m.data, m.stride}; }
 
+// The block's device is current as long as this lives, then the one that was.
+struct OnDevice {
+    int before = -1;
+    hipError_t e;
+    explicit OnDevice(int device)
+    {
+        int current = -1;
+        e = hipGetDevice(&current);
+        if (e != hipSuccess || current == device) return;
+        e = hipSetDevice(device);
+        if (e == hipSuccess) before = current;
+    }
+    ~OnDevice()
+    {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+    OnDevice(const OnDevice&) = delete;
+};
+
 // Work of calls on different streams is made in the order of the calls: they share the workspace.  A call that is captured into a graph runs when the graph is
 // launched: it waits for nothing outside, and is not what a later call waits for, which is still the one before it.
 int enter(bmgd_gated* b, hipStream_t s)
 {
-    GATED_TRY(b, hipSetDevice(b->device));
     if (b->used && b->last == s) return BMGD_OK;
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
     GATED_TRY(b, hipStreamIsCapturing(s, &st));
@@ -401,6 +419,8 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     GATED_DO(check(b, "bmgd_gated_forward", list, 7));
     if (!t.g.data != !t.u.data) return fail(b, BMGD_EINVAL, "bmgd_gated_forward", "g and u are kept together or not at all");
     if (rows == 0) return BMGD_OK;
+    const OnDevice on(b->device);
+    GATED_TRY(b, on.e);
     GATED_DO(enter(b, s));
     const int64_t half = up(c.hidden, 64);
     GatedProduct q{}, y{};
@@ -439,6 +459,8 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
                           {"dup", &t.dup, c.p, c.hidden, true}, {"ddown", &t.ddown, c.hidden, c.out_n, true}};
     GATED_DO(check(b, "bmgd_gated_backward", list, 11));
     if (!t.dgate.data != !t.dup.data) return fail(b, BMGD_EINVAL, "bmgd_gated_backward", "dgate and dup are wanted together or not at all");
+    const OnDevice on(b->device);
+    GATED_TRY(b, on.e);
     GATED_DO(enter(b, s));
     const int64_t half = up(c.hidden, 64);
     const GatedMat h{b->base + b->lay.h, half}, d{b->base + b->lay.d, 2 * half};

@@ -104,3 +104,23 @@ assert run(2, want=2) == [] and b"captured" in lib.bmgd_gated_last_error(block)
 hip.trace_capture(1, 0)
 assert run(2) == ordered(1, 2)
 """)
+
+
+def test_a_call_leaves_the_device_that_was_current(runtime):
+    """The block was made on device 0; a call from a thread whose device is 1 runs on 0 and comes back with 1, also when it fails."""
+    _run(runtime, """
+now = C.c_int()
+def current():
+    hip.hipGetDevice(C.byref(now))
+    return now.value
+hip.hipSetDevice(1)
+assert run(1) == launched(1, device=0) and current() == 1
+backward = lambda: lib.bmgd_gated_backward(block, C.c_int64(16), C.byref(tensors), C.c_void_p(1))
+for i in range(5, 12):
+    tensors[2 * i] = i + 1 << 32
+assert backward() == 0 and current() == 1
+hip.trace_capture(1, 1)
+assert run(2, want=2) == [] and current() == 1
+lib.bmgd_gated_destroy(block)
+assert current() == 1
+""")
