@@ -420,7 +420,7 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     if (!t.g.data != !t.u.data) return fail(b, BMGD_EINVAL, "bmgd_gated_forward", "g and u are kept together or not at all");
     if (rows == 0) return BMGD_OK;
     const OnDevice on(b->device);
-    GATED_TRY(b, on.e);
+    if (on.e != hipSuccess) return hip_fail(b, on.e, "hipSetDevice");
     GATED_DO(enter(b, s));
     const int64_t half = up(c.hidden, 64);
     GatedProduct q{}, y{};
@@ -460,7 +460,7 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
     GATED_DO(check(b, "bmgd_gated_backward", list, 11));
     if (!t.dgate.data != !t.dup.data) return fail(b, BMGD_EINVAL, "bmgd_gated_backward", "dgate and dup are wanted together or not at all");
     const OnDevice on(b->device);
-    GATED_TRY(b, on.e);
+    if (on.e != hipSuccess) return hip_fail(b, on.e, "hipSetDevice");
     GATED_DO(enter(b, s));
     const int64_t half = up(c.hidden, 64);
     const GatedMat h{b->base + b->lay.h, half}, d{b->base + b->lay.d, 2 * half};
