@@ -90,8 +90,8 @@ class GatedBlock:
 
     def close(self):
         if getattr(self, "h", None):
-            B.bmgd_gated_destroy(self.h)
-            self.h = None
+            B.bmgd_gated_destroy(self.h)                       # (waits for the device)
+            self.h = self._keep = None
 
     def __enter__(self):
         return self
