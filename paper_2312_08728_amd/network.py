@@ -45,6 +45,8 @@ class GatedBlock:
                 at = -workspace.data_ptr() % 256
                 workspace = workspace[at:at + need]
         if workspace is not None:
+            if not isinstance(workspace, torch.Tensor) or not workspace.is_cuda or workspace.device.index != torch.cuda.current_device():
+                raise ValueError("workspace: a tensor on the current GPU is wanted")
             cfg.workspace, cfg.workspace_bytes = B._ptr(workspace), workspace.numel() * workspace.element_size()
         self.cfg, self._keep = cfg, workspace
         rc, h = B.bmgd_gated_create(cfg)

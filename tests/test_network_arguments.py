@@ -33,3 +33,13 @@ def test_tensors_that_stand_for_their_negatives_are_refused():
     assert T.pairs([(t, t)], struct.pack("q", 1), torch.float32, -1) == 0
     assert T.matrices((t.reshape(1, 1),), ((1, 1),), torch.float32, -1) == 0
     assert isinstance(T.vectors([t.resolve_neg()], struct.pack("q", 1), torch.float32, -1), bytes)
+
+
+def test_a_workspace_in_host_memory_is_refused():
+    """Kernels cannot reach it."""
+    import numpy as np
+    import torch
+    need = B.bmgd_gated_workspace_bytes(B.bmgd_gated_config(16, 24, 8, 4, B.BMGD_BF16, B.BMGD_ACT_SILU, None, 0))
+    for area in (torch.empty(need + 256, dtype=torch.uint8), np.empty(need + 256, dtype=np.uint8)):
+        with pytest.raises(ValueError, match="workspace"):
+            B.GatedBlock(16, 24, 8, 4, workspace=area)
