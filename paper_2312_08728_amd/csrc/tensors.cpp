@@ -4,8 +4,10 @@
 //   matrices(tensors, shapes, dtype, device)    bytes: address and row stride (int64) of each, zeros for None
 //   vectors(tensors, numels, dtype, device)     bytes: the addresses of contiguous tensors; numels: bytes of int64
 //   pairs(pairs, numels, dtype, device)         (bytes, bytes): the same of the first and of the second tensors
+//   same(groups)                                True if the tensors of every group are what they were when their addresses were read.  A group: (list, item, numels, dtype,
+//                                               addresses), the bytes as above; item: which of the tuple that the list has for each, or -1 for tensors themselves
 //
-// They return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
+// The first three return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -138,6 +140,53 @@ PyObject* pairs_(PyObject* const* args, Py_ssize_t n)
     return answer;
 }
 
+PyObject* same_(PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 1 || !PyTuple_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "same(groups): a tuple of groups");
+        return nullptr;
+    }
+    uint64_t plain = 0;                                        // what kind of tensor the last one was, in torch's words
+    for (Py_ssize_t j = 0; j < PyTuple_GET_SIZE(args[0]); ++j) {
+        PyObject* const group = PyTuple_GET_ITEM(args[0], j);
+        PyObject* g[5] = {};
+        for (Py_ssize_t i = 0; i < 5 && PyTuple_Check(group) && PyTuple_GET_SIZE(group) == 5; ++i) g[i] = PyTuple_GET_ITEM(group, i);
+        const Py_ssize_t bytes = g[4] && PyBytes_Check(g[4]) ? PyBytes_GET_SIZE(g[4]) : -1;
+        if (bytes < 0 || !PyList_Check(g[0]) || !PyBytes_Check(g[2]) || PyBytes_GET_SIZE(g[2]) != bytes) {
+            PyErr_SetString(PyExc_TypeError, "same(): a group is (list, item, numels, dtype, addresses)");
+            return nullptr;
+        }
+        if (!THPDtype_Check(g[3])) {
+            PyErr_SetString(PyExc_TypeError, "a torch.dtype is wanted");
+            return nullptr;
+        }
+        const caffe2::TypeMeta type = c10::scalarTypeToTypeMeta(reinterpret_cast<THPDtype*>(g[3])->scalar_type);
+        const int64_t size = (int64_t)type.itemsize();
+        const Py_ssize_t item = PyLong_AsSsize_t(g[1]);
+        if (item == -1 && PyErr_Occurred()) return nullptr;
+        if (8 * PyList_GET_SIZE(g[0]) != bytes) Py_RETURN_FALSE;
+        for (Py_ssize_t i = 0; 8 * i < bytes; ++i) {
+            PyObject* o = PyList_GET_ITEM(g[0], i);
+            if (item >= 0) o = PyTuple_Check(o) && item < PyTuple_GET_SIZE(o) ? PyTuple_GET_ITEM(o, item) : Py_None;
+            if (!THPVariable_Check(o)) Py_RETURN_FALSE;
+            // (no device is asked for: memory at the address that was read is on the device that was read)
+            const c10::TensorImpl* const t = THPVariable_Unpack(o).unsafeGetTensorImpl();
+            int64_t numel, at;
+            std::memcpy(&numel, PyBytes_AS_STRING(g[2]) + 8 * i, 8);
+            std::memcpy(&at, PyBytes_AS_STRING(g[4]) + 8 * i, 8);
+            const uint64_t kind = t->key_set().raw_repr();
+            if (kind != plain) {
+                if (t->layout() != c10::kStrided || !t->has_storage() || t->is_neg()) Py_RETURN_FALSE;
+                plain = kind;
+            }
+            if (t->dtype() != type || t->numel() != numel || !t->is_contiguous()) Py_RETURN_FALSE;
+            const char* const data = static_cast<const char*>(t->storage().mutable_data());     // (a lazy copy is made now)
+            if ((int64_t)(uintptr_t)(numel ? data + t->storage_offset() * size : nullptr) != at) Py_RETURN_FALSE;
+        }
+    }
+    Py_RETURN_TRUE;
+}
+
 // (no C++ exception leaves these)
 template <PyObject* F(PyObject* const*, Py_ssize_t)> PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -153,6 +202,7 @@ PyMethodDef methods[] = {
     {"matrices", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<matrices_>)), METH_FASTCALL, "addresses and row strides of matrices"},
     {"vectors", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<vectors_>)), METH_FASTCALL, "addresses of contiguous tensors"},
     {"pairs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<pairs_>)), METH_FASTCALL, "addresses of pairs of contiguous tensors"},
+    {"same", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<same_>)), METH_FASTCALL, "whether tensors are where they were"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -18,6 +18,7 @@ _TYPES = {B.BMGD_BF16: torch.bfloat16, B.BMGD_F16: torch.float16, B.BMGD_F32: to
 _CODES = {v: k for k, v in _TYPES.items()}
 _NAMES = ("x", "gate", "up", "down", "y", "g", "u", "dy", "dx", "dgate", "dup", "ddown")      # bmgd_gated_tensors: an address and a stride each
 _FIELDS = [name for name, _ in B.bmgd_adamw_tensor._fields_]                                   # eight bytes each
+_STATE = ("m", "s", "m_scale", "s_scale")
 _REST = bytes(16 * 5)                 # those behind the first seven, which a forward call does not have
 
 
@@ -117,6 +118,7 @@ class AdamW:
     state: None (zeros), or a tuple of tensors per theta that are used in place: (m, s) in fp32, or (m codes int8, s codes uint8,
     m scales, s scales fp32) with ceil(n / 256) scales each.  `self.state` holds them.
     step: the number of updates already made.
+    A tensor that is given other memory (`t.data = ...`), or replaced in `thetas`, `grads`, `copies` or `state`, is followed from the next call on.
     All tensors are contiguous and on one device.  Calls run on `stream` (a torch stream or a handle), by default on torch's current one; the caller orders other
     streams that the tensors are written or read on.
     """
@@ -137,6 +139,7 @@ class AdamW:
         self._n = struct.pack(f"{self.count}q", *sizes)
         blocks = struct.pack(f"{self.count}q", *[-(-n // 256) for n in sizes])
         self._rows[:self.count, _FIELDS.index("n")] = sizes
+        self._groups = {}                                      # by field: its tensors and where they were when `_rows` was filled in
         self._fill("theta", self.thetas, torch.float32, self._n)
         self._seen = None                                      # streams that the moments made here are known to be used on
         if state is None:
@@ -151,8 +154,8 @@ class AdamW:
         kinds = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8, torch.float32, torch.float32)
         if len(self.state) != self.count or any(len(s) != len(kinds) for s in self.state):
             raise ValueError(f"state: {len(kinds)} tensors for each of {self.count} are wanted")
-        for i, (field, kind) in enumerate(zip(("m", "s", "m_scale", "s_scale"), kinds)):
-            self._fill(field, [s[i] for s in self.state], kind, blocks if field.endswith("scale") else self._n)
+        for i, (field, kind) in enumerate(zip(_STATE, kinds)):
+            self._fill(field, self.state, kind, blocks if field.endswith("scale") else self._n, i)
         self.copies = None
         if copies is not None:
             self.copies = list(copies)
@@ -184,8 +187,19 @@ class AdamW:
             raise ValueError(f"{name}: tensor {found} is not one that was asked for")
         return found
 
-    def _fill(self, field, tensors, kind, sizes):
-        self._rows[:self.count, _FIELDS.index(field)] = np.frombuffer(self._addresses(_tensors.vectors, field, tensors, kind, sizes), dtype=np.int64)
+    def _fill(self, field, tensors, kind, sizes, item=-1):
+        found = self._addresses(_tensors.vectors, field, tensors if item < 0 else [s[item] for s in tensors], kind, sizes)
+        self._rows[:self.count, _FIELDS.index(field)] = np.frombuffer(found, dtype=np.int64)
+        self._groups[field] = tensors, item, sizes, kind, found
+        self._watched = tuple(self._groups.values()), tuple(g for name, g in self._groups.items() if name in _STATE)
+
+    def _read_again(self, watched):
+        """Addresses, where a tensor of these has been given other memory (`t.data = ...`, `resize_`) or replaced in its list: 10 ns a tensor if none has."""
+        if not _tensors.same(watched):
+            for field, (tensors, item, sizes, kind, _) in list(self._groups.items()):
+                if len(tensors) != self.count:
+                    raise ValueError(f"{field}: {self.count} tensors are wanted, not {len(tensors)}")
+                self._fill(field, tensors, kind, sizes, item)
 
     def _same_type(self, name, tensors, kinds):
         if len(tensors) != self.count:
@@ -222,6 +236,7 @@ class AdamW:
 
     def step(self, lr=None, grad_scale=1.0, stream=None):
         """One update with the gradients as they stand in stream order, times grad_scale.  Asynchronous."""
+        self._read_again(self._watched[0])
         self.cfg.lr, self.cfg.grad_scale = self.lr if lr is None else lr, grad_scale
         self._launch(stream, B.lib.bmgd_adamw_step, C.byref(self.cfg), self._t, self.count, self.steps + 1)
         self.steps += 1
@@ -233,6 +248,7 @@ class AdamW:
             if out is not None:
                 raise ValueError("moments in 32 bits are the tensors in `state`")
             return self.state
+        self._read_again(self._watched[1])
         if out is None:
             out = [(torch.empty(t.numel(), device=t.device), torch.empty(t.numel(), device=t.device)) for t in self.thetas]
             if out and stream is not None:

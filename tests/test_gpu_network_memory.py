@@ -20,3 +20,41 @@ def test_a_closed_block_holds_no_workspace():
         block.forward(x, gate, up, down, y)
     assert e.value.code == B.BMGD_EINVAL
     block.close()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_steps_follow_tensors_that_are_given_other_memory(bits):
+    """`t.data = ...` and tensors replaced in their lists: the step reads and writes where they are now, nothing where they were."""
+    import torch
+    import paper_2312_08728_amd as B
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda n: torch.randn(n, generator=gen, device="cuda")  # noqa: E731
+    masters, sizes = [new(700), new(33)], (700, 33)
+    grads = [[new(n) for n in sizes] for _ in range(2)]
+    want, copies_want = [t.clone() for t in masters], [torch.zeros(n, dtype=torch.bfloat16, device="cuda") for n in sizes]
+    ref = B.AdamW(want, grads[0], copies_want, state_bits=bits)
+    thetas, copies, mine = [t.clone() for t in masters], [torch.zeros_like(t) for t in copies_want], [t.clone() for t in grads[0]]
+    opt = B.AdamW(thetas, mine, copies, state_bits=bits)
+    for o in (ref, opt):
+        o.step()
+    old = [t.data for t in (*thetas, *copies, *mine, *opt.state[0])]
+    for t in (*thetas, *copies):
+        t.data = t.data.clone()
+    mine[0].data = grads[1][0].clone()
+    opt.grads[1] = grads[1][1].clone()
+    opt.state[0] = tuple(t.clone() for t in opt.state[0])
+    before = [t.clone() for t in old]
+    ref.set_grads(grads[1])
+    for o in (ref, opt):
+        o.step()
+    assert all(torch.equal(a, b) for a, b in zip((*thetas, *copies), (*want, *copies_want)))
+    assert all(torch.equal(a, b) for a, b in zip(old, before))
+    for a, b in zip(opt.moments(), ref.moments()):
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    thetas[0].data = thetas[0].data[:600]
+    with pytest.raises(ValueError, match="theta"):
+        opt.step()
+    thetas[0].data = want[0].double()
+    with pytest.raises(ValueError, match="theta"):
+        opt.step()
+    assert opt.steps == 2

@@ -43,3 +43,36 @@ def test_a_workspace_in_host_memory_is_refused():
     for area in (torch.empty(need + 256, dtype=torch.uint8), np.empty(need + 256, dtype=np.uint8)):
         with pytest.raises(ValueError, match="workspace"):
             B.GatedBlock(16, 24, 8, 4, workspace=area)
+
+
+def test_whether_tensors_are_where_they_were():
+    import struct
+    import torch
+    from paper_2312_08728_amd import _tensors as T
+    a, b, c = torch.zeros(10), torch.zeros(2, 5), torch.zeros(10, dtype=torch.int8)
+    n, where = struct.pack("2q", 10, 10), lambda *t: struct.pack("2q", *(x.data_ptr() for x in t))  # noqa: E731
+    flat, pairs = [a, b], [(c, a), (c, b)]
+    groups = ((flat, -1, n, torch.float32, where(a, b)), (pairs, 0, n, torch.int8, where(c, c)), (pairs, 1, n, torch.float32, where(a, b)))
+    assert T.same(groups) is True and T.same(()) is True
+    old = a.data
+    for other in (torch.zeros(10), old[:5], old.double(), torch.zeros(20)[::2]):
+        a.data = other
+        assert T.same(groups) is False
+    a.data = old
+    assert T.same(groups) is True
+    for of, others in ((flat, (a, None, torch.imag(torch.zeros(10, dtype=torch.complex64).conj()))), (pairs, ((c, a), (c,), [c, b]))):
+        keep = of[1]
+        for other in others:
+            of[1] = other
+            assert T.same(groups) is False
+        of[1] = keep
+    flat.append(a)
+    assert T.same(groups) is False
+    flat.pop()
+    assert T.same(groups) is True
+    for bad in (list(groups), (groups[0][:4],), ((flat, -1, n, torch.float32, b""),), ((tuple(flat), -1, n, torch.float32, where(a, b)),), ((flat, "0", n, torch.float32, where(a, b)),),
+                ((flat, -1, n, "f32", where(a, b)),)):
+        with pytest.raises(TypeError):
+            T.same(bad)
+    with pytest.raises(TypeError):
+        T.same(groups, -1)
