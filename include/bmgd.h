@@ -516,7 +516,8 @@ void bmgd_gated_destroy(bmgd_gated* block);
  * The scale is the block's largest |m| (s); codes are the nearest, but an s > 0 has a code of at least 1.  A block whose largest value
  * is below 2^-126 is held as zeros; a block in which a moment is not finite keeps that as its scale, with codes of zero: it stands for NaN from
  * then on.  All zeros (codes and scales, or fp32) is the state before the first update. */
-typedef struct bmgd_adamw_tensor {      /* device memory; elements lie next to each other, n of each */
+typedef struct bmgd_adamw_tensor {      /* device memory; elements lie next to each other, n of each.  What a step writes must not overlap
+                                           anything else that it is given (not checked; gradients may be one) */
     float*      theta;
     const void* grad;                   /* of cfg->grad_dtype */
     void*       copy;                   /* of cfg->copy_dtype, written; NULL: none */

@@ -119,7 +119,7 @@ class AdamW:
     m scales, s scales fp32) with ceil(n / 256) scales each.  `self.state` holds them.
     step: the number of updates already made.
     A tensor that is given other memory (`t.data = ...`), or replaced in `thetas`, `grads`, `copies` or `state`, is followed from the next call on.
-    All tensors are contiguous and on one device.  Calls run on `stream` (a torch stream or a handle), by default on torch's current one; the caller orders other
+    All tensors are contiguous and on one device; those that a step writes overlap neither each other nor a gradient.  Calls run on `stream` (a torch stream or a handle), by default on torch's current one; the caller orders other
     streams that the tensors are written or read on.
     """
 
@@ -192,6 +192,9 @@ class AdamW:
         self._rows[:self.count, _FIELDS.index(field)] = np.frombuffer(found, dtype=np.int64)
         self._groups[field] = tensors, item, sizes, kind, found
         self._watched = tuple(self._groups.values()), tuple(g for name, g in self._groups.items() if name in _STATE)
+        self._apart = False
+        if field != "grad":
+            self._written = None
 
     def _read_again(self, watched):
         """Addresses, where a tensor of these has been given other memory (`t.data = ...`, `resize_`) or replaced in its list: 10 ns a tensor if none has."""
@@ -200,6 +203,27 @@ class AdamW:
                 if len(tensors) != self.count:
                     raise ValueError(f"{field}: {self.count} tensors are wanted, not {len(tensors)}")
                 self._fill(field, tensors, kind, sizes, item)
+
+    def _spans(self, field):
+        """Where the tensors of a field begin and end (at 0 where they have no elements)."""
+        _, _, sizes, kind, found = self._groups[field]
+        start = np.frombuffer(found, dtype=np.int64)
+        return start, start + np.frombuffer(sizes, dtype=np.int64) * kind.itemsize
+
+    def _check_apart(self):
+        """What a step writes is written once, and is not a gradient.  Looked at before the first step with these addresses."""
+        if self._written is None:
+            starts, ends = (np.concatenate(x) for x in zip(*(self._spans(field) for field in self._groups if field != "grad")))
+            order = np.argsort(starts)
+            starts, ends = starts[order], ends[order]
+            if not np.any(starts[1:] < ends[:-1]):
+                self._written = starts, np.concatenate([[0], ends])
+        if self._written is not None:
+            starts, ends = self._spans("grad")
+            before = self._written[0].searchsorted(ends)         # how many begin before its end; the last of these ends furthest
+            self._apart = not (self._written[1][before] > starts).any()
+        if not self._apart:
+            raise B.BmgdError(B.BMGD_EINVAL, "AdamW: tensors that a step writes overlap each other or a gradient")
 
     def _same_type(self, name, tensors, kinds):
         if len(tensors) != self.count:
@@ -237,6 +261,8 @@ class AdamW:
     def step(self, lr=None, grad_scale=1.0, stream=None):
         """One update with the gradients as they stand in stream order, times grad_scale.  Asynchronous."""
         self._read_again(self._watched[0])
+        if not self._apart:
+            self._check_apart()
         self.cfg.lr, self.cfg.grad_scale = self.lr if lr is None else lr, grad_scale
         self._launch(stream, B.lib.bmgd_adamw_step, C.byref(self.cfg), self._t, self.count, self.steps + 1)
         self.steps += 1

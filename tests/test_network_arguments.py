@@ -76,3 +76,10 @@ def test_whether_tensors_are_where_they_were():
             T.same(bad)
     with pytest.raises(TypeError):
         T.same(groups, -1)
+
+
+def test_an_optimizer_of_no_tensors():
+    opt = B.AdamW([], [])
+    opt.step()
+    assert opt.steps == 1 and opt.moments() == []
+    assert B.AdamW([], [], [], state_bits=8).moments() == []
