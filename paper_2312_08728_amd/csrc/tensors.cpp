@@ -1,11 +1,14 @@
 // What the library's calls need to know of torch tensors, asked for in one go: type, device, sizes, strides and address of a tensor cost 0.4 us from Python,
 // as much as some of these calls take for all their work (64 tensors with moments in 8 bits: 128 tensors, 36 us; here 1.6).
 //
-//   matrices(tensors, shapes, dtype, device)    bytes: address and row stride (int64) of each, zeros for None
+//   matrices(tensors, shapes, dtype, device[, written])    bytes: address and row stride (int64) of each, zeros for None; those from index `written` on are told
+//                                               that they are written, as torch's own in-place operations tell (autograd then refuses values that it has kept)
 //   vectors(tensors, numels, dtype, device)     bytes: the addresses of contiguous tensors; numels: bytes of int64
 //   pairs(pairs, numels, dtype, device)         (bytes, bytes): the same of the first and of the second tensors
 //   same(groups)                                True if the tensors of every group are what they were when their addresses were read.  A group: (list, item, numels, dtype,
 //                                               addresses), the bytes as above; item: which of the tuple that the list has for each, or -1 for tensors themselves
+//
+//   touch(tensors)                              tells the tensors of a list that they have been written
 //
 // The first three return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
 #define PY_SSIZE_T_CLEAN
@@ -44,15 +47,24 @@ const at::Tensor* tensor_of(PyObject* o, const Kind& k)
     return &t;
 }
 
+void touch(const at::Tensor& t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();             // (inference tensors have no count)
+}
+
 PyObject* matrices_(PyObject* const* args, Py_ssize_t n)
 {
     Kind k;
-    if (n != 4 || !PyTuple_Check(args[0]) || !PyTuple_Check(args[1]) || PyTuple_GET_SIZE(args[0]) != PyTuple_GET_SIZE(args[1])) {
+    if ((n != 4 && n != 5) || !PyTuple_Check(args[0]) || !PyTuple_Check(args[1]) || PyTuple_GET_SIZE(args[0]) != PyTuple_GET_SIZE(args[1])) {
         PyErr_SetString(PyExc_TypeError, "matrices(tensors, shapes, dtype, device): two tuples of one length");
         return nullptr;
     }
     if (!kind_of(args[2], args[3], &k)) return nullptr;
-    const Py_ssize_t count = PyTuple_GET_SIZE(args[0]);
+    const Py_ssize_t count = PyTuple_GET_SIZE(args[0]), written = n == 5 ? PyLong_AsSsize_t(args[4]) : count;
+    if (written < 0) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "matrices(): written must not be negative");
+        return nullptr;
+    }
     PyObject* out = PyBytes_FromStringAndSize(nullptr, count * 16);
     if (!out) return nullptr;
     char* to = PyBytes_AS_STRING(out);
@@ -81,6 +93,8 @@ PyObject* matrices_(PyObject* const* args, Py_ssize_t n)
         }
         std::memcpy(to, v, 16);
     }
+    for (Py_ssize_t i = written; i < count; ++i)
+        if (PyTuple_GET_ITEM(args[0], i) != Py_None) touch(THPVariable_Unpack(PyTuple_GET_ITEM(args[0], i)));
     return out;
 }
 
@@ -187,6 +201,17 @@ PyObject* same_(PyObject* const* args, Py_ssize_t n)
     Py_RETURN_TRUE;
 }
 
+PyObject* touch_(PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 1 || !PyList_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "touch(tensors): a list");
+        return nullptr;
+    }
+    for (Py_ssize_t i = 0; i < PyList_GET_SIZE(args[0]); ++i)
+        if (THPVariable_Check(PyList_GET_ITEM(args[0], i))) touch(THPVariable_Unpack(PyList_GET_ITEM(args[0], i)));
+    Py_RETURN_NONE;
+}
+
 // (no C++ exception leaves these)
 template <PyObject* F(PyObject* const*, Py_ssize_t)> PyObject* guarded(PyObject*, PyObject* const* args, Py_ssize_t n)
 {
@@ -203,6 +228,7 @@ PyMethodDef methods[] = {
     {"vectors", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<vectors_>)), METH_FASTCALL, "addresses of contiguous tensors"},
     {"pairs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<pairs_>)), METH_FASTCALL, "addresses of pairs of contiguous tensors"},
     {"same", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<same_>)), METH_FASTCALL, "whether tensors are where they were"},
+    {"touch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<touch_>)), METH_FASTCALL, "tells tensors that they have been written"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -66,8 +66,8 @@ class GatedBlock:
             raise ValueError(f"{name}: shape {shape} is wanted, not {tuple(t.shape)}")
         raise ValueError(f"{name}: the elements of a row must lie next to each other (strides {t.stride()})")
 
-    def _addresses(self, tensors, shapes):
-        found = _tensors.matrices(tensors, shapes, self._type, self._index)
+    def _addresses(self, tensors, shapes, written):
+        found = _tensors.matrices(tensors, shapes, self._type, self._index, written)
         if type(found) is int:
             self._refuse(_NAMES[found], tensors[found], shapes[found])
         return found
@@ -76,7 +76,7 @@ class GatedBlock:
         """y <- Y (and g <- G, u <- U, which `backward` needs).  Asynchronous."""
         rows = x.shape[0]
         hid = (rows, self._hidden)
-        found = self._addresses((x, gate, up, down, y, g, u), ((rows, self._p), self._in, self._in, self._out, (rows, self._out_n), hid, hid))
+        found = self._addresses((x, gate, up, down, y, g, u), ((rows, self._p), self._in, self._in, self._out, (rows, self._out_n), hid, hid), 4)
         rc = B.lib.bmgd_gated_forward(self.h, rows, found + _REST, _stream(stream, self._index))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
@@ -86,7 +86,7 @@ class GatedBlock:
         rows = x.shape[0]
         at, hid, wide = (rows, self._p), (rows, self._hidden), self._in
         out = (rows, self._out_n)
-        found = self._addresses((x, gate, up, down, None, g, u, dy, dx, dgate, dup, ddown), (at, wide, wide, self._out, out, hid, hid, out, at, wide, wide, self._out))
+        found = self._addresses((x, gate, up, down, None, g, u, dy, dx, dgate, dup, ddown), (at, wide, wide, self._out, out, hid, hid, out, at, wide, wide, self._out), 8)
         rc = B.lib.bmgd_gated_backward(self.h, rows, found, _stream(stream, self._index))
         if rc != B.BMGD_OK:
             raise B.BmgdError(rc, B.bmgd_gated_last_error(self.h))
@@ -266,6 +266,9 @@ class AdamW:
         self.cfg.lr, self.cfg.grad_scale = self.lr if lr is None else lr, grad_scale
         self._launch(stream, B.lib.bmgd_adamw_step, C.byref(self.cfg), self._t, self.count, self.steps + 1)
         self.steps += 1
+        _tensors.touch(self.thetas)
+        if self.copies:
+            _tensors.touch(self.copies)
 
     def moments(self, out=None, stream=None):
         """Pairs (m, s) of fp32 tensors with the values that the state stands for; `out`: pairs to write them to (otherwise new ones, which belong to

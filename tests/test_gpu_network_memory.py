@@ -88,3 +88,28 @@ def test_tensors_that_overlap_are_refused(bits):
     with pytest.raises(B.BmgdError, match="overlap"):
         opt.step()
     B.AdamW([flat[:0], flat[:0], flat[:5]], [flat[:0], flat[:0], flat[5:10]], state_bits=bits).step()    # nothing overlaps with no elements
+
+
+def test_autograd_notices_what_the_calls_write():
+    """A value that a graph of torch's has kept, overwritten by the block or by a step, is refused in its backward pass."""
+    import torch
+    import paper_2312_08728_amd as B
+    p, f, c, r = 16, 24, 8, 4
+    x, gate, up, down = (torch.randn(s, device="cuda").bfloat16() for s in ((r, p), (p, f), (p, f), (f, c)))
+    y, g, u = (torch.zeros(r, n, device="cuda", dtype=torch.bfloat16) for n in (c, f, f))
+    theta = torch.ones(50, device="cuda", requires_grad=True)
+    opt = B.AdamW([theta], [torch.ones(50, device="cuda")])
+    w = torch.ones(r, c, device="cuda", dtype=torch.bfloat16, requires_grad=True)
+    with B.GatedBlock(p, f, c, r) as block:
+        kept = (w * y).sum()
+        block.forward(x, gate, up, down, y, g, u)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            kept.backward()
+        dx = torch.zeros_like(x)
+        before = [t._version for t in (x, gate, up, down, g, u, y, dx)]
+        block.backward(y, x, gate, up, down, g, u, dx=dx)
+        assert [t._version for t in (x, gate, up, down, g, u, y, dx)] == [*before[:-1], before[-1] + 1]
+    kept = (theta * theta).sum()
+    opt.step()
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        kept.backward()

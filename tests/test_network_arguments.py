@@ -83,3 +83,27 @@ def test_an_optimizer_of_no_tensors():
     opt.step()
     assert opt.steps == 1 and opt.moments() == []
     assert B.AdamW([], [], [], state_bits=8).moments() == []
+
+
+def test_tensors_are_told_that_they_are_written():
+    """As by torch's own in-place operations: values that autograd has kept for a backward pass are then refused there."""
+    import torch
+    from paper_2312_08728_amd import _tensors as T
+    x, y, z = (torch.zeros(3, 4) for _ in range(3))
+    shapes = ((3, 4),) * 4
+    T.matrices((x, y, None, z), shapes, torch.float32, -1)
+    assert (x._version, y._version, z._version) == (0, 0, 0)
+    T.matrices((x, y, None, z), shapes, torch.float32, -1, 1)
+    assert (x._version, y._version, z._version) == (0, 1, 1)
+    assert T.matrices((x, y, z[:2], z), shapes, torch.float32, -1, 0) == 2 and x._version == 0          # nothing is written then
+    T.touch([x, y])
+    assert (x._version, y._version, z._version) == (1, 2, 1)
+    with torch.inference_mode():
+        quiet = torch.zeros(3, 4)
+    T.touch([quiet])
+    T.matrices((quiet,), ((3, 4),), torch.float32, -1, 0)
+    for call in (lambda: T.touch((x,)), lambda: T.touch(), lambda: T.matrices((x,), ((3, 4),), torch.float32, -1, None)):
+        with pytest.raises(TypeError):
+            call()
+    with pytest.raises(ValueError):
+        T.matrices((x,), ((3, 4),), torch.float32, -1, -1)
