@@ -20,7 +20,7 @@ constexpr int64_t kMaxRows = (int64_t(1) << 30) - 1;
 int64_t up(int64_t n, int64_t m) { return (n + m - 1) / m * m; }
 
 struct Layout {
-    size_t h, d, x, gate, up, down, dy, partial, counter, zeros, total;
+    size_t h, d, x, gate, up, down, dy, partial, counter, zeros, scaled, scale_h, scale_d, total;
 };
 
 bool valid(const bmgd_gated_config& c, const char** why)
@@ -53,6 +53,11 @@ Layout make_layout(const bmgd_gated_config& c)
     l.partial = take(kGatedPartialBytes);
     l.counter = take(kGatedCounters * sizeof(unsigned));
     l.zeros = take(256);
+    if (c.dtype == BMGD_F16) {
+        l.scaled = take(256);
+        l.scale_h = take(r * f64 / 8);
+        l.scale_d = take(2 * r * f64 / 8);
+    }
     l.total = at;
     return l;
 }
@@ -99,6 +104,7 @@ struct bmgd_gated {
     hipStream_t last = nullptr;             // of the last such call
     hipEvent_t order = nullptr;
     char err[256] = "";
+    int turn = 0;                           // of calls in f16, see GatedProduct
     int tile = -1, shares = 0;              // asked for by tests
     bool wide = false;                      // every row has eight elements or more, as loose tiles want them
     struct Kept { int64_t rows = -1; int what = 0; bmgd::GatedCut cut[3]; } kept[32];      // by rows modulo 8 and launch, see plan()
@@ -397,6 +403,16 @@ void plan(bmgd_gated* b, GatedProduct& q, GatedOp op, int64_t rows)
     plan(b, &one, &op, 1, rows, op);
 }
 
+// f16: where the exponents of H and D stand, for a product that writes or reads them.
+void scales(bmgd_gated* b, GatedProduct& q, size_t scale, size_t scale2 = 0)
+{
+    if (b->cfg.dtype != BMGD_F16) return;
+    q.scale = reinterpret_cast<unsigned char*>(b->base + scale);
+    q.scale2 = reinterpret_cast<unsigned char*>(b->base + scale2);
+    q.scaled = reinterpret_cast<unsigned*>(b->base + b->lay.scaled);
+    q.turn = b->turn;
+}
+
 int launch(bmgd_gated* b, const GatedProduct& q, GatedOp op, hipStream_t s)
 {
     const hipError_t e = b->cfg.dtype == BMGD_F16 ? gated_launch_f16(q, op, s) : gated_launch_bf16(q, op, s);
@@ -442,9 +458,12 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     q.out = GatedMat{b->base + b->lay.h, half};
     q.g = plain(t.g);
     q.u = plain(t.u);
+    b->turn ^= 1;
+    scales(b, q, b->lay.scale_h);
     GATED_DO(launch(b, q, kOpUp, s));
 
     y.a = q.out;
+    scales(b, y, b->lay.scale_h);
     y.b_cols = y.loose ? c.out_n : up(c.out_n, 8);
     y.out = plain(t.y);
     return launch(b, y, kOpMul, s);
@@ -507,8 +526,10 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
     if (dgate.M) x = o.use(t.x, rows, c.p, b->lay.x, any_grads, &loose);
     if (input.M) o.use_pair(t.gate, t.up, c.p, c.hidden, b->lay.gate, b->lay.up, any_grads, &loose, &input.b, &input.b2);
     if (rows && o.pack.count) GATED_TRY(b, gated_launch_pack(o.pack, s));
+    b->turn ^= 1;
     if (rows) {
         if (!q.loose) q.K = up(c.out_n, 8);
+        scales(b, q, b->lay.scale_h, b->lay.scale_d);
         q.a = dy;
         q.out = h;
         q.out2 = d;
@@ -533,6 +554,9 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
     dgate.b_cols = 2 * half;
     dgate.out = plain(t.dgate);
     dgate.out2 = plain(t.dup);
+    scales(b, input, b->lay.scale_d);
+    scales(b, ddown, b->lay.scale_h);
+    scales(b, dgate, b->lay.scale_d);
     const GatedProduct *pi = input.M ? &input : nullptr, *pd = ddown.M ? &ddown : nullptr, *pg = dgate.M ? &dgate : nullptr;
     const hipError_t e = c.dtype == BMGD_F16 ? gated_launch_grads_f16(pi, pd, pg, s) : gated_launch_grads_bf16(pi, pd, pg, s);
     if (e != hipSuccess) return hip_fail(b, e, "launch of the gradients of the gated block");

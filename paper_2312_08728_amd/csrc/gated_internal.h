@@ -47,6 +47,11 @@ struct GatedProduct : GatedCut {
     float* partial;     // sums of workgroups that share a tile
     unsigned* counter;  // and how many of them have arrived, per tile; zero between launches
     const void* zeros;  // 256 bytes of zeros
+    // f16 only, NULL otherwise.  H, dG and dU may leave f16's range: then eight neighbouring elements of a row (a piece) are held as multiples of 2^e, e their byte here, at
+    // the offset of the first element over eight.  kOpUp, kOpDown write those of `out` and `out2`, the others read those of their operand.
+    unsigned char *scale, *scale2;
+    unsigned* scaled;   // three words: [0] some call had an e that is not zero, so all are written from then on; [1 + turn] this call has
+    int turn;           // of the call, 0 or 1; its second launch clears the other's word
 };
 
 // rows x columns: 256 x 256, 128 x 128 (two workgroups to a unit; one, steps further ahead), 64 x 64; for few rows 32 x 128 and 16 x 128

@@ -370,6 +370,126 @@ __device__ __forceinline__ void load_shared(const float4v* const* p, const unsig
                  : "v"(far[0]), "v"(far[1]), "v"(far[2]), "v"(far[3]), "s"(p[0]), "s"(p[1]), "s"(p[2]), "s"(p[3]) : "memory");
 }
 
+// H, dG and dU in f16: the operands of the next product, whose range the sums that make them need not keep to (G = U = 300 make 90,000).  Eight neighbouring elements of a row whose
+// largest would be rounded to infinity are held as multiples of 2^e, as small as it takes to bring that one below 2^15, and e goes into a byte of its own.  They have the
+// relative accuracy of f16, and absolutely that of 2^-39 of the eight's largest.  Infinities and NaN stay what they are.  Where nothing is that large this costs a few
+// instructions for eight elements; bytes are written once it has happened to this block.
+constexpr float kLargestHalf = 65520.f;                        // and beyond: rounded to infinity
+__device__ __forceinline__ bool has_no_number(short8v v)       // of f16: infinities and NaN
+{
+    const uint4v w = (__builtin_bit_cast(uint4v, v) & 0x7c007c00u) + 0x04000400u;
+    return ((w[0] | w[1] | w[2] | w[3]) & 0x80008000u) != 0u;
+}
+// value(k): element k of the eight
+template <typename T, typename F> __device__ __forceinline__ void store_scaled(const GatedProduct& q, const GatedMat& to, int64_t r, int64_t c, unsigned char* scale, F value)
+{
+    float top = 0.f;
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k) {
+        const float size = fabsf(value(k));
+        if (size < __builtin_inff()) top = fmaxf(top, size);
+    }
+    int e = 0;
+    if (top >= kLargestHalf) {
+        e = (int)(__float_as_uint(top) >> 23) - 127 - 14;
+        q.scaled[0] = 1u;
+        q.scaled[1 + q.turn] = 1u;
+#pragma unroll 1
+        for (int k = 0; k < 8; ++k) *element(to, r, c + k) = bits_of<T>(ldexpf(value(k), -e));
+    }
+    scale[(r * to.ld + c) >> 3] = (unsigned char)e;            // (0: the eight stand there as they were rounded)
+}
+
+// And their part in the next product: its sum took such elements for what they are held as, so (2^e - 1) times their products are added to the results of this turn, in
+// shared memory.  `found`: for every 16 rows (columns) of the tile a bit for each 32 of the summed index that have an e, 16,384 at a time.  What is not finite is in the sum
+// already.  This is slow, since operands come element by element, and rare (4,096 rows, p = out = 2,048, hidden 4,096: three columns of H out of range 0.41 ms forward for
+// 0.20 and 2.0 backward for 0.45, all of them 7.9 and 27; the widest training step that has none takes as long as before).
+constexpr int kFoundWords = 16;
+__device__ __forceinline__ short finite_or_zero(short b) { return (b & 0x7c00) == 0x7c00 ? (short)0 : b; }
+
+template <typename T, GatedOp OP, int TILE>
+__device__ __forceinline__ void add_scaled(const GatedProduct& q, float* res, int turn, int64_t m0, int64_t n0, int tid, unsigned* found)
+{
+    using S = Shape<TILE>;
+    constexpr int threads = tile_threads<TILE>(), BM = S::BM, BN = S::BN, waves = threads / 64, chunk = 32 * 32 * kFoundWords;
+    constexpr int turns = tile_turns<OP, TILE>(), pitch = tile_pitch<TILE>(), wm = BM / S::WM, wt = wm / turns;
+    const int lane = tid & 63, wave = tid >> 6, i = lane & 15, o = lane >> 4;
+    const bool left = OP != kOpWeight || q.half == 0;          // which operand has exponents
+    const int64_t ld = left ? q.a.ld : q.b.ld, len = OP == kOpInput ? 2 * q.half : q.K, cols = OP == kOpWeight && q.half ? 2 * q.half : q.N;
+    const short *const pa = (const short*)q.a.p, *const pb = (const short*)q.b.p, *const pb2 = (const short*)q.b2.p;
+    for (int64_t k0 = 0; k0 < len; k0 += chunk) {
+        const int64_t here = min(len - k0, (int64_t)chunk);
+        __syncthreads();
+        for (int w = tid; w < 16 * kFoundWords; w += threads) found[w] = 0u;
+        __syncthreads();
+        auto eight = [&](int64_t r, int64_t c) { return *(const unsigned long long*)(q.scale + ((r * ld + c) >> 3)); };        // of columns c to c + 63
+        auto mark = [&](int strip, int64_t block) { atomicOr(found + strip * kFoundWords + (block >> 5), 1u << (block & 31)); };
+        if constexpr (OP != kOpWeight) {
+            const int64_t words = (here + 63) / 64, rows = min((int64_t)BM, q.M - m0);
+            for (int64_t id = tid; id < rows * words; id += threads) {
+                const unsigned long long v = eight(m0 + id / words, k0 + id % words * 64);
+                if ((unsigned)v) mark((int)(id / words) / 16, id % words * 2);
+                if ((unsigned)(v >> 32)) mark((int)(id / words) / 16, id % words * 2 + 1);
+            }
+        } else {
+            const int64_t first = left ? m0 : n0;
+            const int words = (left ? BM : BN) / 64;
+            for (int64_t id = tid; id < here * words; id += threads) {
+                const int64_t c = first + id % words * 64;
+                const unsigned long long v = c < ld ? eight(k0 + id / words, c) : 0u;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if ((unsigned short)(v >> (16 * t))) mark((int)(id % words) * 4 + t, id / words / 32);
+            }
+        }
+        __syncthreads();
+        for (int piece = wave; piece < BM / turns / 16 * (BN / 16); piece += waves) {
+            const int lr = piece / (BN / 16) * 16, lc = piece % (BN / 16) * 16;
+            const int64_t r = m0 + (lr / wt) * wm + turn * wt + lr % wt + i, c = n0 + lc + i;
+            if (r - i >= q.M || c - i >= cols) continue;
+            const int strip = (int)(left ? r - i - m0 : (int64_t)lc) / 16;
+            float4v* const to = reinterpret_cast<float4v*>(res + (lr + i) * pitch + lc + 4 * o);
+            float4v sum = *to;
+            for (int w = 0; w < kFoundWords; ++w)
+                for (unsigned bits = __builtin_amdgcn_readfirstlane(found[strip * kFoundWords + w]); bits; bits &= bits - 1) {
+                    const int64_t k = k0 + 32 * (32 * w + __builtin_ctz(bits)) + 8 * o;
+                    short8v a, b;
+                    int e[8], most = 0;
+#pragma unroll
+                    for (int t = 0; t < 8; ++t) {
+                        const bool second = OP == kOpInput && k >= q.half;
+                        const int64_t kb = k + t - (second ? q.half : 0);
+                        const bool in_a = r < q.M && (OP != kOpWeight || k + t < q.K), in_b = c < cols && kb < q.K;
+                        a[t] = in_a ? finite_or_zero(OP == kOpWeight ? pa[(k + t) * q.a.ld + r] : pa[r * q.a.ld + k + t]) : (short)0;
+                        b[t] = in_b ? finite_or_zero(OP == kOpInput ? (second ? pb2 : pb)[c * q.b.ld + kb] : pb[kb * q.b.ld + c]) : (short)0;
+                        const int64_t at = OP != kOpWeight ? r * ld + k + t : (k + t) * ld + (left ? r : c);
+                        e[t] = (left ? in_a : in_b) ? (int)q.scale[at >> 3] : 0;
+                        most = max(most, e[t]);
+                    }
+                    // the largest e of the wavefront's elements, those that have it; the next one
+                    for (;;) {
+                        int top = most;
+#pragma unroll
+                        for (int d = 1; d < 64; d *= 2) top = max(top, __shfl_xor(top, d));
+                        if (top == 0) break;
+                        short8v only;
+                        most = 0;
+#pragma unroll
+                        for (int t = 0; t < 8; ++t) {
+                            only[t] = e[t] == top ? (left ? a[t] : b[t]) : (short)0;
+                            e[t] = e[t] == top ? 0 : e[t];
+                            most = max(most, e[t]);
+                        }
+                        const float4v part = Half<T>::mma(left ? b : only, left ? only : a, float4v{0.f, 0.f, 0.f, 0.f});
+                        sum += part * (ldexpf(1.f, top) - 1.f);
+                    }
+                }
+            *to = sum;
+        }
+    }
+    __syncthreads();
+}
+
 // Workgroup `id` of a product's tiles_m * tiles_n * splits.  LOOSE: operands at any address, widths as they are.
 template <typename T, GatedOp OP, int TILE, bool LOOSE>
 __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
@@ -385,6 +505,17 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned short*)stage;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    // f16: whether bytes of exponents are written in any case (the products that make H and D), whether there are any (those that read them).  The word comes to
+    // shared memory beside the operands: in a register it would be waited for, and with it whatever is on its way.
+    constexpr bool scales = std::is_same<T, _Float16>::value, makes = OP == kOpUp || OP == kOpDown;
+    unsigned* found = nullptr;
+    if constexpr (scales) {
+        __shared__ unsigned words[16 * kFoundWords];            // (the word fills the first 64)
+        static_assert(BM <= 256 && BN <= 256 && 16 * kFoundWords >= 64, "");
+        found = words;
+        if (wave == 0) load_word_to_lds((const int*)(q.scaled + (makes ? 0 : 1 + q.turn)), (unsigned)(size_t)(__attribute__((address_space(3))) unsigned*)words);
+        if (!makes && blockIdx.x == 0 && tid == 0) q.scaled[2 - q.turn] = 0u;
+    }
     const int split = id % q.splits;
     const int tile = id / q.splits;
     constexpr int kGroup = 8;                                  // tile rows that are walked through together
@@ -764,6 +895,8 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
             }
         }
     };
+    unsigned any = 0u;
+    if constexpr (scales) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // (nothing else is on its way here)
     request_gu(0);
 #pragma unroll 1
     for (int turn = 0; turn < turns; ++turn) {
@@ -797,6 +930,14 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
             if (turn + 1 < turns) request_gu(turn + 1);
         }
         __syncthreads();
+        if constexpr (scales) {
+            if (turn == 0) any = found[0];
+            if constexpr (!makes) {
+                if (any) add_scaled<T, OP, TILE>(q, res, turn, m0, n0, tid, found);
+            }
+        }
+        unsigned again = 0u;                                   // pieces that need exponents, or have an infinity or a NaN
+        static_assert(mine <= 32, "");
         auto work = [&](auto act) {
 #pragma unroll 1
             for (int i = 0; i < mine; ++i) {
@@ -817,7 +958,12 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                         gb[k] = bits_of<T>(g[k]);
                         ub[k] = bits_of<T>(u[k]);
                     }
-                    store8(q.out, r, c, left == 8 ? hb : first_of(hb, left));
+                    if (left < 8) hb = first_of(hb, left);
+                    store8(q.out, r, c, hb);
+                    if constexpr (scales) {
+                        if (any) q.scale[(r * q.out.ld + c) >> 3] = 0;
+                        if (has_no_number(hb)) again |= 1u << i;
+                    }
                     if (q.g.p) {
                         store_some(q.g, r, c, q.N, gb);
                         store_some(q.u, r, c, q.N, ub);
@@ -851,6 +997,13 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                     store8(q.out, r, c, hb);
                     store8(q.out2, r, c, dgb);
                     store8(q.out2, r, c + q.half, dub);
+                    if constexpr (scales) {
+                        if (any) {
+                            unsigned char* const of_d = q.scale2 + ((r * q.out2.ld + c) >> 3);
+                            q.scale[(r * q.out.ld + c) >> 3] = of_d[0] = of_d[q.half >> 3] = 0;
+                        }
+                        if (has_no_number(hb) || has_no_number(dgb) || has_no_number(dub)) again |= 1u << i;
+                    }
                 } else {
                     // (two halves: q.half is a multiple of 64, eight columns never straddle)
                     const bool second = OP == kOpWeight && q.half && c >= q.half;
@@ -867,6 +1020,33 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         };
         if constexpr (OP == kOpUp || OP == kOpDown) with_act(q.act, work);
         else work(std::integral_constant<int, 0>());
+        if constexpr (scales && makes) {
+            while (again) {
+                const int i = __builtin_ctz(again);
+                again &= again - 1u;
+                int64_t r, c;
+                const float* const at = place(turn, i, r, c);
+                const int left = (int)min(q.N - c, (int64_t)8);
+#pragma unroll 1
+                for (int which = 0; which < (OP == kOpUp ? 1 : 3); ++which) {
+                    asm volatile("" : "+s"(which));            // (one piece of code for all three)
+                    store_scaled<T>(q, which ? q.out2 : q.out, r, which == 2 ? c + q.half : c, which ? q.scale2 : q.scale, [&](int k) {
+                        float v = 0.f;
+                        if (k < left)
+                            with_act(q.act, [&](auto act) {
+                                if constexpr (OP == kOpUp) v = act_value<act.value>(at[k]) * at[BN / 2 + k];
+                                else {
+                                    const float u = value_of<T>(reinterpret_cast<const short*>(gus + (2 * i + 1) * threads)[k]);
+                                    float slope;
+                                    const float a = act_both<act.value>(value_of<T>(reinterpret_cast<const short*>(gus + 2 * i * threads)[k]), slope);
+                                    v = which == 0 ? a * u : which == 1 ? at[k] * u * slope : at[k] * a;
+                                }
+                            });
+                        return v;
+                    });
+                }
+            }
+        }
     }
 }
 
