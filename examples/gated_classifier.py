@@ -72,6 +72,7 @@ def train(rows=65_536, p=128, hidden=512, classes=10, buffers=4, batch=1_024, pa
     """Returns (losses of the gated block after every iteration over the buffers, loss of softmax regression after the last one)."""
     host_x, host_y = draw_data(rows, p, classes, seed)
     per = -(-rows // buffers)
+    buffers = -(-rows // per)                               # as many as have rows
     slots = [(torch.empty(per, p, dtype=torch.bfloat16, device="cuda"), torch.empty(per, dtype=torch.int32, device="cuda")) for _ in range(2)]
     copy, compute = torch.cuda.Stream(), torch.cuda.Stream()
     loaded = [torch.cuda.Event() for _ in slots]
