@@ -11,8 +11,12 @@ import struct
 import numpy as np
 import torch
 
-from . import _tensors
 from . import binding as B
+
+try:
+    from . import _tensors
+except ImportError as e:
+    raise ImportError(f"_tensors.so, next to {B.LIB_PATH}, is missing or was built for another torch ({e}): build it first (__graft_entry__.build())") from e
 
 _TYPES = {B.BMGD_BF16: torch.bfloat16, B.BMGD_F16: torch.float16, B.BMGD_F32: torch.float32}
 _CODES = {v: k for k, v in _TYPES.items()}

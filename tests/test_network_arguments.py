@@ -107,3 +107,19 @@ def test_tensors_are_told_that_they_are_written():
             call()
     with pytest.raises(ValueError):
         T.matrices((x,), ((3, 4),), torch.float32, -1, -1)
+
+
+def test_a_missing_module_says_what_to_build(tmp_path):
+    """As the library itself: without _tensors.so the import names it and the way to it."""
+    import os
+    import subprocess
+    import sys
+    here = os.path.dirname(B.__file__)
+    package = tmp_path / "paper_2312_08728_amd"
+    package.mkdir()
+    for name in os.listdir(here):
+        if name.endswith(".py") or name == "libbmgd.so":
+            os.symlink(os.path.join(here, name), package / name)
+    res = subprocess.run([sys.executable, "-c", "import paper_2312_08728_amd"], cwd=tmp_path, env={**os.environ, "PYTHONPATH": str(tmp_path)}, capture_output=True, text=True, timeout=300)
+    last = res.stderr.strip().splitlines()[-1]
+    assert res.returncode == 1 and last.startswith("ImportError") and "_tensors.so" in last and "build" in last, res.stderr
