@@ -435,7 +435,8 @@ void bmgd_destroy(bmgd_ctx* ctx);
  *        BMGD_ACT_GELU  g F(g), F the standard normal distribution function (not its tanh approximation)
  *        BMGD_ACT_RELU  max(g, 0), derivative 0 at 0
  * All matrices are BMGD_BF16 or BMGD_F16; every sum is in fp32 and rounded once.  What lies between two products (H; dG,
- * dU) is rounded to that type, since it is an operand of the matrix instructions.  With BMGD_F16 its range is that of fp32 all the
+ * dU) is rounded to that type, since it is an operand of the matrix instructions (in calls of up to eight rows what the rounding
+ * leaves is kept too).  With BMGD_F16 its range is that of fp32 all the
  * same: eight neighbouring elements of a row (the first eight, the next, ...) whose largest is beyond 65,504 are held as multiples of a
  * power of two.  The matrices of a call, G and U among them, are f16: a G, a U or a result beyond that is infinite. */
 enum { BMGD_ACT_SILU = 0, BMGD_ACT_GELU = 1, BMGD_ACT_RELU = 2 };

@@ -43,8 +43,9 @@ Layout make_layout(const bmgd_gated_config& c)
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t r = at; at += (bytes + 255) / 256 * 256; return r; };
     const size_t r = (size_t)c.max_rows, f64 = (size_t)up(c.hidden, 64), f8 = (size_t)up(c.hidden, 8), p8 = (size_t)up(c.p, 8), c8 = (size_t)up(c.out_n, 8);
-    l.h = take(2 * r * f64);
-    l.d = take(4 * r * f64);
+    const size_t rows_between = std::max(r, 2 * std::min(r, (size_t)kGatedPairRows));
+    l.h = take(2 * rows_between * f64);
+    l.d = take(4 * rows_between * f64);
     l.x = take(2 * r * p8);
     l.gate = take(2 * (size_t)c.p * f8);
     l.up = take(2 * (size_t)c.p * f8);
@@ -55,8 +56,8 @@ Layout make_layout(const bmgd_gated_config& c)
     l.zeros = take(256);
     if (c.dtype == BMGD_F16) {
         l.scaled = take(256);
-        l.scale_h = take(r * f64 / 8);
-        l.scale_d = take(2 * r * f64 / 8);
+        l.scale_h = take(rows_between * f64 / 8);
+        l.scale_d = take(2 * rows_between * f64 / 8);
     }
     l.total = at;
     return l;
@@ -154,7 +155,7 @@ void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_
         double bytes = 0.0;
         for (int i = 0; i < count; ++i) {
             const GatedProduct& q = *qs[i];
-            fits = fits && !(t >= kTile32 && (count > 1 || ops[i] > kOpDown || q.M > k.bm));
+            fits = fits && !(t >= kTile32 && (count > 1 || ops[i] > kOpDown || q.M > k.bm)) && !(q.pair && (ops[i] == kOpUp || ops[i] == kOpDown) && k.bm > 64);
             most_steps = std::max(most_steps, steps_of(q, ops[i]));
             const double M = (double)q.M, N = (double)columns_of(q, ops[i]), K = (double)steps_of(q, ops[i]) * kGatedStep;
             bytes += 2.0 * (M * K + K * N + M * N);
@@ -440,10 +441,12 @@ int forward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream_
     GATED_DO(enter(b, s));
     const int64_t half = up(c.hidden, 64);
     GatedProduct q{}, y{};
+    q.pair = y.pair = rows <= kGatedPairRows;
+    const int64_t between = q.pair ? 2 * rows : rows;          // rows of H
     q.M = rows; q.N = c.hidden; q.K = c.p;
     q.half = half;
     plan(b, q, kOpUp, rows);
-    y.M = rows; y.N = c.out_n; y.K = c.hidden;
+    y.M = between; y.N = c.out_n; y.K = c.hidden;
     plan(b, y, kOpMul, rows);
 
     Operands o{b};
@@ -484,6 +487,8 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
     const int64_t half = up(c.hidden, 64);
     const GatedMat h{b->base + b->lay.h, half}, d{b->base + b->lay.d, 2 * half};
     GatedProduct q{}, input{}, ddown{}, dgate{};
+    q.pair = input.pair = ddown.twice_b = dgate.twice_a = rows <= kGatedPairRows;
+    const int64_t between = q.pair ? 2 * rows : rows;          // rows of H and D
     GatedProduct* list3[3];
     GatedOp ops[3];
     int n = 0;
@@ -493,18 +498,18 @@ int backward(bmgd_gated* b, int64_t rows, const bmgd_gated_tensors& t, hipStream
         plan(b, q, kOpDown, rows);
     }
     if (rows && t.dx.data) {
-        input.M = rows; input.N = c.p; input.K = c.hidden;
+        input.M = between; input.N = c.p; input.K = c.hidden;
         input.half = half;
         list3[n] = &input;
         ops[n++] = kOpInput;
     }
     if (t.ddown.data) {
-        ddown.M = c.hidden; ddown.N = c.out_n; ddown.K = rows;
+        ddown.M = c.hidden; ddown.N = c.out_n; ddown.K = between;
         list3[n] = &ddown;
         ops[n++] = kOpWeight;
     }
     if (t.dgate.data) {
-        dgate.M = c.p; dgate.N = c.hidden; dgate.K = rows;
+        dgate.M = c.p; dgate.N = c.hidden; dgate.K = between;
         dgate.half = half;
         list3[n] = &dgate;
         ops[n++] = kOpWeight;

@@ -43,6 +43,9 @@ struct GatedProduct : GatedCut {
                         // kOpInput: the columns of each half of the left operand; kOpWeight: 0, or the columns of each half of the right operand
     GatedMat out, out2; // result; kOpUp, kOpDown: H in `out`, kOpDown: D = [dG | dU] in `out2`
     GatedMat g, u;      // kOpUp: written unless NULL; kOpDown: read
+    // Calls of few rows (kGatedPairRows): H and D have two rows for one, 2 r what row r is rounded to and 2 r + 1 the rest.  kOpUp, kOpDown write both; kOpMul, kOpInput have M of
+    // them and add pairs of results; kOpWeight has K of them, and its other operand (twice_a, twice_b: the left, the right one) each row twice.
+    int pair, twice_a, twice_b;
     int act;
     float* partial;     // sums of workgroups that share a tile
     unsigned* counter;  // and how many of them have arrived, per tile; zero between launches
@@ -61,6 +64,12 @@ enum { kTileLarge = 0, kTileMedium = 1, kTileDeep = 2, kTileSmall = 3, kTile32 =
 constexpr size_t kGatedPartialBytes = size_t(64) << 20;
 constexpr int kGatedCounters = 4096;
 constexpr int kGatedStep = 64;         // elements of the summed index per step
+// Up to so many rows H and D have the rest of their roundings too: two rows each of a tile of 16, or of a step.  There a rounding is shared by all that a row's sums make, and few
+// of them make an error: beside a result's own rounding it is 1.3 to 1.8 times as large as with many rows (of 36 draws with one row 14 to 39 % are off by more than 1.5 times their own,
+// with eight rows up to 11 %, with 16 up to 3 %, with 64 none).  It takes 1 to 4 % longer (one row, p = 512, hidden 2,048, out 1,000: forward 12.9 us for
+// 12.7, backward 17.4 for 16.9; p = out = 4,096, hidden 8,192: 48.6 for 48.2 and 120.2 for 117.5); 9 to 16 rows, whose pairs need the tile of 32, would take up to 32 % (p = 64,
+// hidden 8,192, out 64, forward: 16.5 for 12.5).
+constexpr int kGatedPairRows = 8;
 
 // Chooses tile and split for the `count` products of one launch, which get one kind of tile.
 // tile >= 0: this one and `want` shares of a tile's sum where they fit (tests).

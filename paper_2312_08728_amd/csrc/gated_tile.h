@@ -124,6 +124,37 @@ template <typename T> __device__ __forceinline__ short bits_of(float x)
 }
 template <typename T> __device__ __forceinline__ float value_of(short b) { return (float)__builtin_bit_cast(T, b); }
 
+// Rounded elements as they are, whatever is done with them next: a product and its rounding can be one instruction with one rounding, and for another use of the same element
+// two with two, which at ties differ by a last place.
+__device__ __forceinline__ short8v settled(short8v v)
+{
+    uint4v w = __builtin_bit_cast(uint4v, v);
+    asm("" : "+v"(w));
+    return __builtin_bit_cast(short8v, w);
+}
+__device__ __forceinline__ bool is_number(float x) { return fabsf(x) < __builtin_inff(); }
+// What is left of x beside the value it was rounded to; nothing where that is no number.
+template <typename T> __device__ __forceinline__ short rest_of(float x, short b)
+{
+    const float v = value_of<T>(b);
+    return bits_of<T>(is_number(v) ? x - v : 0.f);
+}
+// Result (m, n) of kOpWeight in a call of few rows, from what its operands were rounded to: where an infinity is among the products, which a rest may turn into a NaN.
+template <typename T> __device__ __forceinline__ float without_rest(const GatedProduct& q, int64_t m, int64_t n)
+{
+    float sum = 0.f;
+#pragma unroll 1
+    for (int64_t k = 0; k < q.K; k += 2) {
+        const int64_t at_a = (k >> q.twice_a) * q.a.ld + m, at_b = (k >> q.twice_b) * q.b.ld + n;
+        float a = 0.f, b = 0.f;
+        if (m < q.M) a = value_of<T>(((const short*)q.a.p)[at_a]);
+        if (n < (q.half ? 2 * q.half : q.N)) b = value_of<T>(((const short*)q.b.p)[at_b]);
+        const float ab = a * b;
+        sum += std::is_same<T, _Float16>::value ? ldexpf(ab, q.scale[(q.twice_b ? at_a : at_b) >> 3]) : ab;
+    }
+    return sum;
+}
+
 // Eight neighbouring elements at any even address: one instruction all the same.
 typedef short short8u __attribute__((ext_vector_type(8), aligned(2)));
 __device__ __forceinline__ short* element(const GatedMat& m, int64_t r, int64_t c) { return (short*)m.p + r * m.ld + c; }
@@ -181,8 +212,9 @@ template <bool ADJ, int R, int THREADS> struct Mover {
     }
     // Adjacent: element (row, k) at base + row * ld + k; pick(row of the tile) is where its row begins.
     // Strided: element (k, column) at base + k * ld + column; pick(piece of a row of the tile) is where its eight columns begin.
+    // (twice: 1 where the operand has each row twice, which is so in sums of one step only)
     template <typename Pick>
-    __device__ __forceinline__ void start(int64_t ld, int64_t k0, int tid, Pick pick)
+    __device__ __forceinline__ void start(int64_t ld, int64_t k0, int tid, Pick pick, int twice = 0)
     {
         if constexpr (ADJ) {
             const int s = tid & 7;
@@ -195,7 +227,7 @@ template <bool ADJ, int R, int THREADS> struct Mover {
             for (int i = 0; i < kPieces; ++i) {
                 const int k = i * (THREADS / kRow) + tid / kRow;
                 const int c = (tid % kRow) ^ turn(k);
-                src[i] = pick(c) + (k0 + k) * ld;
+                src[i] = pick(c) + ((k0 + k) >> twice) * ld;
             }
         }
     }
@@ -228,7 +260,7 @@ template <bool ADJ, int R, int THREADS> struct Loose {
     // Adjacent: pick(row of the tile) is where its row begins.  Strided: pick(piece of a row of the tile, its first column) is where column 0 of its matrix begins; the
     // matrix has `cols` columns.
     template <typename Pick>
-    __device__ __forceinline__ void start(int64_t ld, int64_t k0, int64_t cols, int tid, Pick pick)
+    __device__ __forceinline__ void start(int64_t ld, int64_t k0, int64_t cols, int tid, Pick pick, int twice = 0)
     {
         if constexpr (ADJ) {
             const int s = tid & 7;
@@ -242,7 +274,7 @@ template <bool ADJ, int R, int THREADS> struct Loose {
                 const int k = i * (THREADS / kRow) + tid / kRow;
                 int64_t col;
                 const unsigned short* const base = pick((tid % kRow) ^ Whole::turn(k), col);
-                src[i] = base + min(col, cols - 8) + (k0 + k) * ld;
+                src[i] = base + min(col, cols - 8) + ((k0 + k) >> twice) * ld;
                 shift[i] = col < cols ? (int)max(col + 8 - cols, (int64_t)0) : 0;         // (results of columns that are not there go nowhere)
             }
         }
@@ -380,8 +412,8 @@ __device__ __forceinline__ bool has_no_number(short8v v)       // of f16: infini
     const uint4v w = (__builtin_bit_cast(uint4v, v) & 0x7c007c00u) + 0x04000400u;
     return ((w[0] | w[1] | w[2] | w[3]) & 0x80008000u) != 0u;
 }
-// value(k): element k of the eight
-template <typename T, typename F> __device__ __forceinline__ void store_scaled(const GatedProduct& q, const GatedMat& to, int64_t r, int64_t c, unsigned char* scale, F value)
+// value(k): element k of the eight.  pair: rows 2 r and 2 r + 1 are theirs (see GatedProduct).
+template <typename T, typename F> __device__ __forceinline__ void store_scaled(const GatedProduct& q, bool pair, const GatedMat& to, int64_t r, int64_t c, unsigned char* scale, F value)
 {
     float top = 0.f;
 #pragma unroll 1
@@ -389,15 +421,23 @@ template <typename T, typename F> __device__ __forceinline__ void store_scaled(c
         const float size = fabsf(value(k));
         if (size < __builtin_inff()) top = fmaxf(top, size);
     }
+    const int64_t row = pair ? 2 * r : r;
     int e = 0;
     if (top >= kLargestHalf) {
         e = (int)(__float_as_uint(top) >> 23) - 127 - 14;
         q.scaled[0] = 1u;
         q.scaled[1 + q.turn] = 1u;
 #pragma unroll 1
-        for (int k = 0; k < 8; ++k) *element(to, r, c + k) = bits_of<T>(ldexpf(value(k), -e));
+        for (int k = 0; k < 8; ++k) {
+            const float v = ldexpf(value(k), -e);
+            unsigned b = (unsigned short)bits_of<T>(v);
+            asm("" : "+v"(b));
+            *element(to, row, c + k) = (short)b;
+            if (pair) *element(to, row + 1, c + k) = rest_of<T>(v, (short)b);
+        }
     }
-    scale[(r * to.ld + c) >> 3] = (unsigned char)e;            // (0: the eight stand there as they were rounded)
+    scale[(row * to.ld + c) >> 3] = (unsigned char)e;          // (0: the eight stand there as they were rounded)
+    if (pair) scale[((row + 1) * to.ld + c) >> 3] = (unsigned char)e;
 }
 
 // And their part in the next product: its sum took such elements for what they are held as, so (2^e - 1) times their products are added to the results of this turn, in
@@ -460,8 +500,8 @@ __device__ __forceinline__ void add_scaled(const GatedProduct& q, float* res, in
                         const bool second = OP == kOpInput && k >= q.half;
                         const int64_t kb = k + t - (second ? q.half : 0);
                         const bool in_a = r < q.M && (OP != kOpWeight || k + t < q.K), in_b = c < cols && kb < q.K;
-                        a[t] = in_a ? finite_or_zero(OP == kOpWeight ? pa[(k + t) * q.a.ld + r] : pa[r * q.a.ld + k + t]) : (short)0;
-                        b[t] = in_b ? finite_or_zero(OP == kOpInput ? (second ? pb2 : pb)[c * q.b.ld + kb] : pb[kb * q.b.ld + c]) : (short)0;
+                        a[t] = in_a ? finite_or_zero(OP == kOpWeight ? pa[((k + t) >> q.twice_a) * q.a.ld + r] : pa[r * q.a.ld + k + t]) : (short)0;
+                        b[t] = in_b ? finite_or_zero(OP == kOpInput ? (second ? pb2 : pb)[c * q.b.ld + kb] : pb[(OP == kOpWeight ? kb >> q.twice_b : kb) * q.b.ld + c]) : (short)0;
                         const int64_t at = OP != kOpWeight ? r * ld + k + t : (k + t) * ld + (left ? r : c);
                         e[t] = (left ? in_a : in_b) ? (int)q.scale[at >> 3] : 0;
                         most = max(most, e[t]);
@@ -539,7 +579,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         if constexpr (a_adj) { const int64_t r = m0 + at; return pa + (r < q.M ? r : q.M - 1) * q.a.ld; }
         else { const int64_t c = m0 + at; return pa + (c < q.a_cols ? c : q.a_cols - 8); }
     };
-    const int half_steps = OP == kOpInput ? (int)(q.half / kStep) : 0;
+    const int half_steps = OP == kOpInput ? (int)(q.half / kStep) : 0, twice_a = OP == kOpWeight ? q.twice_a : 0;
     Mover<b_adj, BN, threads> mb;
     auto start_b = [&](int step) {
         const bool second = OP == kOpInput && step >= half_steps;
@@ -550,7 +590,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                 const int64_t col = n0 + w * (wn / 2) + (in % (wn / 16)) * 8;
                 return (in >= wn / 16 ? pb2 : pb) + (col < q.b_cols ? col : q.b_cols - 8);
             } else { const int64_t col = n0 + 8 * c; return pb + (col < q.b_cols ? col : q.b_cols - 8); }
-        });
+        }, OP == kOpWeight ? q.twice_b : 0);
     };
     if constexpr (!LOOSE) start_b(s0);
     const unsigned lds_a = lds0 + (unsigned)__builtin_amdgcn_readfirstlane(wave * 1024), lds_b = lds_a + stages * a_bytes;
@@ -588,7 +628,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         Sub sub[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x)
-            sub[x].start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { const int at = a_adj ? r : 8 * r; return left_at(at + (at & 64) + 64 * x); });
+            sub[x].start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { const int at = a_adj ? r : 8 * r; return left_at(at + (at & 64) + 64 * x); }, twice_a);
         Reader<a_adj, 128> ra;
         ra.start((wave / S::WN) * 64, lane);
         auto request_sub = [&](int step, int x) { sub[x].request(lds_a + ((step - s0) & 1) * a_bytes + x * sub_bytes, q.a.ld, left_a(step), zeros); };
@@ -656,7 +696,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         // Against the medium kind at up to 256 tiles up to 30 % less time, 8 % in the middle (500 rows, p = 2,048, hidden 4,096, kOpUp: 27.7 us for 35.3),
         // beyond 10 to 50 % more.
         Mover<a_adj, BM, threads> ma;
-        ma.start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { return left_at(a_adj ? r : 8 * r); });
+        ma.start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { return left_at(a_adj ? r : 8 * r); }, twice_a);
         Reader<a_adj, BM> ra;
         ra.start(wrow, lane);
         auto request = [&](int step, int buf) {
@@ -714,7 +754,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         Reader<a_adj, BM> ra;
         ra.start(wrow, lane);
         if constexpr (a_adj) la.start(q.a.ld, (int64_t)s0 * kStep, 0, tid, left_at);
-        else la.start(q.a.ld, (int64_t)s0 * kStep, q.a_cols, tid, [&](int c, int64_t& col) { col = m0 + 8 * c; return pa; });
+        else la.start(q.a.ld, (int64_t)s0 * kStep, q.a_cols, tid, [&](int c, int64_t& col) { col = m0 + 8 * c; return pa; }, twice_a);
         auto second_half = [&](int step) { return OP == kOpInput && step >= half_steps; };
         auto begin_b = [&](int step) {
             const bool second = second_half(step);
@@ -729,7 +769,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                     col = n0 + 8 * c;
                     return pb;
                 }
-            });
+            }, OP == kOpWeight ? q.twice_b : 0);
         };
         begin_b(s0);
         auto left_b = [&](int step) { return q.K - (int64_t)(second_half(step) ? step - half_steps : step) * kStep; };
@@ -770,7 +810,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         }
     } else {
         Mover<a_adj, BM, threads> ma;
-        ma.start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { return left_at(a_adj ? r : 8 * r); });
+        ma.start(q.a.ld, (int64_t)s0 * kStep, tid, [&](int r) { return left_at(a_adj ? r : 8 * r); }, twice_a);
         Reader<a_adj, BM> ra;
         ra.start(wrow, lane);
         auto request = [&](int step, int buf) {
@@ -878,6 +918,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         *reinterpret_cast<float4v*>(v) = *reinterpret_cast<const float4v*>(from);
         *reinterpret_cast<float4v*>(v + 4) = *reinterpret_cast<const float4v*>(from + 4);
     };
+    constexpr bool pairs = BM <= 64;                           // (few rows do not come in larger tiles)
     constexpr int keep = OP == kOpDown ? mine : 1;
     short8v gk[keep], uk[keep];                                // G and U of the next turn, on their way
     short8v* const gus = reinterpret_cast<short8v*>(res + (BM / turns) * pitch) + tid;            // of this turn, a thread's own
@@ -959,9 +1000,21 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                         ub[k] = bits_of<T>(u[k]);
                     }
                     if (left < 8) hb = first_of(hb, left);
-                    store8(q.out, r, c, hb);
+                    const bool pair = pairs && q.pair;
+                    const int64_t row = pair ? 2 * r : r;
+                    if (pairs) hb = settled(hb);
+                    store8(q.out, row, c, hb);
+                    if (pair) {
+                        short8v rest;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) rest[k] = rest_of<T>(act_value<act.value>(g[k]) * u[k], hb[k]);
+                        store8(q.out, row + 1, c, left == 8 ? rest : first_of(rest, left));
+                    }
                     if constexpr (scales) {
-                        if (any) q.scale[(r * q.out.ld + c) >> 3] = 0;
+                        if (any) {
+                            q.scale[(row * q.out.ld + c) >> 3] = 0;
+                            if (pair) q.scale[((row + 1) * q.out.ld + c) >> 3] = 0;
+                        }
                         if (has_no_number(hb)) again |= 1u << i;
                     }
                     if (q.g.p) {
@@ -994,27 +1047,66 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
                         dub[k] = bits_of<T>(dh[k] * a);
                         dgb[k] = bits_of<T>(dh[k] * u * slope);
                     }
-                    store8(q.out, r, c, hb);
-                    store8(q.out2, r, c, dgb);
-                    store8(q.out2, r, c + q.half, dub);
-                    if constexpr (scales) {
-                        if (any) {
-                            unsigned char* const of_d = q.scale2 + ((r * q.out2.ld + c) >> 3);
-                            q.scale[(r * q.out.ld + c) >> 3] = of_d[0] = of_d[q.half >> 3] = 0;
+                    const bool pair = pairs && q.pair, numberless = scales && (has_no_number(hb) || has_no_number(dgb) || has_no_number(dub));
+                    const int64_t row = pair ? 2 * r : r;
+                    if (pairs) {
+                        hb = settled(hb);
+                        dgb = settled(dgb);
+                        dub = settled(dub);
+                    }
+                    store8(q.out, row, c, hb);
+                    store8(q.out2, row, c, dgb);
+                    store8(q.out2, row, c + q.half, dub);
+                    if (pair) {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            float slope;
+                            const float u = value_of<T>(ub[k]), a = act_both<act.value>(value_of<T>(gb[k]), slope);
+                            hb[k] = rest_of<T>(a * u, hb[k]);
+                            dub[k] = rest_of<T>(dh[k] * a, dub[k]);
+                            dgb[k] = rest_of<T>(dh[k] * u * slope, dgb[k]);
                         }
-                        if (has_no_number(hb) || has_no_number(dgb) || has_no_number(dub)) again |= 1u << i;
+                        store8(q.out, row + 1, c, hb);
+                        store8(q.out2, row + 1, c, dgb);
+                        store8(q.out2, row + 1, c + q.half, dub);
+                    }
+                    if constexpr (scales) {
+                        if (any)
+                            for (int64_t at = row; at <= row + pair; ++at) {
+                                unsigned char* const of_d = q.scale2 + ((at * q.out2.ld + c) >> 3);
+                                q.scale[(at * q.out.ld + c) >> 3] = of_d[0] = of_d[q.half >> 3] = 0;
+                            }
+                        if (numberless) again |= 1u << i;
                     }
                 } else {
                     // (two halves: q.half is a multiple of 64, eight columns never straddle)
                     const bool second = OP == kOpWeight && q.half && c >= q.half;
                     const GatedMat& to = second ? q.out2 : q.out;
                     const int64_t cc = second ? c - q.half : c;
+                    const bool pair = OP != kOpWeight && q.pair;
+                    if (pair && (r & 1)) continue;             // (with the row before it)
                     float v[8];
                     floats8(at, v);
+                    if (pair) {
+                        float rest[8];
+                        floats8(at + pitch, rest);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) v[k] += is_number(v[k]) ? rest[k] : 0.f;        // (an infinite weight times a rest may have any sign)
+                    }
                     short8v b;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) b[k] = bits_of<T>(v[k]);
-                    store_some(to, r, cc, q.N, b);
+                    store_some(to, pair ? r >> 1 : r, cc, q.N, b);
+                    if (OP == kOpWeight && (q.twice_a | q.twice_b)) {
+                        float most = 0.f;                      // (NaN where one of the eight is no number)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) most = __builtin_fmaf(v[k], 0.f, most);
+                        if (!(most == 0.f)) {
+#pragma unroll 1
+                            for (int k = 0; k < 8; ++k)
+                                if (cc + k < q.N && !is_number(at[k])) *element(to, r, cc + k) = bits_of<T>(without_rest<T>(q, r, c + k));
+                        }
+                    }
                 }
             }
         };
@@ -1030,7 +1122,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
 #pragma unroll 1
                 for (int which = 0; which < (OP == kOpUp ? 1 : 3); ++which) {
                     asm volatile("" : "+s"(which));            // (one piece of code for all three)
-                    store_scaled<T>(q, which ? q.out2 : q.out, r, which == 2 ? c + q.half : c, which ? q.scale2 : q.scale, [&](int k) {
+                    store_scaled<T>(q, pairs && q.pair, which ? q.out2 : q.out, r, which == 2 ? c + q.half : c, which ? q.scale2 : q.scale, [&](int k) {
                         float v = 0.f;
                         if (k < left)
                             with_act(q.act, [&](auto act) {
