@@ -481,7 +481,8 @@ typedef struct bmgd_gated_tensors {
     bmgd_matrix ddown;
 } bmgd_gated_tensors;
 
-/* Device bytes that a block of this configuration needs; 0 if it is invalid.  Needs no GPU. */
+/* Device bytes that a block of this configuration needs; 0 if it is invalid.  Needs no GPU.  Places for copies of x, gate, up, down and dy are among
+ * them, and for dG and dU, whether the calls to come need these or not. */
 size_t bmgd_gated_workspace_bytes(const bmgd_gated_config* cfg);
 
 /* *out receives the block (its workspace; it holds no weights).  For the HIP device that is current.  Blocks.  Errors:
@@ -549,7 +550,8 @@ void bmgd_adamw_default_config(bmgd_adamw_config* cfg);
 
 /* Update number `step` (>= 1) of all `count` tensors, in one launch for 108 tensors or fewer (more where their
  * addresses are 2^32 elements apart), on `stream`, which must belong to the current device.  `tensors` is host memory, read before the call returns.  Everything is checked before the first launch.
- * Asynchronous, allocates nothing, keeps nothing.  Message of a failure: bmgd_last_error(NULL). */
+ * Asynchronous, allocates nothing, keeps nothing.  A step that is captured into a graph holds its number and rates: every launch of the graph makes that
+ * update, with that bias correction.  Message of a failure: bmgd_last_error(NULL). */
 int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tensor* tensors, int64_t count, int64_t step, void* stream);
 
 /* The fp32 values that moments in 8 bits stand for: m_out[i], s_out[i] (host arrays of device addresses) receive n values each

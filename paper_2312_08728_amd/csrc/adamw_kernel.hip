@@ -14,7 +14,7 @@
 // gets that as its scale and codes of zero, that is, stands for NaN in all its elements from then on: nothing hides it.
 // A wavefront holds a block, four elements a lane; the largest is found with lane exchanges.
 //
-// Measured: 20 M elements in 160 tensors, bf16 gradients and copies, moments in 32 bits: 114 us in two launches, 4.9 TB/s; 100.7 M elements in 8 bits 283 us, 5.7
+// Measured: 20 M elements in 160 tensors, bf16 gradients and copies, moments in 32 bits: 114 us in two launches, 4.9 TB/s; 100.7 M elements in 8 bits 289 us, 5.6
 // TB/s (a copy of 1 GiB reaches 5.1, reads and writes together).  In 8 bits the instructions count as well: with exact roots and quotients throughout, 150 vector
 // instructions an element, it took 387 us.  A workgroup takes 1,024 elements; with 4,096, loads of all four thousands first, it took 2 to 6 % longer.
 #include "../../include/bmgd.h"

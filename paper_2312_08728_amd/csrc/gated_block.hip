@@ -135,7 +135,8 @@ hipError_t gated_launch_pack(const GatedPack& q, hipStream_t stream)
 // with the steps of a workgroup, the rounds that the units need for all workgroups, a rate that takes enough bytes on their way (2.2 us from request to
 // arrival), and where workgroups share tiles
 //      join = join + each splits + megabytes of parts per unit write.
-// Nothing but sizes counts, not what is at hand or wanted besides: Y has the same bits whether G and U are kept or not.
+// It does not know where rows begin: kOpDown, which reads G and U on its way out, takes half as long again where theirs begin at odd places (1,000 rows, p = 512, hidden 2,731,
+// out 1,000: 23 us, by the formula 15).  Nothing but sizes counts, not what is at hand or wanted besides: Y has the same bits whether G and U are kept or not.
 void gated_plan(GatedProduct* const* qs, const GatedOp* ops, int count, int num_cus, int asked_tile, int64_t asked)
 {
     struct Cost { int bm, bn, per_cu, ahead; double lat, thr, once[3], leave[3], join, each, write; };       // [kOpUp, kOpDown, the others]

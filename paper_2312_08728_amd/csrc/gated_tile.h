@@ -13,11 +13,11 @@
 // arrive adds the parts in the order of their index (the result does not depend on who was last) and goes on.
 //
 // What bounds it (bf16, microseconds of the kernels alone).
-//   8,192 rows, p = out = 4,096, hidden 8,192: kOpUp 970, kOpMul 440, kOpDown 540, the gradients 2,160: 1.13, 1.25, 1.02 and 1.27 PFLOP/s, where a library's plain
-//   products of these sizes reach 1.05 to 1.35.  Matrix units busy two thirds of the time at 1.85 GHz (2.1 without load): they and the
+//   8,192 rows, p = out = 4,096, hidden 8,192: kOpUp 945, kOpMul 443, kOpDown 521, the gradients 2,116: 1.16, 1.24, 1.05 and 1.30 PFLOP/s, where a library's plain
+//   products of these sizes reach 1.05 to 1.35.  Matrix units busy half to two thirds of the time (57, 61, 49 and 62 %) at 1.85 GHz (2.1 without load): they and the
 //   way from L2 through shared memory to registers, 256 KB of reads and writes a step, share what shared memory delivers.
-//   One row of the same block: kOpUp 33.4 (134 MB at 4.0 TB/s), kOpMul 16.0: memory, and 2.8 us of an empty launch.
-//   100 rows, p = 200, hidden 600, out 130: kOpDown 6.0, the gradients 9.5: an empty launch, one trip to memory that nothing precedes (2 us) and the
+//   One row of the same block: kOpUp 33.2 (134 MB at 4.0 TB/s), kOpMul 16.0: memory, and 2.8 us of an empty launch.
+//   100 rows, p = 200, hidden 600, out 130: kOpDown 5.6, the gradients 9.7: an empty launch, one trip to memory that nothing precedes (2 us) and the
 //   trips of shared sums (0.8 us each); both loose, which adds 0.5 and 1.0 and saves copies of 3.3.
 #pragma once
 
@@ -64,7 +64,7 @@ __device__ __forceinline__ float logistic(float g)
     return (g < 0.f ? e : 1.f) * __builtin_amdgcn_rcpf(1.f + e);
 }
 // The normal distribution's F(g), and e^(-g^2 / 2) in `bell`.  1 - F(|g|) = e^(-g^2 / 2) P(1 / (1 + 0.35 |g|)): P is the polynomial of degree 7 that is nearest to
-// erfcx(|g| / sqrt 2) / 2 in relative error for |g| up to 13.5 (3.1e-7, fitted here); with the rounding of the exponent 1.5e-6 for |g| < 5.
+// erfcx(|g| / sqrt 2) / 2 in relative error for |g| up to 13.5 (fitted here; with these coefficients 3.6e-7); with the rounding of the exponent 1.5e-6 for |g| < 5.
 __device__ __forceinline__ float normal_cdf(float g, float& bell)
 {
     bell = __builtin_amdgcn_exp2f(g * g * -0.72134752044448170f);
@@ -333,7 +333,7 @@ template <bool ADJ, int R> struct Reader {
 };
 
 // Tile, wavefronts along its rows and columns, steps in shared memory (all but one of them on their way).  A unit holds one workgroup of the large kind, two of the
-// medium, three of the small, two of those for few rows.  Measured beside these: small tiles with four steps (two workgroups to a unit, 3 to 25 %
+// medium, three of the small, two of those for 16 rows, one of those for 32, whose steps take a little more than half of its shared memory.  Measured beside these: small tiles with four steps (two workgroups to a unit, 3 to 25 %
 // slower), medium ones on four wavefronts (5 to 10 % slower) or with four steps (faster by as much on fewer tiles than units, slower by 20 % on more), tiles
 // for few rows with five to eight steps (the same), 256 x 128 with three steps (of 90 products from 500 to 8,192 rows 4 to 10 % faster in three, the same in six, slower in the others).
 template <int TILE> struct Shape;

@@ -263,7 +263,8 @@ class AdamW:
             raise B.BmgdError(rc, B.bmgd_last_error(None))
 
     def step(self, lr=None, grad_scale=1.0, stream=None):
-        """One update with the gradients as they stand in stream order, times grad_scale.  Asynchronous."""
+        """One update with the gradients as they stand in stream order, times grad_scale.  Asynchronous.  A step that is captured into a graph keeps its number
+        (`steps` + 1) and rates: each replay makes that update again, with that bias correction, and `steps` does not count replays."""
         self._read_again(self._watched[0])
         if not self._apart:
             self._check_apart()
