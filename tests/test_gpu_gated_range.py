@@ -259,3 +259,45 @@ def test_long_sums(r, p, f, c):
         block.backward(*data, *out[:3])
         w = _check_backward("silu", *data, *out[:3], None)
         assert min(np.abs(w[k]).max() for k in ("dg", "du")) > 65_520
+
+
+@pytest.mark.parametrize("r", [5, 50])
+def test_a_captured_training_step_that_leaves_the_range_at_some_replays(r):
+    """Forward and backward in one graph, G and U from the one to the other; other calls on the block in between."""
+    import torch
+    import paper_2312_08728_amd as B
+    p, f, c = 64, 200, 72
+    rng = np.random.default_rng(r)
+    x, gate, up, down, dy = (_dev(a, torch.float16) for a in (rng.standard_normal((r, p)), rng.standard_normal((p, f)), rng.standard_normal((p, f)), 1e-3 * rng.standard_normal((f, c)),
+                                                              1e-3 * rng.standard_normal((r, c))))
+    y, g, u = (_empty(r, n, torch.float16) for n in (c, f, f))
+    out, s = _results(r, p, f, c), torch.cuda.Stream()
+    sizes = [1.0, 100.0, 1.0, 30.0, 100.0, 100.0, 1.0, 1.0]
+    with B.GatedBlock(p, f, c, r, dtype=B.BMGD_F16) as block:
+        def step(stream=None):
+            block.forward(x, gate, up, down, y, g, u, stream=stream)
+            block.backward(dy, x, gate, up, down, g, u, *out, stream=stream)
+
+        first = x.clone()
+        want = []
+        for size in sizes:
+            x.copy_(first * size)
+            step()
+            torch.cuda.synchronize()
+            want.append([t.clone() for t in (y, g, u, *out)])
+            _check_forward("silu", x, gate, up, down, y)
+        step(s)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            step(s)
+        for i, size in enumerate(sizes):
+            x.copy_(first * size)
+            torch.cuda.synchronize()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip((y, g, u, *out), want[i]))
+            if i % 3 == 0:
+                step()
+                torch.cuda.synchronize()
+                assert all(torch.equal(a, b) for a, b in zip((y, g, u, *out), want[i]))
