@@ -546,16 +546,19 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     // f16: whether bytes of exponents are written in any case (the products that make H and D), whether there are any (those that read them).  The word comes to
-    // shared memory beside the operands: in a register it would be waited for, and with it whatever is on its way.
+    // shared memory behind the first operands: in a register it would be waited for, and with it whatever is on its way; in front of them they would wait for it.
     constexpr bool scales = std::is_same<T, _Float16>::value, makes = OP == kOpUp || OP == kOpDown;
     unsigned* found = nullptr;
     if constexpr (scales) {
         __shared__ unsigned words[16 * kFoundWords];            // (the word fills the first 64)
         static_assert(BM <= 256 && BN <= 256 && 16 * kFoundWords >= 64, "");
         found = words;
-        if (wave == 0) load_word_to_lds((const int*)(q.scaled + (makes ? 0 : 1 + q.turn)), (unsigned)(size_t)(__attribute__((address_space(3))) unsigned*)words);
         if (!makes && blockIdx.x == 0 && tid == 0) q.scaled[2 - q.turn] = 0u;
     }
+    auto ask_word = [&]() {
+        if constexpr (scales)
+            if (wave == 0) load_word_to_lds((const int*)(q.scaled + (makes ? 0 : 1 + q.turn)), (unsigned)(size_t)(__attribute__((address_space(3))) unsigned*)found);
+    };
     const int split = id % q.splits;
     const int tile = id / q.splits;
     constexpr int kGroup = 8;                                  // tile rows that are walked through together
@@ -635,6 +638,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
         // fragment e of a step: rows 16 (e / 2) .. + 15 of the wavefront's, half e % 2 of the sum
         auto read_a = [&](unsigned t, int e) { return ra.read(t + (e >= 8 ? sub_bytes : 0u), (e >> 1) & 3, e & 1); };
         short8v af[4], bf[2][fn];
+        ask_word();
         if (s0 < s1) {
             request_b(s0, 0);
             request_sub(s0, 0);
@@ -711,6 +715,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
 #pragma unroll
         for (int i = 0; i < stages - 1; ++i)
             if (s0 + i < s1) request(s0 + i, i);
+        ask_word();
         if (s0 < s1) {
             if (s0 + stages - 1 <= s1) wait_and_meet<(stages - 2) * loads>();
             else wait_and_meet<0>();
@@ -779,6 +784,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
             la.request(va[u], q.a.ld, left_a(step), zeros);
             lb.request(vb[u], q.b.ld, left_b(step), zeros);
         };
+        ask_word();                                            // (the compiler's waits would take it for one of the others behind these)
 #pragma unroll
         for (int u = 0; u < ahead; ++u)
             if (s0 + u < s1) request(s0 + u, u);
@@ -821,6 +827,7 @@ __device__ __forceinline__ void tile_body(const GatedProduct& q, int id)
 #pragma unroll
         for (int i = 0; i < stages - 1; ++i)
             if (s0 + i < s1) request(s0 + i, i);
+        ask_word();
         int buf = 0;
         for (int s = s0; s < s1; ++s) {
             const int behind = s1 - 1 - s;                         // steps behind this one
