@@ -558,6 +558,108 @@ int bmgd_adamw_step(const bmgd_adamw_config* cfg, const bmgd_adamw_tensor* tenso
  * (theta, grad and copy are not looked at).  For checkpoints and for going on in 32 bits. */
 int bmgd_adamw_moments(const bmgd_adamw_tensor* tensors, int64_t count, float* const* m_out, float* const* s_out, void* stream);
 
+/* ==== Around a predictor: norm, 8-bit product, log probabilities ==================================================
+ * Calls of one function each, which keep nothing: matrices and vectors are device memory (bmgd_matrix as above: rows any distance apart; element-size alignment is enough),
+ * vectors lie next to each other.  All are asynchronous, allocate nothing, may be captured into a graph, and run on `stream`, which must belong to the
+ * current device.  0 rows: nothing happens (where a gradient of weights is wanted, it is zeros).  Everything is checked before the first launch; errors BMGD_EINVAL,
+ * BMGD_ENOMEM (workspace too small) and BMGD_EHIP, message from bmgd_last_error(NULL).  Results overlap neither operands nor each other but where it is said. */
+
+/* ---- Root-mean-square norm ----
+ *      s = x + residual, rounded to the type;     r = 1 / sqrt(mean_j s_j^2 + eps);     y_j = s_j w_j r
+ * and, or instead of y, 8-bit codes with a scale for each row: codes_j = the integer nearest to 127 s_j w_j / max_k |s_k w_k| (half to even), scale =
+ * max_k |s_k w_k| r / 127, so that scale * codes_j is y_j.  A row whose largest |s w| is below 2^-118 is held as zeros; a row that has a NaN or an
+ * infinity among its s w stands for NaN (scale NaN, codes zero).  Sums are in fp32: |s| below 2^63 / sqrt(n). */
+typedef struct bmgd_norm_config {
+    int64_t n;              /* columns, in [1, 2^20] */
+    double  eps;            /* finite, >= 0; in fp32 too */
+    int32_t dtype;          /* of all matrices but codes, and of weight and dweight: BMGD_F32, BMGD_BF16, BMGD_F16 */
+    int32_t reserved;
+} bmgd_norm_config;
+
+typedef struct bmgd_norm_tensors {
+    bmgd_matrix x;          /* rows x n; backward: the s that was normed */
+    bmgd_matrix residual;   /* forward, optional */
+    bmgd_matrix sum;        /* forward, optional: s; may be x or residual itself */
+    bmgd_matrix y;          /* forward, optional (y or codes is wanted); may be x itself where sum is not, or residual itself */
+    bmgd_matrix codes;      /* forward, optional: int8 */
+    bmgd_matrix dy;         /* backward: rows x n */
+    bmgd_matrix dsum;       /* backward, optional: the gradient that reaches s otherwise */
+    bmgd_matrix dx;         /* backward, written: of x and of residual alike; may be dy or dsum itself */
+    const void* weight;     /* w, n of them; NULL: ones */
+    void*       dweight;    /* backward, optional, written */
+    float*      scales;     /* forward, with codes: one for each row */
+    float*      rstd;       /* r, one for each row: forward writes it (optional), backward reads it */
+    void*       workspace;  /* backward with dweight: 256-byte aligned; calls that may run at the same time have one each */
+    size_t      workspace_bytes;
+} bmgd_norm_tensors;
+
+/* What a backward call with dweight needs; 0 if the configuration is invalid.  Needs no GPU. */
+size_t bmgd_norm_workspace_bytes(const bmgd_norm_config* cfg, int64_t rows);
+int bmgd_norm_forward(const bmgd_norm_config* cfg, int64_t rows, const bmgd_norm_tensors* t, void* stream);
+/*      dx_j = r (w_j dy_j - s_j r^2 mean_k(w_k dy_k s_k)) + dsum_j;      dweight_j = sum over the rows of dy_j s_j r */
+int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const bmgd_norm_tensors* t, void* stream);
+/* out = scales[i] * codes[i, j], rounded to dtype: what the codes of rows stand for. */
+int bmgd_product_values(int64_t rows, int64_t n, const bmgd_matrix* codes, const float* scales, const bmgd_matrix* out, int32_t dtype, void* stream);
+
+/* ---- Product in 8-bit integers ----
+ *      y_ij = x_scales[i] w_scales[j] sum_k x_ik w_jk
+ * x: codes of rows; w: codes of a layer, one row for each of its outputs (the transpose of gate, up, down above).  Sums are in 32-bit integers, exact; the sum
+ * times x_scales[i], times w_scales[j], is in fp32 and then rounded to dtype. */
+typedef struct bmgd_product_config {
+    int64_t p;              /* in [1, 131071]: 128^2 p stays below 2^31 */
+    int64_t out_n;          /* in [1, 2^20] */
+    int32_t dtype;          /* of y (and of the weights that are quantised): BMGD_F32, BMGD_BF16, BMGD_F16 */
+    int32_t reserved;
+} bmgd_product_config;
+
+typedef struct bmgd_product_tensors {
+    bmgd_matrix  x;         /* rows x p, int8 */
+    bmgd_matrix  w;         /* out_n x p, int8.  Calls of many rows are fastest where p and both strides are multiples of 16, and both addresses */
+    bmgd_matrix  y;         /* rows x out_n, written */
+    const float* x_scales;  /* rows */
+    const float* w_scales;  /* out_n */
+} bmgd_product_tensors;
+
+/* Fewer than 2^23 tiles of 128 x 128 results. */
+int bmgd_product_forward(const bmgd_product_config* cfg, int64_t rows, const bmgd_product_tensors* t, void* stream);
+/* A layer's weights (p x out_n, of dtype, as the blocks above have them) laid out for the product, once: w_jk = the integer nearest to weights_kj / w_scales[j]
+ * (half to even), w_scales[j] = max_k |weights_kj| / 127.  Outputs whose largest is below 2^-118 are zeros; those with a NaN or an infinity have a scale of NaN and codes of zero. */
+int bmgd_product_quantize(const bmgd_product_config* cfg, const bmgd_matrix* weights, const bmgd_matrix* w, float* w_scales, void* stream);
+
+/* ---- Log probabilities ----
+ * Of a row of logits x:  ln p_j = x_j - ln sum_k e^(x_k);  entropy -sum_k p_k ln p_k (a logit of -infinity: p = 0, adds nothing).
+ * The `top` most probable classes in falling order, of equal logits the lowest class first, with their ln p.
+ * labels: a negative one leaves its row out (logprob 0, dlogprob not looked at); one that is not below `classes` gives NaN in logprob and in the row of dlogits.
+ * A row of logits that are all -infinity has no distribution: ln p = -infinity, entropy 0, gradient 0.  A row with a NaN or +infinity: all NaN, classes in the
+ * order of its logits with NaN first. */
+typedef struct bmgd_logprobs_config {
+    int64_t classes;        /* in [1, 2^24] */
+    int32_t dtype;          /* of logits and dlogits: BMGD_F32, BMGD_BF16, BMGD_F16 */
+    int32_t top;            /* in [0, 64], not above classes */
+} bmgd_logprobs_config;
+
+typedef struct bmgd_logprobs_tensors {
+    bmgd_matrix    logits;      /* rows x classes */
+    bmgd_matrix    dlogits;     /* backward, written; may be logits itself */
+    const int32_t* labels;      /* rows; optional (without: no logprob, no dlogprob) */
+    float*         logprob;     /* forward, written, each optional: rows */
+    float*         entropy;     /* rows */
+    int32_t*       top_classes; /* rows x top, one row behind the other (where top > 0) */
+    float*         top_logprobs;
+    float*         kept;        /* rows x 3: the row's largest logit, the base-2 logarithm of the sum of e^(x - largest), and its entropy; forward writes
+                                   it, backward reads it */
+    const float*   dlogprob;    /* backward, each optional: rows */
+    const float*   dentropy;
+    void*          workspace;   /* forward, where it needs one: 256-byte aligned; calls that may run at the same time have one each */
+    size_t         workspace_bytes;
+} bmgd_logprobs_tensors;
+
+/* What a forward call needs, 0 for most (or if the configuration is invalid).  Needs no GPU. */
+size_t bmgd_logprobs_workspace_bytes(const bmgd_logprobs_config* cfg, int64_t rows);
+int bmgd_logprobs_forward(const bmgd_logprobs_config* cfg, int64_t rows, const bmgd_logprobs_tensors* t, void* stream);
+/*      dlogits_j = dlogprob ([j = label] - p_j) - dentropy p_j (ln p_j + entropy) */
+int bmgd_logprobs_backward(const bmgd_logprobs_config* cfg, int64_t rows, const bmgd_logprobs_tensors* t, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

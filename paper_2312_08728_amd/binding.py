@@ -35,6 +35,8 @@ EXPORTS = [
     "bmgd_last_error", "bmgd_destroy",
     "bmgd_gated_workspace_bytes", "bmgd_gated_create", "bmgd_gated_forward", "bmgd_gated_backward", "bmgd_gated_last_error", "bmgd_gated_destroy",
     "bmgd_adamw_default_config", "bmgd_adamw_step", "bmgd_adamw_moments",
+    "bmgd_norm_workspace_bytes", "bmgd_norm_forward", "bmgd_norm_backward", "bmgd_product_forward", "bmgd_product_quantize", "bmgd_product_values",
+    "bmgd_logprobs_workspace_bytes", "bmgd_logprobs_forward", "bmgd_logprobs_backward",
 ]
 
 
@@ -87,6 +89,33 @@ class bmgd_adamw_config(C.Structure):
         ("grad_scale", C.c_double), ("grad_dtype", C.c_int32), ("copy_dtype", C.c_int32), ("state_bits", C.c_int32),
         ("reserved", C.c_int32),
     ]
+
+
+class bmgd_norm_config(C.Structure):
+    _fields_ = [("n", C.c_int64), ("eps", C.c_double), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class bmgd_norm_tensors(C.Structure):
+    _fields_ = [(name, bmgd_matrix) for name in ("x", "residual", "sum", "y", "codes", "dy", "dsum", "dx")] + [
+        (name, C.c_void_p) for name in ("weight", "dweight", "scales", "rstd", "workspace")] + [("workspace_bytes", C.c_size_t)]
+
+
+class bmgd_product_config(C.Structure):
+    _fields_ = [("p", C.c_int64), ("out_n", C.c_int64), ("dtype", C.c_int32), ("reserved", C.c_int32)]
+
+
+class bmgd_product_tensors(C.Structure):
+    _fields_ = [(name, bmgd_matrix) for name in ("x", "w", "y")] + [("x_scales", C.c_void_p), ("w_scales", C.c_void_p)]
+
+
+class bmgd_logprobs_config(C.Structure):
+    _fields_ = [("classes", C.c_int64), ("dtype", C.c_int32), ("top", C.c_int32)]
+
+
+class bmgd_logprobs_tensors(C.Structure):
+    _fields_ = [("logits", bmgd_matrix), ("dlogits", bmgd_matrix)] + [
+        (name, C.c_void_p) for name in ("labels", "logprob", "entropy", "top_classes", "top_logprobs", "kept", "dlogprob", "dentropy", "workspace")] + [
+        ("workspace_bytes", C.c_size_t)]
 
 
 def _load() -> C.CDLL:
@@ -148,6 +177,17 @@ def _load() -> C.CDLL:
     lib.bmgd_adamw_default_config.argtypes, lib.bmgd_adamw_default_config.restype = [C.POINTER(bmgd_adamw_config)], None
     lib.bmgd_adamw_step.argtypes, lib.bmgd_adamw_step.restype = [C.POINTER(bmgd_adamw_config), vp, i64, i64, vp], i32
     lib.bmgd_adamw_moments.argtypes, lib.bmgd_adamw_moments.restype = [vp, i64, vp, vp, vp], i32
+    for name in ("norm", "product", "logprobs"):
+        config = C.POINTER(globals()[f"bmgd_{name}_config"])
+        for call in ("forward", "backward"):
+            if f"bmgd_{name}_{call}" in EXPORTS:
+                f = getattr(lib, f"bmgd_{name}_{call}")
+                f.argtypes, f.restype = [config, i64, vp, vp], i32
+        if f"bmgd_{name}_workspace_bytes" in EXPORTS:
+            f = getattr(lib, f"bmgd_{name}_workspace_bytes")
+            f.argtypes, f.restype = [config, i64], C.c_size_t
+    lib.bmgd_product_quantize.argtypes, lib.bmgd_product_quantize.restype = [C.POINTER(bmgd_product_config), vp, vp, vp, vp], i32
+    lib.bmgd_product_values.argtypes, lib.bmgd_product_values.restype = [i64, i64, vp, vp, vp, i32, vp], i32
     return lib
 
 
@@ -402,6 +442,48 @@ def bmgd_adamw_step(cfg, tensors, count, step, stream=None) -> int:
 def bmgd_adamw_moments(tensors, count, m_out, s_out, stream=None) -> int:
     """m_out, s_out: arrays of device addresses (c_void_p)."""
     return lib.bmgd_adamw_moments(tensors, count, m_out, s_out, _stream(stream))
+
+
+def bmgd_norm_workspace_bytes(cfg, rows) -> int:
+    return lib.bmgd_norm_workspace_bytes(C.byref(cfg), rows)
+
+
+def _call(fn, cfg, rows, tensors, stream) -> int:
+    return fn(C.byref(cfg) if cfg is not None else None, rows, C.addressof(tensors) if tensors is not None else None, _stream(stream))
+
+
+def bmgd_norm_forward(cfg, rows, tensors, stream=None) -> int:
+    return _call(lib.bmgd_norm_forward, cfg, rows, tensors, stream)
+
+
+def bmgd_norm_backward(cfg, rows, tensors, stream=None) -> int:
+    return _call(lib.bmgd_norm_backward, cfg, rows, tensors, stream)
+
+
+def bmgd_product_forward(cfg, rows, tensors, stream=None) -> int:
+    return _call(lib.bmgd_product_forward, cfg, rows, tensors, stream)
+
+
+def bmgd_product_quantize(cfg, weights, w, w_scales, stream=None) -> int:
+    """weights, w: a bmgd_matrix each; w_scales: an address."""
+    return lib.bmgd_product_quantize(C.byref(cfg), C.addressof(weights), C.addressof(w), w_scales, _stream(stream))
+
+
+def bmgd_product_values(rows, n, codes, scales, out, dtype, stream=None) -> int:
+    """codes, out: a bmgd_matrix each; scales: an address."""
+    return lib.bmgd_product_values(rows, n, C.addressof(codes), scales, C.addressof(out), dtype, _stream(stream))
+
+
+def bmgd_logprobs_workspace_bytes(cfg, rows) -> int:
+    return lib.bmgd_logprobs_workspace_bytes(C.byref(cfg), rows)
+
+
+def bmgd_logprobs_forward(cfg, rows, tensors, stream=None) -> int:
+    return _call(lib.bmgd_logprobs_forward, cfg, rows, tensors, stream)
+
+
+def bmgd_logprobs_backward(cfg, rows, tensors, stream=None) -> int:
+    return _call(lib.bmgd_logprobs_backward, cfg, rows, tensors, stream)
 
 
 class Reader:

@@ -3,6 +3,8 @@
 //
 //   matrices(tensors, shapes, dtype, device[, written])    bytes: address and row stride (int64) of each, zeros for None; those from index `written` on are told
 //                                               that they are written, as torch's own in-place operations tell (autograd then refuses values that it has kept)
+//   operands(tensors, dtypes, shapes, kinds, device)      bytes: for each tensor address and row stride (kinds has 'm'), or the address of a contiguous one ('v'); zeros for None.
+//                                               Upper case: it is told that it is written
 //   vectors(tensors, numels, dtype, device)     bytes: the addresses of contiguous tensors; numels: bytes of int64
 //   pairs(pairs, numels, dtype, device)         (bytes, bytes): the same of the first and of the second tensors
 //   same(groups)                                True if the tensors of every group are what they were when their addresses were read.  A group: (list, item, numels, dtype,
@@ -10,7 +12,7 @@
 //
 //   touch(tensors)                              tells the tensors of a list that they have been written
 //
-// The first three return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
+// The first four return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -95,6 +97,50 @@ PyObject* matrices_(PyObject* const* args, Py_ssize_t n)
     }
     for (Py_ssize_t i = written; i < count; ++i)
         if (PyTuple_GET_ITEM(args[0], i) != Py_None) touch(THPVariable_Unpack(PyTuple_GET_ITEM(args[0], i)));
+    return out;
+}
+
+PyObject* operands_(PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 5 || !PyTuple_Check(args[0]) || !PyTuple_Check(args[1]) || !PyTuple_Check(args[2]) || !PyBytes_Check(args[3]) ||
+        PyTuple_GET_SIZE(args[1]) != PyTuple_GET_SIZE(args[0]) || PyTuple_GET_SIZE(args[2]) != PyTuple_GET_SIZE(args[0]) || PyBytes_GET_SIZE(args[3]) != PyTuple_GET_SIZE(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "operands(tensors, dtypes, shapes, kinds, device): three tuples and bytes of one length");
+        return nullptr;
+    }
+    const Py_ssize_t count = PyTuple_GET_SIZE(args[0]);
+    const char* const kinds = PyBytes_AS_STRING(args[3]);
+    Py_ssize_t words = 0;
+    for (Py_ssize_t i = 0; i < count; ++i) words += (kinds[i] | 32) == 'm' ? 2 : 1;
+    PyObject* const out = PyBytes_FromStringAndSize(nullptr, words * 8);
+    if (!out) return nullptr;
+    char* to = PyBytes_AS_STRING(out);
+    for (Py_ssize_t i = 0; i < count; ++i) {
+        PyObject *const o = PyTuple_GET_ITEM(args[0], i), *const shape = PyTuple_GET_ITEM(args[2], i);
+        const bool matrix = (kinds[i] | 32) == 'm';
+        int64_t v[2] = {0, 0};
+        if (o != Py_None) {
+            Kind k;
+            if (!kind_of(PyTuple_GET_ITEM(args[1], i), args[4], &k) || !PyTuple_Check(shape)) {
+                Py_DECREF(out);
+                if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "operands(): a shape is a tuple");
+                return nullptr;
+            }
+            const at::Tensor* const t = tensor_of(o, k);
+            bool good = t && t->dim() == (int64_t)PyTuple_GET_SIZE(shape);
+            for (Py_ssize_t d = 0; good && d < PyTuple_GET_SIZE(shape); ++d) good = t->size(d) == PyLong_AsLongLong(PyTuple_GET_ITEM(shape, d));
+            if (good) good = matrix ? t->dim() == 2 && (t->stride(1) == 1 || t->size(1) == 1) : t->is_contiguous();
+            if (PyErr_Occurred() || !good) {
+                Py_DECREF(out);
+                return PyErr_Occurred() ? nullptr : PyLong_FromSsize_t(i);
+            }
+            v[0] = (int64_t)(uintptr_t)t->data_ptr();
+            v[1] = matrix ? t->stride(0) : 0;
+        }
+        std::memcpy(to, v, matrix ? 16 : 8);
+        to += matrix ? 16 : 8;
+    }
+    for (Py_ssize_t i = 0; i < count; ++i)
+        if (!(kinds[i] & 32) && PyTuple_GET_ITEM(args[0], i) != Py_None) touch(THPVariable_Unpack(PyTuple_GET_ITEM(args[0], i)));
     return out;
 }
 
@@ -225,6 +271,7 @@ template <PyObject* F(PyObject* const*, Py_ssize_t)> PyObject* guarded(PyObject*
 
 PyMethodDef methods[] = {
     {"matrices", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<matrices_>)), METH_FASTCALL, "addresses and row strides of matrices"},
+    {"operands", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<operands_>)), METH_FASTCALL, "addresses and row strides of a call's tensors"},
     {"vectors", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<vectors_>)), METH_FASTCALL, "addresses of contiguous tensors"},
     {"pairs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<pairs_>)), METH_FASTCALL, "addresses of pairs of contiguous tensors"},
     {"same", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<same_>)), METH_FASTCALL, "whether tensors are where they were"},
