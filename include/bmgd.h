@@ -566,8 +566,8 @@ int bmgd_adamw_moments(const bmgd_adamw_tensor* tensors, int64_t count, float* c
 
 /* ---- Root-mean-square norm ----
  *      s = x + residual, rounded to the type;     r = 1 / sqrt(mean_j s_j^2 + eps);     y_j = s_j w_j r
- * and, or instead of y, 8-bit codes with a scale for each row: codes_j = the integer nearest to 127 s_j w_j / max_k |s_k w_k| (half to even), scale =
- * max_k |s_k w_k| r / 127, so that scale * codes_j is y_j.  A row whose largest |s w| is below 2^-118 is held as zeros; a row that has a NaN or an
+ * and, or instead of y, 8-bit codes with a scale for each row: codes_j = the integer nearest to s_j w_j ((1 / max_k |s_k w_k|) 127) (in 64 bits; half to even), scale =
+ * max_k |s_k w_k| r / 127, so that scale * codes_j is y_j but for its rounding.  A row whose largest |s w| is below 2^-118 is held as zeros; a row that has a NaN or an
  * infinity among its s w stands for NaN (scale NaN, codes zero).  Sums are in fp32: |s| below 2^63 / sqrt(n). */
 typedef struct bmgd_norm_config {
     int64_t n;              /* columns, in [1, 2^20] */
@@ -622,8 +622,8 @@ typedef struct bmgd_product_tensors {
 
 /* Fewer than 2^23 tiles of 128 x 128 results. */
 int bmgd_product_forward(const bmgd_product_config* cfg, int64_t rows, const bmgd_product_tensors* t, void* stream);
-/* A layer's weights (p x out_n, of dtype, as the blocks above have them) laid out for the product, once: w_jk = the integer nearest to weights_kj / w_scales[j]
- * (half to even), w_scales[j] = max_k |weights_kj| / 127.  Outputs whose largest is below 2^-118 are zeros; those with a NaN or an infinity have a scale of NaN and codes of zero. */
+/* A layer's weights (p x out_n, of dtype, as the blocks above have them) laid out for the product, once: w_jk = the integer nearest to weights_kj ((1 / max_k |weights_kj|) 127)
+ * (in 64 bits; half to even), w_scales[j] = max_k |weights_kj| / 127.  Outputs whose largest is below 2^-118 are zeros; those with a NaN or an infinity have a scale of NaN and codes of zero. */
 int bmgd_product_quantize(const bmgd_product_config* cfg, const bmgd_matrix* weights, const bmgd_matrix* w, float* w_scales, void* stream);
 
 /* ---- Log probabilities ----

@@ -17,7 +17,7 @@ def codes_of(v):
     top = np.abs(v).max(1)
     bad = ~np.isfinite(v).all(1)
     held = ~bad & (top >= LEAST)
-    inv = np.where(held, 127.0 / np.where(held, top, 1.0), 0.0)
+    inv = np.where(held, 1.0 / np.where(held, top, 1.0) * 127.0, 0.0)
     codes = np.rint(np.where(bad[:, None], 0.0, v) * inv[:, None]).astype(np.int64)
     return codes, np.where(bad, np.nan, np.where(held, top, 0.0))
 

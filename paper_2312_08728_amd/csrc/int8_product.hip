@@ -271,7 +271,7 @@ template <typename T> __global__ void __launch_bounds__(256) int8_quantize_kerne
     for (int i = 0; i < 4; ++i) top = tops[i][col] > top ? tops[i][col] : top;
     const float size = __builtin_bit_cast(float, top);
     const bool held = top < 0x7f800000u && size >= 0x1p-118f;
-    const double inv = held ? 127.0 / (double)size : 0.0;
+    const double inv = held ? 1.0 / (double)size * 127.0 : 0.0;
     if (slice == 0 && j < a.out) a.scales[j] = top >= 0x7f800000u ? __builtin_nanf("") : held ? size / 127.f : 0.f;
     for (int k0 = 0; k0 < a.p; k0 += 64) {
         __syncthreads();

@@ -1,8 +1,9 @@
 // Log probabilities of given classes, entropy and the most probable classes of rows of logits, in one pass over them; their gradient.
 //
-// A thread holds its largest logit m so far, s = sum 2^d and w = sum 2^d d, d = (x - m) log2 e; where m grows by g, s becomes s 2^-g and w (w - g s) 2^-g.
-// Threads, wavefronts and parts of a row are put together the same way.  Then ln p_j = x_j - m - ln 2 log2 s and the entropy is ln 2 (log2 s - w / s).
-// x - m is formed before it is scaled: logits of the type's lowest value are as good as others, -infinity adds nothing.
+// A thread holds its largest logit m so far, s = sum 2^d and w = sum 2^d d, d = x log2 e - r with r = m log2 e rounded; where r grows by g, s becomes s 2^-g and
+// w (w - g s) 2^-g.  Threads, wavefronts and parts of a row are put together the same way.  Then ln p_j = ln 2 (d_j - log2 s) and the entropy is ln 2 (log2 s - w / s).
+// d is one instruction with one rounding; r's own rounding is the same for all and leaves with log2 s.  Rows whose largest logit is not below 1e37 in size (all of the
+// type's lowest value, no class at all, infinity) are read once more with d = (x - m) log2 e, which does not leave the range.  -infinity adds nothing.
 //
 // The most probable classes.  A logit and its class are one 64-bit number, larger where the logit is larger and, of equal ones, the class lower; so no two are
 // equal.  Each thread keeps its largest piece of eight; 64 groups of threads have 64 such numbers, and the top-th largest of them is not above the top-th
@@ -23,6 +24,7 @@ typedef unsigned long long Key;
 
 constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147182f;
 constexpr float kLowest = -3.40282347e38f;
+constexpr float kUsual = 1e37f;                  // x log2 e - r is finite, or -infinity for one far below, where m is smaller than this
 constexpr float kFar = -1000.f;                  // 2^-1000 is 0, times this still 0
 constexpr int kMaxTop = 64, kMaxParts = 64;
 constexpr int kList = 512;                       // a segment of fewer classes than 8 top fits whole
@@ -46,13 +48,26 @@ struct Stats {
     float m, s, w;
 };
 
-// 2^(m - to) as a factor for s and w
-__device__ __forceinline__ void refer_to(Stats& a, float to)
+// To another reference
+__device__ __forceinline__ void scale_down(Stats& a, float to, float d)
 {
-    const float d = fmaxf((a.m - to) * kLog2E, kFar), f = __builtin_amdgcn_exp2f(d);
+    d = fmaxf(d, kFar);
+    const float f = __builtin_amdgcn_exp2f(d);
     a.w = f * __builtin_fmaf(d, a.s, a.w);
     a.s *= f;
     a.m = to;
+}
+// r of m: rounded, wherever it is used
+__device__ __forceinline__ float reference(float m)
+{
+    float r = m * kLog2E;
+    asm("" : "+v"(r));
+    return r;
+}
+__device__ __forceinline__ void refer_to(Stats& a, float to)
+{
+    if (fabsf(to) < kUsual) scale_down(a, to, reference(a.m) - reference(to));
+    else scale_down(a, to, (a.m - to) * kLog2E);
 }
 
 __device__ __forceinline__ Stats wave_merge(Stats a)
@@ -88,19 +103,14 @@ template <int W> __device__ __forceinline__ void together()
     }
 }
 
-// Of 64 lanes' numbers the one that has `rank` larger ones before it (none are equal but zeros).
-__device__ __forceinline__ Key ranked(Key v, int rank)
+// Of the wavefront's 64 numbers, which lie in shared memory too, the one with `rank` larger ones, 0 if there is none (they differ, but for zeros).
+__device__ __forceinline__ Key ranked(Key v, const Key* all, int rank)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int size = 2; size <= 64; size *= 2)
-#pragma unroll
-        for (int d = size / 2; d; d /= 2) {
-            const Key o = __shfl_xor(v, d);
-            const bool first = !(lane & d), falling = !(lane & size);
-            v = (first == falling) == (v > o) ? v : o;
-        }
-    return __shfl(v, rank);
+    int larger = 0;
+#pragma unroll 16
+    for (int i = 0; i < 64; ++i) larger += all[i] > v;
+    const unsigned long long found = __ballot(larger == rank);
+    return found ? of_lane(v, __builtin_ctzll(found)) : 0;
 }
 
 template <typename T> __device__ __forceinline__ typename Eight<T>::vec logits_at(const T* x, int j, int end)
@@ -113,20 +123,35 @@ __device__ __forceinline__ float largest(float8v v)
     return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
 }
 
-template <int U> __device__ __forceinline__ void take(Stats& st, const float8v* v, const float* most)
+// ENT: with w
+template <int U, bool ENT> __device__ __forceinline__ void take(Stats& st, const float8v* v, const float* most)
 {
     float m = st.m;
 #pragma unroll
     for (int u = 0; u < U; ++u) m = fmaxf(m, most[u]);
-    if (m > st.m) refer_to(st, m);
+    const float r = reference(m);
+    if (m > st.m) scale_down(st, m, reference(st.m) - r);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float d = (v[u][k] - m) * kLog2E, e = __builtin_amdgcn_exp2f(d);
+            const float d = __builtin_fmaf(v[u][k], kLog2E, -r), e = __builtin_amdgcn_exp2f(d);
             st.s += e;
-            st.w = __builtin_fmaf(e, fmaxf(d, kFar), st.w);
+            if constexpr (ENT) st.w = __builtin_fmaf(e, fmaxf(d, kFar), st.w);
         }
+}
+
+// A row of unusual size: its largest, then the sums
+__device__ __forceinline__ void take_unusual(Stats& st, float8v v)
+{
+    const float m = fmaxf(st.m, largest(v));
+    if (m > st.m) scale_down(st, m, (st.m - m) * kLog2E);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float d = (v[k] - m) * kLog2E, e = __builtin_amdgcn_exp2f(d);
+        st.s += e;
+        st.w = __builtin_fmaf(e, fmaxf(d, kFar), st.w);
+    }
 }
 
 // What is known of a row's distribution: log2 of the sum, entropy; `empty` where all logits are -infinity.
@@ -143,7 +168,13 @@ __device__ __forceinline__ Row finish(const Stats& a)
     r.entropy = r.empty ? 0.f : kLn2 * (r.ls - a.w / a.s);
     return r;
 }
-__device__ __forceinline__ float logprob_of(const Row& r, float x) { return r.empty ? -__builtin_inff() : (x - r.m) - r.ls * kLn2; }
+__device__ __forceinline__ float logprob_of(const Row& r, float x)
+{
+    if (r.empty) return -__builtin_inff();
+    // (what r has lost of m log2 e is in log2 s)
+    const float lost = fabsf(r.m) < kUsual ? __builtin_fmaf(r.m, kLog2E, -reference(r.m)) : 0.f;
+    return __builtin_fmaf(lost - r.ls, kLn2, x - r.m);
+}
 
 template <typename T> __device__ __forceinline__ void write_row(const LogArgs& a, int64_t row, const T* x, const Row& r)
 {
@@ -171,13 +202,14 @@ __device__ __forceinline__ void write_top(const LogArgs& a, int64_t row, int par
 
 constexpr int threads_of(int w) { return w < 4 ? 256 : 64 * w; }
 
-template <typename T, int W, bool TOP> __global__ void __launch_bounds__(threads_of(W)) logprobs_kernel(LogArgs a)
+template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds__(threads_of(W)) logprobs_kernel(LogArgs a)
 {
-    constexpr int kLanes = 64 * W, kRows = threads_of(W) / kLanes, U = 4;
+    constexpr int kLanes = 64 * W, kRows = threads_of(W) / kLanes, U = 4, kTurn = 8 * kLanes * U;
+    typedef typename Eight<T>::vec vec;
     __shared__ Stats parts[W > 1 ? W : 1];
-    __shared__ Key keys[W > 1 ? kLanes : 1];
+    __shared__ Key keys[TOP ? kRows : 1][TOP ? kLanes : 1];
     __shared__ Key list[TOP ? kRows : 1][TOP ? kList : 1];
-    __shared__ Key threshold[W > 1 ? 1 : 1];
+    __shared__ Key threshold;
     __shared__ int counts[kRows];
     const int t = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
     const int64_t row = a.first + (int64_t)blockIdx.x * kRows + mine;
@@ -185,56 +217,76 @@ template <typename T, int W, bool TOP> __global__ void __launch_bounds__(threads
     const int part = blockIdx.y, begin = part * a.span, end = a.classes - begin > a.span ? begin + a.span : a.classes;
     const T* const x = reinterpret_cast<const T*>(a.logits) + row * a.stride;
 
-    Stats st{kLowest, 0.f, 0.f};
+    Stats st{-kUsual, 0.f, 0.f};
     float best = -__builtin_inff();
     int best_at = begin + 8 * t < end ? begin + 8 * t : -1;
     int j = begin + 8 * t;
-    for (; j + 8 * kLanes * (U - 1) + 8 <= end; j += 8 * kLanes * U) {
-        float8v v[U];
-        float most[U];
+    {
+        // turns of U pieces, the next ones on their way; those that end inside a turn have -infinity behind the end
+        vec next[U];
+        auto request = [&](int from) {
+            if (from + kTurn - 8 * kLanes + 8 <= end) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = widen<T>(Eight<T>::load(x + j + 8 * kLanes * u));
+                for (int u = 0; u < U; ++u) next[u] = Eight<T>::load(x + from + 8 * kLanes * u);
+            } else {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            most[u] = largest(v[u]);
-            if constexpr (TOP)
-                if (most[u] > best) {
-                    best = most[u];
-                    best_at = j + 8 * kLanes * u;
+                for (int u = 0; u < U; ++u) {
+                    const int i = from + 8 * kLanes * u;
+                    if (i < end) next[u] = logits_at(x, i, end);
+                    else next[u] = (T)-__builtin_inff();
                 }
-        }
-        take<U>(st, v, most);
-    }
-    for (; j < end; j += 8 * kLanes) {
-        const float8v v = widen<T>(logits_at(x, j, end));
-        const float most = largest(v);
-        if constexpr (TOP)
-            if (most > best) {
-                best = most;
-                best_at = j;
             }
-        take<1>(st, &v, &most);
+        };
+        request(j);
+        while (j < end) {
+            float8v v[U];
+            float most[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = widen<T>(next[u]);
+            const int now = j;
+            j += kTurn;
+            if (j < end) request(j);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                most[u] = largest(v[u]);
+                if constexpr (TOP)
+                    if (most[u] > best) {
+                        best = most[u];
+                        best_at = now + 8 * kLanes * u;
+                    }
+            }
+            take<U, ENT>(st, v, most);
+        }
     }
 
-    st = wave_merge(st);
-    if constexpr (W > 1) {
-        if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = st;
-        if constexpr (TOP) keys[t] = best_at < 0 ? 0 : key_of(best, best_at + 7 < end ? best_at + 7 : end - 1);
-        if (threadIdx.x == 0) counts[0] = 0;
-        __syncthreads();
-        st = parts[0];
-        float m = st.m;
+    auto merged = [&](Stats own) {
+        own = wave_merge(own);
+        if constexpr (W > 1) {
+            if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = own;
+            __syncthreads();
+            float m = parts[0].m;
 #pragma unroll
-        for (int i = 1; i < W; ++i) m = fmaxf(m, parts[i].m);
-        refer_to(st, m);
+            for (int i = 1; i < W; ++i) m = fmaxf(m, parts[i].m);
+            Stats all{m, 0.f, 0.f};
 #pragma unroll
-        for (int i = 1; i < W; ++i) {
-            Stats o = parts[i];
-            refer_to(o, m);
-            st.s += o.s;
-            st.w += o.w;
-        }
-    } else if (t == 0) counts[mine] = 0;
+            for (int i = 0; i < W; ++i) {
+                Stats o = parts[i];
+                refer_to(o, m);
+                all.s += o.s;
+                all.w += o.w;
+            }
+            return all;
+        } else return own;
+    };
+    if constexpr (TOP) keys[mine][t] = best_at < 0 ? 0 : key_of(best, best_at + 7 < end ? best_at + 7 : end - 1);
+    if (t == 0) counts[mine] = 0;
+    st = merged(st);
+    if (!(st.m > -kUsual && st.m < kUsual)) {
+        if constexpr (W > 1) __syncthreads();                   // (`parts` has been read)
+        st = Stats{kLowest, 0.f, 0.f};
+        for (int i = begin + 8 * t; i < end; i += 8 * kLanes) take_unusual(st, widen<T>(logits_at(x, i, end)));
+        st = merged(st);
+    }
     const Row r = finish(st);
     if (t == 0) {
         if (a.parts > 1) {
@@ -249,22 +301,23 @@ template <typename T, int W, bool TOP> __global__ void __launch_bounds__(threads
         Key least;
         if constexpr (W > 1) {
             if (threadIdx.x < 64) {
-                Key k = keys[threadIdx.x];
+                Key k = keys[0][t];
 #pragma unroll
-                for (int i = 1; i < W; ++i) k = keys[64 * i + threadIdx.x] > k ? keys[64 * i + threadIdx.x] : k;
-                k = ranked(k, a.top - 1);
-                if (threadIdx.x == 0) threshold[0] = k;
+                for (int i = 1; i < W; ++i) k = keys[0][64 * i + t] > k ? keys[0][64 * i + t] : k;
+                keys[0][t] = k;
+                together<1>();
+                k = ranked(k, keys[0], a.top - 1);
+                if (t == 0) threshold = k;
             }
             __syncthreads();
-            least = threshold[0];
+            least = threshold;
         } else {
-            least = ranked(best_at < 0 ? 0 : key_of(best, best_at + 7 < end ? best_at + 7 : end - 1), a.top - 1);
-            together<W>();
+            together<1>();
+            least = ranked(keys[mine][t], keys[mine], a.top - 1);
         }
         const bool plain = st.s == st.s;
-        if (plain && best_at >= 0 && key_of(best, best_at) >= least)
-            for (int i = begin + 8 * t; i < end; i += 8 * kLanes) {
-                const float8v v = widen<T>(logits_at(x, i, end));
+        if (plain && best_at >= 0 && key_of(best, best_at) >= least) {
+            auto look = [&](float8v v, int i) {
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
                     const Key q = key_of(v[k], i + k);
@@ -273,7 +326,24 @@ template <typename T, int W, bool TOP> __global__ void __launch_bounds__(threads
                         if (at < kList) list[mine][at] = q;
                     }
                 }
+            };
+            for (int from = begin + 8 * t; from < end; from += 2 * kTurn) {
+                vec v[2 * U];
+#pragma unroll
+                for (int u = 0; u < 2 * U; ++u) {
+                    const int i = from + 8 * kLanes * u;
+                    if (i < end) v[u] = logits_at(x, i, end);
+                }
+#pragma unroll
+                for (int u = 0; u < 2 * U; ++u) {
+                    const int i = from + 8 * kLanes * u;
+                    if (i < end) {
+                        const float8v f = widen<T>(v[u]);
+                        if (ordered(largest(f)) >= (unsigned)(least >> 32)) look(f, i);
+                    }
+                }
             }
+        }
         together<W>();
         const int count = counts[mine];
         if (plain && count <= kList) {
@@ -299,10 +369,10 @@ template <typename T, int W, bool TOP> __global__ void __launch_bounds__(threads
                 k = wave_max(k);
                 if constexpr (W > 1) {
                     __syncthreads();
-                    if ((threadIdx.x & 63) == 0) keys[threadIdx.x >> 6] = k;
+                    if ((threadIdx.x & 63) == 0) keys[0][threadIdx.x >> 6] = k;
                     __syncthreads();
 #pragma unroll
-                    for (int i = 0; i < W; ++i) k = keys[i] > k ? keys[i] : k;
+                    for (int i = 0; i < W; ++i) k = keys[0][i] > k ? keys[0][i] : k;
                 }
                 if (t == 0) write_top(a, row, part, place, k, r);
                 before = k;
@@ -320,7 +390,7 @@ template <typename T> __global__ void __launch_bounds__(256) logprobs_join_kerne
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63;
     const float* const from = a.part_stats + row * a.parts * 3;
-    Stats st{kLowest, 0.f, 0.f};
+    Stats st{kLowest, 0.f, 0.f};                                // (of a size that no part with classes has: adds nothing)
     if (lane < a.parts) st = Stats{from[3 * lane], from[3 * lane + 1], from[3 * lane + 2]};
     st = wave_merge(st);
     const Row r = finish(st);
@@ -355,21 +425,47 @@ template <typename T> __global__ void __launch_bounds__(256) logprobs_join_kerne
 // dlogits: W wavefronts have a row (W = 1), or a chunk of one.
 constexpr int kChunk = 8 * 4 * 256;
 
-template <typename T> __device__ __forceinline__ typename Eight<T>::vec logit_gradients(float8v v, float m, float ls, float entropy, float dl, float dh, bool empty, int mark)
+// What a row's gradients are made of: dlogits = 2^d (both + d of_entropy), d = x log2 e - shift, and dl more at the label.  shift is r + log2 s rounded; what that loses
+// is put into the other two.
+struct Slope {
+    float m, shift, both, of_entropy, dl;
+    int label;
+    bool usual;
+};
+__device__ __forceinline__ Slope slope_of(float m, float ls, float entropy, float dl, float dh, int label)
+{
+    Slope g;
+    g.m = m;
+    g.usual = fabsf(m) < kUsual;
+    g.shift = ls;
+    float lost = 0.f;
+    if (g.usual) {
+        const float r = reference(m), of_ls = (g.shift = r + ls) - r;
+        lost = (r - (g.shift - of_ls)) + (ls - of_ls);
+    }
+    const float f = __builtin_amdgcn_exp2f(-lost);
+    g.of_entropy = -dh * kLn2 * f;
+    g.both = -(dl + dh * (entropy - kLn2 * lost)) * f;
+    g.dl = dl;
+    g.label = label;
+    return g;
+}
+template <bool DH> __device__ __forceinline__ float8v logit_gradients(float8v v, const Slope& g)
 {
     float8v o;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const float d = __builtin_fmaf(v[k] - m, kLog2E, -ls), p = __builtin_amdgcn_exp2f(d);
-        const float g = -p * __builtin_fmaf(dh, __builtin_fmaf(fmaxf(d, kFar), kLn2, entropy), dl);
-        o[k] = empty ? 0.f : k == mark ? g + dl : g;
+        const float d = g.usual ? __builtin_fmaf(v[k], kLog2E, -g.shift) : __builtin_fmaf(v[k] - g.m, kLog2E, -g.shift);
+        const float p = __builtin_amdgcn_exp2f(d);
+        o[k] = DH ? p * __builtin_fmaf(fmaxf(d, kFar), g.of_entropy, g.both) : p * g.both;
     }
-    return narrow<T>(o);
+    return o;
 }
 
-template <typename T, int W> __global__ void __launch_bounds__(256) logprobs_backward_kernel(LogArgs a)
+template <typename T, int W, bool DH> __global__ void __launch_bounds__(256) logprobs_backward_kernel(LogArgs a)
 {
     constexpr int kLanes = 64 * W, kRows = 4 / W, U = 4;
+    typedef typename Eight<T>::vec vec;
     const int t = threadIdx.x % kLanes;
     const int64_t items = W == 1 ? a.rows : a.rows * a.chunks;
     for (int64_t item = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; item < items; item += (int64_t)gridDim.x * kRows) {
@@ -381,13 +477,13 @@ template <typename T, int W> __global__ void __launch_bounds__(256) logprobs_bac
             end = a.classes - begin > kChunk ? begin + kChunk : a.classes;
         }
         const T* const x = reinterpret_cast<const T*>(a.logits) + row * a.stride;
-        T* const d = reinterpret_cast<T*>(a.dlogits) + row * a.dstride;
-        const float m = a.kept[3 * row], ls = a.kept[3 * row + 1], entropy = a.kept[3 * row + 2], dh = a.dentropy ? a.dentropy[row] : 0.f;
+        T* const out = reinterpret_cast<T*>(a.dlogits) + row * a.dstride;
+        const float m = a.kept[3 * row], entropy = a.kept[3 * row + 2], dh = DH ? a.dentropy[row] : 0.f;
         const int label = a.dlogprob ? a.labels[row] : -1;
-        const float dl = label < 0 ? 0.f : label >= a.classes ? __builtin_nanf("") : a.dlogprob[row];
-        const bool empty = m == -__builtin_inff() && label < a.classes;
+        const Slope g = slope_of(m, a.kept[3 * row + 1], entropy, label < 0 ? 0.f : label >= a.classes ? __builtin_nanf("") : a.dlogprob[row], dh, label);
+        const bool empty = m == -__builtin_inff() && g.label < a.classes;
         for (int j = begin + 8 * t; j < end; j += 8 * kLanes * U) {
-            typename Eight<T>::vec v[U];
+            vec v[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = j + 8 * kLanes * u;
@@ -397,9 +493,15 @@ template <typename T, int W> __global__ void __launch_bounds__(256) logprobs_bac
             for (int u = 0; u < U; ++u) {
                 const int i = j + 8 * kLanes * u;
                 if (i >= end) continue;
-                const typename Eight<T>::vec o = logit_gradients<T>(widen<T>(v[u]), m, ls, entropy, dl, dh, empty, label - i);
-                if (i + 8 <= end) Eight<T>::store(d + i, o);
-                else Eight<T>::store_part(d + i, o, end - i);
+                float8v o = logit_gradients<DH>(widen<T>(v[u]), g);
+                if ((unsigned)(g.label - i) < 8u) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] += k == g.label - i ? g.dl : 0.f;
+                }
+                if (empty) o = 0.f;
+                const vec w = narrow<T>(o);
+                if (i + 8 <= end) Eight<T>::store(out + i, w);
+                else Eight<T>::store_part(out + i, w, end - i);
             }
         }
     }
@@ -499,21 +601,25 @@ BMGD_API int bmgd_logprobs_forward(const bmgd_logprobs_config* cfg, int64_t rows
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
-        auto launch = [&](auto w, auto top) {
+        auto launch = [&](auto w, auto top, auto ent) {
             constexpr int W = decltype(w)::value, kRows = threads_of(W) / (64 * W);
-            constexpr bool TOP = decltype(top)::value;
+            constexpr bool TOP = decltype(top)::value, ENT = decltype(ent)::value;
             for (a.first = 0; a.first < rows; a.first += kRowsOfLaunch) {
                 const int64_t now = std::min(rows - a.first, kRowsOfLaunch);
-                hipLaunchKernelGGL((logprobs_kernel<T, W, TOP>), dim3((unsigned)((now + kRows - 1) / kRows), (unsigned)a.parts), dim3(threads_of(W)), 0, s, a);
+                hipLaunchKernelGGL((logprobs_kernel<T, W, TOP, ENT>), dim3((unsigned)((now + kRows - 1) / kRows), (unsigned)a.parts), dim3(threads_of(W)), 0, s, a);
             }
         };
-        auto shaped = [&](auto top) {
-            if (a.span <= 2048) launch(std::integral_constant<int, 1>(), top);
-            else if (a.span <= 16384 || rows * a.parts > 512) launch(std::integral_constant<int, 4>(), top);
-            else launch(std::integral_constant<int, 16>(), top);
+        auto shaped = [&](auto top, auto ent) {
+            if (a.span <= 2048) launch(std::integral_constant<int, 1>(), top, ent);
+            else if (a.span <= 16384 || rows * a.parts > 512) launch(std::integral_constant<int, 4>(), top, ent);
+            else launch(std::integral_constant<int, 16>(), top, ent);
         };
-        if (a.top) shaped(std::true_type());
-        else shaped(std::false_type());
+        auto with_top = [&](auto ent) {
+            if (a.top) shaped(std::true_type(), ent);
+            else shaped(std::false_type(), ent);
+        };
+        if (a.entropy || a.kept) with_top(std::true_type());
+        else with_top(std::false_type());
         if (a.parts > 1) hipLaunchKernelGGL(logprobs_join_kernel<T>, dim3((unsigned)rows), dim3(256), (size_t)std::max(1, a.parts * a.top) * sizeof(Key), s, a);
     });
     return q.launched();
@@ -551,8 +657,13 @@ BMGD_API int bmgd_logprobs_backward(const bmgd_logprobs_config* cfg, int64_t row
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
         const int64_t most = int64_t(1) << 20;
-        if (cfg->classes <= 2048) hipLaunchKernelGGL((logprobs_backward_kernel<T, 1>), dim3((unsigned)std::min((rows + 3) / 4, most)), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((logprobs_backward_kernel<T, 4>), dim3((unsigned)std::min(rows * a.chunks, most)), dim3(256), 0, s, a);
+        auto launch = [&](auto dh) {
+            constexpr bool DH = decltype(dh)::value;
+            if (cfg->classes <= 2048) hipLaunchKernelGGL((logprobs_backward_kernel<T, 1, DH>), dim3((unsigned)std::min((rows + 3) / 4, most)), dim3(256), 0, s, a);
+            else hipLaunchKernelGGL((logprobs_backward_kernel<T, 4, DH>), dim3((unsigned)std::min(rows * a.chunks, most)), dim3(256), 0, s, a);
+        };
+        if (a.dentropy) launch(std::true_type());
+        else launch(std::false_type());
     });
     return q.launched();
 }

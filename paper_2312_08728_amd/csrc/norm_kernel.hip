@@ -133,7 +133,7 @@ template <typename T> __device__ __forceinline__ void write_codes(const NormArgs
 // r of a row from its sum of squares
 __device__ __forceinline__ float rstd_of(const NormArgs& a, float squares) { return 1.f / sqrtf(__builtin_fmaf(squares, a.inv_n, a.eps)); }
 
-// 127 / largest (0 where the row is held as zeros or stands for NaN), and the row's scale
+// (1 / largest) 127, each rounded (0 where the row is held as zeros or stands for NaN), and the row's scale
 template <typename T> __device__ __forceinline__ double scale_of(typename Largest<T>::bits top, float r, float* scale)
 {
     const typename Largest<T>::value v = __builtin_bit_cast(typename Largest<T>::value, top);
@@ -146,7 +146,7 @@ template <typename T> __device__ __forceinline__ double scale_of(typename Larges
         return 0.0;
     }
     *scale = (float)v * r / 127.f;
-    return 127.0 / (double)v;
+    return 1.0 / (double)v * 127.0;
 }
 
 template <typename T> __device__ __forceinline__ typename Eight<T>::vec ones()
