@@ -6,9 +6,10 @@
 // type's lowest value, no class at all, infinity) are read once more with d = (x - m) log2 e, which does not leave the range.  -infinity adds nothing.
 //
 // The most probable classes.  A logit and its class are one 64-bit number, larger where the logit is larger and, of equal ones, the class lower; so no two are
-// equal.  Each thread keeps its largest piece of eight; 64 groups of threads have 64 such numbers, and the top-th largest of them is not above the top-th
-// largest of all.  The few threads that reach it read their logits again (from cache) and list those that do; the place of each in the list is the number of larger ones.
-// Where the list would be too long, or a row has NaN, the classes are found one after the other.
+// equal.  Of what the threads read first (8,192 logits of 16 bits for four wavefronts), 64 groups of threads have their largest numbers; the top-th largest of these is not above the top-th
+// largest of the row.  From then on each piece that reaches it, those read first among them, is put into a list in shared memory as it passes by: about top (row / 8,192) pieces.
+// The classes in the list that reach it are counted against one another: the place of each is the number of larger ones.
+// A row that overflows the list (many equal logits) is read once more, by 64-bit numbers; where these overflow too, or a row has NaN, the classes are found one after the other.
 #include "operator_calls.h"
 #include "rows_device.h"
 
@@ -27,7 +28,8 @@ constexpr float kLowest = -3.40282347e38f;
 constexpr float kUsual = 1e37f;                  // x log2 e - r is finite, or -infinity for one far below, where m is smaller than this
 constexpr float kFar = -1000.f;                  // 2^-1000 is 0, times this still 0
 constexpr int kMaxTop = 64, kMaxParts = 64;
-constexpr int kList = 512;                       // a segment of fewer classes than 8 top fits whole
+constexpr int kList = 512;                       // classes listed at most: a row of fewer than 8 top fits whole
+constexpr int pieces_listed(int w) { return w == 1 ? 64 : 256; }
 
 struct LogArgs {
     const char* logits;
@@ -41,7 +43,7 @@ struct LogArgs {
     float* part_stats;                           // [row][part][3]
     Key* part_keys;                              // [row][part][top]
     int64_t rows, first;                         // first: of the launch
-    int classes, top, parts, span, chunks;
+    int classes, top, parts, span;
 };
 
 struct Stats {
@@ -103,28 +105,32 @@ template <int W> __device__ __forceinline__ void together()
     }
 }
 
-// Of the wavefront's 64 numbers, which lie in shared memory too, the one with `rank` larger ones, 0 if there is none (they differ, but for zeros).
-__device__ __forceinline__ Key ranked(Key v, const Key* all, int rank)
+// Which of `count` numbers are larger
+__device__ __forceinline__ int larger_than(Key v, const Key* all, int count)
 {
     int larger = 0;
-#pragma unroll 16
-    for (int i = 0; i < 64; ++i) larger += all[i] > v;
-    const unsigned long long found = __ballot(larger == rank);
-    return found ? of_lane(v, __builtin_ctzll(found)) : 0;
+#pragma unroll 4
+    for (int i = 0; i < count; ++i) larger += all[i] > v;
+    return larger;
 }
 
-template <typename T> __device__ __forceinline__ typename Eight<T>::vec logits_at(const T* x, int j, int end)
+// Pieces begin at multiples of 16 bytes: `before` elements before the row, which with those behind `end` count as -infinity.
+template <typename T> __device__ __forceinline__ int before_row(const T* x) { return (int)(((uintptr_t)x & 15) / sizeof(T)); }
+template <typename T> __device__ __forceinline__ typename Piece<T>::vec logits_at(const T* x, int j, int begin, int end)
 {
-    return j + 8 <= end ? Eight<T>::load(x + j) : Eight<T>::load_part(x + j, end - j, (T)-__builtin_inff());
+    return j >= begin && j + Piece<T>::N <= end ? Piece<T>::load(x + j) : Piece<T>::load_part(x, j, begin, end, (T)-__builtin_inff());
 }
 
-__device__ __forceinline__ float largest(float8v v)
+template <typename V> __device__ __forceinline__ float largest(V v)
 {
-    return fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    constexpr int N = sizeof(V) / 4;
+    float m = fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+    if constexpr (N == 8) m = fmaxf(m, fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    return m;
 }
 
 // ENT: with w
-template <int U, bool ENT> __device__ __forceinline__ void take(Stats& st, const float8v* v, const float* most)
+template <int U, bool ENT, typename V> __device__ __forceinline__ void take(Stats& st, const V* v, const float* most)
 {
     float m = st.m;
 #pragma unroll
@@ -134,7 +140,7 @@ template <int U, bool ENT> __device__ __forceinline__ void take(Stats& st, const
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < (int)sizeof(V) / 4; ++k) {
             const float d = __builtin_fmaf(v[u][k], kLog2E, -r), e = __builtin_amdgcn_exp2f(d);
             st.s += e;
             if constexpr (ENT) st.w = __builtin_fmaf(e, fmaxf(d, kFar), st.w);
@@ -142,12 +148,12 @@ template <int U, bool ENT> __device__ __forceinline__ void take(Stats& st, const
 }
 
 // A row of unusual size: its largest, then the sums
-__device__ __forceinline__ void take_unusual(Stats& st, float8v v)
+template <typename V> __device__ __forceinline__ void take_unusual(Stats& st, V v)
 {
     const float m = fmaxf(st.m, largest(v));
     if (m > st.m) scale_down(st, m, (st.m - m) * kLog2E);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < (int)sizeof(V) / 4; ++k) {
         const float d = (v[k] - m) * kLog2E, e = __builtin_amdgcn_exp2f(d);
         st.s += e;
         st.w = __builtin_fmaf(e, fmaxf(d, kFar), st.w);
@@ -204,60 +210,121 @@ constexpr int threads_of(int w) { return w < 4 ? 256 : 64 * w; }
 
 template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds__(threads_of(W)) logprobs_kernel(LogArgs a)
 {
-    constexpr int kLanes = 64 * W, kRows = threads_of(W) / kLanes, U = 4, kTurn = 8 * kLanes * U;
-    typedef typename Eight<T>::vec vec;
+    constexpr int kLanes = 64 * W, kRows = threads_of(W) / kLanes, N = Piece<T>::N, U = 4, kTurn = N * kLanes * U, kPieces = pieces_listed(W);
+    typedef typename Piece<T>::vec vec;
+    typedef typename Piece<T>::wide wide;
     __shared__ Stats parts[W > 1 ? W : 1];
-    __shared__ Key keys[TOP ? kRows : 1][TOP ? kLanes : 1];
+    __shared__ Key groups_of[TOP ? kRows : 1][TOP ? (W == 1 ? 64 : 128) : 1];
     __shared__ Key list[TOP ? kRows : 1][TOP ? kList : 1];
+    __shared__ vec pieces[TOP ? kRows : 1][TOP ? kPieces : 1];
+    __shared__ int places[TOP ? kRows : 1][TOP ? kPieces : 1];
     __shared__ Key threshold;
-    __shared__ int counts[kRows];
+    __shared__ int counts[kRows], listed[kRows];
     const int t = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
     const int64_t row = a.first + (int64_t)blockIdx.x * kRows + mine;
     if (row >= a.rows) return;                                  // (whole wavefronts, and none of a workgroup with barriers)
-    const int part = blockIdx.y, begin = part * a.span, end = a.classes - begin > a.span ? begin + a.span : a.classes;
     const T* const x = reinterpret_cast<const T*>(a.logits) + row * a.stride;
+    // the segment [begin, end) of this part, its pieces from `head` on
+    const int part = blockIdx.y, head = part * a.span - before_row(x), begin = max(head, 0), end = part + 1 < a.parts ? min(head + a.span, a.classes) : a.classes;
 
     Stats st{-kUsual, 0.f, 0.f};
-    float best = -__builtin_inff();
-    int best_at = begin + 8 * t < end ? begin + 8 * t : -1;
-    int j = begin + 8 * t;
-    {
-        // turns of U pieces, the next ones on their way; those that end inside a turn have -infinity behind the end
-        vec next[U];
-        auto request = [&](int from) {
-            if (from + kTurn - 8 * kLanes + 8 <= end) {
+    Key least = 0;                                              // at least `top` of the segment's numbers are not below
+    float least_value = -__builtin_inff();
+    vec next[U];
+    int j = head + N * t;
+    auto request = [&]() {
+        if (j >= begin && j + kTurn - N * kLanes + N <= end) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) next[u] = Eight<T>::load(x + from + 8 * kLanes * u);
-            } else {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int i = from + 8 * kLanes * u;
-                    if (i < end) next[u] = logits_at(x, i, end);
-                    else next[u] = (T)-__builtin_inff();
-                }
-            }
-        };
-        request(j);
-        while (j < end) {
-            float8v v[U];
-            float most[U];
-#pragma unroll
-            for (int u = 0; u < U; ++u) v[u] = widen<T>(next[u]);
-            const int now = j;
-            j += kTurn;
-            if (j < end) request(j);
+            for (int u = 0; u < U; ++u) next[u] = Piece<T>::load(x + j + N * kLanes * u);
+        } else {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                most[u] = largest(v[u]);
-                if constexpr (TOP)
+                const int i = j + N * kLanes * u;
+                if (i < end) next[u] = logits_at(x, i, begin, end);
+                else next[u] = (T)-__builtin_inff();
+            }
+        }
+    };
+    // a piece that reaches the threshold
+    auto keep = [&](vec piece, int at) {
+        const int place = atomicAdd(&listed[mine], 1);
+        if (place < kPieces) {
+            pieces[mine][place] = piece;
+            places[mine][place] = at;
+        }
+    };
+    // turns of U pieces, the next ones on their way
+    auto turn = [&](auto first) {
+        vec now[U];
+        float most[U];
+        const int at = j;
+#pragma unroll
+        for (int u = 0; u < U; ++u) now[u] = next[u];
+        j += kTurn;
+        if (j < end) request();
+#pragma unroll
+        for (int u = 0; u < U; ++u) most[u] = largest(widen<T>(now[u]));
+        if constexpr (TOP) {
+            if constexpr (decltype(first)::value) {
+                float best = most[0];
+                int best_at = at;
+#pragma unroll
+                for (int u = 1; u < U; ++u)
                     if (most[u] > best) {
                         best = most[u];
-                        best_at = now + 8 * kLanes * u;
+                        best_at = at + N * kLanes * u;
                     }
+                // (with the last class of the piece: not above what it stands for)
+                Key k = at < end ? key_of(best, min(best_at + N - 1, end - 1)) : 0;
+                const auto larger = [](Key p, Key q) { return p > q ? p : q; };
+                if constexpr (W > 1) {
+                    // 64 groups of the threads; 128, where 64 would leave many to list
+                    const bool few = a.top <= 16;
+                    k = larger(k, from_lane<kSwap1>(k));
+                    if (W == 16 || few) k = larger(k, from_lane<kSwap2>(k));
+                    if (W == 16) k = larger(k, from_lane<kMirror8>(k));
+                    if (W == 16 && few) k = larger(k, from_lane<kMirror16>(k));
+                    const int groups = few ? 64 : 128, of = kLanes / groups;
+                    if (t % of == 0) groups_of[0][t / of] = k;
+                    if (t == 0) threshold = 0;
+                    if (t == 0) counts[0] = listed[0] = 0;
+                    __syncthreads();
+                    if (t < groups) {
+                        k = groups_of[0][t];
+                        if (larger_than(k, groups_of[0], groups) == a.top - 1) threshold = k;
+                    }
+                    __syncthreads();
+                    least = threshold;
+                } else {
+                    groups_of[mine][t] = k;
+                    if (t == 0) counts[mine] = listed[mine] = 0;
+                    together<1>();
+                    const unsigned long long found = __ballot(larger_than(k, groups_of[mine], 64) == a.top - 1);
+                    if (found) least = of_lane(k, __builtin_ctzll(found));
+                }
+                // (equal numbers are zeros, of groups without a class: where there is no top-th, all are listed)
+                if (least) least_value = value_of(least);
             }
-            take<U, ENT>(st, v, most);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = at + N * kLanes * u;
+                if (most[u] >= least_value && i < end) keep(now[u], i);
+            }
         }
-    }
+        wide v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            // (widened again, so that 16 registers and not 32 are held meanwhile)
+            typedef int words __attribute__((ext_vector_type(4)));
+            words raw = __builtin_bit_cast(words, now[u]);
+            if constexpr (TOP) asm("" : "+v"(raw));
+            v[u] = widen<T>(__builtin_bit_cast(vec, raw));
+        }
+        take<U, ENT>(st, v, most);
+    };
+    request();
+    turn(std::true_type());
+    while (j < end) turn(std::false_type());
 
     auto merged = [&](Stats own) {
         own = wave_merge(own);
@@ -276,15 +343,16 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                 all.w += o.w;
             }
             return all;
-        } else return own;
+        } else {
+            together<1>();
+            return own;
+        }
     };
-    if constexpr (TOP) keys[mine][t] = best_at < 0 ? 0 : key_of(best, best_at + 7 < end ? best_at + 7 : end - 1);
-    if (t == 0) counts[mine] = 0;
     st = merged(st);
     if (!(st.m > -kUsual && st.m < kUsual)) {
         if constexpr (W > 1) __syncthreads();                   // (`parts` has been read)
         st = Stats{kLowest, 0.f, 0.f};
-        for (int i = begin + 8 * t; i < end; i += 8 * kLanes) take_unusual(st, widen<T>(logits_at(x, i, end)));
+        for (int i = head + N * t; i < end; i += N * kLanes) take_unusual(st, widen<T>(logits_at(x, i, begin, end)));
         st = merged(st);
     }
     const Row r = finish(st);
@@ -297,51 +365,25 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         } else write_row(a, row, x, r);
     }
     if constexpr (TOP) {
-        // a number that at least `top` of the segment's are not below
-        Key least;
-        if constexpr (W > 1) {
-            if (threadIdx.x < 64) {
-                Key k = keys[0][t];
-#pragma unroll
-                for (int i = 1; i < W; ++i) k = keys[0][64 * i + t] > k ? keys[0][64 * i + t] : k;
-                keys[0][t] = k;
-                together<1>();
-                k = ranked(k, keys[0], a.top - 1);
-                if (t == 0) threshold = k;
+        auto list_class = [&](Key q, int at) {
+            if (at >= begin && at < end && q >= least) {
+                const int place = atomicAdd(&counts[mine], 1);
+                if (place < kList) list[mine][place] = q;
             }
-            __syncthreads();
-            least = threshold;
-        } else {
-            together<1>();
-            least = ranked(keys[mine][t], keys[mine], a.top - 1);
-        }
+        };
         const bool plain = st.s == st.s;
-        if (plain && best_at >= 0 && key_of(best, best_at) >= least) {
-            auto look = [&](float8v v, int i) {
+        const int kept = listed[mine];
+        if (plain && kept <= kPieces) {
+            for (int i = t; i < kept * N; i += kLanes) {
+                const int at = places[mine][i / N] + i % N;
+                list_class(key_of((float)pieces[mine][i / N][i % N], at), at);
+            }
+        } else if (plain) {
+            for (int i = head + N * t; i < end; i += N * kLanes) {
+                const wide v = widen<T>(logits_at(x, i, begin, end));
+                if (largest(v) >= least_value)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const Key q = key_of(v[k], i + k);
-                    if (i + k < end && q >= least) {
-                        const int at = atomicAdd(&counts[mine], 1);
-                        if (at < kList) list[mine][at] = q;
-                    }
-                }
-            };
-            for (int from = begin + 8 * t; from < end; from += 2 * kTurn) {
-                vec v[2 * U];
-#pragma unroll
-                for (int u = 0; u < 2 * U; ++u) {
-                    const int i = from + 8 * kLanes * u;
-                    if (i < end) v[u] = logits_at(x, i, end);
-                }
-#pragma unroll
-                for (int u = 0; u < 2 * U; ++u) {
-                    const int i = from + 8 * kLanes * u;
-                    if (i < end) {
-                        const float8v f = widen<T>(v[u]);
-                        if (ordered(largest(f)) >= (unsigned)(least >> 32)) look(f, i);
-                    }
-                }
+                    for (int k = 0; k < N; ++k) list_class(key_of(v[k], i + k), i + k);
             }
         }
         together<W>();
@@ -349,8 +391,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         if (plain && count <= kList) {
             for (int i = t; i < count; i += kLanes) {
                 const Key q = list[mine][i];
-                int place = 0;
-                for (int o = 0; o < count; ++o) place += list[mine][o] > q;
+                const int place = larger_than(q, list[mine], count);
                 if (place < a.top) write_top(a, row, part, place, q, r);
             }
             if (t >= count && t < a.top) write_top(a, row, part, t, 0, r);       // (a part of fewer than `top` classes)
@@ -358,21 +399,21 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             Key before = ~(Key)0;
             for (int place = 0; place < a.top; ++place) {
                 Key k = 0;
-                for (int i = begin + 8 * t; i < end; i += 8 * kLanes) {
-                    const float8v v = widen<T>(logits_at(x, i, end));
+                for (int i = head + N * t; i < end; i += N * kLanes) {
+                    const wide v = widen<T>(logits_at(x, i, begin, end));
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) {
+                    for (int c = 0; c < N; ++c) {
                         const Key q = key_of(v[c], i + c);
-                        if (i + c < end && q < before && q > k) k = q;
+                        if (i + c >= begin && i + c < end && q < before && q > k) k = q;
                     }
                 }
                 k = wave_max(k);
                 if constexpr (W > 1) {
                     __syncthreads();
-                    if ((threadIdx.x & 63) == 0) keys[0][threadIdx.x >> 6] = k;
+                    if ((threadIdx.x & 63) == 0) groups_of[0][threadIdx.x >> 6] = k;
                     __syncthreads();
 #pragma unroll
-                    for (int i = 0; i < W; ++i) k = keys[0][i] > k ? keys[0][i] : k;
+                    for (int i = 0; i < W; ++i) k = groups_of[0][i] > k ? groups_of[0][i] : k;
                 }
                 if (t == 0) write_top(a, row, part, place, k, r);
                 before = k;
@@ -423,7 +464,7 @@ template <typename T> __global__ void __launch_bounds__(256) logprobs_join_kerne
 }
 
 // dlogits: W wavefronts have a row (W = 1), or a chunk of one.
-constexpr int kChunk = 8 * 4 * 256;
+constexpr int kTurns = 4;                        // pieces of a thread
 
 // What a row's gradients are made of: dlogits = 2^d (both + d of_entropy), d = x log2 e - shift, and dl more at the label.  shift is r + log2 s rounded; what that loses
 // is put into the other two.
@@ -450,11 +491,11 @@ __device__ __forceinline__ Slope slope_of(float m, float ls, float entropy, floa
     g.label = label;
     return g;
 }
-template <bool DH> __device__ __forceinline__ float8v logit_gradients(float8v v, const Slope& g)
+template <bool DH, typename V> __device__ __forceinline__ V logit_gradients(V v, const Slope& g)
 {
-    float8v o;
+    V o;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < (int)sizeof(V) / 4; ++k) {
         const float d = g.usual ? __builtin_fmaf(v[k], kLog2E, -g.shift) : __builtin_fmaf(v[k] - g.m, kLog2E, -g.shift);
         const float p = __builtin_amdgcn_exp2f(d);
         o[k] = DH ? p * __builtin_fmaf(fmaxf(d, kFar), g.of_entropy, g.both) : p * g.both;
@@ -464,44 +505,48 @@ template <bool DH> __device__ __forceinline__ float8v logit_gradients(float8v v,
 
 template <typename T, int W, bool DH> __global__ void __launch_bounds__(256) logprobs_backward_kernel(LogArgs a)
 {
-    constexpr int kLanes = 64 * W, kRows = 4 / W, U = 4;
-    typedef typename Eight<T>::vec vec;
+    constexpr int kLanes = 64 * W, kRows = 4 / W, N = Piece<T>::N, U = kTurns;
+    typedef typename Piece<T>::vec vec;
+    typedef typename Piece<T>::wide wide;
     const int t = threadIdx.x % kLanes;
-    const int64_t items = W == 1 ? a.rows : a.rows * a.chunks;
+    const int64_t items = W == 1 ? a.rows : a.rows * a.parts;
     for (int64_t item = (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes; item < items; item += (int64_t)gridDim.x * kRows) {
         int64_t row = item;
-        int begin = 0, end = a.classes;
+        int part = 0;
         if constexpr (W > 1) {
-            row = items >> 31 ? item / a.chunks : (int64_t)((unsigned)item / (unsigned)a.chunks);
-            begin = (int)(item - row * a.chunks) * kChunk;
-            end = a.classes - begin > kChunk ? begin + kChunk : a.classes;
+            row = items >> 31 ? item / a.parts : (int64_t)((unsigned)item / (unsigned)a.parts);
+            part = (int)(item - row * a.parts);
         }
         const T* const x = reinterpret_cast<const T*>(a.logits) + row * a.stride;
         T* const out = reinterpret_cast<T*>(a.dlogits) + row * a.dstride;
+        const int head = part * a.span - before_row(x), begin = max(head, 0), end = W > 1 ? min(head + a.span, a.classes) : a.classes;
         const float m = a.kept[3 * row], entropy = a.kept[3 * row + 2], dh = DH ? a.dentropy[row] : 0.f;
         const int label = a.dlogprob ? a.labels[row] : -1;
         const Slope g = slope_of(m, a.kept[3 * row + 1], entropy, label < 0 ? 0.f : label >= a.classes ? __builtin_nanf("") : a.dlogprob[row], dh, label);
         const bool empty = m == -__builtin_inff() && g.label < a.classes;
-        for (int j = begin + 8 * t; j < end; j += 8 * kLanes * U) {
-            vec v[U];
+        auto gradients = [&](vec v, int i) {
+            wide o = logit_gradients<DH>(widen<T>(v), g);
+            if (g.label >= 0 && (unsigned)(g.label - i) < (unsigned)N) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = j + 8 * kLanes * u;
-                if (i < end) v[u] = logits_at(x, i, end);
+                for (int k = 0; k < N; ++k) o[k] += k == g.label - i ? g.dl : 0.f;
             }
+            if (empty) o = 0.f;
+            return narrow<T>(o);
+        };
+        for (int j = head + N * t; j < end; j += N * kLanes * U) {
+            if (j >= begin && j + N * kLanes * (U - 1) + N <= end) {
+                vec v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = j + 8 * kLanes * u;
-                if (i >= end) continue;
-                float8v o = logit_gradients<DH>(widen<T>(v[u]), g);
-                if ((unsigned)(g.label - i) < 8u) {
+                for (int u = 0; u < U; ++u) v[u] = Piece<T>::load(x + j + N * kLanes * u);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) o[k] += k == g.label - i ? g.dl : 0.f;
+                for (int u = 0; u < U; ++u) Piece<T>::store(out + j + N * kLanes * u, gradients(v[u], j + N * kLanes * u));
+            } else {
+#pragma unroll 1
+                for (int i = j; i < end && i < j + N * kLanes * U; i += N * kLanes) {
+                    const vec o = gradients(logits_at(x, i, begin, end), i);
+                    if (i >= begin && i + N <= end) Piece<T>::store(out + i, o);
+                    else Piece<T>::store_part(out, i, begin, end, o);
                 }
-                if (empty) o = 0.f;
-                const vec w = narrow<T>(o);
-                if (i + 8 <= end) Eight<T>::store(out + i, w);
-                else Eight<T>::store_part(out + i, w, end - i);
             }
         }
     }
@@ -519,7 +564,7 @@ bool valid(const bmgd_logprobs_config& c)
     return c.classes >= 1 && c.classes <= (1 << 24) && known_type(c.dtype) && c.top >= 0 && c.top <= kMaxTop && c.top <= c.classes;
 }
 
-constexpr int kWide = 16384;                     // a part of a row has this many classes or more
+constexpr int kWide = 8192;                     // a part of a row has this many classes or more
 
 // Parts of a row, where few rows would leave compute units idle.
 int parts_of(int64_t classes, int64_t rows)
@@ -528,7 +573,7 @@ int parts_of(int64_t classes, int64_t rows)
     return (int)std::max<int64_t>(parts, 1);
 }
 // classes of a part: whole pieces of eight
-int span_of(int64_t classes, int parts) { return (int)((classes + parts - 1) / parts + 7) / 8 * 8; }
+int span_of(int64_t classes, int parts) { return (int)((classes + 7 + parts - 1) / parts + 7) / 8 * 8; }
 
 size_t stats_bytes(int64_t rows, int parts) { return ((size_t)rows * parts * 3 * sizeof(float) + 255) / 256 * 256; }
 
@@ -610,7 +655,8 @@ BMGD_API int bmgd_logprobs_forward(const bmgd_logprobs_config* cfg, int64_t rows
             }
         };
         auto shaped = [&](auto top, auto ent) {
-            if (a.span <= 2048) launch(std::integral_constant<int, 1>(), top, ent);
+            // (of 64 groups the 64th largest leaves 300 to list, now and then more than the list holds)
+            if (a.span <= 2048 && (a.top <= 16 || a.classes <= kList)) launch(std::integral_constant<int, 1>(), top, ent);
             else if (a.span <= 16384 || rows * a.parts > 512) launch(std::integral_constant<int, 4>(), top, ent);
             else launch(std::integral_constant<int, 16>(), top, ent);
         };
@@ -652,7 +698,9 @@ BMGD_API int bmgd_logprobs_backward(const bmgd_logprobs_config* cfg, int64_t row
     a.dentropy = t->dentropy;
     a.rows = rows;
     a.classes = (int)cfg->classes;
-    a.chunks = (int)((cfg->classes + kChunk - 1) / kChunk);
+    const int turn = 256 * kTurns * (int)(16 / size_of(cfg->dtype));
+    a.parts = (int)((cfg->classes + 7 + turn - 1) / turn);
+    a.span = span_of(cfg->classes, a.parts);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
@@ -660,7 +708,7 @@ BMGD_API int bmgd_logprobs_backward(const bmgd_logprobs_config* cfg, int64_t row
         auto launch = [&](auto dh) {
             constexpr bool DH = decltype(dh)::value;
             if (cfg->classes <= 2048) hipLaunchKernelGGL((logprobs_backward_kernel<T, 1, DH>), dim3((unsigned)std::min((rows + 3) / 4, most)), dim3(256), 0, s, a);
-            else hipLaunchKernelGGL((logprobs_backward_kernel<T, 4, DH>), dim3((unsigned)std::min(rows * a.chunks, most)), dim3(256), 0, s, a);
+            else hipLaunchKernelGGL((logprobs_backward_kernel<T, 4, DH>), dim3((unsigned)std::min(rows * a.parts, most)), dim3(256), 0, s, a);
         };
         if (a.dentropy) launch(std::true_type());
         else launch(std::false_type());

@@ -3,7 +3,7 @@
 //      s = x + residual, rounded;  r = (mean s^2 + eps)^(-1/2);  y = s w r;  codes = rint(127 s w / max|s w|), scale = max|s w| r / 127
 //      dx = r (w dy - s r^2 mean(w dy s)) + dsum;  dw = sum over the rows of dy s r
 //
-// A row is read once: W wavefronts hold it in registers, NV pieces of eight elements a lane, while its sum (and largest element) is formed, and write the
+// A row is read once: W wavefronts hold it in registers, NV pieces of 16 bytes a lane, while its sum (and largest element) is formed, and write the
 // result from there.  The s that is normed is the rounded one, which the stream goes on with and a backward pass reads.  Codes come from s w alone (r
 // is common to a row) in 64 bits: products of 16-bit elements are exact, so values next to the middle of two codes go where the definition says.
 #include "operator_calls.h"
@@ -54,8 +54,9 @@ template <typename T> __device__ __forceinline__ typename Largest<T>::bits size_
 
 constexpr double kLeastRow = 0x1p-118;         // max / 127 of a row that is held stays a normal number
 
-// Eight codes at any address.
+// Eight codes, or four, at any address.
 struct __attribute__((packed)) Codes8 { unsigned long long v; };
+struct __attribute__((packed)) Codes4 { unsigned v; };
 
 __device__ __forceinline__ unsigned code_of(double v, double inv)
 {
@@ -91,43 +92,57 @@ template <int W, typename V> __device__ __forceinline__ V row_max(V v, V* shared
     return v;
 }
 
-template <typename T> __device__ __forceinline__ typename Eight<T>::vec piece(const T* p, int j, int n)
+template <typename T> __device__ __forceinline__ typename Piece<T>::vec piece(const T* p, int j, int n)
 {
-    return j + 8 <= n ? Eight<T>::load(p + j) : Eight<T>::load_part(p + j, n - j, (T)0.f);
+    return j + Piece<T>::N <= n ? Piece<T>::load(p + j) : Piece<T>::load_part(p, j, 0, n, (T)0.f);
 }
-template <typename T> __device__ __forceinline__ void put(T* p, int j, int n, typename Eight<T>::vec v)
+template <typename T> __device__ __forceinline__ void put(T* p, int j, int n, typename Piece<T>::vec v)
 {
-    if (j + 8 <= n) Eight<T>::store(p + j, v);
-    else Eight<T>::store_part(p + j, v, n - j);
+    if (j + Piece<T>::N <= n) Piece<T>::store(p + j, v);
+    else Piece<T>::store_part(p, j, 0, n, v);
 }
-__device__ __forceinline__ void put_codes(char* p, int j, int n, unsigned long long v)
+template <int N> __device__ __forceinline__ void put_codes(char* p, int j, int n, unsigned long long v)
 {
-    if (j + 8 <= n) reinterpret_cast<Codes8*>(p + j)->v = v;
+    if (j + N <= n) {
+        if constexpr (N == 8) reinterpret_cast<Codes8*>(p + j)->v = v;
+        else reinterpret_cast<Codes4*>(p + j)->v = (unsigned)v;
+    }
     else
         for (int k = 0; j + k < n; ++k) p[j + k] = (char)(v >> 8 * k);
 }
 
-// s of the piece at j; `sum` receives it
-template <typename T> __device__ __forceinline__ typename Eight<T>::vec summed(const NormArgs& a, int64_t row, int j)
+// the sums of a piece's columns
+template <typename T> __device__ __forceinline__ void put_sums(float* p, int j, int n, typename Piece<T>::wide v)
 {
-    typename Eight<T>::vec v = piece(row_of<T>(a.x, row), j, a.n);
+    typedef float loose __attribute__((ext_vector_type(Piece<T>::N), aligned(4)));
+    if (j + Piece<T>::N <= n) *reinterpret_cast<loose*>(p + j) = v;
+    else
+#pragma unroll
+        for (int k = 0; k < Piece<T>::N; ++k)
+            if (j + k < n) p[j + k] = v[k];
+}
+
+// s of the piece at j; `sum` receives it
+template <typename T> __device__ __forceinline__ typename Piece<T>::vec summed(const NormArgs& a, int64_t row, int j)
+{
+    typename Piece<T>::vec v = piece(row_of<T>(a.x, row), j, a.n);
     if (a.residual.data) v = narrow<T>(widen<T>(v) + widen<T>(piece(row_of<T>(a.residual, row), j, a.n)));
     if (a.sum.data) put(row_of<T>(a.sum, row), j, a.n, v);
     return v;
 }
 
-template <typename T> __device__ __forceinline__ void write_y(const NormArgs& a, int64_t row, int j, typename Eight<T>::vec s, typename Eight<T>::vec w, float r)
+template <typename T> __device__ __forceinline__ void write_y(const NormArgs& a, int64_t row, int j, typename Piece<T>::vec s, typename Piece<T>::vec w, float r)
 {
     put(row_of<T>(a.y, row), j, a.n, narrow<T>(widen<T>(s) * widen<T>(w) * r));
 }
 
-template <typename T> __device__ __forceinline__ void write_codes(const NormArgs& a, int64_t row, int j, typename Eight<T>::vec s, typename Eight<T>::vec w, double inv)
+template <typename T> __device__ __forceinline__ void write_codes(const NormArgs& a, int64_t row, int j, typename Piece<T>::vec s, typename Piece<T>::vec w, double inv)
 {
     typedef typename Largest<T>::value value;
     unsigned long long c = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) c |= (unsigned long long)code_of((double)((value)s[k] * (value)w[k]), inv) << 8 * k;
-    put_codes(row_of<char>(a.codes, row), j, a.n, c);
+    for (int k = 0; k < Piece<T>::N; ++k) c |= (unsigned long long)code_of((double)((value)s[k] * (value)w[k]), inv) << 8 * k;
+    put_codes<Piece<T>::N>(row_of<char>(a.codes, row), j, a.n, c);
 }
 
 // r of a row from its sum of squares
@@ -149,11 +164,11 @@ template <typename T> __device__ __forceinline__ double scale_of(typename Larges
     return 1.0 / (double)v * 127.0;
 }
 
-template <typename T> __device__ __forceinline__ typename Eight<T>::vec ones()
+template <typename T> __device__ __forceinline__ typename Piece<T>::vec ones()
 {
-    typename Eight<T>::vec w;
+    typename Piece<T>::vec w;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) w[k] = (T)1.f;
+    for (int k = 0; k < Piece<T>::N; ++k) w[k] = (T)1.f;
     return w;
 }
 
@@ -169,41 +184,41 @@ template <typename T, int W, int NV> __global__ void __launch_bounds__(block_of(
     const int t = threadIdx.x % kLanes;
     const int64_t row = a.first + (int64_t)blockIdx.x * kRows + threadIdx.x / kLanes;
     if (row >= a.rows) return;                                  // (whole wavefronts, and none of a workgroup with barriers)
-    typename Eight<T>::vec s[NV], w[NV];
+    typename Piece<T>::vec s[NV], w[NV];
     float squares = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int j = 8 * (t + i * kLanes);
+        const int j = Piece<T>::N * (t + i * kLanes);
         if (j < a.n) {
             s[i] = piece(row_of<T>(a.x, row), j, a.n);
             w[i] = a.weight ? piece(reinterpret_cast<const T*>(a.weight), j, a.n) : ones<T>();
         }
     }
     if (a.residual.data) {
-        typename Eight<T>::vec q[NV];
+        typename Piece<T>::vec q[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = 8 * (t + i * kLanes);
+            const int j = Piece<T>::N * (t + i * kLanes);
             if (j < a.n) q[i] = piece(row_of<T>(a.residual, row), j, a.n);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = 8 * (t + i * kLanes);
+            const int j = Piece<T>::N * (t + i * kLanes);
             if (j < a.n) s[i] = narrow<T>(widen<T>(s[i]) + widen<T>(q[i]));
         }
     }
     bits top = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int j = 8 * (t + i * kLanes);
+        const int j = Piece<T>::N * (t + i * kLanes);
         if (j >= a.n) continue;
         if (a.sum.data) put(row_of<T>(a.sum, row), j, a.n, s[i]);
-        const float8v v = widen<T>(s[i]);
+        const typename Piece<T>::wide v = widen<T>(s[i]);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) squares = __builtin_fmaf(v[k], v[k], squares);
+        for (int k = 0; k < Piece<T>::N; ++k) squares = __builtin_fmaf(v[k], v[k], squares);
         if (a.codes.data) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < Piece<T>::N; ++k) {
                 const bits b = size_bits<T>((value)s[i][k] * (value)w[i][k]);
                 if (j + k < a.n) top = b > top ? b : top;
             }
@@ -214,7 +229,7 @@ template <typename T, int W, int NV> __global__ void __launch_bounds__(block_of(
     if (a.y.data) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = 8 * (t + i * kLanes);
+            const int j = Piece<T>::N * (t + i * kLanes);
             if (j < a.n) write_y<T>(a, row, j, s[i], w[i], r);
         }
     }
@@ -224,7 +239,7 @@ template <typename T, int W, int NV> __global__ void __launch_bounds__(block_of(
         if (t == 0) a.scales[row] = scale;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = 8 * (t + i * kLanes);
+            const int j = Piece<T>::N * (t + i * kLanes);
             if (j < a.n) write_codes<T>(a, row, j, s[i], w[i], inv);
         }
     }
@@ -242,15 +257,15 @@ template <typename T> __global__ void __launch_bounds__(kLong) norm_forward_long
     const int64_t row = a.first + blockIdx.x;
     float squares = 0.f;
     bits top = 0;
-    for (int j = 8 * threadIdx.x; j < a.n; j += 8 * kLong) {
-        const typename Eight<T>::vec s = summed<T>(a, row, j);
-        const float8v v = widen<T>(s);
+    for (int j = Piece<T>::N * threadIdx.x; j < a.n; j += Piece<T>::N * kLong) {
+        const typename Piece<T>::vec s = summed<T>(a, row, j);
+        const typename Piece<T>::wide v = widen<T>(s);
 #pragma unroll
-        for (int k = 0; k < 8; ++k) squares = __builtin_fmaf(v[k], v[k], squares);
+        for (int k = 0; k < Piece<T>::N; ++k) squares = __builtin_fmaf(v[k], v[k], squares);
         if (a.codes.data) {
-            const typename Eight<T>::vec w = a.weight ? piece(reinterpret_cast<const T*>(a.weight), j, a.n) : ones<T>();
+            const typename Piece<T>::vec w = a.weight ? piece(reinterpret_cast<const T*>(a.weight), j, a.n) : ones<T>();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
+            for (int k = 0; k < Piece<T>::N; ++k) {
                 const bits b = size_bits<T>((value)s[k] * (value)w[k]);
                 if (j + k < a.n) top = b > top ? b : top;
             }
@@ -264,22 +279,23 @@ template <typename T> __global__ void __launch_bounds__(kLong) norm_forward_long
         inv = scale_of<T>(row_max<kLongWaves>(top, tops), r, &scale);
         if (threadIdx.x == 0) a.scales[row] = scale;
     }
-    for (int j = 8 * threadIdx.x; j < a.n; j += 8 * kLong) {
-        typename Eight<T>::vec s;
+    for (int j = Piece<T>::N * threadIdx.x; j < a.n; j += Piece<T>::N * kLong) {
+        typename Piece<T>::vec s;
         if (a.sum.data) s = piece(row_of<T>(a.sum, row), j, a.n);
         else {
             s = piece(row_of<T>(a.x, row), j, a.n);
             if (a.residual.data) s = narrow<T>(widen<T>(s) + widen<T>(piece(row_of<T>(a.residual, row), j, a.n)));
         }
-        const typename Eight<T>::vec w = a.weight ? piece(reinterpret_cast<const T*>(a.weight), j, a.n) : ones<T>();
+        const typename Piece<T>::vec w = a.weight ? piece(reinterpret_cast<const T*>(a.weight), j, a.n) : ones<T>();
         if (a.y.data) write_y<T>(a, row, j, s, w, r);
         if (a.codes.data) write_codes<T>(a, row, j, s, w, inv);
     }
 }
 
-template <typename T> __device__ __forceinline__ float8v input_gradient(float8v d, float8v s, float r, float c, typename Eight<T>::vec dsum, bool has)
+template <typename T>
+__device__ __forceinline__ typename Piece<T>::wide input_gradient(typename Piece<T>::wide d, typename Piece<T>::wide s, float r, float c, typename Piece<T>::vec dsum, bool has)
 {
-    float8v v = (d - s * c) * r;
+    typename Piece<T>::wide v = (d - s * c) * r;
     if (has) v += widen<T>(dsum);
     return v;
 }
@@ -289,13 +305,13 @@ template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(
 {
     constexpr int kLanes = 64 * W, kRows = block_of(W) / kLanes;
     __shared__ float sums[2][16];
-    __shared__ float joined[DW && kRows > 1 ? kRows * NV * 8 * kLanes : 1];
+    __shared__ float joined[DW && kRows > 1 ? kRows * NV * Piece<T>::N * kLanes : 1];
     const int t = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
-    typename Eight<T>::vec w[NV];
-    float8v dw[NV];
+    typename Piece<T>::vec w[NV];
+    typename Piece<T>::wide dw[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int j = 8 * (t + i * kLanes);
+        const int j = Piece<T>::N * (t + i * kLanes);
         w[i] = j < a.n && a.weight ? piece(reinterpret_cast<const T*>(a.weight), j, a.n) : ones<T>();
         dw[i] = 0.f;
     }
@@ -303,10 +319,10 @@ template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(
     for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += (int64_t)gridDim.x * kRows, turn ^= 1) {
         const int64_t row = first + mine;
         if (row >= a.rows) break;                               // (only without barriers)
-        typename Eight<T>::vec s[NV], dy[NV], ds[NV];
+        typename Piece<T>::vec s[NV], dy[NV], ds[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = 8 * (t + i * kLanes);
+            const int j = Piece<T>::N * (t + i * kLanes);
             if (j < a.n) {
                 s[i] = piece(row_of<T>(a.x, row), j, a.n);
                 dy[i] = piece(row_of<T>(a.dy, row), j, a.n);
@@ -317,21 +333,21 @@ template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(
         float along = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = 8 * (t + i * kLanes);
+            const int j = Piece<T>::N * (t + i * kLanes);
             if (j >= a.n) continue;
-            const float8v v = widen<T>(s[i]), g = widen<T>(dy[i]), f = widen<T>(w[i]);
+            const typename Piece<T>::wide v = widen<T>(s[i]), g = widen<T>(dy[i]), f = widen<T>(w[i]);
             // (a last piece has zeros behind the row's end)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) along = __builtin_fmaf(g[k] * f[k], v[k], along);
+            for (int k = 0; k < Piece<T>::N; ++k) along = __builtin_fmaf(g[k] * f[k], v[k], along);
             if constexpr (DW) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) dw[i][k] = __builtin_fmaf(g[k], v[k] * r, dw[i][k]);
+                for (int k = 0; k < Piece<T>::N; ++k) dw[i][k] = __builtin_fmaf(g[k], v[k] * r, dw[i][k]);
             }
         }
         const float c = row_sum<W>(along, sums[turn]) * a.inv_n * r * r;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int j = 8 * (t + i * kLanes);
+            const int j = Piece<T>::N * (t + i * kLanes);
             if (j < a.n)
                 put(row_of<T>(a.dx, row), j, a.n, narrow<T>(input_gradient<T>(widen<T>(dy[i]) * widen<T>(w[i]), widen<T>(s[i]), r, c, ds[i], a.dsum.data != nullptr)));
         }
@@ -341,20 +357,20 @@ template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(
         if constexpr (kRows == 1) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int j = 8 * (t + i * kLanes);
-                if (j < a.n) put(to, j, a.n, dw[i]);
+                const int j = Piece<T>::N * (t + i * kLanes);
+                if (j < a.n) put_sums<T>(to, j, a.n, dw[i]);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) joined[((mine * NV + i) * 8 + k) * kLanes + t] = dw[i][k];
+                for (int k = 0; k < Piece<T>::N; ++k) joined[((mine * NV + i) * Piece<T>::N + k) * kLanes + t] = dw[i][k];
             __syncthreads();
-            for (int q = threadIdx.x; q < NV * 8 * kLanes; q += block_of(W)) {
-                const int at = q % kLanes, k = q / kLanes % 8, i = q / kLanes / 8, j = 8 * (at + i * kLanes) + k;
+            for (int q = threadIdx.x; q < NV * Piece<T>::N * kLanes; q += block_of(W)) {
+                const int at = q % kLanes, k = q / kLanes % Piece<T>::N, i = q / kLanes / Piece<T>::N, j = Piece<T>::N * (at + i * kLanes) + k;
                 float v = 0.f;
 #pragma unroll
-                for (int m = 0; m < kRows; ++m) v += joined[m * NV * 8 * kLanes + q];
+                for (int m = 0; m < kRows; ++m) v += joined[m * NV * Piece<T>::N * kLanes + q];
                 if (j < a.n) to[j] = v;
             }
         }
@@ -369,15 +385,15 @@ template <typename T> __global__ void __launch_bounds__(kLong) norm_backward_lon
     const T *const x = row_of<T>(a.x, row), *const dy = row_of<T>(a.dy, row), *const weight = reinterpret_cast<const T*>(a.weight);
     const float r = a.rstd[row];
     float along = 0.f;
-    for (int j = 8 * threadIdx.x; j < a.n; j += 8 * kLong) {
-        const float8v v = widen<T>(piece(x, j, a.n)), g = widen<T>(piece(dy, j, a.n)), f = widen<T>(weight ? piece(weight, j, a.n) : ones<T>());
+    for (int j = Piece<T>::N * threadIdx.x; j < a.n; j += Piece<T>::N * kLong) {
+        const typename Piece<T>::wide v = widen<T>(piece(x, j, a.n)), g = widen<T>(piece(dy, j, a.n)), f = widen<T>(weight ? piece(weight, j, a.n) : ones<T>());
 #pragma unroll
-        for (int k = 0; k < 8; ++k) along = __builtin_fmaf(g[k] * f[k], v[k], along);
+        for (int k = 0; k < Piece<T>::N; ++k) along = __builtin_fmaf(g[k] * f[k], v[k], along);
     }
     const float c = row_sum<kLongWaves>(along, sums) * a.inv_n * r * r;
-    for (int j = 8 * threadIdx.x; j < a.n; j += 8 * kLong) {
-        const float8v v = widen<T>(piece(x, j, a.n)), d = widen<T>(piece(dy, j, a.n)) * widen<T>(weight ? piece(weight, j, a.n) : ones<T>());
-        typename Eight<T>::vec ds = {};
+    for (int j = Piece<T>::N * threadIdx.x; j < a.n; j += Piece<T>::N * kLong) {
+        const typename Piece<T>::wide v = widen<T>(piece(x, j, a.n)), d = widen<T>(piece(dy, j, a.n)) * widen<T>(weight ? piece(weight, j, a.n) : ones<T>());
+        typename Piece<T>::vec ds = {};
         if (a.dsum.data) ds = piece(row_of<T>(a.dsum, row), j, a.n);
         put(row_of<T>(a.dx, row), j, a.n, narrow<T>(input_gradient<T>(d, v, r, c, ds, a.dsum.data != nullptr)));
     }
@@ -386,16 +402,16 @@ template <typename T> __global__ void __launch_bounds__(kLong) norm_backward_lon
 // Their part of dw: a thread has eight columns and every gridDim.y-th row.
 template <typename T> __global__ void __launch_bounds__(64) norm_columns_kernel(NormArgs a)
 {
-    const int j = 8 * (blockIdx.x * 64 + threadIdx.x);
+    const int j = Piece<T>::N * (blockIdx.x * 64 + threadIdx.x);
     if (j >= a.n) return;
-    float8v dw = 0.f;
+    typename Piece<T>::wide dw = 0.f;
     for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        const float8v v = widen<T>(piece(row_of<T>(a.x, row), j, a.n)), g = widen<T>(piece(row_of<T>(a.dy, row), j, a.n));
+        const typename Piece<T>::wide v = widen<T>(piece(row_of<T>(a.x, row), j, a.n)), g = widen<T>(piece(row_of<T>(a.dy, row), j, a.n));
         const float r = a.rstd[row];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) dw[k] = __builtin_fmaf(g[k], v[k] * r, dw[k]);
+        for (int k = 0; k < Piece<T>::N; ++k) dw[k] = __builtin_fmaf(g[k], v[k] * r, dw[k]);
     }
-    put(a.partial + (int64_t)blockIdx.y * a.n, j, a.n, dw);
+    put_sums<T>(a.partial + (int64_t)blockIdx.y * a.n, j, a.n, dw);
 }
 
 // dweight from the parts, always in the same order: a workgroup has 32 columns, 32 threads of it every 32nd part of one of them.
@@ -426,37 +442,37 @@ struct ValueArgs {
     Side codes, out;
     const float* scales;
     int64_t rows;
-    int n, per_row;         // pieces of eight
+    int n, per_row;         // pieces of Piece<T>::N
 };
 
-// Two pieces of eight codes a thread.
 template <typename T> __global__ void __launch_bounds__(256) values_kernel(ValueArgs a)
 {
+    constexpr int N = Piece<T>::N;
     const int64_t pieces = a.rows * a.per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
         const int64_t row = pieces >> 31 ? i / a.per_row : (int64_t)((unsigned)i / (unsigned)a.per_row);
-        const int j = 8 * (int)(i - row * a.per_row);
+        const int j = N * (int)(i - row * a.per_row);
         const char* const from = row_of<char>(a.codes, row) + j;
         unsigned long long c = 0;
-        if (j + 8 <= a.n) c = reinterpret_cast<const Codes8*>(from)->v;
+        if (j + N <= a.n) c = N == 8 ? reinterpret_cast<const Codes8*>(from)->v : reinterpret_cast<const Codes4*>(from)->v;
         else
             for (int k = 0; j + k < a.n; ++k) c |= (unsigned long long)(unsigned char)from[k] << 8 * k;
         const float scale = a.scales[row];
-        float8v v;
+        typename Piece<T>::wide v;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = scale * (float)(signed char)(c >> 8 * k);
+        for (int k = 0; k < N; ++k) v[k] = scale * (float)(signed char)(c >> 8 * k);
         put(row_of<T>(a.out, row), j, a.n, narrow<T>(v));
     }
 }
 
-constexpr int kRegisterColumns = 8 * 4 * 64 * 16;               // rows up to this length are kept in registers,
-constexpr int kGradientColumns = 8 * 2 * 64 * 16;               // and these in a backward call, which has three rows at a time and dw
+constexpr int kRegisterPieces = 4 * 64 * 16;                    // rows up to this length are kept in registers,
+constexpr int kGradientPieces = 2 * 64 * 16;                    // and these in a backward call, which has three rows at a time and dw
 constexpr int kMaxParts = 512;                                  // of dweight
 
 // f(constant T, W, NV): wavefronts for a row and pieces of eight for a lane
 template <typename T, typename F> void with_shape(int n, int64_t rows, F f)
 {
-    const int pieces = (n + 7) / 8;
+    const int pieces = (n + Piece<T>::N - 1) / Piece<T>::N;
 #define SHAPE(W, NV) f(std::integral_constant<int, W>(), std::integral_constant<int, NV>())
     if (pieces <= 64) SHAPE(1, 1);
     else if (pieces <= 128) SHAPE(1, 2);
@@ -477,10 +493,12 @@ template <typename F> void with_type(int dtype, F f)
 
 bool valid(const bmgd_norm_config& c) { return c.n >= 1 && c.n <= (1 << 20) && known_type(c.dtype) && c.eps >= 0.0 && isfinite(c.eps) && isfinite((float)c.eps); }
 
+int64_t pieces_of(const bmgd_norm_config& c) { return (c.n * (int64_t)size_of(c.dtype) + 15) / 16; }
+
 // Workgroups of a backward call, each of which leaves a part of dweight.
-int64_t parts_of(int64_t n, int64_t rows)
+int64_t parts_of(const bmgd_norm_config& c, int64_t rows)
 {
-    const int64_t at_once = n <= 1024 ? 4 : 1;                  // rows of a workgroup
+    const int64_t at_once = pieces_of(c) <= 128 ? 4 : 1;        // rows of a workgroup
     return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, kMaxParts));
 }
 
@@ -517,7 +535,7 @@ extern "C" {
 BMGD_API size_t bmgd_norm_workspace_bytes(const bmgd_norm_config* cfg, int64_t rows)
 {
     if (!cfg || !valid(*cfg) || rows < 0 || rows > kMaxCallRows) return 0;
-    return ((size_t)parts_of(cfg->n, rows) * (size_t)cfg->n * sizeof(float) + 255) / 256 * 256;
+    return ((size_t)parts_of(*cfg, rows) * (size_t)cfg->n * sizeof(float) + 255) / 256 * 256;
 }
 
 BMGD_API int bmgd_norm_forward(const bmgd_norm_config* cfg, int64_t rows, const bmgd_norm_tensors* t, void* stream)
@@ -556,7 +574,7 @@ BMGD_API int bmgd_norm_forward(const bmgd_norm_config* cfg, int64_t rows, const 
         typedef decltype(type) T;
         for (a.first = 0; a.first < rows; a.first += kRowsOfLaunch) {
             const int64_t now = std::min(rows - a.first, kRowsOfLaunch);
-            if (cfg->n > kRegisterColumns) {
+            if (pieces_of(*cfg) > kRegisterPieces) {
                 hipLaunchKernelGGL(norm_forward_long_kernel<T>, dim3((unsigned)now), dim3(kLong), 0, s, a);
                 continue;
             }
@@ -606,18 +624,18 @@ BMGD_API int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const
     a.dsum = side(t->dsum);
     a.dx = side(t->dx);
     a.partial = static_cast<float*>(t->workspace);
-    const int64_t parts = parts_of(cfg->n, rows);
+    const int64_t parts = parts_of(*cfg, rows);
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
-        if (cfg->n > kGradientColumns) {
+        if (pieces_of(*cfg) > kGradientPieces) {
             if (t->dweight)                                     // (first: dx may be dy)
-                hipLaunchKernelGGL(norm_columns_kernel<T>, dim3((unsigned)((cfg->n + 511) / 512), (unsigned)parts), dim3(64), 0, s, a);
+                hipLaunchKernelGGL(norm_columns_kernel<T>, dim3((unsigned)((pieces_of(*cfg) + 63) / 64), (unsigned)parts), dim3(64), 0, s, a);
             for (a.first = 0; a.first < rows; a.first += kRowsOfLaunch)
                 hipLaunchKernelGGL(norm_backward_long_kernel<T>, dim3((unsigned)std::min(rows - a.first, kRowsOfLaunch)), dim3(kLong), 0, s, a);
         } else {
             with_shape<T>(a.n, rows, [&](auto w, auto nv) {
                 constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-                if constexpr (8 * 64 * W * NV > kGradientColumns) return;
+                if constexpr (64 * W * NV > kGradientPieces) return;
                 else
                 if (t->dweight) hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, true>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
                 else hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, false>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
@@ -646,7 +664,7 @@ BMGD_API int bmgd_product_values(int64_t rows, int64_t n, const bmgd_matrix* cod
     q.address("scales", scales, rows > 0, 4);
     q.apart("out", out->data, codes->data);
     if (q.code != BMGD_OK || rows == 0) return q.code;
-    ValueArgs a{side(*codes), side(*out), scales, rows, (int)n, (int)((n + 7) / 8)};
+    ValueArgs a{side(*codes), side(*out), scales, rows, (int)n, (int)((n * (int64_t)size_of(dtype) + 15) / 16)};
     const unsigned groups = (unsigned)std::min<int64_t>((rows * a.per_row + 255) / 256, int64_t(1) << 20);
     with_type(dtype, [&](auto type) {
         typedef decltype(type) T;

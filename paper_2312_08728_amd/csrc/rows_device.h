@@ -9,39 +9,40 @@
 namespace bmgd {
 namespace {
 
-typedef float float8v __attribute__((ext_vector_type(8)));
-
-// Eight neighbouring elements at any multiple of an element's size: 16-bit ones are one instruction, 32-bit ones two.
-template <typename T> struct Eight {
-    typedef T vec __attribute__((ext_vector_type(8)));
-    typedef T loose __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+// A piece: the neighbouring elements of 16 bytes, eight of 16 bits or four of 32.  At any multiple of an element's size one instruction (where it crosses a line of the
+// cache it takes longer).
+template <typename T> struct Piece {
+    static constexpr int N = 16 / sizeof(T);
+    typedef T vec __attribute__((ext_vector_type(N)));
+    typedef T loose __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+    typedef float wide __attribute__((ext_vector_type(N)));
     static __device__ __forceinline__ vec load(const T* p) { return *reinterpret_cast<const loose*>(p); }
     static __device__ __forceinline__ void store(T* p, vec v) { *reinterpret_cast<loose*>(p) = v; }
-    // the first `count` (1 to 7) of them; `fill` elsewhere
-    static __device__ __forceinline__ vec load_part(const T* p, int count, T fill)
+    // those of elements j, j + 1, ... that are in [begin, end); `fill` elsewhere
+    static __device__ __forceinline__ vec load_part(const T* p, int j, int begin, int end, T fill)
     {
         vec v;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = k < count ? p[k] : fill;
+        for (int k = 0; k < N; ++k) v[k] = j + k >= begin && j + k < end ? p[j + k] : fill;
         return v;
     }
-    static __device__ __forceinline__ void store_part(T* p, vec v, int count)
+    static __device__ __forceinline__ void store_part(T* p, int j, int begin, int end, vec v)
     {
 #pragma unroll
-        for (int k = 0; k < 8; ++k)
-            if (k < count) p[k] = v[k];
+        for (int k = 0; k < N; ++k)
+            if (j + k >= begin && j + k < end) p[j + k] = v[k];
     }
 };
 
-template <typename T> __device__ __forceinline__ float8v widen(typename Eight<T>::vec v)
+template <typename T> __device__ __forceinline__ typename Piece<T>::wide widen(typename Piece<T>::vec v)
 {
     if constexpr (std::is_same<T, float>::value) return v;
-    else return __builtin_convertvector(v, float8v);
+    else return __builtin_convertvector(v, typename Piece<T>::wide);
 }
-template <typename T> __device__ __forceinline__ typename Eight<T>::vec narrow(float8v v)
+template <typename T> __device__ __forceinline__ typename Piece<T>::vec narrow(typename Piece<T>::wide v)
 {
     if constexpr (std::is_same<T, float>::value) return v;
-    else return __builtin_convertvector(v, typename Eight<T>::vec);
+    else return __builtin_convertvector(v, typename Piece<T>::vec);
 }
 
 // The value of another lane of the same 16: lane ^ 1, lane ^ 2, 7 - lane of eight, 15 - lane.
