@@ -105,11 +105,11 @@ template <int W> __device__ __forceinline__ void together()
     }
 }
 
-// Which of `count` numbers are larger
+// How many of `count` numbers are larger
 __device__ __forceinline__ int larger_than(Key v, const Key* all, int count)
 {
     int larger = 0;
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < count; ++i) larger += all[i] > v;
     return larger;
 }
@@ -119,6 +119,23 @@ template <typename T> __device__ __forceinline__ int before_row(const T* x) { re
 template <typename T> __device__ __forceinline__ typename Piece<T>::vec logits_at(const T* x, int j, int begin, int end)
 {
     return j >= begin && j + Piece<T>::N <= end ? Piece<T>::load(x + j) : Piece<T>::load_part(x, j, begin, end, (T)-__builtin_inff());
+}
+
+// What is left of a segment [begin, end) beside its whole pieces: a piece that begins before it (at head), and one that ends behind it.  `whole`: where the
+// whole ones begin.
+struct Edges {
+    int whole, before, behind;                   // (kNowhere: none)
+};
+constexpr int kNowhere = 0x7fffffff;
+template <int N> __device__ __forceinline__ Edges edges_of(int head, int begin, int end)
+{
+    Edges e;
+    const bool early = head < begin;
+    const int last = head + (end - head) / N * N;
+    e.whole = early ? head + N : head;
+    e.before = early ? head : kNowhere;
+    e.behind = last < end && last >= e.whole ? last : kNowhere;
+    return e;
 }
 
 template <typename V> __device__ __forceinline__ float largest(V v)
@@ -182,12 +199,10 @@ __device__ __forceinline__ float logprob_of(const Row& r, float x)
     return __builtin_fmaf(lost - r.ls, kLn2, x - r.m);
 }
 
-template <typename T> __device__ __forceinline__ void write_row(const LogArgs& a, int64_t row, const T* x, const Row& r)
+// at_label: the logit of a label that is one of the classes
+__device__ __forceinline__ void write_row(const LogArgs& a, int64_t row, int label, float at_label, const Row& r)
 {
-    if (a.logprob) {
-        const int label = a.labels[row];
-        a.logprob[row] = label < 0 ? 0.f : label >= a.classes ? __builtin_nanf("") : logprob_of(r, (float)x[label]);
-    }
+    if (a.logprob) a.logprob[row] = label < 0 ? 0.f : label >= a.classes ? __builtin_nanf("") : logprob_of(r, at_label);
     if (a.entropy) a.entropy[row] = r.entropy;
     if (a.kept) {
         a.kept[3 * row] = r.m;
@@ -214,7 +229,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     typedef typename Piece<T>::vec vec;
     typedef typename Piece<T>::wide wide;
     __shared__ Stats parts[W > 1 ? W : 1];
-    __shared__ Key groups_of[TOP ? kRows : 1][TOP ? (W == 1 ? 64 : 128) : 1];
+    __shared__ Key groups_of[TOP ? kRows : 1][TOP ? (W == 1 ? 64 : 128) : 1];                  // (at most half as many as threads)
     __shared__ Key list[TOP ? kRows : 1][TOP ? kList : 1];
     __shared__ vec pieces[TOP ? kRows : 1][TOP ? kPieces : 1];
     __shared__ int places[TOP ? kRows : 1][TOP ? kPieces : 1];
@@ -227,22 +242,23 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     // the segment [begin, end) of this part, its pieces from `head` on
     const int part = blockIdx.y, head = part * a.span - before_row(x), begin = max(head, 0), end = part + 1 < a.parts ? min(head + a.span, a.classes) : a.classes;
 
+    const int label = a.logprob && a.parts == 1 ? a.labels[row] : -1;
     Stats st{-kUsual, 0.f, 0.f};
     Key least = 0;                                              // at least `top` of the segment's numbers are not below
-    float least_value = -__builtin_inff();
+    float least_value = -__builtin_inff(), seen = -__builtin_inff();
+    const Edges edge = edges_of<N>(head, begin, end);
+    // one of the pieces that are not whole, for the first two threads
+    const int edge_at = t == 0 ? edge.before : t == 1 ? edge.behind : kNowhere;
+    vec edge_piece = (vec)(T)-__builtin_inff();
+    if (edge_at != kNowhere) edge_piece = Piece<T>::load_part(x, edge_at, begin, end, (T)-__builtin_inff());
     vec next[U];
-    int j = head + N * t;
+    int j = edge.whole + N * t;
     auto request = [&]() {
-        if (j >= begin && j + kTurn - N * kLanes + N <= end) {
 #pragma unroll
-            for (int u = 0; u < U; ++u) next[u] = Piece<T>::load(x + j + N * kLanes * u);
-        } else {
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = j + N * kLanes * u;
-                if (i < end) next[u] = logits_at(x, i, begin, end);
-                else next[u] = (T)-__builtin_inff();
-            }
+        for (int u = 0; u < U; ++u) {
+            const int i = j + N * kLanes * u;
+            if (i + N <= end) next[u] = Piece<T>::load(x + i);
+            else next[u] = (T)-__builtin_inff();
         }
     };
     // a piece that reaches the threshold
@@ -261,7 +277,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
 #pragma unroll
         for (int u = 0; u < U; ++u) now[u] = next[u];
         j += kTurn;
-        if (j < end) request();
+        if (j + N <= end) request();
 #pragma unroll
         for (int u = 0; u < U; ++u) most[u] = largest(widen<T>(now[u]));
         if constexpr (TOP) {
@@ -275,24 +291,28 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                         best_at = at + N * kLanes * u;
                     }
                 // (with the last class of the piece: not above what it stands for)
-                Key k = at < end ? key_of(best, min(best_at + N - 1, end - 1)) : 0;
+                Key k = at + N <= end ? key_of(best, best_at + N - 1) : 0;
+                if (edge_at != kNowhere) {
+                    const Key of_edge = key_of(largest(widen<T>(edge_piece)), min(edge_at + N, end) - 1);
+                    k = of_edge > k ? of_edge : k;
+                }
                 const auto larger = [](Key p, Key q) { return p > q ? p : q; };
                 if constexpr (W > 1) {
-                    // 64 groups of the threads; 128, where 64 would leave many to list
+                    // 64 groups of four threads; 128 of two, where 64 would leave many to list.  The threads of a group share the counting of larger ones.
                     const bool few = a.top <= 16;
+                    const int of = few ? 4 : 2, each = kLanes / (of * of);
                     k = larger(k, from_lane<kSwap1>(k));
-                    if (W == 16 || few) k = larger(k, from_lane<kSwap2>(k));
-                    if (W == 16) k = larger(k, from_lane<kMirror8>(k));
-                    if (W == 16 && few) k = larger(k, from_lane<kMirror16>(k));
-                    const int groups = few ? 64 : 128, of = kLanes / groups;
+                    if (few) k = larger(k, from_lane<kSwap2>(k));
                     if (t % of == 0) groups_of[0][t / of] = k;
-                    if (t == 0) threshold = 0;
-                    if (t == 0) counts[0] = listed[0] = 0;
-                    __syncthreads();
-                    if (t < groups) {
-                        k = groups_of[0][t];
-                        if (larger_than(k, groups_of[0], groups) == a.top - 1) threshold = k;
+                    if (t == 0) {
+                        threshold = 0;
+                        counts[0] = listed[0] = 0;
                     }
+                    __syncthreads();
+                    int place = larger_than(k, groups_of[0] + t % of * each, each);
+                    place += from_lane<kSwap1>(place);
+                    if (few) place += from_lane<kSwap2>(place);
+                    if (place == a.top - 1) threshold = k;      // (the same from all of a group)
                     __syncthreads();
                     least = threshold;
                 } else {
@@ -304,11 +324,14 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                 }
                 // (equal numbers are zeros, of groups without a class: where there is no top-th, all are listed)
                 if (least) least_value = value_of(least);
+                if (edge_at != kNowhere && key_of(largest(widen<T>(edge_piece)), max(edge_at, begin)) >= least) keep(edge_piece, edge_at);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = at + N * kLanes * u;
-                if (most[u] >= least_value && i < end) keep(now[u], i);
+                // (later turns have higher classes than the threshold's: equal logits do not reach it)
+                const bool reaches = decltype(first)::value ? key_of(most[u], i) >= least : most[u] > least_value;
+                if (reaches && i + N <= end) keep(now[u], i);
             }
         }
         wide v[U];
@@ -321,10 +344,18 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             v[u] = widen<T>(__builtin_bit_cast(vec, raw));
         }
         take<U, ENT>(st, v, most);
+        seen = fmaxf(seen, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
     };
     request();
+    const float at_label = label >= 0 && label < a.classes ? (float)x[label] : 0.f;
     turn(std::true_type());
-    while (j < end) turn(std::false_type());
+    while (j + N <= end) turn(std::false_type());
+    if (edge_at != kNowhere) {
+        const wide v = widen<T>(edge_piece);
+        const float most = largest(v);
+        take<1, ENT>(st, &v, &most);
+        seen = fmaxf(seen, most);
+    }
 
     auto merged = [&](Stats own) {
         own = wave_merge(own);
@@ -351,9 +382,13 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     st = merged(st);
     if (!(st.m > -kUsual && st.m < kUsual)) {
         if constexpr (W > 1) __syncthreads();                   // (`parts` has been read)
+        const bool none = st.s == 0.f && merged(Stats{seen, 0.f, 0.f}).m == -__builtin_inff();
+        if constexpr (W > 1) __syncthreads();
         st = Stats{kLowest, 0.f, 0.f};
-        for (int i = head + N * t; i < end; i += N * kLanes) take_unusual(st, widen<T>(logits_at(x, i, begin, end)));
-        st = merged(st);
+        if (!none) {
+            for (int i = head + N * t; i < end; i += N * kLanes) take_unusual(st, widen<T>(logits_at(x, i, begin, end)));
+            st = merged(st);
+        }
     }
     const Row r = finish(st);
     if (t == 0) {
@@ -362,7 +397,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             to[0] = st.m;
             to[1] = st.s;
             to[2] = st.w;
-        } else write_row(a, row, x, r);
+        } else write_row(a, row, label, at_label, r);
     }
     if constexpr (TOP) {
         auto list_class = [&](Key q, int at) {
@@ -422,34 +457,48 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     }
 }
 
-// A row from its parts (at most 64).  Each part's classes are in falling order, so that the parts' n-th ones, n parts >= top, bound the top-th of the row from below.
+// A row from its parts (at most 64): all that it reads is asked for first.  Each part's classes are in falling order.  The top-th of a part is not above the top-th of the
+// row, nor is the h-th largest of the parts' n-th ones, where h is half of the parts and h n >= top (half of them may have nothing but -infinity).
 template <typename T> __global__ void __launch_bounds__(256) logprobs_join_kernel(LogArgs a)
 {
     extern __shared__ Key list[];
-    __shared__ Key threshold;
+    __shared__ Key bounds[64];
     __shared__ int count;
     const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, keys_of_row = a.parts * a.top;
     const float* const from = a.part_stats + row * a.parts * 3;
+    const Key* const keys = a.part_keys + row * keys_of_row;
+    const int label = a.logprob ? a.labels[row] : -1;
+    Key mine = (int)threadIdx.x < keys_of_row ? keys[threadIdx.x] : 0;
     Stats st{kLowest, 0.f, 0.f};                                // (of a size that no part with classes has: adds nothing)
     if (lane < a.parts) st = Stats{from[3 * lane], from[3 * lane + 1], from[3 * lane + 2]};
+    const int half = a.parts / 2, nth = (a.top + half - 1) / half;
+    Key bound = 0, last = 0;
+    if (a.top && lane < a.parts) {
+        bound = keys[lane * a.top + nth - 1];
+        last = keys[lane * a.top + a.top - 1];
+    }
+    const T* const x = reinterpret_cast<const T*>(a.logits) + row * a.stride;
+    const float at_label = label >= 0 && label < a.classes ? (float)x[label] : 0.f;
     st = wave_merge(st);
     const Row r = finish(st);
     if (threadIdx.x == 0) {
-        write_row(a, row, reinterpret_cast<const T*>(a.logits) + row * a.stride, r);
+        write_row(a, row, label, at_label, r);
         count = 0;
     }
     if (!a.top) return;
-    const Key* const keys = a.part_keys + row * a.parts * a.top;
-    if (threadIdx.x < 64) {
-        const int nth = (a.top + a.parts - 1) / a.parts;
-        const Key least = ~wave_max(lane < a.parts ? ~keys[lane * a.top + nth - 1] : (Key)0);
-        if (threadIdx.x == 0) threshold = least;
-    }
+    if (threadIdx.x < 64) bounds[lane] = bound;
     __syncthreads();
-    for (int i = threadIdx.x; i < a.parts * a.top; i += 256) {
-        const Key q = keys[i];
-        if (q && q >= threshold) list[atomicAdd(&count, 1)] = q;
+    // (parts' numbers differ but for zeros)
+    const unsigned long long found = __ballot(lane < a.parts && larger_than(bound, bounds, 64) == half - 1);
+    Key least = wave_max(last);
+    if (found) {
+        const Key other = of_lane(bound, __builtin_ctzll(found));
+        least = other > least ? other : least;
+    }
+    for (int i = threadIdx.x; i < keys_of_row; i += 256) {
+        if (i >= 256) mine = keys[i];
+        if (mine && mine >= least) list[atomicAdd(&count, 1)] = mine;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < count; i += 256) {
@@ -491,16 +540,11 @@ __device__ __forceinline__ Slope slope_of(float m, float ls, float entropy, floa
     g.label = label;
     return g;
 }
-template <bool DH, typename V> __device__ __forceinline__ V logit_gradients(V v, const Slope& g)
+template <bool DH> __device__ __forceinline__ float logit_gradient(float x, const Slope& g)
 {
-    V o;
-#pragma unroll
-    for (int k = 0; k < (int)sizeof(V) / 4; ++k) {
-        const float d = g.usual ? __builtin_fmaf(v[k], kLog2E, -g.shift) : __builtin_fmaf(v[k] - g.m, kLog2E, -g.shift);
-        const float p = __builtin_amdgcn_exp2f(d);
-        o[k] = DH ? p * __builtin_fmaf(fmaxf(d, kFar), g.of_entropy, g.both) : p * g.both;
-    }
-    return o;
+    const float d = g.usual ? __builtin_fmaf(x, kLog2E, -g.shift) : __builtin_fmaf(x - g.m, kLog2E, -g.shift);
+    const float p = __builtin_amdgcn_exp2f(d);
+    return DH ? p * __builtin_fmaf(fmaxf(d, kFar), g.of_entropy, g.both) : p * g.both;
 }
 
 template <typename T, int W, bool DH> __global__ void __launch_bounds__(256) logprobs_backward_kernel(LogArgs a)
@@ -525,7 +569,9 @@ template <typename T, int W, bool DH> __global__ void __launch_bounds__(256) log
         const Slope g = slope_of(m, a.kept[3 * row + 1], entropy, label < 0 ? 0.f : label >= a.classes ? __builtin_nanf("") : a.dlogprob[row], dh, label);
         const bool empty = m == -__builtin_inff() && g.label < a.classes;
         auto gradients = [&](vec v, int i) {
-            wide o = logit_gradients<DH>(widen<T>(v), g);
+            wide o = widen<T>(v);
+#pragma unroll
+            for (int k = 0; k < N; ++k) o[k] = logit_gradient<DH>(o[k], g);
             if (g.label >= 0 && (unsigned)(g.label - i) < (unsigned)N) {
 #pragma unroll
                 for (int k = 0; k < N; ++k) o[k] += k == g.label - i ? g.dl : 0.f;
@@ -533,20 +579,26 @@ template <typename T, int W, bool DH> __global__ void __launch_bounds__(256) log
             if (empty) o = 0.f;
             return narrow<T>(o);
         };
-        for (int j = head + N * t; j < end; j += N * kLanes * U) {
-            if (j >= begin && j + N * kLanes * (U - 1) + N <= end) {
-                vec v[U];
+        const Edges edge = edges_of<N>(head, begin, end);
+        for (int j = edge.whole + N * t; j + N <= end; j += N * kLanes * U) {
+            vec v[U];
 #pragma unroll
-                for (int u = 0; u < U; ++u) v[u] = Piece<T>::load(x + j + N * kLanes * u);
+            for (int u = 0; u < U; ++u) {
+                const int i = j + N * kLanes * u;
+                if (i + N <= end) v[u] = Piece<T>::load(x + i);
+            }
 #pragma unroll
-                for (int u = 0; u < U; ++u) Piece<T>::store(out + j + N * kLanes * u, gradients(v[u], j + N * kLanes * u));
-            } else {
-#pragma unroll 1
-                for (int i = j; i < end && i < j + N * kLanes * U; i += N * kLanes) {
-                    const vec o = gradients(logits_at(x, i, begin, end), i);
-                    if (i >= begin && i + N <= end) Piece<T>::store(out + i, o);
-                    else Piece<T>::store_part(out, i, begin, end, o);
-                }
+            for (int u = 0; u < U; ++u) {
+                const int i = j + N * kLanes * u;
+                if (i + N <= end) Piece<T>::store(out + i, gradients(v[u], i));
+            }
+        }
+        // the elements of the pieces that are not whole, one for a thread
+        if (t < 2 * N) {
+            const int at = t < N ? edge.before : edge.behind, i = at == kNowhere ? end : at + t % N;
+            if (i >= begin && i < end) {
+                const float o = logit_gradient<DH>((float)x[i], g) + (i == g.label ? g.dl : 0.f);
+                out[i] = (T)(empty ? 0.f : o);
             }
         }
     }
@@ -564,12 +616,12 @@ bool valid(const bmgd_logprobs_config& c)
     return c.classes >= 1 && c.classes <= (1 << 24) && known_type(c.dtype) && c.top >= 0 && c.top <= kMaxTop && c.top <= c.classes;
 }
 
-constexpr int kWide = 8192;                     // a part of a row has this many classes or more
+constexpr int kWide = 1024;                      // a part of a row has this many pieces or more: a turn
 
 // Parts of a row, where few rows would leave compute units idle.
-int parts_of(int64_t classes, int64_t rows)
+int parts_of(const bmgd_logprobs_config& c, int64_t rows)
 {
-    const int64_t parts = std::min<int64_t>(std::min<int64_t>(512 / std::max<int64_t>(rows, 1), kMaxParts), classes / kWide);
+    const int64_t parts = std::min<int64_t>(std::min<int64_t>(512 / std::max<int64_t>(rows, 1), kMaxParts), c.classes * (int64_t)size_of(c.dtype) / 16 / kWide);
     return (int)std::max<int64_t>(parts, 1);
 }
 // classes of a part: whole pieces of eight
@@ -595,7 +647,7 @@ extern "C" {
 BMGD_API size_t bmgd_logprobs_workspace_bytes(const bmgd_logprobs_config* cfg, int64_t rows)
 {
     if (!cfg || !valid(*cfg) || rows < 1 || rows > kMaxCallRows) return 0;
-    const int parts = parts_of(cfg->classes, rows);
+    const int parts = parts_of(*cfg, rows);
     if (parts == 1) return 0;
     return stats_bytes(rows, parts) + ((size_t)rows * parts * cfg->top * sizeof(Key) + 255) / 256 * 256;
 }
@@ -637,7 +689,7 @@ BMGD_API int bmgd_logprobs_forward(const bmgd_logprobs_config* cfg, int64_t rows
     a.rows = rows;
     a.classes = (int)cfg->classes;
     a.top = cfg->top;
-    a.parts = parts_of(cfg->classes, rows);
+    a.parts = parts_of(*cfg, rows);
     a.span = span_of(cfg->classes, a.parts);
     if (a.parts > 1) {
         a.part_stats = static_cast<float*>(t->workspace);
@@ -654,11 +706,15 @@ BMGD_API int bmgd_logprobs_forward(const bmgd_logprobs_config* cfg, int64_t rows
                 hipLaunchKernelGGL((logprobs_kernel<T, W, TOP, ENT>), dim3((unsigned)((now + kRows - 1) / kRows), (unsigned)a.parts), dim3(threads_of(W)), 0, s, a);
             }
         };
+        // A wavefront for each row, if the rows are many or short.  Measured, us, with it and with four for a row (16 bits; no classes, five):
+        //      8,192 x 1,000: 7 and 21, 14 and 38;  8,192 x 4,000: 14 and 23, 21 and 41;  4,097 x 10,001: 19 and 28, 37 and 34;  8,192 x 32,000: 99 and 93;
+        //      1,000 x 10,001, five: 22 and 13;  100 x 4,000, five: 7.6 and 6.2.
+        // (Of 64 groups the 64th largest leaves 300 classes to list, now and then more than the list holds: short rows only.)
+        const int64_t pieces = (int64_t)a.span * (int64_t)sizeof(T) / 16;
+        const bool wave = pieces <= 128 || (rows >= 4 * compute_units() && pieces <= (a.top ? 512 : 2048));
         auto shaped = [&](auto top, auto ent) {
-            // (of 64 groups the 64th largest leaves 300 to list, now and then more than the list holds)
-            if (a.span <= 2048 && (a.top <= 16 || a.classes <= kList)) launch(std::integral_constant<int, 1>(), top, ent);
-            else if (a.span <= 16384 || rows * a.parts > 512) launch(std::integral_constant<int, 4>(), top, ent);
-            else launch(std::integral_constant<int, 16>(), top, ent);
+            if (wave && (a.top <= 16 || a.classes <= kList)) launch(std::integral_constant<int, 1>(), top, ent);
+            else launch(std::integral_constant<int, 4>(), top, ent);
         };
         auto with_top = [&](auto ent) {
             if (a.top) shaped(std::true_type(), ent);
@@ -698,9 +754,10 @@ BMGD_API int bmgd_logprobs_backward(const bmgd_logprobs_config* cfg, int64_t row
     a.dentropy = t->dentropy;
     a.rows = rows;
     a.classes = (int)cfg->classes;
-    const int turn = 256 * kTurns * (int)(16 / size_of(cfg->dtype));
-    a.parts = (int)((cfg->classes + 7 + turn - 1) / turn);
-    a.span = span_of(cfg->classes, a.parts);
+    // parts of up to four pieces for each of 256 threads, alike but for the last one
+    const int piece = 256 * (int)(16 / size_of(cfg->dtype)), pieces = (int)((cfg->classes + 7 + piece - 1) / piece);
+    a.parts = (pieces + kTurns - 1) / kTurns;
+    a.span = (pieces + a.parts - 1) / a.parts * piece;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
