@@ -7,9 +7,9 @@
 //
 // The most probable classes.  A logit and its class are one 64-bit number, larger where the logit is larger and, of equal ones, the class lower; so no two are
 // equal.  Of what the threads read first (8,192 logits of 16 bits for four wavefronts), 64 groups of threads have their largest numbers; the top-th largest of these is not above the top-th
-// largest of the row.  From then on each piece that reaches it, those read first among them, is put into a list in shared memory as it passes by: about top (row / 8,192) pieces.
-// The classes in the list that reach it are counted against one another: the place of each is the number of larger ones.
-// A row that overflows the list (many equal logits) is read once more, by 64-bit numbers; where these overflow too, or a row has NaN, the classes are found one after the other.
+// largest of the row.  Pieces that reach it are put into shared memory as they pass by.  After 2, 4, 8, ... turns their classes that do are counted against one another, the
+// place of each being the number of larger ones; the top-th of them is what later ones have to reach, so that between two counts about as many are listed as are wanted.
+// Where a list overflows (logits that rise all along a row) or a row has NaN, the classes are found one after the other.
 #include "operator_calls.h"
 #include "rows_device.h"
 
@@ -28,8 +28,8 @@ constexpr float kLowest = -3.40282347e38f;
 constexpr float kUsual = 1e37f;                  // x log2 e - r is finite, or -infinity for one far below, where m is smaller than this
 constexpr float kFar = -1000.f;                  // 2^-1000 is 0, times this still 0
 constexpr int kMaxTop = 64, kMaxParts = 64;
-constexpr int kList = 512;                       // classes listed at most: a row of fewer than 8 top fits whole
-constexpr int pieces_listed(int w) { return w == 1 ? 64 : 256; }
+constexpr int kList = 512;                       // classes listed between two counts at most: a row of fewer than 8 top fits whole,
+constexpr int pieces_kept(int w) { return w == 1 ? 80 : 256; }         // and pieces: 64, and two that are not whole
 
 struct LogArgs {
     const char* logits;
@@ -109,7 +109,7 @@ template <int W> __device__ __forceinline__ void together()
 __device__ __forceinline__ int larger_than(Key v, const Key* all, int count)
 {
     int larger = 0;
-#pragma unroll 8
+#pragma unroll 4
     for (int i = 0; i < count; ++i) larger += all[i] > v;
     return larger;
 }
@@ -225,16 +225,17 @@ constexpr int threads_of(int w) { return w < 4 ? 256 : 64 * w; }
 
 template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds__(threads_of(W)) logprobs_kernel(LogArgs a)
 {
-    constexpr int kLanes = 64 * W, kRows = threads_of(W) / kLanes, N = Piece<T>::N, U = 4, kTurn = N * kLanes * U, kPieces = pieces_listed(W);
+    constexpr int kLanes = 64 * W, kRows = threads_of(W) / kLanes, N = Piece<T>::N, U = 4, kTurn = N * kLanes * U, kPieces = pieces_kept(W);
     typedef typename Piece<T>::vec vec;
     typedef typename Piece<T>::wide wide;
     __shared__ Stats parts[W > 1 ? W : 1];
     __shared__ Key groups_of[TOP ? kRows : 1][TOP ? (W == 1 ? 64 : 128) : 1];                  // (at most half as many as threads)
     __shared__ Key list[TOP ? kRows : 1][TOP ? kList : 1];
+    __shared__ Key sorted[TOP ? kRows : 1][2][TOP ? kMaxTop : 1];
     __shared__ vec pieces[TOP ? kRows : 1][TOP ? kPieces : 1];
     __shared__ int places[TOP ? kRows : 1][TOP ? kPieces : 1];
     __shared__ Key threshold;
-    __shared__ int counts[kRows], listed[kRows];
+    __shared__ int kept[kRows][2], listed[kRows][2];            // how many pieces and classes, in turn: one is cleared while the other is in use
     const int t = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
     const int64_t row = a.first + (int64_t)blockIdx.x * kRows + mine;
     if (row >= a.rows) return;                                  // (whole wavefronts, and none of a workgroup with barriers)
@@ -245,7 +246,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     const int label = a.logprob && a.parts == 1 ? a.labels[row] : -1;
     Stats st{-kUsual, 0.f, 0.f};
     Key least = 0;                                              // at least `top` of the segment's numbers are not below
-    float least_value = -__builtin_inff(), seen = -__builtin_inff();
+    float seen = -__builtin_inff();
     const Edges edge = edges_of<N>(head, begin, end);
     // one of the pieces that are not whole, for the first two threads
     const int edge_at = t == 0 ? edge.before : t == 1 ? edge.behind : kNowhere;
@@ -261,13 +262,41 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             else next[u] = (T)-__builtin_inff();
         }
     };
-    // a piece that reaches the threshold
+    int in_use = 0, have = 0;                                   // have: numbers in sorted[mine][in_use]
+    bool over = false;
     auto keep = [&](vec piece, int at) {
-        const int place = atomicAdd(&listed[mine], 1);
+        const int place = atomicAdd(&kept[mine][in_use], 1);
         if (place < kPieces) {
             pieces[mine][place] = piece;
             places[mine][place] = at;
         }
+    };
+    auto count_kept = [&]() {
+        together<W>();
+        const int held = kept[mine][in_use];
+        over |= held > kPieces;
+        for (int i = t; i < min(held, kPieces) * N; i += kLanes) {
+            const int at = places[mine][i / N] + i % N;
+            const Key q = key_of((float)pieces[mine][i / N][i % N], at);
+            if (at >= begin && at < end && q >= least) {
+                const int place = atomicAdd(&listed[mine][in_use], 1);
+                if (place < kList) list[mine][place] = q;
+            }
+        }
+        together<W>();
+        const int fresh = min(listed[mine][in_use], kList);
+        over |= listed[mine][in_use] > kList;
+        const Key* const old = sorted[mine][in_use];
+        for (int i = t; i < have + fresh; i += kLanes) {
+            const Key q = i < have ? old[i] : list[mine][i - have];
+            const int place = larger_than(q, old, have) + larger_than(q, list[mine], fresh);
+            if (place < a.top) sorted[mine][in_use ^ 1][place] = q;
+        }
+        together<W>();
+        if (t == 0) kept[mine][in_use] = listed[mine][in_use] = 0;
+        in_use ^= 1;
+        have = min(have + fresh, a.top);
+        if (have == a.top) least = sorted[mine][in_use][have - 1];
     };
     // turns of U pieces, the next ones on their way
     auto turn = [&](auto first) {
@@ -277,7 +306,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
 #pragma unroll
         for (int u = 0; u < U; ++u) now[u] = next[u];
         j += kTurn;
-        if (j + N <= end) request();
+        request();
 #pragma unroll
         for (int u = 0; u < U; ++u) most[u] = largest(widen<T>(now[u]));
         if constexpr (TOP) {
@@ -306,7 +335,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                     if (t % of == 0) groups_of[0][t / of] = k;
                     if (t == 0) {
                         threshold = 0;
-                        counts[0] = listed[0] = 0;
+                        kept[0][0] = kept[0][1] = listed[0][0] = listed[0][1] = 0;
                     }
                     __syncthreads();
                     int place = larger_than(k, groups_of[0] + t % of * each, each);
@@ -317,20 +346,20 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                     least = threshold;
                 } else {
                     groups_of[mine][t] = k;
-                    if (t == 0) counts[mine] = listed[mine] = 0;
+                    if (t == 0) kept[mine][0] = kept[mine][1] = listed[mine][0] = listed[mine][1] = 0;
                     together<1>();
                     const unsigned long long found = __ballot(larger_than(k, groups_of[mine], 64) == a.top - 1);
                     if (found) least = of_lane(k, __builtin_ctzll(found));
                 }
                 // (equal numbers are zeros, of groups without a class: where there is no top-th, all are listed)
-                if (least) least_value = value_of(least);
                 if (edge_at != kNowhere && key_of(largest(widen<T>(edge_piece)), max(edge_at, begin)) >= least) keep(edge_piece, edge_at);
             }
+            const float value = least ? value_of(least) : -__builtin_inff();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = at + N * kLanes * u;
                 // (later turns have higher classes than the threshold's: equal logits do not reach it)
-                const bool reaches = decltype(first)::value ? key_of(most[u], i) >= least : most[u] > least_value;
+                const bool reaches = decltype(first)::value ? key_of(most[u], i) >= least : most[u] > value;
                 if (reaches && i + N <= end) keep(now[u], i);
             }
         }
@@ -344,12 +373,18 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             v[u] = widen<T>(__builtin_bit_cast(vec, raw));
         }
         take<U, ENT>(st, v, most);
-        seen = fmaxf(seen, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+#pragma unroll
+        for (int u = 0; u < U; ++u) seen = fmaxf(seen, most[u]);
     };
     request();
     const float at_label = label >= 0 && label < a.classes ? (float)x[label] : 0.f;
     turn(std::true_type());
-    while (j + N <= end) turn(std::false_type());
+    const int turns = (end - edge.whole + kTurn - 1) / kTurn;   // (of the row: some threads have nothing left in the last one)
+    for (int n = 1; n < turns; ++n) {
+        turn(std::false_type());
+        if constexpr (TOP)
+            if (!(n & (n + 1)) && n + 1 < turns) count_kept();
+    }
     if (edge_at != kNowhere) {
         const wide v = widen<T>(edge_piece);
         const float most = largest(v);
@@ -400,36 +435,9 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         } else write_row(a, row, label, at_label, r);
     }
     if constexpr (TOP) {
-        auto list_class = [&](Key q, int at) {
-            if (at >= begin && at < end && q >= least) {
-                const int place = atomicAdd(&counts[mine], 1);
-                if (place < kList) list[mine][place] = q;
-            }
-        };
-        const bool plain = st.s == st.s;
-        const int kept = listed[mine];
-        if (plain && kept <= kPieces) {
-            for (int i = t; i < kept * N; i += kLanes) {
-                const int at = places[mine][i / N] + i % N;
-                list_class(key_of((float)pieces[mine][i / N][i % N], at), at);
-            }
-        } else if (plain) {
-            for (int i = head + N * t; i < end; i += N * kLanes) {
-                const wide v = widen<T>(logits_at(x, i, begin, end));
-                if (largest(v) >= least_value)
-#pragma unroll
-                    for (int k = 0; k < N; ++k) list_class(key_of(v[k], i + k), i + k);
-            }
-        }
-        together<W>();
-        const int count = counts[mine];
-        if (plain && count <= kList) {
-            for (int i = t; i < count; i += kLanes) {
-                const Key q = list[mine][i];
-                const int place = larger_than(q, list[mine], count);
-                if (place < a.top) write_top(a, row, part, place, q, r);
-            }
-            if (t >= count && t < a.top) write_top(a, row, part, t, 0, r);       // (a part of fewer than `top` classes)
+        count_kept();
+        if (st.s == st.s && !over) {
+            if (t < a.top) write_top(a, row, part, t, t < have ? sorted[mine][in_use][t] : 0, r);          // (a part may have fewer than `top` classes)
         } else {
             Key before = ~(Key)0;
             for (int place = 0; place < a.top; ++place) {
