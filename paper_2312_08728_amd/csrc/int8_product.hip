@@ -135,16 +135,74 @@ template <typename T, int RF> __global__ void __launch_bounds__(64 * kFewWaves) 
 
 constexpr int kStep = 128;          // codes of a row that a step takes
 
+// Wait until at most N of this wavefront's loads to shared memory are on their way and its reads of shared memory are done, then for the others.
+template <int N> __device__ __forceinline__ void wait_and_meet()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
+}
+
 // A tile of BM rows and BN columns by WM x WN wavefronts.  A step of an operand lies in shared memory as rows of 128 bytes, eight pieces of 16; piece c of row r
-// lies in place c ^ (r & 7), so that the rows that an instruction's lanes read at the same piece lie in different banks.  Loose: operands at any
-// address, through registers.
-template <int BM_, int BN_, int WM_, int WN_, bool LOOSE_> struct Tile {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kThreads = 64 * WM * WN;
-    static constexpr bool LOOSE = LOOSE_;
+// lies in place c ^ (r & 7), so that the rows that an instruction's lanes read at the same piece lie in different banks.
+//   loose      operands at any address, through registers, AHEAD steps on their way, two places in shared memory
+//   otherwise  straight to shared memory, AHEAD steps on their way
+template <int BM_, int BN_, int WM_, int WN_, int AHEAD_, bool LOOSE_> struct Tile {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kThreads = 64 * WM * WN, AHEAD = AHEAD_;
+    static constexpr bool LOOSE = LOOSE_, kHalves = BM * BN == 256 * 256 && !LOOSE;
     static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;                   // 16 x 16 results of a wavefront
+    static constexpr int kPlaces = LOOSE ? 2 : AHEAD + 1;
     static constexpr int kBytes = (BM + BN) * kStep;                             // of a step
     static constexpr int PM = BM * 8 / kThreads, PN = BN * 8 / kThreads;         // pieces that a thread brings
+    static constexpr size_t kShared = (size_t)kPlaces * kBytes;
 };
+
+// The results of a wavefront leave through its own part of shared memory, so that rows are written in whole lines, as many at a time as it holds.
+template <typename T, class C> __device__ __forceinline__ void write_tile(const ProductArgs& a, const int4v (&sum)[C::FM][C::FN], char* shared, int64_t row0, int col0, int wave, int lane)
+{
+    constexpr int kRow = C::FN * 16 * (int)sizeof(T), kChunks = kRow / 16, kTurn = kChunks < 8 ? kChunks - 1 : 7;
+    constexpr int kOnce = C::BM * C::BN * (int)sizeof(T) > (int)C::kShared ? C::FM / 2 : C::FM;
+    static_assert(kOnce * 16 * kRow * C::WM * C::WN <= (int)C::kShared, "");
+    typedef T four __attribute__((ext_vector_type(4)));
+    const int in = lane & 15, q = lane >> 4;
+    char* const own = shared + wave * (kOnce * 16 * kRow);
+    float sw[C::FN][4];
+#pragma unroll
+    for (int g = 0; g < C::FN; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sw[g][i] = a.sw[min(col0 + 16 * g + 4 * q + i, a.out - 1)];
+    __syncthreads();
+#pragma unroll
+    for (int first = 0; first < C::FM; first += kOnce) {
+#pragma unroll
+        for (int f = 0; f < kOnce; ++f) {
+            const float sx = a.sx[min(row0 + 16 * (first + f) + in, a.rows - 1)];
+#pragma unroll
+            for (int g = 0; g < C::FN; ++g) {
+                const float4v v = scaled(sum[first + f][g], sx, sw[g]);
+                four o;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
+                const int at = (16 * g + 4 * q) * (int)sizeof(T);
+                *reinterpret_cast<four*>(own + (16 * f + in) * kRow + 16 * ((at >> 4) ^ (in & kTurn)) + (at & 15)) = o;
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll 2
+        for (int i = lane; i < kOnce * 16 * kChunks; i += 64) {
+            const int r = i / kChunks, c = i % kChunks, j = col0 + c * (16 / (int)sizeof(T));
+            const int64_t row = row0 + 16 * first + r;
+            const typename Piece<T>::vec v = *reinterpret_cast<const typename Piece<T>::vec*>(own + r * kRow + 16 * (c ^ (r & kTurn)));
+            if (row >= a.rows) continue;
+            T* const to = reinterpret_cast<T*>(a.y) + row * a.ldy;
+            if (j + Piece<T>::N <= a.out) Piece<T>::store(to + j, v);
+            else if (j < a.out) Piece<T>::store_part(to, j, 0, a.out, v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    }
+}
 
 template <typename T, class C> __global__ void __launch_bounds__(C::kThreads) int8_tile_kernel(ProductArgs a)
 {
@@ -168,76 +226,165 @@ template <typename T, class C> __global__ void __launch_bounds__(C::kThreads) in
     for (int i = 0; i < C::PM; ++i) px[i] = a.x + min(row0 + r0 + i * (C::kThreads / 8), a.rows - 1) * a.ldx;
 #pragma unroll
     for (int i = 0; i < C::PN; ++i) pw[i] = a.w + (int64_t)min(col0 + r0 + i * (C::kThreads / 8), a.out - 1) * a.ldw;
-    int4v held[C::LOOSE ? C::PM + C::PN : 1];
-    auto request = [&](int step, int buffer) {
+    // piece i of x or w of a step, straight to shared memory (behind the end of a row: any, w is taken as zero there)
+    auto bring_x = [&](int step, int place, int i) {
         const int k = step * kStep + c0;
-        if constexpr (C::LOOSE) {
-#pragma unroll
-            for (int i = 0; i < C::PM; ++i) held[i] = codes_at(px[i], k, a.p);
-#pragma unroll
-            for (int i = 0; i < C::PN; ++i) held[C::PM + i] = codes_at(pw[i], k, a.p);
-        } else {
-            const int from = k < a.p ? k : 0;                   // (pieces behind the end: any, x is taken as zero there)
-            const unsigned to = base + buffer * C::kBytes + wave * 1024;
-#pragma unroll
-            for (int i = 0; i < C::PM; ++i) load_to_lds(reinterpret_cast<const unsigned short*>(px[i] + from), to + i * C::kThreads * 16);
-#pragma unroll
-            for (int i = 0; i < C::PN; ++i) load_to_lds(reinterpret_cast<const unsigned short*>(pw[i] + from), to + C::BM * kStep + i * C::kThreads * 16);
-        }
+        load_to_lds(reinterpret_cast<const unsigned short*>(px[i] + (k < a.p ? k : 0)), base + place * C::kBytes + wave * 1024 + i * C::kThreads * 16);
     };
-    auto arrive = [&](int buffer) {
-        if constexpr (C::LOOSE) {
-            char* const to = shared + buffer * C::kBytes + threadIdx.x * 16;
-#pragma unroll
-            for (int i = 0; i < C::PM; ++i) *reinterpret_cast<int4v*>(to + i * C::kThreads * 16) = held[i];
-#pragma unroll
-            for (int i = 0; i < C::PN; ++i) *reinterpret_cast<int4v*>(to + C::BM * kStep + i * C::kThreads * 16) = held[C::PM + i];
-        } else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
+    auto bring_w = [&](int step, int place, int i) {
+        const int k = step * kStep + c0;
+        load_to_lds(reinterpret_cast<const unsigned short*>(pw[i] + (k < a.p ? k : 0)), base + place * C::kBytes + C::BM * kStep + wave * 1024 + i * C::kThreads * 16);
     };
-
-    int4v sum[C::FM][C::FN] = {};
     const int m0 = wave / C::WN * (C::FM * 16), n0 = wave % C::WN * (C::FN * 16);
-    auto multiply = [&](int step, int buffer) {
-        const char* const xs = shared + buffer * C::kBytes + (m0 + in) * kStep;
-        const char* const ws = shared + buffer * C::kBytes + C::BM * kStep + (n0 + in) * kStep;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int place = 16 * ((4 * h + q) ^ (in & 7));
-            int4v x[C::FM], w[C::FN];
-#pragma unroll
-            for (int f = 0; f < C::FM; ++f) x[f] = *reinterpret_cast<const int4v*>(xs + f * 16 * kStep + place);
-#pragma unroll
-            for (int f = 0; f < C::FN; ++f) w[f] = *reinterpret_cast<const int4v*>(ws + f * 16 * kStep + place);
-            if (!C::LOOSE && step * kStep + 64 * h + 16 * q >= a.p)
-#pragma unroll
-                for (int f = 0; f < C::FM; ++f) x[f] = 0;
-#pragma unroll
-            for (int f = 0; f < C::FM; ++f)
-#pragma unroll
-                for (int g = 0; g < C::FN; ++g) sum[f][g] = mma(w[g], x[f], sum[f][g]);
-        }
+    // operands of an instruction: 16 rows (f) at half h of a step
+    auto read_x = [&](int place, int f, int h) {
+        return *reinterpret_cast<const int4v*>(shared + place * C::kBytes + (m0 + 16 * f + in) * kStep + 16 * ((4 * h + q) ^ (in & 7)));
     };
+    auto read_w = [&](int place, int g, int h) {
+        return *reinterpret_cast<const int4v*>(shared + place * C::kBytes + (C::BM + n0 + 16 * g + in) * kStep + 16 * ((4 * h + q) ^ (in & 7)));
+    };
+    // whether lanes of half h of this step are behind the end
+    auto behind = [&](int step, int h) { return step * kStep + 64 * h + 16 * q >= a.p; };
+    int4v sum[C::FM][C::FN] = {};
 
-    request(0, 0);
-    for (int step = 0; step < steps; ++step) {
-        arrive(step & 1);
-        if (step + 1 < steps) request(step + 1, (step + 1) & 1);
-        multiply(step, step & 1);
-    }
-
+    if constexpr (C::kHalves) {
+        // All of w's operands of a step are in registers before half of x's rows have been multiplied; so the first half of x's rows and w make room for the step
+        // after the next one in the middle of a step, the second half at the next one's beginning: each is asked for a whole step before it is needed, and nothing is waited for at once.
+        // A wavefront's first 64 rows are pieces 0 and 2 of its threads (rows 0-63 and 128-191 of the tile), the other 64 pieces 1 and 3.
+        static_assert(C::PM == 4 && C::PN == 4 && C::FM == 8 && C::FN == 4 && C::WM == 2, "");
+        constexpr int kLate = 8;                                // loads of a thread on their way at a wait: a half of x, w, a half of x
+        auto bring_half = [&](int step, int half) {
+            bring_x(step, step & 1, half);
+            bring_x(step, step & 1, half + 2);
+        };
+        auto bring_all_w = [&](int step) {
 #pragma unroll
-    for (int g = 0; g < C::FN; ++g) {
-        const int j = col0 + n0 + 16 * g + 4 * q;
-        float sw[4];
+            for (int i = 0; i < 4; ++i) bring_w(step, step & 1, i);
+        };
+        int4v xf[4], wf[2][4];
+        bring_all_w(0);
+        bring_half(0, 0);
+        bring_half(0, 1);
+        if (steps > 1) {
+            bring_half(1, 0);
+            bring_all_w(1);
+            wait_and_meet<6>();
+        } else wait_and_meet<0>();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sw[i] = j + i < a.out ? a.sw[j + i] : 0.f;
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int f = 0; f < C::FM; ++f) {
-            const int64_t row = row0 + m0 + 16 * f + in;
-            if (row < a.rows && j < a.out) put_four(reinterpret_cast<T*>(a.y) + row * a.ldy + j, scaled(sum[f][g], a.sx[row], sw), a.out - j);
+            for (int g = 0; g < 4; ++g) wf[h][g] = read_w(0, g, h);
+        xf[0] = read_x(0, 0, 0);
+        xf[1] = read_x(0, 0, 1);
+        for (int s = 0; s < steps; ++s) {
+            const bool next = s + 1 < steps, after = s + 2 < steps;
+            if (!next && a.p % kStep) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    if (behind(s, h))
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) wf[h][g] = 0;
+            }
+#pragma unroll
+            for (int f = 0; f < 8; ++f) {
+                if (f == 1 && next) bring_half(s + 1, 1);
+                if (f == 3) {
+                    if (next) wait_and_meet<kLate>();
+                    else wait_and_meet<0>();
+                }
+                if (f == 4 && after) bring_half(s + 2, 0);
+                if (f == 5 && after) bring_all_w(s + 2);
+                if (f == 7) {
+                    if (after) wait_and_meet<kLate>();
+                    else wait_and_meet<0>();
+                }
+                if (f < 7) {
+                    xf[(2 * f + 2) & 3] = read_x(s & 1, f + 1, 0);
+                    xf[(2 * f + 3) & 3] = read_x(s & 1, f + 1, 1);
+                } else if (next) {
+                    xf[0] = read_x((s + 1) & 1, 0, 0);
+                    xf[1] = read_x((s + 1) & 1, 0, 1);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) sum[f][g] = mma(wf[h][g], xf[(2 * f + h) & 3], sum[f][g]);
+                    if (f == 7 && next) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g) wf[h][g] = read_w((s + 1) & 1, g, h);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+    } else {
+        auto multiply = [&](int step, int place) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                int4v x[C::FM], w[C::FN];
+#pragma unroll
+                for (int f = 0; f < C::FM; ++f) x[f] = read_x(place, f, h);
+#pragma unroll
+                for (int g = 0; g < C::FN; ++g) w[g] = read_w(place, g, h);
+                if (!C::LOOSE && step + 1 == steps && behind(step, h))
+#pragma unroll
+                    for (int g = 0; g < C::FN; ++g) w[g] = 0;
+#pragma unroll
+                for (int f = 0; f < C::FM; ++f)
+#pragma unroll
+                    for (int g = 0; g < C::FN; ++g) sum[f][g] = mma(w[g], x[f], sum[f][g]);
+            }
+        };
+        if constexpr (C::LOOSE) {
+            int4v held[C::AHEAD][C::PM + C::PN];
+            auto request = [&](int step, int to) {
+                const int k = step * kStep + c0;
+#pragma unroll
+                for (int i = 0; i < C::PM; ++i) held[to][i] = codes_at(px[i], k, a.p);
+#pragma unroll
+                for (int i = 0; i < C::PN; ++i) held[to][C::PM + i] = codes_at(pw[i], k, a.p);
+            };
+#pragma unroll
+            for (int i = 0; i < C::AHEAD; ++i)
+                if (i < steps) request(i, i);
+            for (int first = 0; first < steps; first += C::AHEAD) {
+#pragma unroll
+                for (int i = 0; i < C::AHEAD; ++i) {
+                    const int step = first + i;
+                    if (step >= steps) break;
+                    const int place = step & 1;
+                    char* const to = shared + place * C::kBytes + threadIdx.x * 16;
+#pragma unroll
+                    for (int k = 0; k < C::PM; ++k) *reinterpret_cast<int4v*>(to + k * C::kThreads * 16) = held[i][k];
+#pragma unroll
+                    for (int k = 0; k < C::PN; ++k) *reinterpret_cast<int4v*>(to + C::BM * kStep + k * C::kThreads * 16) = held[i][C::PM + k];
+                    __syncthreads();
+                    if (step + C::AHEAD < steps) request(step + C::AHEAD, i);
+                    multiply(step, place);
+                }
+            }
+        } else {
+            auto request = [&](int step, int place) {
+#pragma unroll
+                for (int i = 0; i < C::PM; ++i) bring_x(step, place, i);
+#pragma unroll
+                for (int i = 0; i < C::PN; ++i) bring_w(step, place, i);
+            };
+#pragma unroll
+            for (int i = 0; i < C::AHEAD; ++i)
+                if (i < steps) request(i, i);
+            int place = 0;
+            for (int step = 0; step < steps; ++step) {
+                if (step + C::AHEAD <= steps) wait_and_meet<(C::AHEAD - 1) * (C::PM + C::PN)>();
+                else wait_and_meet<0>();
+                // (to the place of the step before this one, which all have read)
+                if (step + C::AHEAD < steps) request(step + C::AHEAD, place == 0 ? C::AHEAD : place - 1);
+                multiply(step, place);
+                place = place == C::AHEAD ? 0 : place + 1;
+            }
         }
     }
+    write_tile<T, C>(a, sum, shared, row0 + m0, col0 + n0, wave, lane);
 }
 
 struct QuantArgs {
@@ -299,7 +446,7 @@ template <typename T, class C> hipError_t launch_tile(ProductArgs a, hipStream_t
 {
     a.tiles_m = (int)((a.rows + C::BM - 1) / C::BM);
     a.tiles_n = (a.out + C::BN - 1) / C::BN;
-    constexpr size_t bytes = 2 * C::kBytes;
+    constexpr size_t bytes = C::kShared;
     if constexpr (bytes > 65536) {
         // once per device
         static std::atomic<uint64_t> done{0};
@@ -329,9 +476,9 @@ template <typename T> hipError_t launch_product(const ProductArgs& a, hipStream_
     const bool loose = all & 15;
     const int64_t units = compute_units();
     auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.out + n - 1) / n); };
-    if (!loose && tiles(256, 256) >= units) return launch_tile<T, Tile<256, 256, 2, 4, false>>(a, s);
-    if (tiles(128, 128) >= units) return loose ? launch_tile<T, Tile<128, 128, 2, 2, true>>(a, s) : launch_tile<T, Tile<128, 128, 2, 2, false>>(a, s);
-    return loose ? launch_tile<T, Tile<64, 64, 2, 2, true>>(a, s) : launch_tile<T, Tile<64, 64, 2, 2, false>>(a, s);
+    if (!loose && tiles(256, 256) >= units) return launch_tile<T, Tile<256, 256, 2, 4, 1, false>>(a, s);
+    if (tiles(128, 128) >= units) return loose ? launch_tile<T, Tile<128, 128, 2, 2, 1, true>>(a, s) : launch_tile<T, Tile<128, 128, 2, 2, 1, false>>(a, s);
+    return loose ? launch_tile<T, Tile<64, 64, 2, 2, 4, true>>(a, s) : launch_tile<T, Tile<64, 64, 2, 2, 3, false>>(a, s);
 }
 
 void check(Call& q, const bmgd_product_config* cfg)
