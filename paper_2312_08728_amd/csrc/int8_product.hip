@@ -78,17 +78,18 @@ __device__ __forceinline__ float4v scaled(int4v c, float sx, const float* sw)
 
 constexpr int kFewWaves = 8;
 
-// Up to 16 RF rows: a workgroup makes 16 columns of them, its wavefronts share the sum, every operand comes from memory once and straight to registers.
+// 16 RF rows and 16 columns for a workgroup, whose wavefronts share the sum; every operand comes straight to registers.
 template <typename T, int RF> __global__ void __launch_bounds__(64 * kFewWaves) int8_few_kernel(ProductArgs a)
 {
-    constexpr int U = 8;
+    constexpr int U = RF > 2 ? 4 : 8;
     __shared__ int4v parts[kFewWaves][RF][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, in = lane & 15, q = lane >> 4;
     const int col = blockIdx.x * 16;
+    const int64_t row0 = (int64_t)blockIdx.y * (16 * RF);
     const char* const w = a.w + (int64_t)min(col + in, a.out - 1) * a.ldw;
     const char* x[RF];
 #pragma unroll
-    for (int f = 0; f < RF; ++f) x[f] = a.x + min((int64_t)16 * f + in, a.rows - 1) * a.ldx;
+    for (int f = 0; f < RF; ++f) x[f] = a.x + min(row0 + 16 * f + in, a.rows - 1) * a.ldx;
     int4v sum[RF] = {};
     const int whole = a.p >> 6, each = (whole + kFewWaves - 1) / kFewWaves;
     int s = wave * each;
@@ -124,7 +125,7 @@ template <typename T, int RF> __global__ void __launch_bounds__(64 * kFewWaves) 
     int4v c = parts[0][wave][lane];
 #pragma unroll
     for (int i = 1; i < kFewWaves; ++i) c += parts[i][wave][lane];
-    const int64_t row = 16 * wave + in;
+    const int64_t row = row0 + 16 * wave + in;
     const int j = col + 4 * q;
     if (row >= a.rows || j >= a.out) return;
     float sw[4];
@@ -466,19 +467,33 @@ template <typename T, class C> hipError_t launch_tile(ProductArgs a, hipStream_t
 
 template <typename T> hipError_t launch_product(const ProductArgs& a, hipStream_t s)
 {
-    if (a.rows <= 32) {
-        const dim3 grid((unsigned)((a.out + 15) / 16)), block(64 * kFewWaves);
-        if (a.rows <= 16) hipLaunchKernelGGL((int8_few_kernel<T, 1>), grid, block, 0, s, a);
-        else hipLaunchKernelGGL((int8_few_kernel<T, 2>), grid, block, 0, s, a);
+    auto few = [&](auto rf) {
+        constexpr int RF = decltype(rf)::value;
+        hipLaunchKernelGGL((int8_few_kernel<T, RF>), dim3((unsigned)((a.out + 15) / 16), (unsigned)((a.rows + 16 * RF - 1) / (16 * RF))), dim3(64 * kFewWaves), 0, s, a);
         return hipGetLastError();
-    }
+    };
+    if (a.rows <= 16) return few(std::integral_constant<int, 1>());
+    if (a.rows <= 32) return few(std::integral_constant<int, 2>());
     const uintptr_t all = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.p | (uintptr_t)a.ldx | (uintptr_t)a.ldw;
     const bool loose = all & 15;
     const int64_t units = compute_units();
     auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.out + n - 1) / n); };
-    if (!loose && tiles(256, 256) >= units) return launch_tile<T, Tile<256, 256, 2, 4, 1, false>>(a, s);
-    if (tiles(128, 128) >= units) return loose ? launch_tile<T, Tile<128, 128, 2, 2, 1, true>>(a, s) : launch_tile<T, Tile<128, 128, 2, 2, 1, false>>(a, s);
-    return loose ? launch_tile<T, Tile<64, 64, 2, 2, 4, true>>(a, s) : launch_tile<T, Tile<64, 64, 2, 2, 3, false>>(a, s);
+    if (loose) return tiles(128, 128) >= units ? launch_tile<T, Tile<128, 128, 2, 2, 1, true>>(a, s) : launch_tile<T, Tile<64, 64, 2, 2, 4, true>>(a, s);
+    // Measured, us (rows x p x out): 2,048 x 4,096 x 4,096: tiles of 256 48, of 128 two or three to a unit 36, of 128 alone with one step more on its way 48, of 64 x 128 44, of 64 63;
+    //      2,000 x 2,000 x 2,000: 30, 19, 17, 20, 24;  512 x 4,096 x 4,096: 44, 23, 22, 17, 18;  256 x 4,096 x 4,096: 44, 23, 22, 16, 13.
+    if (tiles(256, 256) >= units) return launch_tile<T, Tile<256, 256, 2, 4, 1, false>>(a, s);
+    if (tiles(128, 128) > units) return launch_tile<T, Tile<128, 128, 2, 2, 1, false>>(a, s);
+    if (tiles(128, 128) > units / 2) return launch_tile<T, Tile<128, 128, 2, 2, 2, false>>(a, s);
+    if (tiles(64, 128) > units * 3 / 4) return launch_tile<T, Tile<64, 128, 2, 2, 2, false>>(a, s);
+    // Few tiles of 64, many steps: workgroups of 16 columns, which read the same rows more often.  Their operands come at 12 TB/s in all and 45 GB/s to a unit, a step of a tile
+    // takes 0.28 us: 100 x 8,192 x 1,000: 13 and 22 us;  64 x 4,096 x 4,096: 12 and 13;  128 x 4,096 x 4,096: 24 and 13.
+    const auto few_us = [&](int64_t rf) {
+        const double each = 16.0 * (double)(rf + 1) * a.p, groups = (double)((a.out + 15) / 16) * (double)((a.rows + 16 * rf - 1) / (16 * rf));
+        return 4.8 + std::max(each * groups / 12e6, each / 45e3);
+    };
+    const double tile_us = 4.0 + 0.28 * ((a.p + kStep - 1) / kStep), two = few_us(2), four = few_us(4);
+    if (std::min(two, four) < tile_us) return two < four ? few(std::integral_constant<int, 2>()) : few(std::integral_constant<int, 4>());
+    return launch_tile<T, Tile<64, 64, 2, 2, 3, false>>(a, s);
 }
 
 void check(Call& q, const bmgd_product_config* cfg)
