@@ -589,11 +589,11 @@ typedef struct bmgd_norm_tensors {
     void*       dweight;    /* backward, optional, written */
     float*      scales;     /* forward, with codes: one for each row */
     float*      rstd;       /* r, one for each row: forward writes it (optional), backward reads it */
-    void*       workspace;  /* backward with dweight: 256-byte aligned; calls that may run at the same time have one each */
+    void*       workspace;  /* backward with dweight, where it needs one: 256-byte aligned; calls that may run at the same time have one each */
     size_t      workspace_bytes;
 } bmgd_norm_tensors;
 
-/* What a backward call with dweight needs; 0 if the configuration is invalid.  Needs no GPU. */
+/* What a backward call with dweight needs, 0 for small ones (or if the configuration is invalid).  Needs no GPU. */
 size_t bmgd_norm_workspace_bytes(const bmgd_norm_config* cfg, int64_t rows);
 int bmgd_norm_forward(const bmgd_norm_config* cfg, int64_t rows, const bmgd_norm_tensors* t, void* stream);
 /*      dx_j = r (w_j dy_j - s_j r^2 mean_k(w_k dy_k s_k)) + dsum_j;      dweight_j = sum over the rows of dy_j s_j r */

@@ -30,8 +30,9 @@ struct NormArgs {
     float* rstd;
     float* partial;         // of dweight: a row of n for each workgroup
     int64_t rows, first;    // first: of the launch, see kRowsOfLaunch
-    int n;
+    int n, row_groups;      // row_groups: workgroups that go through rows, see norm_backward_kernel
     float eps, inv_n;
+    char* dweight;
 };
 
 // What the largest |s w| of a row is found in: products of two 16-bit numbers are exact in 32 bits, those of 32-bit numbers in 64.
@@ -300,12 +301,67 @@ __device__ __forceinline__ typename Piece<T>::wide input_gradient(typename Piece
     return v;
 }
 
-// A workgroup goes through rows blockIdx.x, blockIdx.x + gridDim.x, ... (kRows at a time) and keeps its part of dw in registers.
-template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(block_of(W)) norm_backward_kernel(NormArgs a)
+// How a backward call finds dw.
+enum Weights {
+    kNoWeights,
+    kParts,                 // each workgroup keeps its part of dw in registers and leaves it for norm_join_kernel
+    kColumns                // other workgroups of the launch, `row_groups` and following, read the same rows again, four pieces of columns each: r is given, so dw waits for nothing
+};
+
+// dw of four pieces of columns, from all rows: every kSlices-th row for a thread, then the slices in order.
+template <typename T, int THREADS> __device__ __forceinline__ void column_sums(const NormArgs& a, int group, float* shared)
+{
+    constexpr int N = Piece<T>::N, kSlices = THREADS / 4, U = 4;
+    typedef typename Piece<T>::wide wide;
+    const int slice = threadIdx.x / 4, mine = threadIdx.x % 4, j = N * (4 * group + mine);
+    wide dw = 0.f;
+    if (j < a.n) {
+        const T *const x = row_of<T>(a.x, 0), *const dy = row_of<T>(a.dy, 0);
+        int64_t row = slice;
+        for (; row + (U - 1) * kSlices < a.rows; row += U * kSlices) {
+            typename Piece<T>::vec s[U], g[U];
+            float r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s[u] = piece(x + (row + u * kSlices) * a.x.stride, j, a.n);
+                g[u] = piece(dy + (row + u * kSlices) * a.dy.stride, j, a.n);
+                r[u] = a.rstd[row + u * kSlices];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) dw += widen<T>(g[u]) * (widen<T>(s[u]) * r[u]);
+        }
+        for (; row < a.rows; row += kSlices) dw += widen<T>(piece(dy + row * a.dy.stride, j, a.n)) * (widen<T>(piece(x + row * a.x.stride, j, a.n)) * a.rstd[row]);
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k) shared[slice * (4 * N + 1) + mine * N + k] = dw[k];
+    __syncthreads();
+    // 16 slices for a thread, then these
+    constexpr int kGroups = kSlices / 16;
+    const int col = threadIdx.x % (4 * N), part = threadIdx.x / (4 * N);
+    float v = 0.f;
+    if (part < kGroups)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v += shared[(part * 16 + i) * (4 * N + 1) + col];
+    __syncthreads();
+    if (part < kGroups) shared[part * (4 * N) + col] = v;
+    __syncthreads();
+    if (part == 0) {
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < kGroups; ++i) v += shared[i * (4 * N) + col];
+        const int to = N * 4 * group + col;
+        if (to < a.n) reinterpret_cast<T*>(a.dweight)[to] = (T)v;
+    }
+}
+
+// A workgroup goes through rows blockIdx.x, blockIdx.x + row_groups, ... (kRows at a time).
+template <typename T, int W, int NV, Weights DW> __global__ void __launch_bounds__(block_of(W)) norm_backward_kernel(NormArgs a)
 {
     constexpr int kLanes = 64 * W, kRows = block_of(W) / kLanes;
     __shared__ float sums[2][16];
-    __shared__ float joined[DW && kRows > 1 ? kRows * NV * Piece<T>::N * kLanes : 1];
+    __shared__ float joined[DW == kParts && kRows > 1 ? kRows * NV * Piece<T>::N * kLanes : DW == kColumns ? block_of(W) / 4 * (4 * Piece<T>::N + 1) : 1];
+    if constexpr (DW == kColumns)
+        if ((int)blockIdx.x >= a.row_groups) return column_sums<T, block_of(W)>(a, blockIdx.x - a.row_groups, joined);
     const int t = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
     typename Piece<T>::vec w[NV];
     typename Piece<T>::wide dw[NV];
@@ -316,7 +372,7 @@ template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(
         dw[i] = 0.f;
     }
     int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += (int64_t)gridDim.x * kRows, turn ^= 1) {
+    for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += (int64_t)a.row_groups * kRows, turn ^= 1) {
         const int64_t row = first + mine;
         if (row >= a.rows) break;                               // (only without barriers)
         typename Piece<T>::vec s[NV], dy[NV], ds[NV];
@@ -339,7 +395,7 @@ template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(
             // (a last piece has zeros behind the row's end)
 #pragma unroll
             for (int k = 0; k < Piece<T>::N; ++k) along = __builtin_fmaf(g[k] * f[k], v[k], along);
-            if constexpr (DW) {
+            if constexpr (DW == kParts) {
 #pragma unroll
                 for (int k = 0; k < Piece<T>::N; ++k) dw[i][k] = __builtin_fmaf(g[k], v[k] * r, dw[i][k]);
             }
@@ -352,7 +408,7 @@ template <typename T, int W, int NV, bool DW> __global__ void __launch_bounds__(
                 put(row_of<T>(a.dx, row), j, a.n, narrow<T>(input_gradient<T>(widen<T>(dy[i]) * widen<T>(w[i]), widen<T>(s[i]), r, c, ds[i], a.dsum.data != nullptr)));
         }
     }
-    if constexpr (DW) {
+    if constexpr (DW == kParts) {
         float* const to = a.partial + (int64_t)blockIdx.x * a.n;
         if constexpr (kRows == 1) {
 #pragma unroll
@@ -502,6 +558,15 @@ int64_t parts_of(const bmgd_norm_config& c, int64_t rows)
     return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, kMaxParts));
 }
 
+// Whether dw is found by workgroups of its own: no second launch, but every row is read twice, 64 bytes at a time.  Measured, us, with them and with parts that are joined (rows x n):
+//      bf16 1,000 x 512: 7 and 10;  2,000 x 512: 11 and 11;  500 x 4,096: 8 and 15;  1,000 x 4,096: 12 and 16;  1,000 x 1,365 (rows that begin inside a line): 28 and 13;
+//      fp32 1,000 x 512: 8 and 10;  500 x 4,096: 10 and 16;  1,000 x 4,096: 18 and 17.
+bool by_columns(const bmgd_norm_config& c, int64_t rows)
+{
+    const int64_t bytes = c.n * (int64_t)size_of(c.dtype);
+    return pieces_of(c) <= kGradientPieces && bytes % 16 == 0 && rows <= 1024 && rows * bytes <= (int64_t(8) << 20);
+}
+
 void check(Call& q, const bmgd_norm_config* cfg, int64_t rows, const void* t)
 {
     if (!cfg || !t) return q.refuse(BMGD_EINVAL, "cfg and tensors must not be NULL");
@@ -534,7 +599,7 @@ extern "C" {
 
 BMGD_API size_t bmgd_norm_workspace_bytes(const bmgd_norm_config* cfg, int64_t rows)
 {
-    if (!cfg || !valid(*cfg) || rows < 0 || rows > kMaxCallRows) return 0;
+    if (!cfg || !valid(*cfg) || rows < 0 || rows > kMaxCallRows || by_columns(*cfg, rows)) return 0;
     return ((size_t)parts_of(*cfg, rows) * (size_t)cfg->n * sizeof(float) + 255) / 256 * 256;
 }
 
@@ -605,9 +670,10 @@ BMGD_API int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const
     for (const bmgd_matrix* in : {&t->dy, &t->dsum})
         if (in->data && in->data == t->dx.data && rows > 1 && in->stride != t->dx.stride) q.refuse("dx", "begins where an operand does, with another stride");
     for (const void* in : {(const void*)t->x.data, (const void*)t->dy.data, (const void*)t->dsum.data, (const void*)t->dx.data, t->weight}) q.apart("dweight", t->dweight, in);
-    if (t->dweight && some) {
+    const size_t need = t->dweight && some ? bmgd_norm_workspace_bytes(cfg, rows) : 0;
+    if (need) {
         if (!t->workspace || (reinterpret_cast<uintptr_t>(t->workspace) & 255)) q.refuse("workspace", "256-byte aligned device memory is wanted for dweight");
-        else if (t->workspace_bytes < bmgd_norm_workspace_bytes(cfg, rows)) q.refuse(BMGD_ENOMEM, "workspace too small");
+        else if (t->workspace_bytes < need) q.refuse(BMGD_ENOMEM, "workspace too small");
     }
     if (q.code != BMGD_OK) return q.code;
     const hipStream_t s = static_cast<hipStream_t>(stream);
@@ -624,7 +690,10 @@ BMGD_API int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const
     a.dsum = side(t->dsum);
     a.dx = side(t->dx);
     a.partial = static_cast<float*>(t->workspace);
-    const int64_t parts = parts_of(*cfg, rows);
+    const int64_t parts = parts_of(*cfg, rows), lasts = (pieces_of(*cfg) + 3) / 4;
+    a.row_groups = (int)parts;
+    a.dweight = static_cast<char*>(t->dweight);
+    const bool columns = t->dweight && by_columns(*cfg, rows), at_once = columns && t->dx.data != t->dy.data;
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
         if (pieces_of(*cfg) > kGradientPieces) {
@@ -632,18 +701,25 @@ BMGD_API int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const
                 hipLaunchKernelGGL(norm_columns_kernel<T>, dim3((unsigned)((pieces_of(*cfg) + 63) / 64), (unsigned)parts), dim3(64), 0, s, a);
             for (a.first = 0; a.first < rows; a.first += kRowsOfLaunch)
                 hipLaunchKernelGGL(norm_backward_long_kernel<T>, dim3((unsigned)std::min(rows - a.first, kRowsOfLaunch)), dim3(kLong), 0, s, a);
-        } else {
-            with_shape<T>(a.n, rows, [&](auto w, auto nv) {
-                constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
-                if constexpr (64 * W * NV > kGradientPieces) return;
-                else
-                if (t->dweight) hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, true>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
-                else hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, false>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
-            });
+            return;
         }
+        with_shape<T>(a.n, rows, [&](auto w, auto nv) {
+            constexpr int W = decltype(w)::value, NV = decltype(nv)::value;
+            if constexpr (64 * W * NV <= kGradientPieces) {
+                if (at_once) hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kColumns>), dim3((unsigned)(parts + lasts)), dim3(block_of(W)), 0, s, a);
+                else if (columns) {
+                    // dx takes the place of dy: dw first, the same sums
+                    a.row_groups = 0;
+                    hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kColumns>), dim3((unsigned)lasts), dim3(block_of(W)), 0, s, a);
+                    a.row_groups = (int)parts;
+                    hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kNoWeights>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
+                } else if (t->dweight) hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kParts>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
+                else hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kNoWeights>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
+            }
+        });
     });
-    int rc = q.launched();
-    if (rc != BMGD_OK || !t->dweight) return rc;
+    const int rc = q.launched();
+    if (rc != BMGD_OK || !t->dweight || columns) return rc;
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
         hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)((cfg->n + 31) / 32)), dim3(1024), 0, s, a.partial, static_cast<T*>(t->dweight), (int)parts, a.n);

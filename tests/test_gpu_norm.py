@@ -110,7 +110,7 @@ def test_sum_in_place(kind, n):
 
 @pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("rows,n,pad", [(1, 1, 0), (3, 7, 2), (9, 512, 0), (130, 520, 1), (5, 1024, 0), (3, 1365, 0), (700, 2048, 0), (3, 4096, 3), (1100, 4104, 0), (2, 8192, 0), (600, 8000, 0),
-                                        (2, 16_384, 1), (3, 16_390, 0), (2, 33_000, 0), (2100, 64, 0)])
+                                        (2, 16_384, 1), (3, 16_390, 0), (2, 33_000, 0), (2100, 64, 0), (1024, 64, 0), (1024, 72, 3), (1023, 2048, 0), (65, 16_384, 0), (300, 8192, 0)])
 @pytest.mark.parametrize("way", ["all", "plain"])
 def test_backward(kind, rows, n, pad, way):
     import torch
@@ -132,8 +132,8 @@ def test_backward(kind, rows, n, pad, way):
     assert (np.abs(_np(dx) - dx64) <= np.abs(dx64) * HALF[kind] + size * (_chain(n) + 10) * 2.0 ** -24 + TINY[kind]).all()
     assert int((flat == 3).sum()) >= flat.numel() - dx.numel()
     if way == "all":
-        # a part has at most ceil(rows / 512) + 4 rows of a lane, 512 parts are added 16 in a row and then 32
-        chain = -(-rows // 512) + 4 + 16 + 32 + 4
+        # a part has at most ceil(rows / 512) + 4 rows of a lane, 512 parts are added 16 in a row and then 32; or a thread has every 64th row of 1,024, 16 threads are added and then up to 16
+        chain = max(-(-rows // 512) + 4 + 16 + 32, min(16, -(-rows // 64)) + 16 + 16) + 4
         size = (np.abs(dy64 * s64) * r64[:, None]).sum(0)
         assert (np.abs(_np(dw) - dw64) <= np.abs(dw64) * HALF[kind] + size * chain * 2.0 ** -24 + TINY[kind]).all()
         for into in (dy, ds):                                            # in place, always the same bits
@@ -239,12 +239,11 @@ def test_rows_beyond_32_bits_and_many_rows():
     assert (y == 1.0).all()
 
 
-@pytest.mark.parametrize("n", [40, 5000])
-def test_a_training_step_in_a_graph(n):
+@pytest.mark.parametrize("n,rows", [(40, 300), (41, 300), (5000, 900), (4096, 1100)])
+def test_a_training_step_in_a_graph(n, rows):
     """Forward and backward with the weight's gradient, captured and replayed on other inputs, eager calls in between."""
     import torch
     import paper_2312_08728_amd as B
-    rows = 300
     op = B.RMSNorm(n)
     new = lambda: torch.randn(rows, n, device="cuda").bfloat16()  # noqa: E731
     x, dy, w = new(), new(), torch.randn(n, device="cuda").bfloat16()
@@ -286,5 +285,6 @@ def test_refusals():
             op.backward(*args)
     with pytest.raises(ValueError, match="workspace"):
         op.backward(x, x.clone(), None, f, x, dweight=x[0].clone(), workspace=torch.zeros(1 << 20))
+    many, of_many = torch.zeros(5000, 16, dtype=torch.bfloat16, device="cuda"), torch.zeros(5000, device="cuda")
     with pytest.raises(B.BmgdError, match="workspace"):
-        op.backward(x, x.clone(), None, f, x, dweight=x[0].clone(), workspace=torch.zeros(63, device="cuda"))       # (256 bytes are needed)
+        op.backward(many, many.clone(), None, of_many, many, dweight=x[0].clone(), workspace=torch.zeros(64, device="cuda"))

@@ -75,15 +75,16 @@ def test_norm_results_that_meet():
     _refused(forward(sum=_at(FAR), y=_at(FAR)), "sum")
     _refused(forward(codes=_at(FAR), x=_at(FAR)), "codes")
     _refused(forward(sum=_at(FAR, 65), x=_at(FAR, 64)), "stride")
-    backward = lambda **kw: B.bmgd_norm_backward(cfg, 4, new(**kw))  # noqa: E731
+    rows = 5000
+    backward = lambda **kw: B.bmgd_norm_backward(cfg, rows, new(**kw))  # noqa: E731
     _refused(backward(dx=_at(FAR), x=_at(FAR)), "dx")
     _refused(backward(dx=_at(50 * FAR, 65), dy=_at(50 * FAR, 64)), "dx", "stride")
     _refused(backward(dweight=FAR, weight=FAR), "dweight")
     _refused(backward(rstd=None), "rstd")
     _refused(backward(workspace=None), "workspace")
     _refused(backward(workspace=FAR + 128), "workspace")
-    need = B.bmgd_norm_workspace_bytes(cfg, 4)
-    assert need and need % 256 == 0 and B.bmgd_norm_workspace_bytes(cfg, 1 << 29) >= need
+    need = B.bmgd_norm_workspace_bytes(cfg, rows)
+    assert need and need % 256 == 0 and B.bmgd_norm_workspace_bytes(cfg, 1 << 29) >= need and B.bmgd_norm_workspace_bytes(cfg, 4) == 0
     _refused(backward(workspace_bytes=need - 1), "workspace", code=B.BMGD_ENOMEM)
 
 
