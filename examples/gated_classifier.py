@@ -4,8 +4,8 @@
 
 Algorithm 1 with another predictor and another update: buffers of rows stream from pinned host memory into one of two
 slots on the device while the other is computed on; every pass over a buffer draws the partition that the library's own
-runs draw (Context.get_perm), and every mini-batch makes a forward pass, the gradient of the mean cross-entropy, a
-backward pass and one AdamW step over the three weights.  Masters are fp32; the block multiplies by their bf16 copies,
+runs draw (Context.get_perm), and every mini-batch makes a forward pass, the gradient of the mean cross-entropy (LogProbs), a
+backward pass and one AdamW step over the weights.  With --norm rows are normed (RMSNorm, with a weight that is trained) before the block.  Masters are fp32; the block multiplies by their bf16 copies,
 which the step leaves.  The labels come from a gated block, so that no linear predictor fits them.
 """
 from __future__ import annotations
@@ -34,41 +34,57 @@ def draw_data(rows, p, classes, seed):
 
 
 class GatedClassifier:
-    """Weights, their gradients and bf16 copies, the block and the optimizer."""
+    """Weights, their gradients and bf16 copies, the block, the log probabilities, the optimizer, and the norm before the block if there is one."""
 
-    def __init__(self, p, hidden, classes, batch, lr, state_bits, seed):
+    def __init__(self, p, hidden, classes, batch, lr, state_bits, seed, norm=False):
         gen = torch.Generator(device="cuda").manual_seed(seed)
         shapes = [(p, hidden), (p, hidden), (hidden, classes)]
-        self.masters = [torch.randn(s, generator=gen, device="cuda") / s[0] ** 0.5 for s in shapes]
+        self.masters = [torch.randn(s, generator=gen, device="cuda") / s[0] ** 0.5 for s in shapes] + [torch.ones(p, device="cuda")] * norm
         self.weights = [m.bfloat16() for m in self.masters]
         self.grads = [torch.zeros_like(w) for w in self.weights]
         self.block = B.GatedBlock(p, hidden, classes, batch, dtype=B.BMGD_BF16, activation=B.BMGD_ACT_SILU)
         self.optimizer = B.AdamW(self.masters, self.grads, copies=self.weights, lr=lr, weight_decay=0.01, state_bits=state_bits)
         new = lambda n: torch.empty(batch, n, dtype=torch.bfloat16, device="cuda")  # noqa: E731
         self.y, self.g, self.u = new(classes), new(hidden), new(hidden)
+        self.scores = B.LogProbs(classes, dtype=B.BMGD_BF16)
+        self.logprob, self.kept = torch.empty(batch, device="cuda"), torch.empty(batch, 3, device="cuda")
+        self.norm = B.RMSNorm(p, dtype=B.BMGD_BF16) if norm else None
+        if norm:
+            self.normed, self.dnormed, self.rstd = new(p), new(p), torch.empty(batch, device="cuda")
+
+    def forward(self, x, stream, keep=False):
+        """Logits of the rows x; with `keep` what a backward pass needs stays."""
+        n = x.shape[0]
+        if self.norm:
+            self.norm.forward(x, self.weights[3], y=self.normed[:n], rstd=self.rstd[:n], stream=stream)
+            x = self.normed[:n]
+        g, u = (self.g[:n], self.u[:n]) if keep else (None, None)
+        self.block.forward(x, *self.weights[:3], self.y[:n], g=g, u=u, stream=stream)
+        return self.y[:n]
 
     def step(self, x, labels, lr, stream):
         """One update from the rows x."""
         n = x.shape[0]
-        y, g, u = self.y[:n], self.g[:n], self.u[:n]
-        self.block.forward(x, *self.weights, y, g=g, u=u, stream=stream)
-        dy = torch.softmax(y.float(), 1)
-        dy[torch.arange(n, device="cuda"), labels.long()] -= 1.0
-        self.block.backward((dy / n).bfloat16(), x, *self.weights, g, u, dgate=self.grads[0], dup=self.grads[1], ddown=self.grads[2], stream=stream)
+        y, kept, rows = self.forward(x, stream, keep=True), self.kept[:n], self.normed[:n] if self.norm else x
+        self.scores.forward(y, kept=kept, stream=stream)
+        self.scores.backward(y, kept, y, labels=labels, dlogprob=torch.full((n,), -1.0 / n, device="cuda"), stream=stream)     # the logits' gradient takes their place
+        dx = self.dnormed[:n] if self.norm else None
+        self.block.backward(y, rows, *self.weights[:3], self.g[:n], self.u[:n], dx=dx, dgate=self.grads[0], dup=self.grads[1], ddown=self.grads[2], stream=stream)
+        if self.norm:
+            self.norm.backward(dx, x, self.weights[3], self.rstd[:n], dx, dweight=self.grads[3], stream=stream)
         self.optimizer.step(lr=lr, stream=stream)
 
     def loss(self, x, labels, stream):
         """Mean cross-entropy, mini-batch by mini-batch."""
         total = torch.zeros((), dtype=torch.float64, device="cuda")
         for xs, ls in zip(x.split(self.y.shape[0]), labels.split(self.y.shape[0])):
-            y = self.y[: xs.shape[0]]
-            self.block.forward(xs, *self.weights, y, stream=stream)
-            y = y.double()
-            total += (torch.logsumexp(y, 1) - y.gather(1, ls.long()[:, None])[:, 0]).sum()
+            logprob = self.logprob[: xs.shape[0]]
+            self.scores.forward(self.forward(xs, stream), labels=ls, logprob=logprob, stream=stream)
+            total -= logprob.double().sum()
         return float(total) / x.shape[0]
 
 
-def train(rows=65_536, p=128, hidden=512, classes=10, buffers=4, batch=1_024, passes=2, iterations=4, lr=3e-3, state_bits=32, seed=0, say=print):
+def train(rows=65_536, p=128, hidden=512, classes=10, buffers=4, batch=1_024, passes=2, iterations=4, lr=3e-3, state_bits=32, seed=0, norm=False, say=print):
     """Returns (losses of the gated block after every iteration over the buffers, loss of softmax regression after the last one)."""
     host_x, host_y = draw_data(rows, p, classes, seed)
     per = -(-rows // buffers)
@@ -77,7 +93,7 @@ def train(rows=65_536, p=128, hidden=512, classes=10, buffers=4, batch=1_024, pa
     copy, compute = torch.cuda.Stream(), torch.cuda.Stream()
     loaded = [torch.cuda.Event() for _ in slots]
     read = [torch.cuda.Event() for _ in slots]
-    model = GatedClassifier(p, hidden, classes, batch, lr, state_bits, seed + 1)
+    model = GatedClassifier(p, hidden, classes, batch, lr, state_bits, seed + 1, norm)
     # softmax regression on the same buffers; also the source of the partitions
     linear = B.Context(p, per, batch, 0.5, passes, model=B.BMGD_SOFTMAX, n_classes=classes, seed=seed)
     torch.cuda.synchronize()
@@ -129,6 +145,7 @@ def main():
         ap.add_argument("--" + name, type=int, default=value)
     ap.add_argument("--lr", type=float, default=3e-3)
     ap.add_argument("--state-bits", type=int, choices=(8, 32), default=32)
+    ap.add_argument("--norm", action="store_true", help="norm rows before the block")
     train(**{k: v for k, v in vars(ap.parse_args()).items()})
 
 
