@@ -467,33 +467,44 @@ template <typename T, class C> hipError_t launch_tile(ProductArgs a, hipStream_t
 
 template <typename T> hipError_t launch_product(const ProductArgs& a, hipStream_t s)
 {
+    const uintptr_t all = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.p | (uintptr_t)a.ldx | (uintptr_t)a.ldw;
+    const bool loose = all & 15;
+    const int64_t units = compute_units();
+    auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.out + n - 1) / n); };
+    auto tile = [&](auto of) {
+        typedef decltype(of) C;
+        return launch_tile<T, C>(a, s);
+    };
+    // Measured, us (rows x p x out): 2,048 x 4,096 x 4,096: tiles of 256 48, of 128 two or three to a unit 36, of 128 alone with one step more on its way 48, of 64 x 128 44, of 64 63;
+    //      2,000 x 2,000 x 2,000: 30, 19, 17, 20, 24;  512 x 4,096 x 4,096: 44, 23, 22, 17, 18;  256 x 4,096 x 4,096: 44, 23, 22, 16, 13.  Loose: 4,097 x 2,319 x 2,965: of 128 66, of 64 92;
+    //      2,000 x 2,001 x 2,000: of 128 27, with eight wavefronts and one step more on its way 23, of 64 33.
+    if (loose) {
+        if (tiles(128, 128) > units) return tile(Tile<128, 128, 2, 2, 1, true>());
+        if (tiles(128, 128) > units / 2) return tile(Tile<128, 128, 2, 4, 2, true>());
+    } else {
+        if (tiles(256, 256) >= units) return tile(Tile<256, 256, 2, 4, 1, false>());
+        if (tiles(128, 128) > units) return tile(Tile<128, 128, 2, 2, 1, false>());
+        if (tiles(128, 128) > units / 2) return tile(Tile<128, 128, 2, 2, 2, false>());
+        if (tiles(64, 128) > units * 3 / 4) return tile(Tile<64, 128, 2, 2, 2, false>());
+    }
+    // Few tiles.  A step of one takes 0.17 us (32 x 32), 0.21 (32 x 64) or 0.28 (64 x 64), loose ones 0.24, 0.31 and 0.42.  Workgroups of 16 columns without steps read rows more
+    // often: their operands come at 12 TB/s in all (4.4 where pieces cross lines) and 45 GB/s to a unit.  Measured, us, tiles and these: 64 x 4,096 x 4,096: 9.4 and 12;  100 x 8,192 x 1,000:
+    // 15 and 13;  16 x 4,096 x 8,192: 9.4 and 10.2;  1 x 4,096 x 8,192: 9.4 and 8.1;  333 x 1,365 x 1,000, loose: 7.4 and 15.
+    const bool small = tiles(32, 32) <= (loose ? units : 2 * units), flat = tiles(32, 64) <= units;
+    const double tile_us = 4.0 + (small ? loose ? 0.24 : 0.17 : flat ? loose ? 0.31 : 0.21 : loose ? 0.42 : 0.28) * ((a.p + kStep - 1) / kStep);
+    auto few_us = [&](int64_t rf) {
+        const double each = (16.0 + (double)std::min(16 * rf, a.rows)) * a.p, groups = (double)((a.out + 15) / 16) * (double)((a.rows + 16 * rf - 1) / (16 * rf));
+        return 4.8 + std::max(each * groups / (loose ? 4.4e6 : 12e6), each / 45e3);
+    };
     auto few = [&](auto rf) {
         constexpr int RF = decltype(rf)::value;
         hipLaunchKernelGGL((int8_few_kernel<T, RF>), dim3((unsigned)((a.out + 15) / 16), (unsigned)((a.rows + 16 * RF - 1) / (16 * RF))), dim3(64 * kFewWaves), 0, s, a);
         return hipGetLastError();
     };
-    if (a.rows <= 16) return few(std::integral_constant<int, 1>());
-    if (a.rows <= 32) return few(std::integral_constant<int, 2>());
-    const uintptr_t all = reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w) | (uintptr_t)a.p | (uintptr_t)a.ldx | (uintptr_t)a.ldw;
-    const bool loose = all & 15;
-    const int64_t units = compute_units();
-    auto tiles = [&](int64_t m, int64_t n) { return (a.rows + m - 1) / m * ((a.out + n - 1) / n); };
-    if (loose) return tiles(128, 128) >= units ? launch_tile<T, Tile<128, 128, 2, 2, 1, true>>(a, s) : launch_tile<T, Tile<64, 64, 2, 2, 4, true>>(a, s);
-    // Measured, us (rows x p x out): 2,048 x 4,096 x 4,096: tiles of 256 48, of 128 two or three to a unit 36, of 128 alone with one step more on its way 48, of 64 x 128 44, of 64 63;
-    //      2,000 x 2,000 x 2,000: 30, 19, 17, 20, 24;  512 x 4,096 x 4,096: 44, 23, 22, 17, 18;  256 x 4,096 x 4,096: 44, 23, 22, 16, 13.
-    if (tiles(256, 256) >= units) return launch_tile<T, Tile<256, 256, 2, 4, 1, false>>(a, s);
-    if (tiles(128, 128) > units) return launch_tile<T, Tile<128, 128, 2, 2, 1, false>>(a, s);
-    if (tiles(128, 128) > units / 2) return launch_tile<T, Tile<128, 128, 2, 2, 2, false>>(a, s);
-    if (tiles(64, 128) > units * 3 / 4) return launch_tile<T, Tile<64, 128, 2, 2, 2, false>>(a, s);
-    // Few tiles of 64, many steps: workgroups of 16 columns, which read the same rows more often.  Their operands come at 12 TB/s in all and 45 GB/s to a unit, a step of a tile
-    // takes 0.28 us: 100 x 8,192 x 1,000: 13 and 22 us;  64 x 4,096 x 4,096: 12 and 13;  128 x 4,096 x 4,096: 24 and 13.
-    const auto few_us = [&](int64_t rf) {
-        const double each = 16.0 * (double)(rf + 1) * a.p, groups = (double)((a.out + 15) / 16) * (double)((a.rows + 16 * rf - 1) / (16 * rf));
-        return 4.8 + std::max(each * groups / 12e6, each / 45e3);
-    };
-    const double tile_us = 4.0 + 0.28 * ((a.p + kStep - 1) / kStep), two = few_us(2), four = few_us(4);
-    if (std::min(two, four) < tile_us) return two < four ? few(std::integral_constant<int, 2>()) : few(std::integral_constant<int, 4>());
-    return launch_tile<T, Tile<64, 64, 2, 2, 3, false>>(a, s);
+    const double one = few_us(1), two = few_us(2), four = few_us(4), best = std::min(one, std::min(two, four));
+    if (best < tile_us && a.rows < (1 << 19)) return one == best ? few(std::integral_constant<int, 1>()) : two == best ? few(std::integral_constant<int, 2>()) : few(std::integral_constant<int, 4>());
+    if (loose) return small ? tile(Tile<32, 32, 2, 2, 6, true>()) : flat ? tile(Tile<32, 64, 2, 2, 4, true>()) : tile(Tile<64, 64, 2, 4, 4, true>());
+    return small ? tile(Tile<32, 32, 2, 2, 4, false>()) : flat ? tile(Tile<32, 64, 1, 4, 3, false>()) : tile(Tile<64, 64, 2, 4, 3, false>());
 }
 
 void check(Call& q, const bmgd_product_config* cfg)
