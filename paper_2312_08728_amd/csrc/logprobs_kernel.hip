@@ -7,7 +7,7 @@
 //
 // The most probable classes.  A logit and its class are one 64-bit number, larger where the logit is larger and, of equal ones, the class lower; so no two are
 // equal.  Of what the threads read first (8,192 logits of 16 bits for four wavefronts), 64 groups of threads have their largest numbers; the top-th largest of these is not above the top-th
-// largest of the row.  Pieces that reach it are put into shared memory as they pass by.  After 2, 4, 8, ... turns their classes that do are counted against one another, the
+// largest of the row.  Pieces that reach it are put into shared memory as they pass by.  After 2, 4, 8, ... turns (from 64 / top on) their classes that do are counted against one another, the
 // place of each being the number of larger ones; the top-th of them is what later ones have to reach, so that between two counts about as many are listed as are wanted.
 // Where a list overflows (logits that rise all along a row) or a row has NaN, the classes are found one after the other.
 #include "operator_calls.h"
@@ -105,13 +105,14 @@ template <int W> __device__ __forceinline__ void together()
     }
 }
 
-// How many of `count` numbers are larger
+// How many of `count` numbers in shared memory are larger than v, which four neighbouring lanes have: each looks at a quarter
 __device__ __forceinline__ int larger_than(Key v, const Key* all, int count)
 {
     int larger = 0;
 #pragma unroll 4
-    for (int i = 0; i < count; ++i) larger += all[i] > v;
-    return larger;
+    for (int i = threadIdx.x & 3; i < count; i += 4) larger += all[i] > v;
+    larger += from_lane<kSwap1>(larger);
+    return larger + from_lane<kSwap2>(larger);
 }
 
 // Pieces begin at multiples of 16 bytes: `before` elements before the row, which with those behind `end` count as -infinity.
@@ -229,7 +230,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     typedef typename Piece<T>::vec vec;
     typedef typename Piece<T>::wide wide;
     __shared__ Stats parts[W > 1 ? W : 1];
-    __shared__ Key groups_of[TOP ? kRows : 1][TOP ? (W == 1 ? 64 : 128) : 1];                  // (at most half as many as threads)
+    __shared__ Key groups_of[TOP ? kRows : 1][TOP ? (W > 1 ? 128 : 64) : 1];
     __shared__ Key list[TOP ? kRows : 1][TOP ? kList : 1];
     __shared__ Key sorted[TOP ? kRows : 1][2][TOP ? kMaxTop : 1];
     __shared__ vec pieces[TOP ? kRows : 1][TOP ? kPieces : 1];
@@ -287,10 +288,10 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         const int fresh = min(listed[mine][in_use], kList);
         over |= listed[mine][in_use] > kList;
         const Key* const old = sorted[mine][in_use];
-        for (int i = t; i < have + fresh; i += kLanes) {
+        for (int i = t / 4; i < have + fresh; i += kLanes / 4) {
             const Key q = i < have ? old[i] : list[mine][i - have];
             const int place = larger_than(q, old, have) + larger_than(q, list[mine], fresh);
-            if (place < a.top) sorted[mine][in_use ^ 1][place] = q;
+            if (t % 4 == 0 && place < a.top) sorted[mine][in_use ^ 1][place] = q;
         }
         together<W>();
         if (t == 0) kept[mine][in_use] = listed[mine][in_use] = 0;
@@ -327,28 +328,31 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                 }
                 const auto larger = [](Key p, Key q) { return p > q ? p : q; };
                 if constexpr (W > 1) {
-                    // 64 groups of four threads; 128 of two, where 64 would leave many to list.  The threads of a group share the counting of larger ones.
-                    const bool few = a.top <= 16;
-                    const int of = few ? 4 : 2, each = kLanes / (of * of);
+                    // 64 groups of four threads; where 64 would leave many to list 128 of two, each of which is counted by four threads too
+                    const bool few = a.top <= 32;
                     k = larger(k, from_lane<kSwap1>(k));
                     if (few) k = larger(k, from_lane<kSwap2>(k));
+                    const int of = few ? 4 : 2;
                     if (t % of == 0) groups_of[0][t / of] = k;
                     if (t == 0) {
                         threshold = 0;
                         kept[0][0] = kept[0][1] = listed[0][0] = listed[0][1] = 0;
                     }
                     __syncthreads();
-                    int place = larger_than(k, groups_of[0] + t % of * each, each);
-                    place += from_lane<kSwap1>(place);
-                    if (few) place += from_lane<kSwap2>(place);
-                    if (place == a.top - 1) threshold = k;      // (the same from all of a group)
+                    for (int i = t / 4; i < kLanes / of; i += kLanes / 4) {
+                        k = groups_of[0][i];
+                        if (larger_than(k, groups_of[0], kLanes / of) == a.top - 1) threshold = k;
+                    }
                     __syncthreads();
                     least = threshold;
                 } else {
-                    groups_of[mine][t] = k;
                     if (t == 0) kept[mine][0] = kept[mine][1] = listed[mine][0] = listed[mine][1] = 0;
+                    groups_of[mine][t] = k;
                     together<1>();
-                    const unsigned long long found = __ballot(larger_than(k, groups_of[mine], 64) == a.top - 1);
+                    int place = 0;
+#pragma unroll 8
+                    for (int i = 0; i < 64; ++i) place += groups_of[mine][i] > k;
+                    const unsigned long long found = __ballot(place == a.top - 1);
                     if (found) least = of_lane(k, __builtin_ctzll(found));
                 }
                 // (equal numbers are zeros, of groups without a class: where there is no top-th, all are listed)
@@ -380,10 +384,13 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     const float at_label = label >= 0 && label < a.classes ? (float)x[label] : 0.f;
     turn(std::true_type());
     const int turns = (end - edge.whole + kTurn - 1) / kTurn;   // (of the row: some threads have nothing left in the last one)
-    for (int n = 1; n < turns; ++n) {
-        turn(std::false_type());
+    for (int n = 1;; ++n) {
+        const bool more = n < turns;
+        if (more) turn(std::false_type());
+        // (before 64 / top turns fewer than 128 pieces are expected)
         if constexpr (TOP)
-            if (!(n & (n + 1)) && n + 1 < turns) count_kept();
+            if (!more || (!(n & (n + 1)) && a.top * (n + 1) >= 64 && n + 1 < turns)) count_kept();
+        if (!more) break;
     }
     if (edge_at != kNowhere) {
         const wide v = widen<T>(edge_piece);
@@ -435,7 +442,6 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         } else write_row(a, row, label, at_label, r);
     }
     if constexpr (TOP) {
-        count_kept();
         if (st.s == st.s && !over) {
             if (t < a.top) write_top(a, row, part, t, t < have ? sorted[mine][in_use][t] : 0, r);          // (a part may have fewer than `top` classes)
         } else {
@@ -470,7 +476,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
 template <typename T> __global__ void __launch_bounds__(256) logprobs_join_kernel(LogArgs a)
 {
     extern __shared__ Key list[];
-    __shared__ Key bounds[64];
+    __shared__ Key bounds[64], at_half;
     __shared__ int count;
     const int64_t row = blockIdx.x;
     const int lane = threadIdx.x & 63, keys_of_row = a.parts * a.top;
@@ -493,27 +499,26 @@ template <typename T> __global__ void __launch_bounds__(256) logprobs_join_kerne
     if (threadIdx.x == 0) {
         write_row(a, row, label, at_label, r);
         count = 0;
+        at_half = 0;
     }
     if (!a.top) return;
     if (threadIdx.x < 64) bounds[lane] = bound;
     __syncthreads();
     // (parts' numbers differ but for zeros)
-    const unsigned long long found = __ballot(lane < a.parts && larger_than(bound, bounds, 64) == half - 1);
+    const Key counted = bounds[threadIdx.x / 4];
+    if (counted && larger_than(counted, bounds, 64) == half - 1) at_half = counted;
     Key least = wave_max(last);
-    if (found) {
-        const Key other = of_lane(bound, __builtin_ctzll(found));
-        least = other > least ? other : least;
-    }
+    __syncthreads();
+    least = at_half > least ? at_half : least;
     for (int i = threadIdx.x; i < keys_of_row; i += 256) {
         if (i >= 256) mine = keys[i];
         if (mine && mine >= least) list[atomicAdd(&count, 1)] = mine;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < count; i += 256) {
+    for (int i = threadIdx.x / 4; i < count; i += 64) {
         const Key q = list[i];
-        int place = 0;
-        for (int o = 0; o < count; ++o) place += list[o] > q;
-        if (place < a.top) {
+        const int place = larger_than(q, list, count);
+        if (threadIdx.x % 4 == 0 && place < a.top) {
             a.top_classes[row * a.top + place] = class_of(q);
             a.top_logprobs[row * a.top + place] = logprob_of(r, value_of(q));
         }
