@@ -9,7 +9,8 @@
 // equal.  Of what the threads read first (8,192 logits of 16 bits for four wavefronts), 64 groups of threads have their largest numbers; the top-th largest of these is not above the top-th
 // largest of the row.  Pieces that reach it are put into shared memory as they pass by.  After 2, 4, 8, ... turns (from 64 / top on) their classes that do are counted against one another, the
 // place of each being the number of larger ones; the top-th of them is what later ones have to reach, so that between two counts about as many are listed as are wanted.
-// Where a list overflows (logits that rise all along a row) or a row has NaN, the classes are found one after the other.
+// Where a list overflows (logits that rise all along a row), the row is read again with the bound that came of it; where it does so again, or a row has NaN, the
+// classes are found one after the other.
 #include "operator_calls.h"
 #include "rows_device.h"
 
@@ -254,7 +255,8 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     vec edge_piece = (vec)(T)-__builtin_inff();
     if (edge_at != kNowhere) edge_piece = Piece<T>::load_part(x, edge_at, begin, end, (T)-__builtin_inff());
     vec next[U];
-    int j = edge.whole + N * t;
+    // (the four threads of a group are a quarter of a turn apart: the first pieces, which win where logits are equal, are in different groups)
+    int j = edge.whole + N * (W > 1 ? t % 4 * (kLanes / 4) + t / 4 : t);
     auto request = [&]() {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -384,13 +386,11 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
     const float at_label = label >= 0 && label < a.classes ? (float)x[label] : 0.f;
     turn(std::true_type());
     const int turns = (end - edge.whole + kTurn - 1) / kTurn;   // (of the row: some threads have nothing left in the last one)
-    for (int n = 1;; ++n) {
-        const bool more = n < turns;
-        if (more) turn(std::false_type());
+    for (int n = 1; n < turns; ++n) {
+        turn(std::false_type());
         // (before 64 / top turns fewer than 128 pieces are expected)
         if constexpr (TOP)
-            if (!more || (!(n & (n + 1)) && a.top * (n + 1) >= 64 && n + 1 < turns)) count_kept();
-        if (!more) break;
+            if (!(n & (n + 1)) && a.top * (n + 1) >= 64 && n + 1 < turns) count_kept();
     }
     if (edge_at != kNowhere) {
         const wide v = widen<T>(edge_piece);
@@ -442,6 +442,17 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         } else write_row(a, row, label, at_label, r);
     }
     if constexpr (TOP) {
+        for (bool again = false;; again = true) {
+            count_kept();
+            if (!over || again) break;
+            // What was listed, though not all, bounds the row's top-th from below: everything that reaches it, once more.
+            over = false;
+            have = 0;
+            for (int i = head + N * t; i < end; i += N * kLanes) {
+                const vec v = logits_at(x, i, begin, end);
+                if (key_of(largest(widen<T>(v)), max(i, begin)) >= least) keep(v, i);
+            }
+        }
         if (st.s == st.s && !over) {
             if (t < a.top) write_top(a, row, part, t, t < have ? sorted[mine][in_use][t] : 0, r);          // (a part may have fewer than `top` classes)
         } else {

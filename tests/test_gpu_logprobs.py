@@ -171,6 +171,23 @@ def test_rows_of_trouble(kind, classes, top):
     _gradient(kind, op, out, x, x64, labels, logp, entropy)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("classes,top", [(600, 64), (5000, 17), (20_000, 20), (20_000, 64), (90_000, 33)])
+def test_equal_logits(kind, classes, top):
+    """As many rows as one launch has workgroups for: equal in all classes, in a few values, in all but some, masked but for some."""
+    import torch
+    x = torch.zeros(600, classes)
+    x[150:300] = torch.randint(0, 3, (150, classes), generator=torch.Generator().manual_seed(0)).float()
+    x[300:] = -math.inf
+    allowed = torch.randint(0, classes, (300, 10), generator=torch.Generator().manual_seed(1))
+    x[300:].scatter_(1, allowed, 1.5)
+    x[450:] = torch.where(x[450:] > 0, x[450:], torch.zeros(()))
+    x = x.to(_types()[kind][0]).cuda()
+    _check(kind, x[::50], np.zeros(12, dtype=np.int64), top)              # (rows far apart)
+    _, out = _forward(kind, x, torch.zeros(600, dtype=torch.int32, device="cuda"), top)
+    assert (out["top_classes"][::50].cpu().numpy() == O.best(_np(x[::50]), top)).all() and (out["top_classes"][:150] == torch.arange(top, device="cuda")).all()
+
+
 def test_results_alone():
     """Each result by itself has the bits that it has with the others; no labels are needed without logprob."""
     import torch
