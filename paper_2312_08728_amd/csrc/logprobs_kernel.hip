@@ -9,11 +9,11 @@
 // equal.  Of what the threads read first (8,192 logits of 16 bits for four wavefronts), 64 groups of threads have their largest numbers; the top-th largest of these is not above the top-th
 // largest of the row.  Pieces that reach it are put into shared memory as they pass by.  After 2, 4, 8, ... turns (from 64 / top on) their classes that do are counted against one another, the
 // place of each being the number of larger ones; the top-th of them is what later ones have to reach, so that between two counts about as many are listed as are wanted.
-// Where a list overflows (logits that rise all along a row), the row is read again with the bound that came of it; where it does so again, or a row has NaN, the
+// Where a list overflows (logits that rise all along a row), the row is read again with a bound that comes of all of it; where it does so again, or a row has NaN, the
 // classes are found one after the other.
 //
-// What bounds it (us).  8,192 x 32,000, bf16: 93 without classes (5.6 TB/s), 118 with eight: memory, and counting that four workgroups to a unit do not hide.  4,097 x 10,001, f16: 25, of which 15 are vector
-// instructions (12 an element); the gradient 30 (5.5 TB/s).  16 x 100,003, fp32, twenty classes: 12, two launches.  1 x 1,000: 4.9, a launch and a chain of one trip to memory, a count and sums.
+// What bounds it (us).  8,192 x 32,000, bf16: 93 without classes (5.6 TB/s), 118 with eight: memory, and counting that four workgroups to a unit do not hide.  4,097 x 10,001, f16: 25, of which memory 16,
+// the rest a launch, the first trip and the last turn; the gradient 30 (5.5 TB/s).  16 x 100,003, fp32, twenty classes: 12, two launches.  1 x 1,000: 4.9, a launch and a chain of one trip to memory, a count and sums.
 #include "operator_calls.h"
 #include "rows_device.h"
 
@@ -32,7 +32,7 @@ constexpr float kLowest = -3.40282347e38f;
 constexpr float kUsual = 1e37f;                  // x log2 e - r is finite, or -infinity for one far below, where m is smaller than this
 constexpr float kFar = -1000.f;                  // 2^-1000 is 0, times this still 0
 constexpr int kMaxTop = 64, kMaxParts = 64;
-constexpr int kList = 512;                       // classes listed between two counts at most: a row of fewer than 8 top fits whole,
+constexpr int kList = 640;                       // classes listed between two counts at most: a row of fewer than 8 top fits whole,
 constexpr int pieces_kept(int w) { return w == 1 ? 80 : 256; }         // and pieces: 64, and two that are not whole
 
 struct LogArgs {
@@ -304,6 +304,34 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         have = min(have + fresh, a.top);
         if (have == a.top) least = sorted[mine][in_use][have - 1];
     };
+    // From each thread's largest number the top-th largest of groups of them, 0 if there are fewer.  (Numbers differ but for zeros, of threads without a class.)
+    auto larger = [](Key p, Key q) { return p > q ? p : q; };
+    auto bound = [&](Key k) -> Key {
+        if constexpr (W > 1) {
+            // 64 groups of four threads; where 64 would leave many to list 128 of two, each of which is counted by four threads too
+            const bool few = a.top <= 32;
+            k = larger(k, from_lane<kSwap1>(k));
+            if (few) k = larger(k, from_lane<kSwap2>(k));
+            const int of = few ? 4 : 2;
+            if (t % of == 0) groups_of[0][t / of] = k;
+            if (t == 0) threshold = 0;
+            __syncthreads();
+            for (int i = t / 4; i < kLanes / of; i += kLanes / 4) {
+                k = groups_of[0][i];
+                if (larger_than(k, groups_of[0], kLanes / of) == a.top - 1) threshold = k;
+            }
+            __syncthreads();
+            return threshold;
+        } else {
+            groups_of[mine][t] = k;
+            together<1>();
+            int place = 0;
+#pragma unroll 8
+            for (int i = 0; i < 64; ++i) place += groups_of[mine][i] > k;
+            const unsigned long long found = __ballot(place == a.top - 1);
+            return found ? of_lane(k, __builtin_ctzll(found)) : 0;
+        }
+    };
     // turns of U pieces, the next ones on their way
     auto turn = [&](auto first) {
         vec now[U];
@@ -327,40 +355,10 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                     }
                 // (with the last class of the piece: not above what it stands for)
                 Key k = at + N <= end ? key_of(best, best_at + N - 1) : 0;
-                if (edge_at != kNowhere) {
-                    const Key of_edge = key_of(largest(widen<T>(edge_piece)), min(edge_at + N, end) - 1);
-                    k = of_edge > k ? of_edge : k;
-                }
-                const auto larger = [](Key p, Key q) { return p > q ? p : q; };
-                if constexpr (W > 1) {
-                    // 64 groups of four threads; where 64 would leave many to list 128 of two, each of which is counted by four threads too
-                    const bool few = a.top <= 32;
-                    k = larger(k, from_lane<kSwap1>(k));
-                    if (few) k = larger(k, from_lane<kSwap2>(k));
-                    const int of = few ? 4 : 2;
-                    if (t % of == 0) groups_of[0][t / of] = k;
-                    if (t == 0) {
-                        threshold = 0;
-                        kept[0][0] = kept[0][1] = listed[0][0] = listed[0][1] = 0;
-                    }
-                    __syncthreads();
-                    for (int i = t / 4; i < kLanes / of; i += kLanes / 4) {
-                        k = groups_of[0][i];
-                        if (larger_than(k, groups_of[0], kLanes / of) == a.top - 1) threshold = k;
-                    }
-                    __syncthreads();
-                    least = threshold;
-                } else {
-                    if (t == 0) kept[mine][0] = kept[mine][1] = listed[mine][0] = listed[mine][1] = 0;
-                    groups_of[mine][t] = k;
-                    together<1>();
-                    int place = 0;
-#pragma unroll 8
-                    for (int i = 0; i < 64; ++i) place += groups_of[mine][i] > k;
-                    const unsigned long long found = __ballot(place == a.top - 1);
-                    if (found) least = of_lane(k, __builtin_ctzll(found));
-                }
-                // (equal numbers are zeros, of groups without a class: where there is no top-th, all are listed)
+                if (edge_at != kNowhere) k = larger(k, key_of(largest(widen<T>(edge_piece)), min(edge_at + N, end) - 1));
+                if (t == 0) kept[mine][0] = kept[mine][1] = listed[mine][0] = listed[mine][1] = 0;
+                least = bound(k);
+                // (where there is no top-th, all are listed)
                 if (edge_at != kNowhere && key_of(largest(widen<T>(edge_piece)), max(edge_at, begin)) >= least) keep(edge_piece, edge_at);
             }
             const float value = least ? value_of(least) : -__builtin_inff();
@@ -448,9 +446,13 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         for (bool again = false;; again = true) {
             count_kept();
             if (!over || again) break;
-            // What was listed, though not all, bounds the row's top-th from below: everything that reaches it, once more.
+            // The bound again, of all that the threads have read, and everything that reaches it.
             over = false;
             have = 0;
+            Key k = 0;
+            for (int i = head + N * (W > 1 ? t % 4 * (kLanes / 4) + t / 4 : t); i < end; i += N * kLanes)
+                k = larger(k, key_of(largest(widen<T>(logits_at(x, i, begin, end))), min(i + N, end) - 1));
+            least = larger(least, bound(k));
             for (int i = head + N * t; i < end; i += N * kLanes) {
                 const vec v = logits_at(x, i, begin, end);
                 if (key_of(largest(widen<T>(v)), max(i, begin)) >= least) keep(v, i);

@@ -8,7 +8,7 @@
 // is common to a row) in 64 bits: products of 16-bit elements are exact, so values next to the middle of two codes go where the definition says.
 //
 // What bounds it (us).  8,192 rows of 8,192, bf16, residual, 8 bits: 93 (470 MB, 5.0 TB/s), the values of the codes 65 (335 MB): memory.  Backward of 8,192 rows of 4,096 with dsum 52
-// (268 MB, 5.2 TB/s) and 5.9 for the 512 parts of dw.  777 rows of 1,365, f16: 4.6, 1,000 rows of 512 backward, fp32: 7.5, one row: 3.5: a launch (2.8) and a trip to memory.
+// (268 MB, 5.2 TB/s) and 4.4 for the 512 parts of dw.  777 rows of 1,365, f16: 4.6, 1,000 rows of 512 backward, fp32: 7.5, one row: 3.5: a launch (2.8) and a trip to memory.
 #include "operator_calls.h"
 #include "rows_device.h"
 
@@ -473,20 +473,29 @@ template <typename T> __global__ void __launch_bounds__(64) norm_columns_kernel(
     put_sums<T>(a.partial + (int64_t)blockIdx.y * a.n, j, a.n, dw);
 }
 
-// dweight from the parts, always in the same order: a workgroup has 32 columns, 32 threads of it every 32nd part of one of them.
+// dweight from the parts, always in the same order: a workgroup has 16 columns, 64 threads of it every 64th part of one of them; then eight and eight of these.
 template <typename T> __global__ void __launch_bounds__(1024) norm_join_kernel(const float* __restrict__ partial, T* __restrict__ dweight, int parts, int n)
 {
-    __shared__ float sums[32][33];
-    const int col = threadIdx.x & 31, slice = threadIdx.x >> 5, j = blockIdx.x * 32 + col;
+    __shared__ float sums[64][17], eights[8][16];
+    const int col = threadIdx.x & 15, slice = threadIdx.x >> 4, j = blockIdx.x * 16 + col;
     float v = 0.f;
-    if (j < n)
-        for (int g = slice; g < parts; g += 32) v += partial[(int64_t)g * n + j];
+    if (j < n) {
+#pragma unroll 8
+        for (int g = slice; g < parts; g += 64) v += partial[(int64_t)g * n + j];
+    }
     sums[slice][col] = v;
+    __syncthreads();
+    if (slice < 8) {
+        v = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v += sums[8 * slice + i][col];
+        eights[slice][col] = v;
+    }
     __syncthreads();
     if (slice == 0 && j < n) {
         v = 0.f;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v += sums[i][col];
+        for (int i = 0; i < 8; ++i) v += eights[i][col];
         dweight[j] = (T)v;
     }
 }
@@ -725,7 +734,7 @@ BMGD_API int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const
     if (rc != BMGD_OK || !t->dweight || columns) return rc;
     with_type(cfg->dtype, [&](auto type) {
         typedef decltype(type) T;
-        hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)((cfg->n + 31) / 32)), dim3(1024), 0, s, a.partial, static_cast<T*>(t->dweight), (int)parts, a.n);
+        hipLaunchKernelGGL(norm_join_kernel<T>, dim3((unsigned)((cfg->n + 15) / 16)), dim3(1024), 0, s, a.partial, static_cast<T*>(t->dweight), (int)parts, a.n);
     });
     return q.launched();
 }

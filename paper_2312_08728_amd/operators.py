@@ -44,9 +44,13 @@ def _refuse(name, t, kind, shape, matrix, index):
 
 def _rows_of(name, t):
     """Rows and GPU of a call's first matrix."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
-        raise ValueError(f"{name}: a matrix on a GPU is wanted")
-    return t.shape[0], t.get_device()
+    try:
+        index = t.get_device()
+        if index >= 0:
+            return t.shape[0], index
+    except (AttributeError, IndexError):
+        pass
+    raise ValueError(f"{name}: a matrix on a GPU is wanted")
 
 
 def _places(names, tensors, kinds, shapes, how, index):
@@ -91,8 +95,7 @@ class RMSNorm:
     n: columns.  dtype: of all matrices but codes, and of the weight (BMGD_F32, BMGD_BF16, BMGD_F16).
     """
 
-    _FORWARD = ("x", "residual", "sum", "y", "codes", "weight", "scales", "rstd")
-    _BACKWARD = ("x", "dy", "dsum", "dx", "weight", "dweight", "rstd")
+    _NAMES = ("x", "residual", "sum", "y", "codes", "dy", "dsum", "dx", "weight", "dweight", "scales", "rstd")       # bmgd_norm_tensors
 
     def __init__(self, n, dtype=B.BMGD_BF16, eps=1e-6):
         self._type = t = _type_of(dtype)
@@ -102,27 +105,27 @@ class RMSNorm:
             raise ValueError("eps must be finite in 32 bits and >= 0")
         self.n, self.cfg = n, B.bmgd_norm_config(n, eps, dtype, 0)
         self._cfg = C.byref(self.cfg)
-        self._in = (t, t, t, t, _BYTE, t, _FLOAT, _FLOAT)
-        self._back = (t, t, t, t, t, t, _FLOAT)
+        self._kinds = (t, t, t, t, _BYTE, t, t, t, t, t, _FLOAT, _FLOAT)
+        self._of_n = (n,)
 
     def forward(self, x, weight=None, y=None, residual=None, sum=None, codes=None, scales=None, rstd=None, stream=None):
         """Writes y, or codes and scales, or all three; sum <- s and rstd <- 1 / sqrt(mean s^2 + eps) where they are given (`backward` reads both; s is x
         without a residual).  weight None: ones.  sum may be x or residual, y may be x (without sum there) or residual."""
         rows, index = _rows_of("x", x)
-        at, of = (rows, self.n), (rows,)
-        found = _places(self._FORWARD, (x, residual, sum, y, codes, weight, scales, rstd), self._in, (at, at, at, at, at, (self.n,), of, of), b"mmMMMvVV", index)
-        # x residual sum y codes | dy dsum dx | weight dweight scales rstd workspace bytes
-        tensors = found[:80] + bytes(48) + found[80:88] + bytes(8) + found[88:] + _NONE16
+        at, of, n = (rows, self.n), (rows,), self._of_n
+        tensors = _places(self._NAMES, (x, residual, sum, y, codes, None, None, None, weight, None, scales, rstd), self._kinds, (at, at, at, at, at, at, at, at, n, n, of, of),
+                          b"mmMMMmmmvvVV", index) + _NONE16
         _run(B.lib.bmgd_norm_forward, (self._cfg, rows, tensors), stream, index)
 
     def backward(self, dy, s, weight, rstd, dx, dweight=None, dsum=None, workspace=None, stream=None):
         """dx <- the gradient of x (and of residual alike) from dy, the s that was normed and the forward call's rstd, plus dsum, the gradient that reaches s besides;
         dweight <- the weight's.  dx may be dy or dsum."""
         rows, index = _rows_of("s", s)
-        at = (rows, self.n)
-        found = _places(self._BACKWARD, (s, dy, dsum, dx, weight, dweight, rstd), self._back, (at, at, at, at, (self.n,), (self.n,), (rows,)), b"mmmMvVv", index)
+        at, of, n = (rows, self.n), (rows,), self._of_n
+        found = _places(self._NAMES, (s, None, None, None, None, dy, dsum, dx, weight, dweight, None, rstd), self._kinds, (at, at, at, at, at, at, at, at, n, n, of, of),
+                        b"mmmmmmmMvVvv", index)
         keep, place = _workspace(B.lib.bmgd_norm_workspace_bytes(self._cfg, rows) if dweight is not None and rows else 0, workspace, stream, index)
-        tensors = found[:16] + bytes(64) + found[16:80] + bytes(8) + found[80:] + place
+        tensors = found + place
         _run(B.lib.bmgd_norm_backward, (self._cfg, rows, tensors), stream, index)
 
     def values(self, codes, scales, out, stream=None):
@@ -178,8 +181,7 @@ class LogProbs:
     classes: columns; dtype: of the logits (BMGD_F32, BMGD_BF16, BMGD_F16); top: up to 64.  Labels are int32: a negative one leaves its row out.
     """
 
-    _FORWARD = ("logits", "labels", "logprob", "entropy", "top_classes", "top_logprobs", "kept")
-    _BACKWARD = ("logits", "dlogits", "labels", "kept", "dlogprob", "dentropy")
+    _NAMES = ("logits", "dlogits", "labels", "logprob", "entropy", "top_classes", "top_logprobs", "kept", "dlogprob", "dentropy")       # bmgd_logprobs_tensors
 
     def __init__(self, classes, dtype=B.BMGD_BF16, top=0):
         self._type = t = _type_of(dtype)
@@ -189,23 +191,22 @@ class LogProbs:
             raise ValueError("top must be in [0, 64] and not above classes")
         self.classes, self.top, self.cfg = classes, top, B.bmgd_logprobs_config(classes, dtype, top)
         self._cfg = C.byref(self.cfg)
-        self._in = (t, _INT, _FLOAT, _FLOAT, _INT, _FLOAT, _FLOAT)
-        self._back = (t, t, _INT, _FLOAT, _FLOAT, _FLOAT)
+        self._kinds = (t, t, _INT, _FLOAT, _FLOAT, _INT, _FLOAT, _FLOAT, _FLOAT, _FLOAT)
 
     def forward(self, logits, labels=None, logprob=None, entropy=None, top_classes=None, top_logprobs=None, kept=None, workspace=None, stream=None):
         """Writes what is given: logprob (of labels, rows of them), entropy (rows), top_classes and top_logprobs (rows x top each; both wanted where top is not 0),
         kept (rows x 3, fp32: what `backward` needs)."""
         rows, index = _rows_of("logits", logits)
-        of, best = (rows,), (rows, self.top)
-        found = _places(self._FORWARD, (logits, labels, logprob, entropy, top_classes, top_logprobs, kept), self._in,
-                        ((rows, self.classes), of, of, of, best, best, (rows, 3)), b"mvVVVVV", index)
+        at, of, best = (rows, self.classes), (rows,), (rows, self.top)
+        found = _places(self._NAMES, (logits, None, labels, logprob, entropy, top_classes, top_logprobs, kept, None, None), self._kinds,
+                        (at, at, of, of, of, best, best, (rows, 3), of, of), b"mmvVVVVVvv", index)
         keep, place = _workspace(B.lib.bmgd_logprobs_workspace_bytes(self._cfg, rows), workspace, stream, index)
-        _run(B.lib.bmgd_logprobs_forward, (self._cfg, rows, found[:16] + _NONE16 + found[16:] + _NONE16 + place), stream, index)
+        _run(B.lib.bmgd_logprobs_forward, (self._cfg, rows, found + place), stream, index)
 
     def backward(self, logits, kept, dlogits, labels=None, dlogprob=None, dentropy=None, stream=None):
         """dlogits <- dlogprob ([j = label] - p_j) - dentropy p_j (ln p_j + entropy), from the forward call's `kept`.  dlogits may be logits."""
         rows, index = _rows_of("logits", logits)
         at, of = (rows, self.classes), (rows,)
-        found = _places(self._BACKWARD, (logits, dlogits, labels, kept, dlogprob, dentropy), self._back, (at, at, of, (rows, 3), of, of), b"mMvvvv", index)
-        # logits dlogits labels | logprob entropy top_classes top_logprobs | kept dlogprob dentropy workspace bytes
-        _run(B.lib.bmgd_logprobs_backward, (self._cfg, rows, found[:40] + bytes(32) + found[40:] + _NONE16), stream, index)
+        found = _places(self._NAMES, (logits, dlogits, labels, None, None, None, None, kept, dlogprob, dentropy), self._kinds, (at, at, of, of, of, of, of, (rows, 3), of, of),
+                        b"mMvvvvvvvv", index)
+        _run(B.lib.bmgd_logprobs_backward, (self._cfg, rows, found + _NONE16), stream, index)

@@ -132,8 +132,8 @@ def test_backward(kind, rows, n, pad, way):
     assert (np.abs(_np(dx) - dx64) <= np.abs(dx64) * HALF[kind] + size * (_chain(n) + 10) * 2.0 ** -24 + TINY[kind]).all()
     assert int((flat == 3).sum()) >= flat.numel() - dx.numel()
     if way == "all":
-        # a part has at most ceil(rows / 512) + 4 rows of a lane, 512 parts are added 16 in a row and then 32; or a thread has every 64th row of 1,024, 16 threads are added and then up to 16
-        chain = max(-(-rows // 512) + 4 + 16 + 32, min(16, -(-rows // 64)) + 16 + 16) + 4
+        # a part has at most ceil(rows / 512) + 4 rows of a lane, 512 parts are added eight by eight by eight; or a thread has every 64th row of 1,024, 16 threads are added and then up to 16
+        chain = max(-(-rows // 512) + 4 + 8 + 8 + 8, min(16, -(-rows // 64)) + 16 + 16) + 4
         size = (np.abs(dy64 * s64) * r64[:, None]).sum(0)
         assert (np.abs(_np(dw) - dw64) <= np.abs(dw64) * HALF[kind] + size * chain * 2.0 ** -24 + TINY[kind]).all()
         for into in (dy, ds):                                            # in place, always the same bits
