@@ -8,7 +8,7 @@
 // is common to a row) in 64 bits: products of 16-bit elements are exact, so values next to the middle of two codes go where the definition says.
 //
 // What bounds it (us).  8,192 rows of 8,192, bf16, residual, 8 bits: 93 (470 MB, 5.0 TB/s), the values of the codes 65 (335 MB): memory.  Backward of 8,192 rows of 4,096 with dsum 52
-// (268 MB, 5.2 TB/s) and 4.4 for the 512 parts of dw.  777 rows of 1,365, f16: 4.6, 1,000 rows of 512 backward, fp32: 7.5, one row: 3.5: a launch (2.8) and a trip to memory.
+// (268 MB, 5.3 TB/s) and 4.4 for the 512 parts of dw.  777 rows of 1,365, f16: 4.6, 1,000 rows of 512 backward, fp32: 7.5, one row: 3.5: a launch (2.8) and a trip to memory.
 #include "operator_calls.h"
 #include "rows_device.h"
 
@@ -62,12 +62,18 @@ constexpr double kLeastRow = 0x1p-118;         // max / 127 of a row that is hel
 struct __attribute__((packed)) Codes8 { unsigned long long v; };
 struct __attribute__((packed)) Codes4 { unsigned v; };
 
+// (the code is the lowest byte)
 __device__ __forceinline__ unsigned code_of(double v, double inv)
 {
 #pragma clang fp contract(off)
     // rounded to 2^-53 first, as v inv of the definition; then, half to even, to the integer that the low bits hold
     const double scaled = v * inv;
-    return (unsigned)__builtin_bit_cast(unsigned long long, scaled + 0x1.8p52) & 255u;
+    return (unsigned)__builtin_bit_cast(unsigned long long, scaled + 0x1.8p52);
+}
+// the lowest bytes of four words
+__device__ __forceinline__ unsigned lowest_bytes(const unsigned* w)
+{
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u), __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u);
 }
 
 // Sums (and largest) of a row over its W wavefronts, in the order of the wavefronts.
@@ -98,7 +104,11 @@ template <int W, typename V> __device__ __forceinline__ V row_max(V v, V* shared
 
 template <typename T> __device__ __forceinline__ typename Piece<T>::vec piece(const T* p, int j, int n)
 {
-    return j + Piece<T>::N <= n ? Piece<T>::load(p + j) : Piece<T>::load_part(p, j, 0, n, (T)0.f);
+    if (j + Piece<T>::N <= n) return Piece<T>::load(p + j);
+    if (sizeof(T) == 4 || n < Piece<T>::N) return Piece<T>::load_part(p, j, 0, n, (T)0.f);
+    // a row's last piece: its last 16 bytes, moved down, zeros behind them (element by element it takes as long as all others together)
+    const unsigned __int128 last = __builtin_bit_cast(unsigned __int128, Piece<T>::load(p + n - Piece<T>::N));
+    return __builtin_bit_cast(typename Piece<T>::vec, last >> 8 * (int)sizeof(T) * (j + Piece<T>::N - n));
 }
 template <typename T> __device__ __forceinline__ void put(T* p, int j, int n, typename Piece<T>::vec v)
 {
@@ -143,9 +153,11 @@ template <typename T> __device__ __forceinline__ void write_y(const NormArgs& a,
 template <typename T> __device__ __forceinline__ void write_codes(const NormArgs& a, int64_t row, int j, typename Piece<T>::vec s, typename Piece<T>::vec w, double inv)
 {
     typedef typename Largest<T>::value value;
-    unsigned long long c = 0;
+    unsigned code[Piece<T>::N];
 #pragma unroll
-    for (int k = 0; k < Piece<T>::N; ++k) c |= (unsigned long long)code_of((double)((value)s[k] * (value)w[k]), inv) << 8 * k;
+    for (int k = 0; k < Piece<T>::N; ++k) code[k] = code_of((double)((value)s[k] * (value)w[k]), inv);
+    unsigned long long c = lowest_bytes(code);
+    if constexpr (Piece<T>::N == 8) c |= (unsigned long long)lowest_bytes(code + 4) << 32;
     put_codes<Piece<T>::N>(row_of<char>(a.codes, row), j, a.n, c);
 }
 
@@ -374,21 +386,37 @@ template <typename T, int W, int NV, Weights DW> __global__ void __launch_bounds
         w[i] = j < a.n && a.weight ? piece(reinterpret_cast<const T*>(a.weight), j, a.n) : ones<T>();
         dw[i] = 0.f;
     }
-    int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * kRows; first < a.rows; first += (int64_t)a.row_groups * kRows, turn ^= 1) {
-        const int64_t row = first + mine;
-        if (row >= a.rows) break;                               // (only without barriers)
-        typename Piece<T>::vec s[NV], dy[NV], ds[NV];
+    // rows on their way while the one before is worked on: two where registers allow it (8,192 x 2,048, bf16, with dw: 26 us, with one 29.5)
+    constexpr bool kAhead = NV <= 2;
+    typename Piece<T>::vec s[NV], dy[NV], ds[NV], s2[NV], dy2[NV], ds2[NV];
+    float r = 0.f, r2 = 0.f;
+    auto load = [&](int64_t row, typename Piece<T>::vec(&to_s)[NV], typename Piece<T>::vec(&to_dy)[NV], typename Piece<T>::vec(&to_ds)[NV], float& to_r) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int j = Piece<T>::N * (t + i * kLanes);
             if (j < a.n) {
-                s[i] = piece(row_of<T>(a.x, row), j, a.n);
-                dy[i] = piece(row_of<T>(a.dy, row), j, a.n);
-                if (a.dsum.data) ds[i] = piece(row_of<T>(a.dsum, row), j, a.n);
+                to_s[i] = piece(row_of<T>(a.x, row), j, a.n);
+                to_dy[i] = piece(row_of<T>(a.dy, row), j, a.n);
+                if (a.dsum.data) to_ds[i] = piece(row_of<T>(a.dsum, row), j, a.n);
             }
         }
-        const float r = a.rstd[row];
+        to_r = a.rstd[row];
+    };
+    int turn = 0;
+    int64_t row = (int64_t)blockIdx.x * kRows + mine;
+    const int64_t step = (int64_t)a.row_groups * kRows;
+    if (kAhead && row < a.rows) load(row, s2, dy2, ds2, r2);
+    for (; row < a.rows; row += step, turn ^= 1) {              // (one wavefront after the other where there are no barriers)
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                s[i] = s2[i];
+                dy[i] = dy2[i];
+                ds[i] = ds2[i];
+            }
+            r = r2;
+            if (row + step < a.rows) load(row + step, s2, dy2, ds2, r2);
+        } else load(row, s, dy, ds, r);
         float along = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -458,17 +486,29 @@ template <typename T> __global__ void __launch_bounds__(kLong) norm_backward_lon
     }
 }
 
-// Their part of dw: a thread has eight columns and every gridDim.y-th row.
+// Their part of dw: a thread has a piece of columns and every gridDim.y-th row, four at a time.
 template <typename T> __global__ void __launch_bounds__(64) norm_columns_kernel(NormArgs a)
 {
+    typedef typename Piece<T>::vec vec;
+    constexpr int U = 4;
     const int j = Piece<T>::N * (blockIdx.x * 64 + threadIdx.x);
     if (j >= a.n) return;
     typename Piece<T>::wide dw = 0.f;
-    for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        const typename Piece<T>::wide v = widen<T>(piece(row_of<T>(a.x, row), j, a.n)), g = widen<T>(piece(row_of<T>(a.dy, row), j, a.n));
-        const float r = a.rstd[row];
+    for (int64_t row = blockIdx.y; row < a.rows; row += U * (int64_t)gridDim.y) {
+        vec s[U], g[U];
+        float r[U];
 #pragma unroll
-        for (int k = 0; k < Piece<T>::N; ++k) dw[k] = __builtin_fmaf(g[k], v[k] * r, dw[k]);
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = row + u * (int64_t)gridDim.y;
+            if (at < a.rows) {
+                s[u] = piece(row_of<T>(a.x, at), j, a.n);
+                g[u] = piece(row_of<T>(a.dy, at), j, a.n);
+                r[u] = a.rstd[at];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (row + u * (int64_t)gridDim.y < a.rows) dw += widen<T>(g[u]) * (widen<T>(s[u]) * r[u]);
     }
     put_sums<T>(a.partial + (int64_t)blockIdx.y * a.n, j, a.n, dw);
 }
@@ -566,8 +606,12 @@ int64_t pieces_of(const bmgd_norm_config& c) { return (c.n * (int64_t)size_of(c.
 // Workgroups of a backward call, each of which leaves a part of dweight.
 int64_t parts_of(const bmgd_norm_config& c, int64_t rows)
 {
-    const int64_t at_once = pieces_of(c) <= 128 ? 4 : 1;        // rows of a workgroup
-    return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, kMaxParts));
+    // So many that units are busy, so few that the parts are little beside the rows.  Rows that begin inside lines want more on their way: 8,192 x 1,365, bf16: 33 us with 1,024 parts, 45 with 512;
+    // 8,192 x 2,048: 27 and 26.
+    const bool crossing = c.n * (int64_t)size_of(c.dtype) % 16 != 0;
+    const int64_t pieces = pieces_of(c), at_once = pieces <= 128 ? 4 : 1;                                          // rows of a workgroup
+    if (pieces > kGradientPieces) return std::max<int64_t>(1, std::min<int64_t>(rows / 32, kMaxParts));
+    return std::max<int64_t>(1, std::min<int64_t>((rows + at_once - 1) / at_once, pieces > 1024 ? kMaxParts / 2 : crossing && pieces > 128 && pieces <= 256 ? 2 * kMaxParts : kMaxParts));
 }
 
 // Whether dw is found by workgroups of its own: no second launch, but every row is read twice, 64 bytes at a time.  Measured, us, with them and with parts that are joined (rows x n):
@@ -726,7 +770,12 @@ BMGD_API int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const
                     a.row_groups = (int)parts;
                     hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kNoWeights>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
                 } else if (t->dweight) hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kParts>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
-                else hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kNoWeights>), dim3((unsigned)parts), dim3(block_of(W)), 0, s, a);
+                else {
+                    // (nothing is left behind, so as many workgroups as units take: 8,192 x 1,365, bf16, with dsum: 29 us, with 512 of them 52)
+                    constexpr int kRows = block_of(W) / (64 * W);
+                    a.row_groups = (int)std::min<int64_t>((rows + kRows - 1) / kRows, NV * W <= 8 ? 4 * kMaxParts : kMaxParts);
+                    hipLaunchKernelGGL((norm_backward_kernel<T, W, NV, kNoWeights>), dim3((unsigned)a.row_groups), dim3(block_of(W)), 0, s, a);
+                }
             }
         });
     });
