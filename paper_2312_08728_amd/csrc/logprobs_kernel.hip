@@ -32,8 +32,8 @@ constexpr float kLowest = -3.40282347e38f;
 constexpr float kUsual = 1e37f;                  // x log2 e - r is finite, or -infinity for one far below, where m is smaller than this
 constexpr float kFar = -1000.f;                  // 2^-1000 is 0, times this still 0
 constexpr int kMaxTop = 64, kMaxParts = 64;
-constexpr int kList = 640;                       // classes listed between two counts at most: a row of fewer than 8 top fits whole,
-constexpr int pieces_kept(int w) { return w == 1 ? 80 : 256; }         // and pieces: 64, and two that are not whole
+constexpr int kList = 640;                       // classes listed between two counts at most: 64 pieces of eight and some more,
+constexpr int pieces_kept(int w) { return w == 1 ? 168 : 256; }        // and pieces: with a wavefront to a row one of 640 fp32 logits fits whole
 
 struct LogArgs {
     const char* logits;

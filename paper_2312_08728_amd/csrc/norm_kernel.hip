@@ -679,6 +679,16 @@ BMGD_API int bmgd_norm_forward(const bmgd_norm_config* cfg, int64_t rows, const 
     q.apart("sum", t->sum.data, t->codes.data);
     q.apart("y", t->y.data, t->codes.data);
     for (const void* in : {t->x.data, t->residual.data}) q.apart("codes", t->codes.data, in);
+    q.apart("rstd", t->rstd, t->codes.data ? t->scales : nullptr);
+    for (const void* out : {t->sum.data, t->y.data, t->codes.data}) {
+        q.apart("a result", out, t->weight);
+        q.apart("a result", out, t->rstd);
+        if (t->codes.data) q.apart("a result", out, t->scales);
+    }
+    for (const void* in : {(const void*)t->x.data, (const void*)t->residual.data, t->weight}) {
+        q.apart("rstd", t->rstd, in);
+        if (t->codes.data) q.apart("scales", t->scales, in);
+    }
     // (in place means element by element)
     for (const bmgd_matrix* in : {&t->x, &t->residual})
         for (const bmgd_matrix* out : {&t->sum, &t->y})
@@ -725,7 +735,7 @@ BMGD_API int bmgd_norm_backward(const bmgd_norm_config* cfg, int64_t rows, const
     for (const void* in : {(const void*)t->x.data, t->weight, (const void*)t->rstd}) q.apart("dx", t->dx.data, in);
     for (const bmgd_matrix* in : {&t->dy, &t->dsum})
         if (in->data && in->data == t->dx.data && rows > 1 && in->stride != t->dx.stride) q.refuse("dx", "begins where an operand does, with another stride");
-    for (const void* in : {(const void*)t->x.data, (const void*)t->dy.data, (const void*)t->dsum.data, (const void*)t->dx.data, t->weight}) q.apart("dweight", t->dweight, in);
+    for (const void* in : {(const void*)t->x.data, (const void*)t->dy.data, (const void*)t->dsum.data, (const void*)t->dx.data, t->weight, (const void*)t->rstd}) q.apart("dweight", t->dweight, in);
     const size_t need = t->dweight && some ? bmgd_norm_workspace_bytes(cfg, rows) : 0;
     if (need) {
         if (!t->workspace || (reinterpret_cast<uintptr_t>(t->workspace) & 255)) q.refuse("workspace", "256-byte aligned device memory is wanted for dweight");
@@ -800,6 +810,7 @@ BMGD_API int bmgd_product_values(int64_t rows, int64_t n, const bmgd_matrix* cod
     q.matrix("out", *out, rows, n, rows > 0, size_of(dtype));
     q.address("scales", scales, rows > 0, 4);
     q.apart("out", out->data, codes->data);
+    q.apart("out", out->data, scales);
     if (q.code != BMGD_OK || rows == 0) return q.code;
     ValueArgs a{side(*codes), side(*out), scales, rows, (int)n, (int)((n * (int64_t)size_of(dtype) + 15) / 16)};
     const unsigned groups = (unsigned)std::min<int64_t>((rows * a.per_row + 255) / 256, int64_t(1) << 20);

@@ -75,11 +75,15 @@ def test_norm_results_that_meet():
     _refused(forward(sum=_at(FAR), y=_at(FAR)), "sum")
     _refused(forward(codes=_at(FAR), x=_at(FAR)), "codes")
     _refused(forward(sum=_at(FAR, 65), x=_at(FAR, 64)), "stride")
+    for kw in (dict(scales=50 * FAR, rstd=50 * FAR), dict(y=_at(50 * FAR), weight=50 * FAR), dict(sum=_at(50 * FAR), rstd=50 * FAR), dict(codes=_at(50 * FAR), scales=50 * FAR),
+               dict(x=_at(50 * FAR), rstd=50 * FAR), dict(residual=_at(50 * FAR), scales=50 * FAR), dict(weight=50 * FAR, rstd=50 * FAR)):
+        _refused(forward(**kw), "written")
     rows = 5000
     backward = lambda **kw: B.bmgd_norm_backward(cfg, rows, new(**kw))  # noqa: E731
     _refused(backward(dx=_at(FAR), x=_at(FAR)), "dx")
     _refused(backward(dx=_at(50 * FAR, 65), dy=_at(50 * FAR, 64)), "dx", "stride")
     _refused(backward(dweight=FAR, weight=FAR), "dweight")
+    _refused(backward(dweight=50 * FAR, rstd=50 * FAR), "dweight")
     _refused(backward(rstd=None), "rstd")
     _refused(backward(workspace=None), "workspace")
     _refused(backward(workspace=FAR + 128), "workspace")
@@ -112,7 +116,7 @@ def test_product():
                  (_at(FAR, 63), _at(2 * FAR), 3 * FAR), (_at(FAR), _at(2 * FAR, 63), 3 * FAR)):
         _refused(B.bmgd_product_quantize(ok(), *args), "bmgd_product_quantize")
     good = (4, 64, _at(FAR), 2 * FAR, _at(3 * FAR), B.BMGD_F32)
-    for i, bad in ((0, -1), (0, 1 << 30), (1, 0), (1, (1 << 20) + 1), (2, NONE), (2, _at(FAR, 63)), (3, 0), (3, FAR + 1), (4, NONE), (4, _at(FAR)), (4, _at(3 * FAR + 2)), (5, 3)):
+    for i, bad in ((0, -1), (0, 1 << 30), (1, 0), (1, (1 << 20) + 1), (2, NONE), (2, _at(FAR, 63)), (3, 0), (3, FAR + 1), (4, NONE), (4, _at(FAR)), (4, _at(2 * FAR)), (4, _at(3 * FAR + 2)), (5, 3)):
         _refused(B.bmgd_product_values(*good[:i], bad, *good[i + 1:]), "bmgd_product_values")
     assert B.bmgd_product_values(0, 64, NONE, 0, NONE, B.BMGD_F32) == B.BMGD_OK
 
