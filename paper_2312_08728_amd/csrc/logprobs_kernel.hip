@@ -33,7 +33,7 @@ constexpr float kUsual = 1e37f;                  // x log2 e - r is finite, or -
 constexpr float kFar = -1000.f;                  // 2^-1000 is 0, times this still 0
 constexpr int kMaxTop = 64, kMaxParts = 64;
 constexpr int kList = 640;                       // classes listed between two counts at most: 64 pieces of eight and some more,
-constexpr int pieces_kept(int w) { return w == 1 ? 168 : 256; }        // and pieces: with a wavefront to a row one of 640 fp32 logits fits whole
+constexpr int pieces_kept(int w) { return w == 1 ? 168 : 256; }        // and pieces: with a wavefront to a row one of 660 fp32 or 1,320 16-bit logits fits whole
 
 struct LogArgs {
     const char* logits;
@@ -277,6 +277,34 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             places[mine][place] = at;
         }
     };
+    // What is listed without the classes below a closer bound: two numbers of `nth` lanes are not below the nth largest of the lanes' second numbers.  (Of 64 lanes' largest
+    // numbers the 64th leaves most of a short row.  8,192 x 600, fp32, the 64 most probable classes: 150 us without it, 42 with it.)
+    auto without_lower = [&](int n) {
+        Key first = 0, second = 0;
+        for (int i = t; i < n; i += 64) {
+            const Key q = list[mine][i], lower = q < first ? q : first;
+            second = lower > second ? lower : second;
+            first = q > first ? q : first;
+        }
+        groups_of[mine][t] = second;
+        together<1>();
+        int place = 0;
+#pragma unroll 8
+        for (int i = 0; i < 64; ++i) place += groups_of[mine][i] > second;
+        const unsigned long long found = __ballot(place == (a.top + 1) / 2 - 1);
+        const Key closer = found ? of_lane(second, __builtin_ctzll(found)) : 0;
+        // (to places that have been read)
+        int left = 0;
+        for (int i = 0; i < n; i += 64) {
+            const Key q = i + t < n ? list[mine][i + t] : 0;
+            const bool stays = i + t < n && q >= closer;
+            const unsigned long long all = __ballot(stays);
+            if (stays) list[mine][left + __popcll(all & ((1ull << t) - 1))] = q;
+            left += __popcll(all);
+        }
+        together<1>();
+        return left;
+    };
     auto count_kept = [&]() {
         together<W>();
         const int held = kept[mine][in_use];
@@ -290,8 +318,10 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             }
         }
         together<W>();
-        const int fresh = min(listed[mine][in_use], kList);
+        int fresh = min(listed[mine][in_use], kList);
         over |= listed[mine][in_use] > kList;
+        if constexpr (W == 1)
+            if (fresh > 2 * kMaxTop) fresh = without_lower(fresh);
         const Key* const old = sorted[mine][in_use];
         for (int i = t / 4; i < have + fresh; i += kLanes / 4) {
             const Key q = i < have ? old[i] : list[mine][i - have];
@@ -738,11 +768,14 @@ BMGD_API int bmgd_logprobs_forward(const bmgd_logprobs_config* cfg, int64_t rows
         // A wavefront for each row, if the rows are many or short.  Measured, us, with it and with four for a row (16 bits; no classes, five):
         //      8,192 x 1,000: 7 and 21, 14 and 38;  8,192 x 4,000: 14 and 23, 21 and 41;  4,097 x 10,001: 19 and 28, 37 and 34;  8,192 x 32,000: 99 and 93;
         //      1,000 x 10,001, five: 22 and 13;  100 x 4,000, five: 7.6 and 6.2.
-        // (Of 64 groups the 64th largest leaves 300 classes to list, now and then more than the list holds: short rows only.)
+        // Of 64 groups the 64th largest leaves 300 classes to list, now and then more than the list holds.  So more than 16 only where all of a row's pieces are kept, and
+        // with few rows, each of which then takes as long as the call, more than 32:
+        //      8,192 x 700, the 64 most probable: 45 and 172, 20: 19 and 49;  8,192 x 1,300, 64: 51 and 74;  100 x 1,000, 64: 18 and 31, 32: 8.2 and 6.6.
         const int64_t pieces = (int64_t)a.span * (int64_t)sizeof(T) / 16;
-        const bool wave = pieces <= 128 || (rows >= 4 * compute_units() && pieces <= (a.top ? 512 : 2048));
+        const bool many = rows >= 4 * compute_units(), wave = pieces <= 128 || (many && pieces <= (a.top ? 512 : 2048));
+        const bool listed = a.top <= 16 || (pieces + 2 <= pieces_kept(1) && (many || a.top > 32));
         auto shaped = [&](auto top, auto ent) {
-            if (wave && (a.top <= 16 || a.classes <= kList)) launch(std::integral_constant<int, 1>(), top, ent);
+            if (wave && listed) launch(std::integral_constant<int, 1>(), top, ent);
             else launch(std::integral_constant<int, 4>(), top, ent);
         };
         auto with_top = [&](auto ent) {

@@ -137,6 +137,15 @@ def test_most_probable_classes(kind, top, rows, classes):
     _check(kind, x, _labels(rows, classes), top)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("top", [17, 33, 64])
+@pytest.mark.parametrize("classes", [130, 655, 662, 1318, 1333])
+def test_most_probable_classes_of_many_short_rows(kind, top, classes):
+    """So many rows that each is a wavefront's: lists that are shortened first, pieces that just fit."""
+    x, _ = _logits(1100, classes, _types()[kind][0], pad=classes % 3, shift=classes % 4, seed=classes + top)
+    _check(kind, x, _labels(1100, classes), top)
+
+
 def _rows_of_trouble(classes, dtype):
     """Rows by name, each with its own difficulty."""
     import torch
@@ -172,7 +181,7 @@ def test_rows_of_trouble(kind, classes, top):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("classes,top", [(600, 64), (5000, 17), (20_000, 20), (20_000, 64), (90_000, 33)])
+@pytest.mark.parametrize("classes,top", [(600, 64), (600, 33), (1300, 20), (1300, 64), (5000, 17), (20_000, 20), (20_000, 64), (90_000, 33)])
 def test_equal_logits(kind, classes, top):
     """As many rows as one launch has workgroups for: equal in all classes, in a few values, in all but some, masked but for some."""
     import torch
