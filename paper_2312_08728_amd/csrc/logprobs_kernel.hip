@@ -277,6 +277,11 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             places[mine][place] = at;
         }
     };
+    // The piece that begins before the segment is listed in the first turn, the one that ends behind it after the last: it has the highest classes of all, so a threshold of
+    // its own would hide equal logits of the turns between.
+    auto keep_edge = [&]() {
+        if (key_of(largest(widen<T>(edge_piece)), max(edge_at, begin)) >= least) keep(edge_piece, edge_at);
+    };
     // What is listed without the classes below a closer bound: two numbers of `nth` lanes are not below the nth largest of the lanes' second numbers.  (Of 64 lanes' largest
     // numbers the 64th leaves most of a short row.  8,192 x 600, fp32, the 64 most probable classes: 150 us without it, 42 with it.)
     auto without_lower = [&](int n) {
@@ -385,17 +390,18 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
                     }
                 // (with the last class of the piece: not above what it stands for)
                 Key k = at + N <= end ? key_of(best, best_at + N - 1) : 0;
-                if (edge_at != kNowhere) k = larger(k, key_of(largest(widen<T>(edge_piece)), min(edge_at + N, end) - 1));
+                const bool early = t == 0 && edge_at != kNowhere;
+                if (early) k = larger(k, key_of(largest(widen<T>(edge_piece)), min(edge_at + N, end) - 1));
                 if (t == 0) kept[mine][0] = kept[mine][1] = listed[mine][0] = listed[mine][1] = 0;
                 least = bound(k);
                 // (where there is no top-th, all are listed)
-                if (edge_at != kNowhere && key_of(largest(widen<T>(edge_piece)), max(edge_at, begin)) >= least) keep(edge_piece, edge_at);
+                if (early) keep_edge();
             }
             const float value = least ? value_of(least) : -__builtin_inff();
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int i = at + N * kLanes * u;
-                // (later turns have higher classes than the threshold's: equal logits do not reach it)
+                // (later turns have higher classes than the threshold's, which is never of the piece behind the whole ones: equal logits do not reach it)
                 const bool reaches = decltype(first)::value ? key_of(most[u], i) >= least : most[u] > value;
                 if (reaches && i + N <= end) keep(now[u], i);
             }
@@ -428,6 +434,8 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         const float most = largest(v);
         take<1, ENT>(st, &v, &most);
         seen = fmaxf(seen, most);
+        if constexpr (TOP)
+            if (t == 1) keep_edge();
     }
 
     auto merged = [&](Stats own) {
