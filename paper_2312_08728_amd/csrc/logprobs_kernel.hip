@@ -84,16 +84,18 @@ __device__ __forceinline__ Stats wave_merge(Stats a)
     return a;
 }
 
-// Larger numbers for larger logits, one for both zeros, NaN above all.
+// Larger numbers for larger logits, one for both zeros, one for all NaN above all others.  (Not the largest of 32 bits: with class 0 that would be the largest of all 64-bit
+// numbers, which stands for "nothing yet" where classes are found one after the other.)
+constexpr unsigned kOrderedNan = ~1u;
 __device__ __forceinline__ unsigned ordered(float x)
 {
     const int b = __builtin_bit_cast(int, x + 0.f);
-    return x != x ? ~0u : (unsigned)b ^ ((unsigned)(b >> 31) | 0x80000000u);
+    return x != x ? kOrderedNan : (unsigned)b ^ ((unsigned)(b >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(Key k)
 {
     const unsigned u = (unsigned)(k >> 32);
-    return __builtin_bit_cast(float, u & 0x80000000u ? u ^ 0x80000000u : ~u);           // (~0: NaN)
+    return __builtin_bit_cast(float, u & 0x80000000u ? u ^ 0x80000000u : ~u);           // (kOrderedNan: NaN)
 }
 __device__ __forceinline__ Key key_of(float x, int at) { return (Key)ordered(x) << 32 | (0xffffffffu - (unsigned)at); }
 __device__ __forceinline__ int class_of(Key k) { return (int)(0xffffffffu - (unsigned)k); }
@@ -499,7 +501,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
         if (st.s == st.s && !over) {
             if (t < a.top) write_top(a, row, part, t, t < have ? sorted[mine][in_use][t] : 0, r);          // (a part may have fewer than `top` classes)
         } else {
-            Key before = ~(Key)0;
+            Key before = ~(Key)0;                               // above every class's number
             for (int place = 0; place < a.top; ++place) {
                 Key k = 0;
                 for (int i = head + N * t; i < end; i += N * kLanes) {

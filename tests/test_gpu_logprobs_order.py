@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from oracle import operators as O
-from test_gpu_logprobs import _types
+from test_gpu_logprobs import _check, _labels, _types
 
 pytestmark = pytest.mark.gpu
 
@@ -69,3 +69,18 @@ def test_logits_of_few_values(kind, rows, classes, top):
     op.forward(x, top_classes=best, top_logprobs=logprobs)
     want = torch.sort(x.float(), dim=1, descending=True, stable=True)[1][:, :top]
     assert torch.equal(best.long(), want)
+
+@pytest.mark.parametrize("kind", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("classes,top", [(1, 1), (3, 3), (7, 7), (64, 64), (64, 5), (700, 64), (2500, 9), (9001, 3), (40_000, 64), (50_257, 5)])
+def test_nan_at_the_first_class(kind, classes, top):
+    """NaN comes first, in the order of its classes, class 0 too: rows that are all NaN, that have one at class 0, at class 0 and others, at all classes but 0."""
+    import torch
+    nan = float("nan")
+    x = torch.randn(5, classes, generator=torch.Generator().manual_seed(classes))
+    x[0] = nan
+    x[1, 0] = nan
+    x[2, 0], x[2, classes // 2], x[2, classes - 1] = nan, nan, nan
+    x[3, 1:] = nan
+    x[4, 0], x[4, classes - 1] = nan, float("inf")
+    x = x.to(_types()[kind][0]).cuda()
+    _check(kind, x, _labels(5, classes), top)
