@@ -2,8 +2,8 @@
 //
 // A thread holds its largest logit m so far, s = sum 2^d and w = sum 2^d d, d = x log2 e - r with r = m log2 e rounded; where r grows by g, s becomes s 2^-g and
 // w (w - g s) 2^-g.  Threads, wavefronts and parts of a row are put together the same way.  Then ln p_j = ln 2 (d_j - log2 s) and the entropy is ln 2 (log2 s - w / s).
-// d is one instruction with one rounding; r's own rounding is the same for all and leaves with log2 s.  Rows whose largest logit is not below 1e37 in size (all of the
-// type's lowest value, no class at all, infinity) are read once more with d = (x - m) log2 e, which does not leave the range.  -infinity adds nothing.
+// d is one instruction with one rounding; r's own rounding is the same for all and leaves with log2 s.  Rows whose largest logit is not below 2^24 in size (masked in all
+// classes with some large number or the type's lowest, no class at all, infinity) are read once more with d = (x - m) log2 e.  -infinity adds nothing.
 //
 // The most probable classes.  A logit and its class are one 64-bit number, larger where the logit is larger and, of equal ones, the class lower; so no two are
 // equal.  Of what the threads read first (8,192 logits of 16 bits for four wavefronts), 64 groups of threads have their largest numbers; the top-th largest of these is not above the top-th
@@ -29,7 +29,7 @@ typedef unsigned long long Key;
 
 constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147182f;
 constexpr float kLowest = -3.40282347e38f;
-constexpr float kUsual = 1e37f;                  // x log2 e - r is finite, or -infinity for one far below, where m is smaller than this
+constexpr float kUsual = 16777216.f;             // where m is smaller than 2^24 r is off by 1 at most, so 2^d of the largest logit is about 1 (at 1e10 it would be 2^440)
 constexpr float kFar = -1000.f;                  // 2^-1000 is 0, times this still 0
 constexpr int kMaxTop = 64, kMaxParts = 64;
 constexpr int kList = 640;                       // classes listed between two counts at most: 64 pieces of eight and some more,
@@ -70,15 +70,20 @@ __device__ __forceinline__ float reference(float m)
     asm("" : "+v"(r));
     return r;
 }
-__device__ __forceinline__ void refer_to(Stats& a, float to)
+// What a Stats' sums refer to: r of m, m log2 e itself, or, in parts of one row, whichever is due to the size of the part's own m.
+enum Refers { kRounded, kItself, kEither };
+template <Refers OF> __device__ __forceinline__ void refer_to(Stats& a, float to)
 {
-    if (fabsf(to) < kUsual) scale_down(a, to, reference(a.m) - reference(to));
-    else scale_down(a, to, (a.m - to) * kLog2E);
+    const bool rounded = OF == kRounded || (OF == kEither && fabsf(a.m) < kUsual), to_rounded = OF == kRounded || (OF == kEither && fabsf(to) < kUsual);
+    float d;
+    if (rounded) d = to_rounded ? reference(a.m) - reference(to) : __builtin_fmaf(-to, kLog2E, reference(a.m));
+    else d = to_rounded ? __builtin_fmaf(a.m, kLog2E, -reference(to)) : (a.m - to) * kLog2E;
+    scale_down(a, to, d);
 }
 
-__device__ __forceinline__ Stats wave_merge(Stats a)
+template <Refers OF> __device__ __forceinline__ Stats wave_merge(Stats a)
 {
-    refer_to(a, wave_max(a.m));
+    refer_to<OF>(a, wave_max(a.m));
     a.s = wave_sum(a.s);
     a.w = wave_sum(a.w);
     return a;
@@ -440,8 +445,9 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             if (t == 1) keep_edge();
     }
 
-    auto merged = [&](Stats own) {
-        own = wave_merge(own);
+    auto merged = [&](Stats own, auto of) {
+        constexpr Refers OF = decltype(of)::value;
+        own = wave_merge<OF>(own);
         if constexpr (W > 1) {
             if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = own;
             __syncthreads();
@@ -452,7 +458,7 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
 #pragma unroll
             for (int i = 0; i < W; ++i) {
                 Stats o = parts[i];
-                refer_to(o, m);
+                refer_to<OF>(o, m);
                 all.s += o.s;
                 all.w += o.w;
             }
@@ -462,15 +468,17 @@ template <typename T, int W, bool TOP, bool ENT> __global__ void __launch_bounds
             return own;
         }
     };
-    st = merged(st);
+    constexpr std::integral_constant<Refers, kRounded> rounded;
+    constexpr std::integral_constant<Refers, kItself> itself;
+    st = merged(st, rounded);
     if (!(st.m > -kUsual && st.m < kUsual)) {
         if constexpr (W > 1) __syncthreads();                   // (`parts` has been read)
-        const bool none = st.s == 0.f && merged(Stats{seen, 0.f, 0.f}).m == -__builtin_inff();
+        const bool none = st.s == 0.f && merged(Stats{seen, 0.f, 0.f}, itself).m == -__builtin_inff();
         if constexpr (W > 1) __syncthreads();
         st = Stats{kLowest, 0.f, 0.f};
         if (!none) {
             for (int i = head + N * t; i < end; i += N * kLanes) take_unusual(st, widen<T>(logits_at(x, i, begin, end)));
-            st = merged(st);
+            st = merged(st, itself);
         }
     }
     const Row r = finish(st);
@@ -550,7 +558,7 @@ template <typename T> __global__ void __launch_bounds__(256) logprobs_join_kerne
     }
     const T* const x = reinterpret_cast<const T*>(a.logits) + row * a.stride;
     const float at_label = label >= 0 && label < a.classes ? (float)x[label] : 0.f;
-    st = wave_merge(st);
+    st = wave_merge<kEither>(st);
     const Row r = finish(st);
     if (threadIdx.x == 0) {
         write_row(a, row, label, at_label, r);
