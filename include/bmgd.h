@@ -646,8 +646,9 @@ typedef struct bmgd_logprobs_tensors {
     float*         entropy;     /* rows */
     int32_t*       top_classes; /* rows x top, one row behind the other (where top > 0) */
     float*         top_logprobs;
-    float*         kept;        /* rows x 3: the row's largest logit, the base-2 logarithm of the sum of e^(x - largest), and its entropy; forward writes
-                                   it, backward reads it */
+    float*         kept;        /* rows x 3, which forward writes and backward reads: the row's largest logit, the base-2 logarithm of the sum of 2^(x log2(e) - r), and its
+                                   entropy.  r: largest * 1.44269504f rounded to fp32, where largest is not below 2^24 in size as it is: r is not the exact
+                                   product, so this is not the sum of e^(x - largest) */
     const float*   dlogprob;    /* backward, each optional: rows */
     const float*   dentropy;
     void*          workspace;   /* forward, where it needs one: 256-byte aligned; calls that may run at the same time have one each */

@@ -189,7 +189,7 @@ template <typename V> __device__ __forceinline__ void take_unusual(Stats& st, V 
     }
 }
 
-// What is known of a row's distribution: log2 of the sum, entropy; `empty` where all logits are -infinity.
+// What is known of a row's distribution: log2 of the sum (relative to what its Stats refer to), entropy; `empty` where all logits are -infinity.
 struct Row {
     float m, ls, entropy;
     bool empty;

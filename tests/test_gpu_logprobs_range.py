@@ -92,3 +92,23 @@ def test_masks_of_a_finite_number(kind, fill, classes):
     x[2, :] = fill
     x[3, classes // 4: classes // 2] = fill
     _both(kind, _round(kind, x), 5)
+
+
+@pytest.mark.parametrize("classes", [5, 900, 9001, 50_257])
+def test_what_is_kept(classes):
+    """The largest logit, log2 of the sum of 2^(x log2 e - r) and the entropy, r = fl(largest log2 e) up to 2^24 and largest log2 e beyond: with r again it is the logarithm of
+    the sum of e^x.  (log2 e as the kernels have it, 1.44269504f: off by less than 2^-25 of it, of every difference x - largest; they are below 80 here.)"""
+    import torch
+    shifts = np.array([0.0, 30.0, -1000.0, 1.0e6, -9.0e6, 2.0 ** 24 + 64, -1.0e9, 1.0e12])
+    x = torch.randn(len(shifts), classes, generator=torch.Generator().manual_seed(2)) * 5
+    x = (x.double() + torch.from_numpy(shifts)[:, None]).float()
+    _, out = T._forward("f32", x.cuda(), torch.zeros(len(shifts), dtype=torch.int32, device="cuda"), 2)
+    kept, x64 = out["kept"].cpu().numpy(), x.double().numpy()
+    largest = x64.max(1)
+    assert (kept[:, 0] == largest).all() and (kept[:, 2] == out["entropy"].cpu().numpy()).all()
+    log2e = np.float32(1.44269504)
+    lost = np.where(np.abs(largest) < BORDER, largest * float(log2e) - (kept[:, 0] * log2e).astype(np.float64), 0.0)
+    want = np.log2(np.exp(x64 - largest[:, None]).sum(1)) + lost
+    # the sum's roundings are relative, so log2 e of them in the logarithm, which is rounded to fp32 within two steps of a number below 32
+    assert (np.abs(kept[:, 1] - want) <= 1.45 * T.E * T._sum_error(classes) + 80 * 1.45 * 2.0 ** -25 + 2 * 32 * 2.0 ** -23).all()
+    assert (np.abs(lost[3:5]) > 1e-3).any()
