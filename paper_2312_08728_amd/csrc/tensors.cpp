@@ -3,8 +3,9 @@
 //
 //   matrices(tensors, shapes, dtype, device[, written])    bytes: address and row stride (int64) of each, zeros for None; those from index `written` on are told
 //                                               that they are written, as torch's own in-place operations tell (autograd then refuses values that it has kept)
-//   operands(tensors, dtypes, shapes, kinds, device)      bytes: for each tensor address and row stride (kinds has 'm'), or the address of a contiguous one ('v'); zeros for None.
-//                                               Upper case: it is told that it is written
+//   operands(tensors, dtypes, shapes, kinds, device[, tell])      bytes: for each tensor address and row stride (kinds has 'm'), or the address of a contiguous one ('v'); zeros
+//                                               for None.  Upper case: it is told that it is written, unless `tell` is False
+//   told(tensors, kinds)                        tells those that kinds has in upper case, for calls that may still be refused when operands() returns
 //   vectors(tensors, numels, dtype, device)     bytes: the addresses of contiguous tensors; numels: bytes of int64
 //   pairs(pairs, numels, dtype, device)         (bytes, bytes): the same of the first and of the second tensors
 //   same(groups)                                True if the tensors of every group are what they were when their addresses were read.  A group: (list, item, numels, dtype,
@@ -12,7 +13,7 @@
 //
 //   touch(tensors)                              tells the tensors of a list that they have been written
 //
-// The first four return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
+// matrices, operands, vectors and pairs return the index of the first tensor (of pairs: the first pair) that is not what was asked for instead, an int: the caller says what is wrong with it.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
@@ -100,11 +101,18 @@ PyObject* matrices_(PyObject* const* args, Py_ssize_t n)
     return out;
 }
 
+// those of a tuple that are in upper case
+void tell(PyObject* tensors, const char* kinds)
+{
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(tensors); ++i)
+        if (!(kinds[i] & 32) && THPVariable_Check(PyTuple_GET_ITEM(tensors, i))) touch(THPVariable_Unpack(PyTuple_GET_ITEM(tensors, i)));
+}
+
 PyObject* operands_(PyObject* const* args, Py_ssize_t n)
 {
-    if (n != 5 || !PyTuple_Check(args[0]) || !PyTuple_Check(args[1]) || !PyTuple_Check(args[2]) || !PyBytes_Check(args[3]) ||
+    if ((n != 5 && n != 6) || !PyTuple_Check(args[0]) || !PyTuple_Check(args[1]) || !PyTuple_Check(args[2]) || !PyBytes_Check(args[3]) ||
         PyTuple_GET_SIZE(args[1]) != PyTuple_GET_SIZE(args[0]) || PyTuple_GET_SIZE(args[2]) != PyTuple_GET_SIZE(args[0]) || PyBytes_GET_SIZE(args[3]) != PyTuple_GET_SIZE(args[0])) {
-        PyErr_SetString(PyExc_TypeError, "operands(tensors, dtypes, shapes, kinds, device): three tuples and bytes of one length");
+        PyErr_SetString(PyExc_TypeError, "operands(tensors, dtypes, shapes, kinds, device[, tell]): three tuples and bytes of one length");
         return nullptr;
     }
     const Py_ssize_t count = PyTuple_GET_SIZE(args[0]);
@@ -139,9 +147,18 @@ PyObject* operands_(PyObject* const* args, Py_ssize_t n)
         std::memcpy(to, v, matrix ? 16 : 8);
         to += matrix ? 16 : 8;
     }
-    for (Py_ssize_t i = 0; i < count; ++i)
-        if (!(kinds[i] & 32) && PyTuple_GET_ITEM(args[0], i) != Py_None) touch(THPVariable_Unpack(PyTuple_GET_ITEM(args[0], i)));
+    if (n == 5 || args[5] != Py_False) tell(args[0], kinds);
     return out;
+}
+
+PyObject* told_(PyObject* const* args, Py_ssize_t n)
+{
+    if (n != 2 || !PyTuple_Check(args[0]) || !PyBytes_Check(args[1]) || PyBytes_GET_SIZE(args[1]) != PyTuple_GET_SIZE(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "told(tensors, kinds): a tuple and bytes of one length");
+        return nullptr;
+    }
+    tell(args[0], PyBytes_AS_STRING(args[1]));
+    Py_RETURN_NONE;
 }
 
 PyObject* vectors_(PyObject* const* args, Py_ssize_t n)
@@ -272,6 +289,7 @@ template <PyObject* F(PyObject* const*, Py_ssize_t)> PyObject* guarded(PyObject*
 PyMethodDef methods[] = {
     {"matrices", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<matrices_>)), METH_FASTCALL, "addresses and row strides of matrices"},
     {"operands", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<operands_>)), METH_FASTCALL, "addresses and row strides of a call's tensors"},
+    {"told", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<told_>)), METH_FASTCALL, "tells a call's tensors that they have been written"},
     {"vectors", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<vectors_>)), METH_FASTCALL, "addresses of contiguous tensors"},
     {"pairs", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<pairs_>)), METH_FASTCALL, "addresses of pairs of contiguous tensors"},
     {"same", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<same_>)), METH_FASTCALL, "whether tensors are where they were"},

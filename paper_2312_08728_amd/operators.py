@@ -54,14 +54,14 @@ def _rows_of(name, t):
 
 
 def _places(names, tensors, kinds, shapes, how, index):
-    found = _tensors.operands(tensors, kinds, shapes, how, index)
+    found = _tensors.operands(tensors, kinds, shapes, how, index, False)
     if type(found) is int:
         _refuse(names[found], tensors[found], kinds[found], shapes[found], how[found] in b"mM", index)
     return found
 
 
-def _run(fn, args, stream, index):
-    """The call on the device of its tensors."""
+def _run(fn, args, stream, index, tensors, how):
+    """The call on the device of its tensors.  Those that it writes are told so, unless it is refused."""
     stream = _stream(stream, index)
     if torch._C._cuda_getDevice() == index:
         rc = fn(*args, stream)
@@ -70,6 +70,7 @@ def _run(fn, args, stream, index):
             rc = fn(*args, stream)
     if rc != B.BMGD_OK:
         raise B.BmgdError(rc, B.bmgd_last_error(None))
+    _tensors.told(tensors, how)
 
 
 def _workspace(need, given, stream, index):
@@ -113,20 +114,19 @@ class RMSNorm:
         without a residual).  weight None: ones.  sum may be x or residual, y may be x (without sum there) or residual."""
         rows, index = _rows_of("x", x)
         at, of, n = (rows, self.n), (rows,), self._of_n
-        tensors = _places(self._NAMES, (x, residual, sum, y, codes, None, None, None, weight, None, scales, rstd), self._kinds, (at, at, at, at, at, at, at, at, n, n, of, of),
-                          b"mmMMMmmmvvVV", index) + _NONE16
-        _run(B.lib.bmgd_norm_forward, (self._cfg, rows, tensors), stream, index)
+        tensors, how = (x, residual, sum, y, codes, None, None, None, weight, None, scales, rstd), b"mmMMMmmmvvVV"
+        found = _places(self._NAMES, tensors, self._kinds, (at, at, at, at, at, at, at, at, n, n, of, of), how, index)
+        _run(B.lib.bmgd_norm_forward, (self._cfg, rows, found + _NONE16), stream, index, tensors, how)
 
     def backward(self, dy, s, weight, rstd, dx, dweight=None, dsum=None, workspace=None, stream=None):
         """dx <- the gradient of x (and of residual alike) from dy, the s that was normed and the forward call's rstd, plus dsum, the gradient that reaches s besides;
         dweight <- the weight's.  dx may be dy or dsum."""
         rows, index = _rows_of("s", s)
         at, of, n = (rows, self.n), (rows,), self._of_n
-        found = _places(self._NAMES, (s, None, None, None, None, dy, dsum, dx, weight, dweight, None, rstd), self._kinds, (at, at, at, at, at, at, at, at, n, n, of, of),
-                        b"mmmmmmmMvVvv", index)
+        tensors, how = (s, None, None, None, None, dy, dsum, dx, weight, dweight, None, rstd), b"mmmmmmmMvVvv"
+        found = _places(self._NAMES, tensors, self._kinds, (at, at, at, at, at, at, at, at, n, n, of, of), how, index)
         keep, place = _workspace(B.lib.bmgd_norm_workspace_bytes(self._cfg, rows) if dweight is not None and rows else 0, workspace, stream, index)
-        tensors = found + place
-        _run(B.lib.bmgd_norm_backward, (self._cfg, rows, tensors), stream, index)
+        _run(B.lib.bmgd_norm_backward, (self._cfg, rows, found + place), stream, index, tensors, how)
 
     def values(self, codes, scales, out, stream=None):
         """out <- scales[i] codes[i, j], in the type of `out` (any of the three)."""
@@ -137,8 +137,9 @@ def _values(codes, scales, out, n, stream):
     rows, index = _rows_of("codes", codes)
     if not isinstance(out, torch.Tensor) or out.dtype not in _CODES:
         raise ValueError("out: a tensor of 32-bit or 16-bit floats is wanted")
-    found = _places(("codes", "out", "scales"), (codes, out, scales), (_BYTE, out.dtype, _FLOAT), ((rows, n), (rows, n), (rows,)), b"mMv", index)
-    _run(B.lib.bmgd_product_values, (rows, n, found[:16], struct.unpack_from("P", found, 32)[0], found[16:32], _CODES[out.dtype]), stream, index)
+    tensors = codes, out, scales
+    found = _places(("codes", "out", "scales"), tensors, (_BYTE, out.dtype, _FLOAT), ((rows, n), (rows, n), (rows,)), b"mMv", index)
+    _run(B.lib.bmgd_product_values, (rows, n, found[:16], struct.unpack_from("P", found, 32)[0], found[16:32], _CODES[out.dtype]), stream, index, tensors, b"mMv")
 
 
 class Int8Product:
@@ -160,15 +161,17 @@ class Int8Product:
     def forward(self, x, x_scales, w, w_scales, y, stream=None):
         """y <- the product of the codes x (rows x p, a scale for each row) and w (out_n x p, a scale for each output)."""
         rows, index = _rows_of("x", x)
-        found = _places(("x", "w", "y", "x_scales", "w_scales"), (x, w, y, x_scales, w_scales), self._kinds,
+        tensors = x, w, y, x_scales, w_scales
+        found = _places(("x", "w", "y", "x_scales", "w_scales"), tensors, self._kinds,
                         ((rows, self.p), (self.out_n, self.p), (rows, self.out_n), (rows,), (self.out_n,)), b"mmMvv", index)
-        _run(B.lib.bmgd_product_forward, (self._cfg, rows, found), stream, index)
+        _run(B.lib.bmgd_product_forward, (self._cfg, rows, found), stream, index, tensors, b"mmMvv")
 
     def quantize(self, weights, w, w_scales, stream=None):
         """Lays a layer's weights (p x out_n, as GatedBlock has them) out for the product, once: w <- codes (out_n x p), w_scales <- a scale for each output."""
         _, index = _rows_of("weights", weights)
-        found = _places(("weights", "w", "w_scales"), (weights, w, w_scales), (self._type, _BYTE, _FLOAT), ((self.p, self.out_n), (self.out_n, self.p), (self.out_n,)), b"mMV", index)
-        _run(B.lib.bmgd_product_quantize, (self._cfg, found[:16], found[16:32], struct.unpack_from("P", found, 32)[0]), stream, index)
+        tensors = weights, w, w_scales
+        found = _places(("weights", "w", "w_scales"), tensors, (self._type, _BYTE, _FLOAT), ((self.p, self.out_n), (self.out_n, self.p), (self.out_n,)), b"mMV", index)
+        _run(B.lib.bmgd_product_quantize, (self._cfg, found[:16], found[16:32], struct.unpack_from("P", found, 32)[0]), stream, index, tensors, b"mMV")
 
     def values(self, codes, scales, out, stream=None):
         """out <- scales[i] codes[i, j] of rows of p codes, in the type of `out` (any of the three)."""
@@ -198,15 +201,15 @@ class LogProbs:
         kept (rows x 3, fp32: what `backward` needs)."""
         rows, index = _rows_of("logits", logits)
         at, of, best = (rows, self.classes), (rows,), (rows, self.top)
-        found = _places(self._NAMES, (logits, None, labels, logprob, entropy, top_classes, top_logprobs, kept, None, None), self._kinds,
-                        (at, at, of, of, of, best, best, (rows, 3), of, of), b"mmvVVVVVvv", index)
+        tensors, how = (logits, None, labels, logprob, entropy, top_classes, top_logprobs, kept, None, None), b"mmvVVVVVvv"
+        found = _places(self._NAMES, tensors, self._kinds, (at, at, of, of, of, best, best, (rows, 3), of, of), how, index)
         keep, place = _workspace(B.lib.bmgd_logprobs_workspace_bytes(self._cfg, rows), workspace, stream, index)
-        _run(B.lib.bmgd_logprobs_forward, (self._cfg, rows, found + place), stream, index)
+        _run(B.lib.bmgd_logprobs_forward, (self._cfg, rows, found + place), stream, index, tensors, how)
 
     def backward(self, logits, kept, dlogits, labels=None, dlogprob=None, dentropy=None, stream=None):
         """dlogits <- dlogprob ([j = label] - p_j) - dentropy p_j (ln p_j + entropy), from the forward call's `kept`.  dlogits may be logits."""
         rows, index = _rows_of("logits", logits)
         at, of = (rows, self.classes), (rows,)
-        found = _places(self._NAMES, (logits, dlogits, labels, None, None, None, None, kept, dlogprob, dentropy), self._kinds, (at, at, of, of, of, of, of, (rows, 3), of, of),
-                        b"mMvvvvvvvv", index)
-        _run(B.lib.bmgd_logprobs_backward, (self._cfg, rows, found + _NONE16), stream, index)
+        tensors, how = (logits, dlogits, labels, None, None, None, None, kept, dlogprob, dentropy), b"mMvvvvvvvv"
+        found = _places(self._NAMES, tensors, self._kinds, (at, at, of, of, of, of, of, (rows, 3), of, of), how, index)
+        _run(B.lib.bmgd_logprobs_backward, (self._cfg, rows, found + _NONE16), stream, index, tensors, how)
