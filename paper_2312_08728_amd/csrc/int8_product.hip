@@ -491,11 +491,12 @@ template <typename T> hipError_t launch_product(const ProductArgs& a, hipStream_
         if (tiles(128, 128) > units / 2) return tile(Tile<128, 128, 2, 2, 2, false>());
         if (tiles(64, 128) > units * 3 / 4) return tile(Tile<64, 128, 2, 2, 2, false>());
     }
-    // Few tiles.  A step of one takes 0.17 us (32 x 32), 0.21 (32 x 64) or 0.28 (64 x 64), loose ones 0.24, 0.31 and 0.42.  Workgroups of 16 columns without steps read rows more
+    // Few tiles.  A step of one takes 0.17 us (32 x 32) or 0.28 (64 x 64), loose ones 0.24 and 0.42, of 32 x 64 0.31 (aligned: 0.21, but where these are no more than units
+    // tiles of 32 x 32 are two to a unit at most).  Workgroups of 16 columns without steps read rows more
     // often: their operands come at 12 TB/s in all (4.4 where pieces cross lines) and 45 GB/s to a unit.  Measured, us, tiles and these: 64 x 4,096 x 4,096: 9.4 and 12;  100 x 8,192 x 1,000:
     // 15 and 13;  16 x 4,096 x 8,192: 9.4 and 10.2;  1 x 4,096 x 8,192: 9.4 and 8.1;  333 x 1,365 x 1,000, loose: 7.4 and 15.
-    const bool small = tiles(32, 32) <= (loose ? units : 2 * units), flat = tiles(32, 64) <= units;
-    const double tile_us = 4.0 + (small ? loose ? 0.24 : 0.17 : flat ? loose ? 0.31 : 0.21 : loose ? 0.42 : 0.28) * ((a.p + kStep - 1) / kStep);
+    const bool small = tiles(32, 32) <= (loose ? units : 2 * units), flat = loose && tiles(32, 64) <= units;
+    const double tile_us = 4.0 + (small ? loose ? 0.24 : 0.17 : flat ? 0.31 : loose ? 0.42 : 0.28) * ((a.p + kStep - 1) / kStep);
     auto few_us = [&](int64_t rf) {
         const double each = (16.0 + (double)std::min(16 * rf, a.rows)) * a.p, groups = (double)((a.out + 15) / 16) * (double)((a.rows + 16 * rf - 1) / (16 * rf));
         return 4.8 + std::max(each * groups / (loose ? 4.4e6 : 12e6), each / 45e3);
@@ -508,7 +509,7 @@ template <typename T> hipError_t launch_product(const ProductArgs& a, hipStream_
     const double one = few_us(1), two = few_us(2), four = few_us(4), best = std::min(one, std::min(two, four));
     if (best < tile_us && a.rows < (1 << 19)) return one == best ? few(std::integral_constant<int, 1>()) : two == best ? few(std::integral_constant<int, 2>()) : few(std::integral_constant<int, 4>());
     if (loose) return small ? tile(Tile<32, 32, 2, 2, 6, true>()) : flat ? tile(Tile<32, 64, 2, 2, 4, true>()) : tile(Tile<64, 64, 2, 4, 4, true>());
-    return small ? tile(Tile<32, 32, 2, 2, 4, false>()) : flat ? tile(Tile<32, 64, 1, 4, 3, false>()) : tile(Tile<64, 64, 2, 4, 3, false>());
+    return small ? tile(Tile<32, 32, 2, 2, 4, false>()) : tile(Tile<64, 64, 2, 4, 3, false>());
 }
 
 void check(Call& q, const bmgd_product_config* cfg)
