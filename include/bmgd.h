@@ -568,7 +568,8 @@ int bmgd_adamw_moments(const bmgd_adamw_tensor* tensors, int64_t count, float* c
  *      s = x + residual, rounded to the type;     r = 1 / sqrt(mean_j s_j^2 + eps);     y_j = s_j w_j r
  * and, or instead of y, 8-bit codes with a scale for each row: codes_j = the integer nearest to s_j w_j ((1 / max_k |s_k w_k|) 127) (in 64 bits; half to even), scale =
  * max_k |s_k w_k| r / 127, so that scale * codes_j is y_j but for its rounding.  A row whose largest |s w| is below 2^-118 is held as zeros; a row that has a NaN or an
- * infinity among its s w stands for NaN (scale NaN, codes zero).  Sums are in fp32: |s| below 2^63 / sqrt(n). */
+ * infinity among its s w stands for NaN (scale NaN, codes zero).  Sums and products are in fp32: |s| below 2^63 / sqrt(n), |s w| below 2^127 (beyond, y and scale are
+ * infinite or NaN); where eps is 0, r loses bits in rows whose root mean square is below 2^-63. */
 typedef struct bmgd_norm_config {
     int64_t n;              /* columns, in [1, 2^20] */
     double  eps;            /* finite, >= 0; in fp32 too */
