@@ -12,8 +12,8 @@
 // Where a list overflows (logits that rise all along a row), the row is read again with a bound that comes of all of it; where it does so again, or a row has NaN, the
 // classes are found one after the other.
 //
-// What bounds it (us).  8,192 x 32,000, bf16: 93 without classes (5.6 TB/s), 118 with eight: memory, and counting that four workgroups to a unit do not hide.  4,097 x 10,001, f16: 25, of which memory 16,
-// the rest a launch, the first trip and the last turn; the gradient 30 (5.5 TB/s).  16 x 100,003, fp32, twenty classes: 12, two launches.  1 x 1,000: 4.9, a launch and a chain of one trip to memory, a count and sums.
+// What bounds it (us, sets of tensors in turn that are larger together than the caches).  8,192 x 32,000, bf16: 94 without classes (5.6 TB/s), 119 with eight: memory, and counting that four workgroups to a unit
+// do not hide.  4,097 x 10,001, f16: 22 by itself and 25 in front of its gradient, of which memory 16, the rest a launch, the first trip and the last turn; the gradient 30 (5.5 TB/s).  16 x 100,003, fp32, twenty classes: 12, two launches.  1 x 1,000: 4.9, a launch and a chain of one trip to memory, a count and sums.
 #include "operator_calls.h"
 #include "rows_device.h"
 
@@ -783,12 +783,13 @@ BMGD_API int bmgd_logprobs_forward(const bmgd_logprobs_config* cfg, int64_t rows
                 hipLaunchKernelGGL((logprobs_kernel<T, W, TOP, ENT>), dim3((unsigned)((now + kRows - 1) / kRows), (unsigned)a.parts), dim3(threads_of(W)), 0, s, a);
             }
         };
-        // A wavefront for each row, if the rows are many or short.  Measured, us, with it and with four for a row (16 bits; no classes, five):
-        //      8,192 x 1,000: 7 and 21, 14 and 38;  8,192 x 4,000: 14 and 23, 21 and 41;  4,097 x 10,001: 19 and 28, 37 and 34;  8,192 x 32,000: 99 and 93;
-        //      1,000 x 10,001, five: 22 and 13;  100 x 4,000, five: 7.6 and 6.2.
+        // A wavefront for each row, if the rows are many or short.  Measured, us, with it and with four for a row (16 bits, with entropy, sets of tensors in turn that are
+        // larger together than the caches; no classes, five):
+        //      8,192 x 1,000: 9 and 24, 15 and 42;  8,192 x 4,000: 17 and 29, 24 and 48;  4,097 x 10,001: 22 and 30, 30 and 39 (so that with classes too a wavefront would do for many rows
+        //      of this length);  8,192 x 16,000: 56 and 53;  8,192 x 32,000: 101 and 94, eight: 130 and 119;  1,000 x 10,001, five: 16 and 13;  100 x 4,000, five: 7.9 and 6.4.
         // Of 64 groups the 64th largest leaves 300 classes to list, now and then more than the list holds.  So more than 16 only where all of a row's pieces are kept, and
         // with few rows, each of which then takes as long as the call, more than 32:
-        //      8,192 x 700, the 64 most probable: 45 and 172, 20: 19 and 49;  8,192 x 1,300, 64: 51 and 74;  100 x 1,000, 64: 18 and 31, 32: 8.2 and 6.6.
+        //      8,192 x 700, the 64 most probable: 45 and 170, 20: 19 and 48;  8,192 x 1,300, 64: 51 and 75;  100 x 1,000, 64: 17 and 35, 32: 8.5 and 6.7.
         const int64_t pieces = (int64_t)a.span * (int64_t)sizeof(T) / 16;
         const bool many = rows >= 4 * compute_units(), wave = pieces <= 128 || (many && pieces <= (a.top ? 512 : 2048));
         const bool listed = a.top <= 16 || (pieces + 2 <= pieces_kept(1) && (many || a.top > 32));
